@@ -402,6 +402,193 @@ DQGAN_API uint64_t dqgan_launch_count(const dqgan_handle* h);
 DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_msg, int64_t d, int64_t k,
                                           float lr, void* cuda_stream);
 
+/*
+ * Operators of a token model's workers.  The paper leaves F(w; xi), the
+ * stochastic gradient a worker compresses, to the caller's model; for a model
+ * over tokens these calls are the ends of that gradient that a matrix
+ * product does not cover, batched over the workers like
+ * dqgan_workers_compress_all: worker m reads its parameters at
+ * params + m * p_stride (its lookahead point, or p_stride = 0: one vector for
+ * all workers) and writes its gradient at g + m * g_stride (the row the
+ * worker step then reads).
+ *
+ *   layer norm    mu, s^2 a row's mean and variance (divisor: the width),
+ *                 r = 1 / sqrt(s^2 + eps), h = (x - mu) r, y = h weight + bias;
+ *                 with a = dy weight: dx = r (a - mean(a) - h mean(a h)),
+ *                 dweight = sum over rows of dy h, dbias = sum of dy.
+ *   embedding     y_i = scale * table[token_i];
+ *                 dtable[v] = scale * sum over i with token_i = v of dy_i.
+ *   distillation  from a teacher's top logits.  Per row with student logits z,
+ *                 teacher entries (id_k, t_k), temperature T and weight c:
+ *                 p_k = exp(t_k / T - L), L = log sum_k exp(t_k / T) or given;
+ *                 q = softmax(z / T); loss = c T^2 sum_k p_k (log p_k - log q_id_k);
+ *                 dz = scale c T (q sum_k p_k - sum_k p_k at id_k).
+ *                 One entry a row with t = 0, T = 1 is cross entropy.
+ *
+ * Conventions, where they differ from or add to the ones above:
+ *   - An operator handle has its own stream, scratch and error text.  It keeps
+ *     nothing of a call for the next one.  Nothing is allocated by the calls
+ *     that compute, so they can be captured in a CUDA graph.
+ *   - Activations are rows of `width` (or `vocab`) values of the config's dtype
+ *     at a stride of at least that many elements; worker m's rows follow
+ *     worker m - 1's.  Pointers need the alignment of their element only;
+ *     rows that start on 16-byte boundaries are read and written fastest.
+ *   - Parameters, gradients, statistics and losses are fp32, and so is all
+ *     arithmetic: sums, softmax statistics and norms are held in 32 bits
+ *     and a 16-bit result is rounded once.  Every sum has a fixed order, so the
+ *     same call on the same data gives the same bits.
+ *   - Sizes of 0 rows or tokens are allowed (gradients of nothing are 0).
+ *   - An output may be the input named with it below (same pointer and stride);
+ *     no other overlap is allowed.
+ */
+#define DQGAN_F32 0
+#define DQGAN_BF16 1
+#define DQGAN_F16 2
+
+/* Layer norm.  32 bytes, no implicit padding.
+ *   width  1 <= width <= 65536;  workers  1 <= workers <= 4096;
+ *   dtype  of x, y, dy, dx;  eps  >= 0, finite;  reserved  0. */
+typedef struct dqgan_layer_norm_config {
+  int64_t width;
+  int32_t workers;
+  int32_t dtype;
+  float eps;
+  uint32_t reserved;
+  void* cuda_stream;
+} dqgan_layer_norm_config;
+
+/* Embedding.  56 bytes, no implicit padding.
+ *   vocab       rows of a table, 1 <= vocab <= 2^24;
+ *   width       1 <= width <= 65536;
+ *   max_tokens  largest number of tokens a worker of a call has, in [1, 2^24];
+ *               workers * max_tokens and workers * vocab at most 2^28;
+ *   workers     1 <= workers <= 4096;
+ *   table_dtype of the table;  dtype  of y and dy;
+ *   token_bits  32 or 64, signed integers;  scale  finite;  reserved  0. */
+typedef struct dqgan_embedding_config {
+  int64_t vocab;
+  int64_t width;
+  int64_t max_tokens;
+  int32_t workers;
+  int32_t table_dtype;
+  int32_t dtype;
+  int32_t token_bits;
+  float scale;
+  uint32_t reserved;
+  void* cuda_stream;
+} dqgan_embedding_config;
+
+/* Distillation.  40 bytes, no implicit padding.
+ *   vocab          1 <= vocab <= 2^24;
+ *   k              teacher entries a row, 1 <= k <= 1024;
+ *   dtype          of the student's logits and their gradient;
+ *   teacher_dtype  of the teacher's logits;
+ *   temperature    > 0, finite;  reserved  0. */
+typedef struct dqgan_distillation_config {
+  int64_t vocab;
+  int32_t k;
+  int32_t dtype;
+  int32_t teacher_dtype;
+  float temperature;
+  uint32_t reserved[2];
+  void* cuda_stream;
+} dqgan_distillation_config;
+
+typedef struct dqgan_operator dqgan_operator;
+
+/* Create an operator on the current device, with its scratch space (layer
+ * norm and embedding: for the gradients; distillation has none).  On error
+ * *out is NULL, dqgan_operator_last_error(NULL) holds the reason and nothing
+ * stays allocated.  The test hook DQGAN_TEST_FAIL_ALLOC of dqgan_create
+ * applies here too. */
+DQGAN_API int dqgan_layer_norm_create(const dqgan_layer_norm_config* cfg, dqgan_operator** out);
+DQGAN_API int dqgan_embedding_create(const dqgan_embedding_config* cfg, dqgan_operator** out);
+DQGAN_API int dqgan_distillation_create(const dqgan_distillation_config* cfg, dqgan_operator** out);
+
+/* Release the operator (synchronises its stream first).  NULL is a no-op. */
+DQGAN_API int dqgan_operator_destroy(dqgan_operator* op);
+
+/* Wait for the operator's stream; DQGAN_ERR_CUDA if enqueued work failed. */
+DQGAN_API int dqgan_operator_synchronize(dqgan_operator* op);
+
+/* Kernels the operator has launched so far. */
+DQGAN_API uint64_t dqgan_operator_launch_count(const dqgan_operator* op);
+
+/* Text of the last error on this operator, or of this thread's last failed
+ * create call when op is NULL.  Never NULL. */
+DQGAN_API const char* dqgan_operator_last_error(const dqgan_operator* op);
+
+/*
+ * Layer norm of workers * rows rows.  weight, bias: worker m's at + m * p_stride
+ * floats (0: shared, else >= width); NULL: ones, zeros.  mean, rstd: fp32, one a
+ * row, or both NULL.  y may be x.
+ */
+DQGAN_API int dqgan_layer_norm_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
+                                       const float* weight, const float* bias, int64_t p_stride, void* y,
+                                       int64_t y_stride, float* mean, float* rstd);
+
+/*
+ * Its gradient, from the forward pass's x, mean and rstd.  dweight, dbias:
+ * worker m's at + m * g_stride floats (>= width for more than one worker),
+ * written, or added to with accumulate != 0; either may be NULL, and so may
+ * dx.  dx may be dy.  A worker's rows share its weight, so dweight and dbias sum over its rows;
+ * with p_stride = 0 the workers' gradients still stay apart, as Algorithm 2
+ * compresses them apart.
+ */
+DQGAN_API int dqgan_layer_norm_backward(dqgan_operator* op, int64_t rows, const void* dy, int64_t dy_stride,
+                                        const void* x, int64_t x_stride, const float* weight, int64_t p_stride,
+                                        const float* mean, const float* rstd, void* dx, int64_t dx_stride,
+                                        float* dweight, float* dbias, int64_t g_stride, int32_t accumulate);
+
+/*
+ * Embedding of workers * tokens tokens (tokens <= max_tokens).  ids: worker m's
+ * at + m * tokens.  A place whose id is outside [0, vocab) holds no token: its
+ * row of y is 0.  table: vocab rows of width values, contiguous, worker m's
+ * at + m * p_stride elements of table_dtype (0: shared, else >= vocab * width).
+ */
+DQGAN_API int dqgan_embedding_forward(dqgan_operator* op, int64_t tokens, const void* ids, const void* table,
+                                      int64_t p_stride, void* y, int64_t y_stride);
+
+/*
+ * Its gradient, over the tokens sorted by id: worker m's vocab * width floats
+ * at dtable + m * g_stride (>= vocab * width for more than one worker).  Every
+ * row is written (0 where no token fell); with accumulate != 0 the rows that
+ * have tokens are added to and the others are left alone (a table that also
+ * serves as the output layer's weight).  A row's dy are summed in the order of
+ * their places within runs, and the runs' sums in order.  Rows of dy whose
+ * place holds no token are not read.
+ */
+DQGAN_API int dqgan_embedding_backward(dqgan_operator* op, int64_t tokens, const void* ids, const void* dy,
+                                       int64_t dy_stride, float* dtable, int64_t g_stride, int32_t accumulate);
+
+/*
+ * Distillation loss of `rows` rows of logits.  ids, values: the teacher's k
+ * entries of row r at + r * teacher_stride (elements, >= k); an entry whose id
+ * is outside [0, vocab) is left out, whatever its value, and so is one whose
+ * value is -inf; an id may come more than once.  teacher_lse: L of each row, or
+ * NULL (the entries' own).  weights: c of each row, or NULL (ones).  A row with
+ * weight 0 or without an entry does not count: its logits are not read, and
+ * its loss, lse and gradient are 0.  A student logit of -inf has q = 0 (an
+ * entry there makes the loss +inf; a row of nothing else, NaN).
+ * loss: one a row.  lse: log sum_v exp(z_v / T), one a row, or NULL.
+ */
+DQGAN_API int dqgan_distillation_forward(dqgan_operator* op, int64_t rows, const void* logits, int64_t logits_stride,
+                                         const int32_t* ids, const void* values, int64_t teacher_stride,
+                                         const float* teacher_lse, const float* weights, float* loss, float* lse);
+
+/* The gradient of scale * sum of losses with respect to the logits, from the
+ * forward pass's lse.  dlogits may be logits. */
+DQGAN_API int dqgan_distillation_backward(dqgan_operator* op, int64_t rows, const void* logits, int64_t logits_stride,
+                                          const float* lse, const int32_t* ids, const void* values,
+                                          int64_t teacher_stride, const float* teacher_lse, const float* weights,
+                                          float scale, void* dlogits, int64_t dlogits_stride);
+
+/* Both in one call, which reads the logits from memory once.  lse may be NULL; dlogits may be logits. */
+DQGAN_API int dqgan_distillation_step(dqgan_operator* op, int64_t rows, const void* logits, int64_t logits_stride,
+                                      const int32_t* ids, const void* values, int64_t teacher_stride,
+                                      const float* teacher_lse, const float* weights, float scale, float* loss,
+                                      float* lse, void* dlogits, int64_t dlogits_stride);
+
 /* Text of the last error on this handle, or of the last failed
  * create / validate / layout call in this thread when h is NULL.
  * Never NULL; valid until the next call on the same handle / thread. */

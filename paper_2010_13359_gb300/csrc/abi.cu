@@ -339,6 +339,10 @@ namespace dq {
 
 int set_thread_error(int code, const char* msg) { return set_error(nullptr, code, "%s", msg); }
 
+void arm_device_allocation() { arm_allocation_failure(); }
+
+cudaError_t device_allocate(void** p, size_t bytes) { return dq_malloc(p, bytes); }
+
 bool message_layout(const dqgan_config& c, Layout* out) {
   if (!check_config(&c).empty()) return false;
   const int64_t nb = (c.compressor == DQGAN_SIGN || c.compressor == DQGAN_SQUANT || c.compressor == DQGAN_QSGD)

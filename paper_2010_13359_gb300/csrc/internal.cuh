@@ -37,6 +37,11 @@ bool message_layout(const dqgan_config& cfg, Layout* out);
 // Records `msg` as this thread's last error (dqgan_last_error(NULL)); returns code.
 int set_thread_error(int code, const char* msg);
 
+// Device allocations of the library, with the test hook DQGAN_TEST_FAIL_ALLOC
+// (read by arm_device_allocation, at the start of a create call).
+void arm_device_allocation();
+cudaError_t device_allocate(void** p, size_t bytes);
+
 // Arguments shared by every worker-side (compress) kernel.  One launch covers
 // `nworkers` consecutive workers starting at `worker0`; launch row y (blockIdx.y)
 // is worker worker0 + y.

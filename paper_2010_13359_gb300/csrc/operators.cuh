@@ -1,0 +1,137 @@
+// Declarations of the token-model operators (not part of the C-ABI): argument
+// blocks, launchers, and the element types' conversions.  Their arithmetic is
+// fp32; unlike the compress and server kernels they may use fused
+// multiply-adds (written out as fmaf: the library is built without contraction).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "internal.cuh"
+
+namespace dq {
+
+struct LayerNormArgs {
+  const void* x;        // worker m's row r at x + (m * rows + r) * x_ld elements
+  const void* dy;       // backward
+  void* out;            // y, or dx (backward; may be nullptr)
+  int64_t x_ld, dy_ld, out_ld;
+  const float* weight;  // worker m's at + m * p_stride, or nullptr (ones)
+  const float* bias;    // forward; nullptr: zeros
+  int64_t p_stride;
+  float* mean;          // one a row (forward: or nullptr)
+  float* rstd;
+  float* dweight;       // backward; worker m's at + m * g_stride, or nullptr
+  float* dbias;
+  int64_t g_stride;
+  float* scratch;       // backward: layer_norm_scratch_bytes
+  int64_t rows;         // per worker
+  int64_t width;
+  int32_t workers;
+  int32_t dtype;
+  float eps;
+  int32_t accumulate;
+};
+
+struct EmbeddingArgs {
+  const void* ids;      // worker m's at + m * tokens, int32 or int64
+  const void* table;    // forward; worker m's at + m * p_stride elements
+  int64_t p_stride;
+  void* y;              // forward
+  const void* dy;       // backward
+  int64_t ld;           // row stride of y or dy
+  float* dtable;        // backward; worker m's at + m * g_stride
+  int64_t g_stride;
+  void* scratch;        // backward: embedding_scratch_bytes
+  int64_t tokens;       // per worker
+  int64_t vocab;
+  int64_t width;
+  int32_t workers;
+  int32_t table_dtype;
+  int32_t dtype;
+  int32_t token_bits;
+  float scale;
+  int32_t accumulate;
+};
+
+struct DistillationArgs {
+  const void* logits;       // row r at + r * ld
+  int64_t ld;
+  void* dlogits;            // backward and step
+  int64_t dld;
+  const int32_t* ids;       // row r's k entries at + r * teacher_ld
+  const void* values;
+  int64_t teacher_ld;
+  const float* teacher_lse; // or nullptr
+  const float* weights;     // or nullptr
+  float* loss;              // forward and step
+  float* lse;               // forward and step: written, or nullptr; backward: read
+  int64_t rows;
+  int64_t vocab;
+  int32_t k;
+  int32_t dtype;
+  int32_t teacher_dtype;
+  float temperature;
+  float scale;
+};
+
+enum class DistillationWay { kForward, kBackward, kStep };
+
+size_t layer_norm_scratch_bytes(int64_t width, int32_t workers);
+cudaError_t launch_layer_norm_forward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches);
+cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches);
+
+size_t embedding_scratch_bytes(int64_t vocab, int64_t width, int64_t max_tokens, int32_t workers);
+cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t stream, uint64_t* launches);
+cudaError_t launch_embedding_backward(const EmbeddingArgs& a, cudaStream_t stream, uint64_t* launches);
+
+cudaError_t launch_distillation(const DistillationArgs& a, DistillationWay way, cudaStream_t stream,
+                                uint64_t* launches);
+
+__host__ __device__ constexpr int64_t ceil_div(int64_t x, int64_t m) { return (x + m - 1) / m; }
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) {
+  return __float2bfloat16_rn(x);
+}
+template <>
+__device__ __forceinline__ __half from_float<__half>(float x) {
+  return __float2half_rn(x);
+}
+
+// Calls f with a value of the element type that `dtype` names.
+template <typename F>
+inline cudaError_t with_dtype(int32_t dtype, F&& f) {
+  switch (dtype) {
+    case DQGAN_F32: return f(float{});
+    case DQGAN_BF16: return f(__nv_bfloat16{});
+    case DQGAN_F16: return f(__half{});
+  }
+  return cudaErrorInvalidValue;
+}
+
+// Sum over the block in a fixed order (warp butterflies, then the warps' sums
+// in order); every thread gets it.  `shared`: 32 floats, reused by the next call.
+__device__ __forceinline__ float block_sum(float x, float* shared) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
+  const int warps = (int)(blockDim.x + 31) / 32;
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) shared[threadIdx.x / 32] = x;
+  __syncthreads();
+  float s = shared[0];
+  for (int i = 1; i < warps; ++i) s += shared[i];
+  return s;
+}
+
+}  // namespace dq

@@ -52,6 +52,8 @@ class Config(ctypes.Structure):
 
 assert ctypes.sizeof(Config) == 56
 
+F32, BF16, F16 = 0, 1, 2
+
 SERVER_OMD, SERVER_OADAM = 0, 1
 OADAM_ADAPTIVE, OADAM_BIAS_CORRECTION = 1, 2
 
@@ -91,7 +93,7 @@ def load_library(path: str = LIBRARY) -> ctypes.CDLL:
     L = ctypes.CDLL(path)
     H = ctypes.c_void_p
     P = ctypes.c_void_p
-    i32, i64, u64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64
+    i32, i64, u64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
     cfgp = ctypes.POINTER(Config)
     sig = {
         "dqgan_message_layout": (ctypes.c_int, [cfgp, ctypes.POINTER(i64), ctypes.POINTER(i64),
@@ -123,6 +125,20 @@ def load_library(path: str = LIBRARY) -> ctypes.CDLL:
         "dqgan_workers_compress_range": (ctypes.c_int, [H, i32, i32, P, i64, P]),
         "dqgan_set_local_workers": (ctypes.c_int, [H, i32, i32]),
         "dqgan_get_server_state": (ctypes.c_int, [H, i32, P]),
+        "dqgan_layer_norm_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_embedding_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_distillation_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_operator_destroy": (ctypes.c_int, [H]),
+        "dqgan_operator_synchronize": (ctypes.c_int, [H]),
+        "dqgan_operator_launch_count": (u64, [H]),
+        "dqgan_operator_last_error": (ctypes.c_char_p, [H]),
+        "dqgan_layer_norm_forward": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, i64, P, P]),
+        "dqgan_layer_norm_backward": (ctypes.c_int, [H, i64, P, i64, P, i64, P, i64, P, P, P, i64, P, P, i64, i32]),
+        "dqgan_embedding_forward": (ctypes.c_int, [H, i64, P, P, i64, P, i64]),
+        "dqgan_embedding_backward": (ctypes.c_int, [H, i64, P, P, i64, P, i64, i32]),
+        "dqgan_distillation_forward": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, P, P, P]),
+        "dqgan_distillation_backward": (ctypes.c_int, [H, i64, P, i64, P, P, P, i64, P, P, f32, P, i64]),
+        "dqgan_distillation_step": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, P, f32, P, P, P, i64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
