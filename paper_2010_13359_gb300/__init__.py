@@ -5,7 +5,8 @@ The compute lives in ``libdqgan.so`` (CUDA kernels behind the C-ABI of
 the seeded synthetic inputs; ``games`` closes Algorithm 2 around a min-max
 operator (the bilinear game of Section 2.2).  ``operators`` binds the kernels a
 token model's workers need around their matrix products (layer norm, embedding,
-distillation, with their gradients).
+distillation, with their gradients), and ``token_model`` closes Algorithm 2
+around a model made of them.
 """
 from . import dqgan  # noqa: F401
 from .dqgan import (  # noqa: F401
