@@ -3,17 +3,528 @@
 //   mu = mean(x), s^2 = mean((x - mu)^2), r = 1 / sqrt(s^2 + eps), h = (x - mu) r
 //   y = h weight + bias
 //   a = dy weight, dx = r (a - mean(a) - h mean(a h)), dweight = sum dy h, dbias = sum dy
+//
+// Both directions are bound by memory (forward: 2, backward: 3 values moved per
+// element at 8 and 14 operations), so each row is read once and kept on chip: a
+// group of kLanes threads holds it, 16 values to a thread.  The variance is taken
+// from the deviations, in a second sum over the same registers, so that a large
+// mean costs no digits.  Rows longer than 16,384 values are read again from the
+// caches instead.
 #include "device_common.cuh"
 #include "operators.cuh"
 
 namespace dq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kPerThread = 16;  // values of a row in one thread
+constexpr int kMaxOnChip = 1024 * kPerThread;
 
-// One block per row: three passes over it, the later ones out of the caches.
+// Two fp32 operations in one instruction, each rounded as the single one.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)),
+        "l"(reinterpret_cast<const uint64_t&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t&>(d))
+      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Elements (e, e + 1) of a pack, and back.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) layer_norm_forward_kernel(LayerNormArgs a) {
+__device__ __forceinline__ float2 pair_of(const uint4& p, int e);
+template <>
+__device__ __forceinline__ float2 pair_of<float>(const uint4& p, int e) {
+  const float* v = reinterpret_cast<const float*>(&p);
+  return make_float2(v[e], v[e + 1]);
+}
+template <>
+__device__ __forceinline__ float2 pair_of<__nv_bfloat16>(const uint4& p, int e) {
+  const uint32_t v = reinterpret_cast<const uint32_t*>(&p)[e / 2];  // a bf16 is the upper half of an fp32
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 pair_of<__half>(const uint4& p, int e) {
+  return __half22float2(reinterpret_cast<const __half2*>(&p)[e / 2]);
+}
+
+template <typename T>
+__device__ __forceinline__ void set_pair(uint4& p, int e, float2 v);
+template <>
+__device__ __forceinline__ void set_pair<float>(uint4& p, int e, float2 v) {
+  float* to = reinterpret_cast<float*>(&p);
+  to[e] = v.x;
+  to[e + 1] = v.y;
+}
+template <>
+__device__ __forceinline__ void set_pair<__nv_bfloat16>(uint4& p, int e, float2 v) {
+  reinterpret_cast<__nv_bfloat162*>(&p)[e / 2] = __float22bfloat162_rn(v);
+}
+template <>
+__device__ __forceinline__ void set_pair<__half>(uint4& p, int e, float2 v) {
+  reinterpret_cast<__half2*>(&p)[e / 2] = __float22half2_rn(v);
+}
+
+__device__ __forceinline__ void copy16_async(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+// A thread's share of a row: N packs of E values.  kVec: pack i of lane t holds
+// values (i * kLanes + t) * E and the E - 1 after it; else (rows that do not
+// start on 16-byte boundaries) value e of pack i is (i * E + e) * kLanes + t, so
+// that single-element accesses of a warp are adjacent.
+template <typename T, int kLanes, bool kVec>
+struct Slice {
+  static constexpr int E = 16 / (int)sizeof(T);
+  static constexpr int N = kPerThread / E;
+
+  __device__ __forceinline__ static int at(int i, int e, int lane) {
+    return kVec ? (i * kLanes + lane) * E + e : (i * E + e) * kLanes + lane;
+  }
+
+  // The row's packs, 0 past its end.
+  __device__ __forceinline__ static void load(const T* row, int width, int lane, uint4 (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (kVec && at(i, E - 1, lane) < width) {
+        x[i] = *reinterpret_cast<const uint4*>(row + at(i, 0, lane));
+      } else {
+        T* v = reinterpret_cast<T*>(&x[i]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = at(i, e, lane) < width ? row[at(i, e, lane)] : from_float<T>(0.f);
+      }
+    }
+  }
+
+  // The same into this thread's places of a ring stage (`stride` packs apart).
+  __device__ __forceinline__ static void fetch(const T* row, int width, int lane, uint4* to, int stride) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int left = (width - at(i, 0, lane)) * (int)sizeof(T);
+      const int bytes = left >= 16 ? 16 : left > 0 ? left : 0;
+      copy16_async(to + i * stride, row + (bytes > 0 ? at(i, 0, lane) : 0), bytes);
+    }
+  }
+
+  __device__ __forceinline__ static void store(T* row, int width, int lane, const uint4 (&y)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (kVec && at(i, E - 1, lane) < width) {
+        __stcs(reinterpret_cast<uint4*>(row + at(i, 0, lane)), y[i]);
+      } else {
+        const T* v = reinterpret_cast<const T*>(&y[i]);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (at(i, e, lane) < width) row[at(i, e, lane)] = v[e];
+      }
+    }
+  }
+
+  // f(i, e, column) for every value of the row that this lane holds.
+  template <typename F>
+  __device__ __forceinline__ static void each(int width, int lane, F&& f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (at(i, e, lane) < width) f(i, e, at(i, e, lane));
+  }
+
+  // A worker's parameters at this lane's columns (`missing` where there are none
+  // or past the end).  They come from the caches; 16 bytes at a time where they
+  // are aligned, which a parameter vector's segments need not be.
+  __device__ __forceinline__ static void params(const float* p, float missing, int width, int lane,
+                                                float2 (&w)[N][E / 2]) {
+    const bool aligned = ((uintptr_t)p & 15u) == 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (kVec && p && aligned && at(i, E - 1, lane) < width) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(p + at(i, e, lane));
+          w[i][e / 2] = make_float2(v.x, v.y);
+          w[i][e / 2 + 1] = make_float2(v.z, v.w);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const int c0 = at(i, e, lane), c1 = at(i, e + 1, lane);
+          w[i][e / 2] = make_float2(p && c0 < width ? p[c0] : missing, p && c1 < width ? p[c1] : missing);
+        }
+      }
+    }
+  }
+};
+
+// The first half of a sum of K values over the kLanes threads of a row: above a
+// warp, each warp's sum goes to its slots of `shared`.
+template <int kLanes, int K>
+__device__ __forceinline__ void row_sum_publish(float (&v)[K], float* shared) {
+  constexpr int kWide = kLanes < 32 ? kLanes : 32;
+#pragma unroll
+  for (int o = kWide / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(kFullMask, v[k], o);
+  if constexpr (kLanes > 32)
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) shared[threadIdx.x / 32 * K + k] = v[k];
+}
+
+// Waits for the other threads of this thread's row (nothing up to a warp).
+template <int kLanes>
+__device__ __forceinline__ void row_wait() {
+  if constexpr (kLanes > 32)
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / kLanes), "n"(kLanes) : "memory");
+}
+
+// The second half, after row_wait: the warps' sums in a fixed tree; every thread
+// gets the total.
+template <int kLanes, int K>
+__device__ __forceinline__ void row_sum_collect(float (&v)[K], const float* shared) {
+  if constexpr (kLanes > 32) {
+    constexpr int kWarps = kLanes / 32;
+    const float* mine = shared + ((int)threadIdx.x / 32 & ~(kWarps - 1)) * K;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float s[kWarps];
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) s[i] = mine[i * K + k];
+#pragma unroll
+      for (int w = 1; w < kWarps; w *= 2)
+#pragma unroll
+        for (int i = 0; i + w < kWarps; i += 2 * w) s[i] += s[i + w];
+      v[k] = s[0];
+    }
+  }
+}
+
+// A block's threads: one row for each kLanes of them.  Register use decides
+// (forward: three blocks of 256 on an SM; backward: one of 512, or of 256 in
+// 32 bits, whose rows take twice the shared memory).
+template <int kLanes>
+constexpr int forward_threads() {
+  return kLanes > 256 ? kLanes : 256;
+}
+template <typename T, int kLanes>
+constexpr int backward_threads() {
+  constexpr int kLeast = sizeof(T) == 4 ? 256 : 512;
+  return kLanes > kLeast ? kLanes : kLeast;
+}
+
+// Rows on their way or at work in shared memory, `rows` vectors of them to a stage.
+template <typename T>
+constexpr int stages_that_fit(int threads, int rows, int bytes, int most) {
+  const int fit = bytes / (rows * threads * kPerThread * (int)sizeof(T));
+  return fit > most ? most : fit;
+}
+template <typename T, int kLanes>
+constexpr int forward_stages() {
+  return stages_that_fit<T>(forward_threads<kLanes>(), 1, (kLanes > 256 ? 128 : 64) << 10, 4);
+}
+template <typename T, int kLanes>
+constexpr int backward_stages() {
+  return stages_that_fit<T>(backward_threads<T, kLanes>(), 2, 200 << 10, 6);
+}
+
+// Forward.  Blocks walk over a worker's rows, with its weight and bias in
+// registers.  The next rows are on their way while one is worked on: every
+// thread copies its own packs to its own places in shared memory, so no barrier
+// guards them.
+template <typename T, int kLanes, bool kVec>
+__global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : kLanes > 256 ? 2 : 3)
+    layer_norm_forward_kernel(LayerNormArgs a) {
+  dq_pdl_enter();
+  using S = Slice<T, kLanes, kVec>;
+  constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kStages = forward_stages<T, kLanes>();
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ float shared[2][kThreads / 32];
+  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][pack][thread]
+  const int width = (int)a.width, lane = threadIdx.x % kLanes;
+  const int64_t m = blockIdx.y, step = (int64_t)gridDim.x * kGroups;
+  const int64_t first = (int64_t)blockIdx.x * kGroups;
+  const T* xs = static_cast<const T*>(a.x) + m * a.rows * a.x_ld;
+  T* ys = static_cast<T*>(a.out) + m * a.rows * a.out_ld;
+  const auto fetch = [&](int64_t r, int stage) {
+    if (!kVec) return;
+    if (r < a.rows) S::fetch(xs + r * a.x_ld, width, lane, ring + stage * S::N * kThreads + threadIdx.x, kThreads);
+    copies_begun();
+  };
+  const int64_t mine = first + threadIdx.x / kLanes;
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(mine + s * step, s);
+  float2 w[S::N][S::E / 2], b[S::N][S::E / 2];
+  S::params(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, width, lane, w);
+  S::params(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, width, lane, b);
+  const float inv_width = 1.f / (float)width;
+  int stage = 0;
+  for (int64_t r0 = first; r0 < a.rows; r0 += step) {
+    const int64_t r = r0 + threadIdx.x / kLanes;
+    const bool live = r < a.rows;
+    uint4 p[S::N];
+    if (kVec) {
+      fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+      wait_copies<kStages - 1>();
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) p[i] = ring[(stage * S::N + i) * kThreads + threadIdx.x];
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    } else if (live) {
+      S::load(xs + r * a.x_ld, width, lane, p);
+    }
+    float2 x[S::N][S::E / 2], t = both(0.f);
+#pragma unroll
+    for (int i = 0; i < S::N; ++i)
+#pragma unroll
+      for (int e = 0; e < S::E; e += 2) {
+        x[i][e / 2] = pair_of<T>(p[i], e);
+        t = add2(t, x[i][e / 2]);
+      }
+    float s[1] = {t.x + t.y};
+    row_sum_publish<kLanes, 1>(s, shared[0]);
+    row_wait<kLanes>();
+    row_sum_collect<kLanes, 1>(s, shared[0]);
+    const float mean = s[0] / (float)width;
+    t = both(0.f);
+#pragma unroll
+    for (int i = 0; i < S::N; ++i)
+#pragma unroll
+      for (int e = 0; e < S::E; e += 2) {
+        float2 d = add2(x[i][e / 2], both(-mean));
+        x[i][e / 2] = d;
+        if (!kVec || S::at(i, S::E - 1, lane) >= width) {  // nothing past the row's end counts
+          if (S::at(i, e, lane) >= width) d.x = 0.f;
+          if (S::at(i, e + 1, lane) >= width) d.y = 0.f;
+        }
+        t = fma2(d, d, t);
+      }
+    s[0] = t.x + t.y;
+    row_sum_publish<kLanes, 1>(s, shared[1]);
+    row_wait<kLanes>();
+    row_sum_collect<kLanes, 1>(s, shared[1]);
+    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_width, a.eps));
+#pragma unroll
+    for (int i = 0; i < S::N; ++i)
+#pragma unroll
+      for (int e = 0; e < S::E; e += 2)
+        set_pair<T>(p[i], e, fma2(mul2(x[i][e / 2], both(rstd)), w[i][e / 2], b[i][e / 2]));
+    if (live) {
+      S::store(ys + r * a.out_ld, width, lane, p);
+      if (lane == 0 && a.mean) {
+        a.mean[m * a.rows + r] = mean;
+        a.rstd[m * a.rows + r] = rstd;
+      }
+    }
+  }
+}
+
+// Backward.  A block walks over rows of one worker, its rows ahead on their way
+// as above, and keeps each column's sums for dweight and dbias in registers; what
+// it has at the end goes to its row of the scratch space, and a second kernel
+// adds the blocks' rows up in order (with one block per worker it is the
+// result).  A row's sums are published while the row before is finished from its
+// packs in shared memory, which hides the exchange between the row's warps:
+// one barrier a row.
+template <typename T, int kLanes, bool kVec>
+__global__ void __launch_bounds__(backward_threads<T, kLanes>(), 1) layer_norm_backward_kernel(LayerNormArgs a) {
+  dq_pdl_enter();
+  using S = Slice<T, kLanes, kVec>;
+  constexpr int kThreads = backward_threads<T, kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kStages = backward_stages<T, kLanes>();
+  constexpr bool kRing = kVec && kStages >= 3;  // else a row is read again from the caches
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ float shared[2][kThreads / 32 * 2];
+  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][x, dy][pack][thread]
+  const int width = (int)a.width, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int64_t m = blockIdx.y, parts = gridDim.x, step = parts * kGroups;
+  const int64_t first = (int64_t)blockIdx.x * kGroups;
+  const T* xs = static_cast<const T*>(a.x) + m * a.rows * a.x_ld;
+  const T* dys = static_cast<const T*>(a.dy) + m * a.rows * a.dy_ld;
+
+  const auto fetch = [&](int64_t r, int stage) {
+    if (!kRing) return;
+    if (r < a.rows) {
+      uint4* to = ring + stage * 2 * S::N * kThreads + threadIdx.x;
+      S::fetch(xs + r * a.x_ld, width, lane, to, kThreads);
+      S::fetch(dys + r * a.dy_ld, width, lane, to + S::N * kThreads, kThreads);
+    }
+    copies_begun();
+  };
+  const auto take = [&](int64_t r, int stage, uint4 (&x)[S::N], uint4 (&g)[S::N]) {
+    if (kRing) {
+      const uint4* from = ring + stage * 2 * S::N * kThreads + threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < S::N; ++i) {
+        x[i] = from[i * kThreads];
+        g[i] = from[(S::N + i) * kThreads];
+      }
+    } else {
+      S::load(xs + r * a.x_ld, width, lane, x);
+      S::load(dys + r * a.dy_ld, width, lane, g);
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 2; ++s) fetch(first + group + s * step, s);
+
+  float2 w[S::N][S::E / 2], sw[S::N][S::E / 2], sb[S::N][S::E / 2];
+  S::params(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, width, lane, w);
+#pragma unroll
+  for (int i = 0; i < S::N; ++i)
+#pragma unroll
+    for (int e = 0; e < S::E / 2; ++e) sw[i][e] = sb[i][e] = both(0.f);
+  const float inv_width = 1.f / (float)width;
+
+  float s[2] = {0.f, 0.f}, mean = 0.f, rstd = 0.f;  // of the row before
+  float next_mean = 0.f, next_rstd = 0.f;           // of the row at hand
+  if (first + group < a.rows) {
+    next_mean = a.mean[m * a.rows + first + group];
+    next_rstd = a.rstd[m * a.rows + first + group];
+  }
+  int stage = 0, before = 0, parity = 0;
+  int64_t last = -1;  // the row before
+  for (int64_t r0 = first; r0 < a.rows + step; r0 += step) {
+    const int64_t r = r0 + group;
+    float sum[2] = {0.f, 0.f};
+    const float new_mean = next_mean, new_rstd = next_rstd;
+    if (kRing) {  // the stage of the row before last is free
+      fetch(r + (kStages - 2) * step, stage + kStages - 2 >= kStages ? stage - 2 : stage + kStages - 2);
+      wait_copies<kStages - 2 >= 0 ? kStages - 2 : 0>();
+    }
+    if (r < a.rows) {
+      if (r + step < a.rows) {
+        next_mean = a.mean[m * a.rows + r + step];
+        next_rstd = a.rstd[m * a.rows + r + step];
+      }
+      uint4 x[S::N], g[S::N];
+      take(r, stage, x, g);
+      float2 s0 = both(0.f), s1 = both(0.f);
+#pragma unroll
+      for (int i = 0; i < S::N; ++i)
+#pragma unroll
+        for (int e = 0; e < S::E; e += 2) {  // past the row's end dy is 0
+          const float2 h = mul2(add2(pair_of<T>(x[i], e), both(-new_mean)), both(new_rstd));
+          const float2 d = pair_of<T>(g[i], e);
+          sw[i][e / 2] = fma2(d, h, sw[i][e / 2]);
+          sb[i][e / 2] = add2(sb[i][e / 2], d);
+          const float2 wd = mul2(d, w[i][e / 2]);
+          s0 = add2(s0, wd);
+          s1 = fma2(wd, h, s1);
+        }
+      sum[0] = s0.x + s0.y;
+      sum[1] = s1.x + s1.y;
+    }
+    row_sum_publish<kLanes, 2>(sum, shared[parity]);
+    if (last >= 0 && a.out) {
+      uint4 x[S::N], g[S::N];
+      take(last, before, x, g);
+      row_sum_collect<kLanes, 2>(s, shared[parity ^ 1]);
+      // dx = rstd (dy w - c1 - h c2)
+      const float c1 = s[0] * inv_width, c2 = s[1] * inv_width;
+#pragma unroll
+      for (int i = 0; i < S::N; ++i)
+#pragma unroll
+        for (int e = 0; e < S::E; e += 2) {
+          const float2 h = mul2(add2(pair_of<T>(x[i], e), both(-mean)), both(rstd));
+          const float2 wd = fma2(pair_of<T>(g[i], e), w[i][e / 2], both(-c1));
+          set_pair<T>(g[i], e, mul2(fma2(h, both(-c2), wd), both(rstd)));
+        }
+      S::store(static_cast<T*>(a.out) + (m * a.rows + last) * a.out_ld, width, lane, g);
+    }
+    row_wait<kLanes>();
+    s[0] = sum[0];
+    s[1] = sum[1];
+    mean = new_mean;
+    rstd = new_rstd;
+    last = r < a.rows ? r : -1;
+    before = stage;
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+    parity ^= 1;
+  }
+  if (!a.dweight && !a.dbias) return;
+  // the groups' sums in order, through shared memory in the ring's place
+  float* sums = reinterpret_cast<float*>(dynamic);
+  if (kRing) asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const auto value = [&](int i, int e) {
+      const float2 v = which == 0 ? sw[i][e / 2] : sb[i][e / 2];
+      return e % 2 == 0 ? v.x : v.y;
+    };
+    if (kGroups > 1) {
+      __syncthreads();
+      S::each(width, lane, [&](int i, int e, int c) { sums[group * width + c] = value(i, e); });
+      __syncthreads();
+    }
+    float* out = which == 0 ? a.dweight : a.dbias;
+    if (!out) continue;
+    out += m * a.g_stride;
+    const bool whole = parts == 1;
+    float* part = a.scratch + ((m * parts + blockIdx.x) * 2 + which) * a.width;
+    const auto put = [&](int c, float v) {
+      if (whole) out[c] = a.accumulate ? out[c] + v : v;
+      else part[c] = v;
+    };
+    if (kGroups > 1) {
+      for (int c = threadIdx.x; c < width; c += kThreads) {
+        float v = sums[c];
+        for (int k = 1; k < kGroups; ++k) v += sums[k * width + c];
+        put(c, v);
+      }
+    } else {
+      S::each(width, lane, [&](int i, int e, int c) { put(c, value(i, e)); });
+    }
+  }
+}
+
+// The blocks' rows of the scratch space, added up in order: a block takes 32
+// columns of one worker's dweight or dbias, its warps every kWarps-th row.
+constexpr int kJoinWarps = 8;
+
+__global__ void __launch_bounds__(kJoinWarps * 32) layer_norm_join_kernel(LayerNormArgs a, int parts) {
+  dq_pdl_enter();
+  __shared__ float shared[kJoinWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, which = blockIdx.z;
+  const int64_t m = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
+  float* out = which == 0 ? a.dweight : a.dbias;
+  if (!out) return;
+  float v = 0.f;
+  if (c < a.width)
+#pragma unroll 4
+    for (int p = warp; p < parts; p += kJoinWarps) v += a.scratch[((m * parts + p) * 2 + which) * a.width + c];
+  shared[warp][lane] = v;
+  __syncthreads();
+  if (warp != 0 || c >= a.width) return;
+#pragma unroll
+  for (int i = 1; i < kJoinWarps; ++i) v += shared[i][lane];
+  out += m * a.g_stride + c;
+  *out = a.accumulate ? *out + v : v;
+}
+
+// Rows of more than kMaxOnChip values, one block each: further passes over the
+// row come out of the caches.
+constexpr int kLongThreads = 512;
+
+template <typename T>
+__global__ void __launch_bounds__(kLongThreads) layer_norm_forward_long_kernel(LayerNormArgs a) {
   dq_pdl_enter();
   __shared__ float shared[32];
   const int64_t row = blockIdx.x;
@@ -23,15 +534,15 @@ __global__ void __launch_bounds__(kThreads) layer_norm_forward_kernel(LayerNormA
   const float* weight = a.weight ? a.weight + m * a.p_stride : nullptr;
   const float* bias = a.bias ? a.bias + m * a.p_stride : nullptr;
   float s = 0.f;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) s += to_float(x[c]);
+  for (int64_t c = threadIdx.x; c < a.width; c += kLongThreads) s += to_float(x[c]);
   const float mean = block_sum(s, shared) / (float)a.width;
   s = 0.f;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) {
+  for (int64_t c = threadIdx.x; c < a.width; c += kLongThreads) {
     const float d = to_float(x[c]) - mean;
     s = fmaf(d, d, s);
   }
   const float rstd = 1.f / sqrtf(block_sum(s, shared) / (float)a.width + a.eps);
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) {
+  for (int64_t c = threadIdx.x; c < a.width; c += kLongThreads) {
     const float h = (to_float(x[c]) - mean) * rstd;
     y[c] = from_float<T>(fmaf(h, weight ? weight[c] : 1.f, bias ? bias[c] : 0.f));
   }
@@ -41,9 +552,8 @@ __global__ void __launch_bounds__(kThreads) layer_norm_forward_kernel(LayerNormA
   }
 }
 
-// dx: one block per row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) layer_norm_dx_kernel(LayerNormArgs a) {
+__global__ void __launch_bounds__(kLongThreads) layer_norm_dx_long_kernel(LayerNormArgs a) {
   dq_pdl_enter();
   __shared__ float shared[32];
   const int64_t row = blockIdx.x;
@@ -54,24 +564,24 @@ __global__ void __launch_bounds__(kThreads) layer_norm_dx_kernel(LayerNormArgs a
   const float* weight = a.weight ? a.weight + m * a.p_stride : nullptr;
   const float mean = a.mean[row], rstd = a.rstd[row];
   float s1 = 0.f, s2 = 0.f;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) {
+  for (int64_t c = threadIdx.x; c < a.width; c += kLongThreads) {
     const float g = to_float(dy[c]) * (weight ? weight[c] : 1.f);
     s1 += g;
     s2 = fmaf(g, (to_float(x[c]) - mean) * rstd, s2);
   }
   const float c1 = block_sum(s1, shared) / (float)a.width;
   const float c2 = block_sum(s2, shared) / (float)a.width;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) {
+  for (int64_t c = threadIdx.x; c < a.width; c += kLongThreads) {
     const float g = to_float(dy[c]) * (weight ? weight[c] : 1.f);
     const float h = (to_float(x[c]) - mean) * rstd;
-    dx[c] = from_float<T>(rstd * (g - c1 - h * c2));
+    dx[c] = from_float<T>(rstd * (g - fmaf(h, c2, c1)));
   }
 }
 
 // dweight and dbias: a block takes 32 columns of one worker; its 8 warps take
 // every eighth row and their sums are added in order.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) layer_norm_dparams_kernel(LayerNormArgs a) {
+__global__ void __launch_bounds__(256) layer_norm_dparams_long_kernel(LayerNormArgs a) {
   dq_pdl_enter();
   __shared__ float sw[8][32], sb[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
@@ -103,16 +613,87 @@ __global__ void __launch_bounds__(kThreads) layer_norm_dparams_kernel(LayerNormA
   }
 }
 
+// Blocks of the backward pass over all workers.
+int64_t backward_blocks(int64_t workers) { return max64(workers, device_sms()); }
+
+template <int kLanes>
+struct Lanes {
+  static constexpr int value = kLanes;
+};
+
+// Calls f with the number of threads that hold a row of `width` values.
+template <typename F>
+cudaError_t with_lanes(int64_t width, F&& f) {
+  if (width <= 8 * kPerThread) return f(Lanes<8>{});
+  if (width <= 16 * kPerThread) return f(Lanes<16>{});
+  if (width <= 32 * kPerThread) return f(Lanes<32>{});
+  if (width <= 64 * kPerThread) return f(Lanes<64>{});
+  if (width <= 128 * kPerThread) return f(Lanes<128>{});
+  if (width <= 256 * kPerThread) return f(Lanes<256>{});
+  if (width <= 512 * kPerThread) return f(Lanes<512>{});
+  return f(Lanes<1024>{});
+}
+
+bool rows_aligned(const void* p, int64_t ld, size_t size) {
+  return ((uintptr_t)p & 15u) == 0 && ld * (int64_t)size % 16 == 0;
+}
+
+template <typename T, int kLanes, bool kVec>
+cudaError_t forward(const LayerNormArgs& a, cudaStream_t stream) {
+  constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kShared = kVec ? forward_stages<T, kLanes>() * kThreads * kPerThread * (int)sizeof(T) : 0;
+  static std::atomic<int> kept[kKeptDevices];
+  int resident = 0;
+  const cudaError_t st =
+      resident_ctas(layer_norm_forward_kernel<T, kLanes, kVec>, kThreads, kShared, kShared, kept, &resident);
+  if (st != cudaSuccess) return st;
+  const int64_t blocks = min64(max64(resident / a.workers, 1), ceil_div(a.rows, kGroups));
+  return launch_pdl(layer_norm_forward_kernel<T, kLanes, kVec>, dim3((unsigned)blocks, (unsigned)a.workers),
+                    dim3(kThreads), kShared, stream, a);
+}
+
+template <typename T, int kLanes, bool kVec>
+cudaError_t backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches) {
+  constexpr int kThreads = backward_threads<T, kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kStages = backward_stages<T, kLanes>();
+  constexpr int kRing = kVec && kStages >= 3 ? kStages * 2 * kThreads * kPerThread * (int)sizeof(T) : 0;
+  constexpr int kSums = kGroups > 1 ? kThreads * kPerThread * 4 : 0;
+  constexpr int kShared = kRing > kSums ? kRing : kSums;
+  static std::atomic<int> kept[kKeptDevices];
+  int resident = 0;
+  cudaError_t st = resident_ctas(layer_norm_backward_kernel<T, kLanes, kVec>, kThreads, kShared, kShared, kept, &resident);
+  if (st != cudaSuccess) return st;
+  const bool sums = a.dweight || a.dbias;
+  const int64_t most = sums ? backward_blocks(a.workers) : max64(a.workers, resident);
+  const int64_t parts = max64(1, min64(most / a.workers, ceil_div(a.rows, kGroups)));
+  ++*launches;
+  st = launch_pdl(layer_norm_backward_kernel<T, kLanes, kVec>, dim3((unsigned)parts, (unsigned)a.workers), dim3(kThreads),
+                  kShared, stream, a);
+  if (st != cudaSuccess || !sums || parts == 1) return st;
+  ++*launches;
+  return launch_pdl(layer_norm_join_kernel, dim3((unsigned)ceil_div(a.width, 32), (unsigned)a.workers, 2),
+                    dim3(kJoinWarps * 32), 0, stream, a, (int)parts);
+}
+
 }  // namespace
 
-size_t layer_norm_scratch_bytes(int64_t, int32_t) { return 0; }
+size_t layer_norm_scratch_bytes(int64_t width, int32_t workers) {
+  return width <= kMaxOnChip ? 8 * (size_t)width * (size_t)backward_blocks(workers) : 0;
+}
 
 cudaError_t launch_layer_norm_forward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches) {
   const int64_t rows = a.rows * a.workers;
   if (rows == 0) return cudaSuccess;
   ++*launches;
   return with_dtype(a.dtype, [&](auto t) {
-    return launch_pdl(layer_norm_forward_kernel<decltype(t)>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
+    using T = decltype(t);
+    if (a.width > kMaxOnChip)
+      return launch_pdl(layer_norm_forward_long_kernel<T>, dim3((unsigned)rows), dim3(kLongThreads), 0, stream, a);
+    const bool vec = rows_aligned(a.x, a.x_ld, sizeof(T)) && rows_aligned(a.out, a.out_ld, sizeof(T));
+    return with_lanes(a.width, [&](auto lanes) {
+      constexpr int kLanes = decltype(lanes)::value;
+      return vec ? forward<T, kLanes, true>(a, stream) : forward<T, kLanes, false>(a, stream);
+    });
   });
 }
 
@@ -120,16 +701,24 @@ cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, cudaStream_t stre
   const int64_t rows = a.rows * a.workers;
   return with_dtype(a.dtype, [&](auto t) {
     using T = decltype(t);
+    if (a.width <= kMaxOnChip) {
+      const bool vec = rows_aligned(a.x, a.x_ld, sizeof(T)) && rows_aligned(a.dy, a.dy_ld, sizeof(T)) &&
+                       (!a.out || rows_aligned(a.out, a.out_ld, sizeof(T)));
+      return with_lanes(a.width, [&](auto lanes) {
+        constexpr int kLanes = decltype(lanes)::value;
+        return vec ? backward<T, kLanes, true>(a, stream, launches) : backward<T, kLanes, false>(a, stream, launches);
+      });
+    }
     // the parameters' gradients first: dx may be dy
     if (a.dweight || a.dbias) {
       ++*launches;
-      const cudaError_t st = launch_pdl(layer_norm_dparams_kernel<T>, dim3((unsigned)ceil_div(a.width, 32), a.workers),
-                                        dim3(kThreads), 0, stream, a);
+      const cudaError_t st = launch_pdl(layer_norm_dparams_long_kernel<T>,
+                                        dim3((unsigned)ceil_div(a.width, 32), a.workers), dim3(256), 0, stream, a);
       if (st != cudaSuccess) return st;
     }
     if (!a.out || rows == 0) return cudaSuccess;
     ++*launches;
-    return launch_pdl(layer_norm_dx_kernel<T>, dim3((unsigned)rows), dim3(kThreads), 0, stream, a);
+    return launch_pdl(layer_norm_dx_long_kernel<T>, dim3((unsigned)rows), dim3(kLongThreads), 0, stream, a);
   });
 }
 
