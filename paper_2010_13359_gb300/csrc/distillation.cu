@@ -3,7 +3,13 @@
 //
 //   p_k = exp(t_k / T - L), q = softmax(z / T), P = sum p_k
 //   loss = c T^2 sum p_k (log p_k - log q_id_k), dz = scale c T (P q - p at the ids)
+//
+// Bound by memory: the logits in, the gradient out, and about five operations and
+// one exponential a value for each of the two passes over a row (its softmax's
+// maximum and sum, then the gradient).  So a row is read once and held in
+// registers between them.
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "operators.cuh"
@@ -13,6 +19,21 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxEntries = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float teacher_value(const DistillationArgs& a, int64_t row, int k) {
+  const int64_t i = row * a.teacher_ld + k;
+  if (a.teacher_dtype == DQGAN_F32) return static_cast<const float*>(a.values)[i];
+  if (a.teacher_dtype == DQGAN_BF16) return to_float(static_cast<const __nv_bfloat16*>(a.values)[i]);
+  return to_float(static_cast<const __half*>(a.values)[i]);
+}
+
+// 2^x, subnormal results flushed to 0.
+__device__ __forceinline__ float exp2_ftz(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 __device__ __forceinline__ float block_max(float x, float* shared) {
 #pragma unroll
@@ -25,9 +46,11 @@ __device__ __forceinline__ float block_max(float x, float* shared) {
   return x;
 }
 
-// One block per row.
-template <typename T, typename E, DistillationWay kWay>
-__global__ void __launch_bounds__(kThreads) distillation_kernel(DistillationArgs a) {
+// Rows that do not fit on chip: one block each, which reads its row once for the
+// maximum, once for the sum and once for the gradient, the later times out of the
+// L2 as far as that holds them.
+template <typename T, DistillationWay kWay>
+__global__ void __launch_bounds__(kThreads) distillation_long_kernel(DistillationArgs a) {
   dq_pdl_enter();
   __shared__ float shared[32];
   __shared__ int32_t id[kMaxEntries];
@@ -42,7 +65,7 @@ __global__ void __launch_bounds__(kThreads) distillation_kernel(DistillationArgs
   float most = -INFINITY;
   for (int k = threadIdx.x; k < a.k; k += kThreads) {
     const int32_t v = a.ids[row * a.teacher_ld + k];
-    const float t = to_float(static_cast<const E*>(a.values)[row * a.teacher_ld + k]) * inv_t;
+    const float t = teacher_value(a, row, k) * inv_t;
     const bool there = v >= 0 && v < a.vocab && t != -INFINITY;
     id[k] = there ? v : -1;
     p[k] = there ? t : -INFINITY;
@@ -131,12 +154,349 @@ __global__ void __launch_bounds__(kThreads) distillation_kernel(DistillationArgs
   }
 }
 
-template <typename T, typename E>
-cudaError_t launch(const DistillationArgs& a, DistillationWay way, cudaStream_t stream) {
-  auto kernel = way == DistillationWay::kForward    ? distillation_kernel<T, E, DistillationWay::kForward>
-                : way == DistillationWay::kBackward ? distillation_kernel<T, E, DistillationWay::kBackward>
-                                                    : distillation_kernel<T, E, DistillationWay::kStep>;
-  return launch_pdl(kernel, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
+// The kernel for rows of up to kMaxPacks 16-byte packs a thread: a row belongs to
+// a cluster of `pieces` blocks (1, 2, 4 or 8), each of which holds its piece in
+// registers.  A warp takes its own maximum and sum of exponentials and writes the
+// pair to every block of the cluster; one cluster barrier later each block joins
+// all pairs and turns its registers into the gradient.  The block's last warp
+// prepares the teacher's entries meanwhile.  Two to sixteen blocks share an SM,
+// so one's loads overlap another's arithmetic.
+//
+// Rows need not start on 16-byte boundaries: packs are aligned ones, the first and
+// last of a row partly its neighbours', whose values are masked and not written.
+constexpr int kMaxPacks = 8;
+
+template <typename T>
+struct Packs {
+  static constexpr int E = 16 / (int)sizeof(T);
+
+  static __device__ __forceinline__ float value(const uint4& p, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(reinterpret_cast<const uint32_t*>(&p)[e]);
+    else return to_float(reinterpret_cast<const T*>(&p)[e]);
+  }
+
+  static __device__ __forceinline__ uint32_t lowest() {  // -inf, in every element of a word
+    return sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+  }
+
+  static __device__ __forceinline__ float max_of(const uint4& p) {  // NaN where nothing else
+    if constexpr (sizeof(T) == 4) {
+      return fmaxf(fmaxf(value(p, 0), value(p, 1)), fmaxf(value(p, 2), value(p, 3)));
+    } else if constexpr (std::is_same<T, __half>::value) {
+      const __half2* v = reinterpret_cast<const __half2*>(&p);
+      const __half2 m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    } else {
+      const __nv_bfloat162* v = reinterpret_cast<const __nv_bfloat162*>(&p);
+      const __nv_bfloat162 m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    }
+  }
+};
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFullMask, x, o);
+  return x;
+}
+__device__ __forceinline__ float warp_max(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(kFullMask, x, o));
+  return x;
+}
+
+// What a block's last warp makes of the teacher's entries, for the block's piece
+// [lo, hi) of the vocabulary.  Arrays of k: logp (log p, or -inf where there is no entry), z (the logits at the
+// ids), at (the id where this entry is the first with it and in the piece, else
+// -1), sum (p summed over the id's entries, at its first).
+struct Teacher {
+  float* logp;
+  float* z;
+  int32_t* at;
+  float* sum;
+  int32_t* table;  // table_size slots: entry + 1, or 0
+  int32_t table_size;
+};
+__host__ __device__ constexpr int32_t table_size(int32_t k) {
+  int32_t n = 32;
+  while (n < 2 * k) n *= 2;
+  return n;
+}
+__host__ __device__ constexpr int32_t teacher_bytes(int32_t k) { return 16 * k + 4 * table_size(k); }
+
+// Returns sum p_k (the same in every lane; 0 where the row has no entry).
+template <typename T>
+__device__ __forceinline__ float prepare_teacher(const DistillationArgs& a, int64_t row, const Teacher& t, int lo,
+                                                 int hi, bool want_all, const T* z) {
+  const int lane = threadIdx.x & 31;
+  const float inv_t = 1.f / a.temperature;
+  float most = -INFINITY;
+  for (int k = lane; k < a.k; k += 32) {
+    const int32_t id = a.ids[row * a.teacher_ld + k];
+    float v = teacher_value(a, row, k) * inv_t;
+    const bool there = id >= 0 && id < a.vocab && v != -INFINITY;
+    if (!there) v = -INFINITY;
+    most = fmaxf(most, v);
+    t.logp[k] = v;
+    const bool mine = there && id >= lo && id < hi;
+    t.at[k] = mine ? id : -1;
+    t.z[k] = there && (mine || want_all) ? to_float(z[id]) : 0.f;
+  }
+  for (int i = lane; i < t.table_size; i += 32) t.table[i] = 0;
+  most = warp_max(most);
+  if (most == -INFINITY) return 0.f;
+  float lse;
+  if (a.teacher_lse) {
+    lse = a.teacher_lse[row];
+  } else {
+    float s = 0.f;
+    for (int k = lane; k < a.k; k += 32) s += exp2_ftz((t.logp[k] - most) * kLog2e);
+    lse = most + logf(warp_sum(s));
+  }
+  __syncwarp();
+  float mass = 0.f;
+  for (int k0 = 0; k0 < a.k; k0 += 32) {
+    const int k = k0 + lane;
+    const float logp = k < a.k ? t.logp[k] - lse : -INFINITY;
+    const float p = exp2_ftz(logp * kLog2e);
+    mass += p;
+    if (k < a.k) t.logp[k] = logp;
+    // an id's entries are joined at the first: within these 32 by lane, with
+    // earlier ones through the table (one lane an id at a time, so that its sum has one order)
+    const int32_t id = k < a.k ? t.at[k] : -1;
+    const unsigned same = __match_any_sync(kFullMask, id);
+    const bool leads = id >= 0 && __ffs(same) - 1 == lane;
+    float joined = p;
+    if (__any_sync(kFullMask, id >= 0 && (same & (same - 1)) != 0))
+      for (int l = 0; l < 32; ++l) {
+        const float other = __shfl_sync(kFullMask, p, l);
+        if (l != lane && (same >> l & 1u)) joined += other;
+      }
+    int first = -1;
+    if (leads) {
+      unsigned slot = (unsigned)id * 2654435761u >> 16;
+      for (;;) {
+        slot &= (unsigned)t.table_size - 1u;
+        int32_t found = t.table[slot];
+        if (found == 0) found = atomicCAS(t.table + slot, 0, k + 1);
+        if (found == 0) {
+          first = k;
+          break;
+        }
+        if (t.at[found - 1] == id) {
+          first = found - 1;
+          break;
+        }
+        ++slot;
+      }
+    }
+    __syncwarp();
+    if (leads && first == k) t.sum[k] = joined;
+    if (leads && first != k) t.sum[first] += joined;
+    if (k < a.k && !(leads && first == k)) t.at[k] = -1;
+    __syncwarp();
+  }
+  return warp_sum(mass);
+}
+
+template <typename T, DistillationWay kWay, int kBlock>
+__global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(DistillationArgs a, int pieces) {
+  dq_pdl_enter();
+  using P = Packs<T>;
+  constexpr int E = P::E, kWarps = kBlock / 32;
+  constexpr bool kStats = kWay != DistillationWay::kBackward;
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ float2 pairs[kStats ? 8 * kWarps : 1];  // (maximum, sum) of every warp of the cluster
+  __shared__ float mass_of_row;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int piece = blockIdx.x % pieces;
+  const int64_t row = blockIdx.x / pieces;
+  const T* z = static_cast<const T*>(a.logits) + row * a.ld;
+  T* dz = kWay == DistillationWay::kForward ? nullptr : static_cast<T*>(a.dlogits) + row * a.dld;
+  const int shift = (int)((uintptr_t)z % 16 / sizeof(T));  // values of the first pack before the row
+  const int vocab = (int)a.vocab, packs = (shift + vocab + E - 1) / E;
+  const int p_lo = packs / pieces * piece + min(piece, packs % pieces);
+  const int p_hi = packs / pieces * (piece + 1) + min(piece + 1, packs % pieces);
+  const int lo = max(p_lo * E - shift, 0), hi = min(p_hi * E - shift, vocab);
+  const uint4* from = reinterpret_cast<const uint4*>(z - shift);
+  const bool same_shift = (uintptr_t)z % 16 == (uintptr_t)dz % 16;
+
+  const auto put = [&](int pack, const uint4& v) {
+    const int first = pack * E - shift;
+    if (same_shift && first >= 0 && first + E <= vocab) {
+      __stcs(reinterpret_cast<uint4*>(dz + first), v);
+    } else {
+      const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (first + i >= 0 && first + i < vocab) dz[first + i] = e[i];
+    }
+  };
+
+  const float c = a.weights ? a.weights[row] : 1.f;
+  if (c == 0.f) {
+    if (kStats && piece == 0 && threadIdx.x == 0) {
+      a.loss[row] = 0.f;
+      if (a.lse) a.lse[row] = 0.f;
+    }
+    if (kWay != DistillationWay::kForward)
+      for (int p = p_lo + (int)threadIdx.x; p < p_hi; p += kBlock) put(p, make_uint4(0, 0, 0, 0));
+    return;
+  }
+
+  uint4 x[kMaxPacks];
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kMaxPacks; ++i) {
+    const int p = p_lo + (int)threadIdx.x + i * kBlock;
+    x[i] = make_uint4(P::lowest(), P::lowest(), P::lowest(), P::lowest());
+    if (p < p_hi) x[i] = __ldcs(from + p);
+  }
+  Teacher t;
+  t.table_size = table_size(a.k);
+  t.table = reinterpret_cast<int32_t*>(dynamic);
+  t.logp = reinterpret_cast<float*>(t.table + t.table_size);
+  t.z = t.logp + a.k;
+  t.sum = t.z + a.k;
+  t.at = reinterpret_cast<int32_t*>(t.sum + a.k);
+  if (warp == kWarps - 1) {
+    const float mass = prepare_teacher(a, row, t, lo, hi, kStats && piece == 0, z);
+    if (lane == 0) mass_of_row = mass;
+  }
+  // neighbours' values in the row's first and last packs
+#pragma unroll
+  for (int i = 0; i < kMaxPacks; ++i) {
+    const int p = p_lo + (int)threadIdx.x + i * kBlock, first = p * E - shift;
+    if (p < p_hi && (first < 0 || first + E > vocab)) {
+      T* e = reinterpret_cast<T*>(&x[i]);
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
+    }
+  }
+
+  // a value's q: exp2((v * mul + add) * by) * (1 / sum), in that order: the difference first, so that
+  // the type's lowest values do not overflow
+  const float inv_t = 1.f / a.temperature;
+  float mul = 1.f, add, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f;
+  if (kStats) {
+#pragma unroll
+    for (int i = 0; i < kMaxPacks; ++i) top = fmaxf(top, P::max_of(x[i]));
+    top = warp_max(top);
+    const float at = top == -INFINITY ? 0.f : top;  // nothing but -inf in this warp: a sum of 0
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxPacks; ++i) {
+      if (p_lo + (int)threadIdx.x + i * kBlock >= p_hi) break;
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        s0 += exp2_ftz((P::value(x[i], e) - at) * by);
+        s1 += exp2_ftz((P::value(x[i], e + 1) - at) * by);
+      }
+    }
+    const float sum = warp_sum(s0 + s1);
+    if (pieces == 1) {
+      if (lane == 0) pairs[warp] = make_float2(top, sum);
+      __syncthreads();
+    } else {
+      if (lane < pieces) {
+        const uint32_t mine = smem_addr(pairs + piece * kWarps + warp);
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(top), "f"(sum) : "memory");
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    // every warp joins the pairs, in the same order
+    const int n = pieces * kWarps;
+    float most = -INFINITY;
+    for (int i = lane; i < n; i += 32) most = fmaxf(most, pairs[i].x);
+    top = warp_max(most);
+    float total = 0.f;
+    for (int i = lane; i < n; i += 32) {
+      const float2 pair = pairs[i];
+      // a sum of 0 stays out: its maximum is -inf; a NaN goes in
+      if (pair.y != 0.f) total = fmaf(pair.y, exp2_ftz((pair.x - top) * by), total);
+    }
+    total = warp_sum(total);
+    add = -top;
+    inv_sum = 1.f / total;
+    log_sum = logf(total);
+    if (top == -INFINITY) inv_sum = log_sum = NAN;
+  } else {
+    __syncthreads();
+    mul = inv_t;
+    add = -a.lse[row];
+    by = kLog2e;
+  }
+  const float mass = mass_of_row;
+
+  if (kStats && piece == 0 && warp == 0) {
+    float loss = 0.f;
+    if (mass > 0.f)
+      for (int k = lane; k < a.k; k += 32) {
+        const float logp = t.logp[k];
+        const float p = exp2_ftz(logp * kLog2e);
+        if (p > 0.f) loss = fmaf(p, logp - ((t.z[k] - top) * inv_t - log_sum), loss);
+      }
+    loss = warp_sum(loss);
+    if (lane == 0) {
+      a.loss[row] = mass > 0.f ? c * a.temperature * a.temperature * loss : 0.f;
+      if (a.lse) a.lse[row] = mass > 0.f ? fmaf(top, inv_t, log_sum) : 0.f;
+    }
+  }
+  if (kWay == DistillationWay::kForward) return;
+
+  const float factor = a.scale * c * a.temperature, coef = factor * mass * inv_sum;
+  const bool none = !(mass > 0.f);
+#pragma unroll
+  for (int i = 0; i < kMaxPacks; ++i) {
+    const int p = p_lo + (int)threadIdx.x + i * kBlock;
+    if (p >= p_hi) break;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (!none) {
+      T* e = reinterpret_cast<T*>(&v);
+#pragma unroll
+      for (int j = 0; j < E; ++j) e[j] = from_float<T>(exp2_ftz(fmaf(P::value(x[i], j), mul, add) * by) * coef);
+    }
+    put(p, v);
+  }
+  if (none) return;
+  __syncthreads();  // the entries' own gradients over what was written there
+  for (int k = threadIdx.x; k < a.k; k += kBlock)
+    if (t.at[k] >= 0)
+      dz[t.at[k]] = from_float<T>(fmaf(exp2_ftz(fmaf(t.z[k], mul, add) * by), coef, -factor * t.sum[k]));
+}
+
+template <typename T, DistillationWay kWay, int kBlock>
+cudaError_t launch_held(const DistillationArgs& a, int pieces, cudaStream_t stream) {
+  const bool cluster = kWay != DistillationWay::kBackward;
+  return launch_pdl_cluster(distillation_kernel<T, kWay, kBlock>, cluster ? pieces : 1,
+                            dim3((unsigned)(a.rows * pieces)), dim3(kBlock), (size_t)teacher_bytes(a.k), stream, a,
+                            pieces);
+}
+
+template <typename T, DistillationWay kWay>
+cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
+  constexpr int64_t E = 16 / (int64_t)sizeof(T);
+  const int64_t packs = a.vocab / E + 2;  // at most, with the row's first and last in part
+  // the smallest block that holds a row; above 512 threads, more blocks
+  int block = 64, pieces = 1;
+  while (block < 512 && packs > (int64_t)block * kMaxPacks) block *= 2;
+  while (pieces < 8 && packs > (int64_t)block * kMaxPacks * pieces) pieces *= 2;
+  if (packs > (int64_t)block * kMaxPacks * pieces) block = 1024;
+  if (packs > (int64_t)block * kMaxPacks * pieces)
+    return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
+  // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle
+  while (pieces < 8 && a.rows * pieces * 2 <= device_sms() && packs > (int64_t)block * pieces) pieces *= 2;
+  switch (block) {
+    case 64: return launch_held<T, kWay, 64>(a, pieces, stream);
+    case 128: return launch_held<T, kWay, 128>(a, pieces, stream);
+    case 256: return launch_held<T, kWay, 256>(a, pieces, stream);
+    case 512: return launch_held<T, kWay, 512>(a, pieces, stream);
+  }
+  return launch_held<T, kWay, 1024>(a, pieces, stream);
 }
 
 }  // namespace
@@ -146,7 +506,13 @@ cudaError_t launch_distillation(const DistillationArgs& a, DistillationWay way, 
   if (a.rows == 0) return cudaSuccess;
   ++*launches;
   return with_dtype(a.dtype, [&](auto t) {
-    return with_dtype(a.teacher_dtype, [&](auto e) { return launch<decltype(t), decltype(e)>(a, way, stream); });
+    using T = decltype(t);
+    switch (way) {
+      case DistillationWay::kForward: return launch<T, DistillationWay::kForward>(a, stream);
+      case DistillationWay::kBackward: return launch<T, DistillationWay::kBackward>(a, stream);
+      case DistillationWay::kStep: return launch<T, DistillationWay::kStep>(a, stream);
+    }
+    return cudaErrorInvalidValue;
   });
 }
 
