@@ -154,17 +154,21 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
   }
 }
 
-// The kernel for rows of up to kMaxPacks 16-byte packs a thread: a row belongs to
-// a cluster of `pieces` blocks (1, 2, 4 or 8), each of which holds its piece in
-// registers.  A warp takes its own maximum and sum of exponentials and writes the
-// pair to every block of the cluster; one cluster barrier later each block joins
-// all pairs and turns its registers into the gradient.  The block's last warp
-// prepares the teacher's entries meanwhile.  Two to sixteen blocks share an SM,
-// so one's loads overlap another's arithmetic.
+// The kernel for rows that fit on chip: a row belongs to a cluster of `pieces`
+// blocks (1 to 8), each of which holds its piece in shared memory, every worker
+// thread the packs that it copied there itself.  A warp takes its own maximum and
+// sum of exponentials and writes the pair to every block of the cluster; one
+// cluster barrier later each block joins all pairs and turns its packs into the
+// gradient.  One more warp prepares the teacher's entries meanwhile (as a
+// worker's extra task that took half of the block's time at the barrier).  Three
+// blocks or more share an SM, so one's loads overlap another's arithmetic.
 //
 // Rows need not start on 16-byte boundaries: packs are aligned ones, the first and
 // last of a row partly its neighbours', whose values are masked and not written.
-constexpr int kMaxPacks = 8;
+constexpr int kPacksPerThread = 16;  // about: what a warp does once a row costs it as much as 6 packs
+constexpr int kMostWorkers = 256;
+constexpr int kPieceBytes = kMostWorkers * kPacksPerThread * 16;
+constexpr int kMostShared = 220 << 10;
 
 template <typename T>
 struct Packs {
@@ -205,7 +209,7 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
-// What a block's last warp makes of the teacher's entries, for the block's piece
+// What a block's extra warp makes of the teacher's entries, for the block's piece
 // [lo, hi) of the vocabulary.  Arrays of k: logp (log p, or -inf where there is no entry), z (the logits at the
 // ids), at (the id where this entry is the first with it and in the piece, else
 // -1), sum (p summed over the id's entries, at its first).
@@ -231,16 +235,31 @@ __device__ __forceinline__ float prepare_teacher(const DistillationArgs& a, int6
   const int lane = threadIdx.x & 31;
   const float inv_t = 1.f / a.temperature;
   float most = -INFINITY;
-  for (int k = lane; k < a.k; k += 32) {
-    const int32_t id = a.ids[row * a.teacher_ld + k];
-    float v = teacher_value(a, row, k) * inv_t;
-    const bool there = id >= 0 && id < a.vocab && v != -INFINITY;
-    if (!there) v = -INFINITY;
-    most = fmaxf(most, v);
-    t.logp[k] = v;
-    const bool mine = there && id >= lo && id < hi;
-    t.at[k] = mine ? id : -1;
-    t.z[k] = there && (mine || want_all) ? to_float(z[id]) : 0.f;
+  for (int k0 = lane; k0 < a.k; k0 += 128) {  // four loads of each kind on their way at once
+    int32_t id[4];
+    float v[4], x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k0 + 32 * i;
+      id[i] = k < a.k ? a.ids[row * a.teacher_ld + k] : -1;
+      v[i] = k < a.k ? teacher_value(a, row, k) * inv_t : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (id[i] >= a.vocab || v[i] == -INFINITY) id[i] = -1;
+      const bool mine = id[i] >= lo && id[i] < hi;
+      x[i] = id[i] >= 0 && (mine || want_all) ? to_float(z[id[i]]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k0 + 32 * i;
+      if (id[i] < 0) v[i] = -INFINITY;
+      most = fmaxf(most, v[i]);
+      if (k >= a.k) continue;
+      t.logp[k] = v[i];
+      t.at[k] = id[i] >= lo && id[i] < hi ? id[i] : -1;
+      t.z[k] = x[i];
+    }
   }
   for (int i = lane; i < t.table_size; i += 32) t.table[i] = 0;
   most = warp_max(most);
@@ -299,16 +318,18 @@ __device__ __forceinline__ float prepare_teacher(const DistillationArgs& a, int6
   return warp_sum(mass);
 }
 
-template <typename T, DistillationWay kWay, int kBlock>
-__global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(DistillationArgs a, int pieces) {
+template <typename T, DistillationWay kWay, int kWorkers>
+__global__ void __launch_bounds__(kWorkers + 32, 1536 / (kWorkers + 32))
+    distillation_kernel(DistillationArgs a, int pieces) {
   dq_pdl_enter();
   using P = Packs<T>;
-  constexpr int E = P::E, kWarps = kBlock / 32;
+  constexpr int E = P::E, kWarps = kWorkers / 32;
   constexpr bool kStats = kWay != DistillationWay::kBackward;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ float2 pairs[kStats ? 8 * kWarps : 1];  // (maximum, sum) of every warp of the cluster
+  __shared__ float2 pairs[kStats ? 8 * kWarps : 1];  // (maximum, sum) of every worker warp of the cluster
   __shared__ float mass_of_row;
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const bool works = warp < kWarps;
   const int piece = blockIdx.x % pieces;
   const int64_t row = blockIdx.x / pieces;
   const T* z = static_cast<const T*>(a.logits) + row * a.ld;
@@ -318,19 +339,34 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(Dis
   const int p_lo = packs / pieces * piece + min(piece, packs % pieces);
   const int p_hi = packs / pieces * (piece + 1) + min(piece + 1, packs % pieces);
   const int lo = max(p_lo * E - shift, 0), hi = min(p_hi * E - shift, vocab);
-  const uint4* from = reinterpret_cast<const uint4*>(z - shift);
   const bool same_shift = (uintptr_t)z % 16 == (uintptr_t)dz % 16;
-
-  const auto put = [&](int pack, const uint4& v) {
+  // a worker's packs: p_mine, p_mine + kWorkers, ... (n of them)
+  const int p_mine = p_lo + (int)threadIdx.x;
+  const int n = works && p_mine < p_hi ? (p_hi - p_mine + kWorkers - 1) / kWorkers : 0;
+  // packs that are the row's alone; the others are its first and last
+  const int f_lo = piece == 0 && shift > 0 ? p_lo + 1 : p_lo;
+  const int f_hi = piece == pieces - 1 && (shift + vocab) % E != 0 ? p_hi - 1 : p_hi;
+  const auto put_values = [&](int pack, const uint4& v) {
     const int first = pack * E - shift;
-    if (same_shift && first >= 0 && first + E <= vocab) {
-      __stcs(reinterpret_cast<uint4*>(dz + first), v);
-    } else {
-      const T* e = reinterpret_cast<const T*>(&v);
+    const T* e = reinterpret_cast<const T*>(&v);
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (first + i >= 0 && first + i < vocab) dz[first + i] = e[i];
+    for (int i = 0; i < E; ++i)
+      if (first + i >= 0 && first + i < vocab) dz[first + i] = e[i];
+  };
+  // writes gradient_of(i) at this thread's pack i for every i
+  const auto put_all = [&](auto&& gradient_of) {
+    if (!same_shift) {
+      for (int i = 0; i < n; ++i) put_values(p_mine + i * kWorkers, gradient_of(i));
+      return;
     }
+    uint4* to = reinterpret_cast<uint4*>(dz - shift) + p_mine;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const uint4 v = gradient_of(i);
+      if ((unsigned)(p_mine + i * kWorkers - f_lo) < (unsigned)(f_hi - f_lo)) __stcs(to + i * kWorkers, v);
+    }
+    if (n > 0 && p_mine < f_lo) put_values(p_mine, gradient_of(0));
+    if (n > 0 && p_mine + (n - 1) * kWorkers >= max(f_hi, f_lo)) put_values(p_mine + (n - 1) * kWorkers, gradient_of(n - 1));
   };
 
   const float c = a.weights ? a.weights[row] : 1.f;
@@ -340,18 +376,10 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(Dis
       if (a.lse) a.lse[row] = 0.f;
     }
     if (kWay != DistillationWay::kForward)
-      for (int p = p_lo + (int)threadIdx.x; p < p_hi; p += kBlock) put(p, make_uint4(0, 0, 0, 0));
+      put_all([](int) { return make_uint4(0, 0, 0, 0); });
     return;
   }
 
-  uint4 x[kMaxPacks];
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kMaxPacks; ++i) {
-    const int p = p_lo + (int)threadIdx.x + i * kBlock;
-    x[i] = make_uint4(P::lowest(), P::lowest(), P::lowest(), P::lowest());
-    if (p < p_hi) x[i] = __ldcs(from + p);
-  }
   Teacher t;
   t.table_size = table_size(a.k);
   t.table = reinterpret_cast<int32_t*>(dynamic);
@@ -359,62 +387,70 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(Dis
   t.z = t.logp + a.k;
   t.sum = t.z + a.k;
   t.at = reinterpret_cast<int32_t*>(t.sum + a.k);
-  if (warp == kWarps - 1) {
-    const float mass = prepare_teacher(a, row, t, lo, hi, kStats && piece == 0, z);
-    if (lane == 0) mass_of_row = mass;
-  }
-  // neighbours' values in the row's first and last packs
-#pragma unroll
-  for (int i = 0; i < kMaxPacks; ++i) {
-    const int p = p_lo + (int)threadIdx.x + i * kBlock, first = p * E - shift;
-    if (p < p_hi && (first < 0 || first + E > vocab)) {
-      T* e = reinterpret_cast<T*>(&x[i]);
-#pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
-    }
-  }
+  uint4* const held = reinterpret_cast<uint4*>(dynamic + teacher_bytes(a.k)) + threadIdx.x;  // this thread's packs
+  const uint4* from = reinterpret_cast<const uint4*>(z - shift) + p_mine;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) copy16_async(held + i * kWorkers, from + i * kWorkers, 16);
 
   // a value's q: exp2((v * mul + add) * by) * (1 / sum), in that order: the difference first, so that
   // the type's lowest values do not overflow
   const float inv_t = 1.f / a.temperature;
-  float mul = 1.f, add, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f;
-  if (kStats) {
+  float mul = 1.f, add = 0.f, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f, top = -INFINITY, sum = 0.f;
+  if (!works) {
+    const float mass = prepare_teacher(a, row, t, lo, hi, kStats && piece == 0, z);
+    if (lane == 0) mass_of_row = mass;
+  } else {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // neighbours' values in the row's first and last packs
+    const auto mask = [&](int i) {
+      const int first = (p_mine + i * kWorkers) * E - shift;
+      T* e = reinterpret_cast<T*>(held + i * kWorkers);
 #pragma unroll
-    for (int i = 0; i < kMaxPacks; ++i) top = fmaxf(top, P::max_of(x[i]));
-    top = warp_max(top);
-    const float at = top == -INFINITY ? 0.f : top;  // nothing but -inf in this warp: a sum of 0
-    float s0 = 0.f, s1 = 0.f;
+      for (int j = 0; j < E; ++j)
+        if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
+    };
+    if (n > 0 && p_mine < f_lo) mask(0);
+    if (n > 0 && p_mine + (n - 1) * kWorkers >= f_hi) mask(n - 1);
+    if (kStats) {
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) top = fmaxf(top, P::max_of(held[i * kWorkers]));
+      top = warp_max(top);
+      const float2 at = both(top == -INFINITY ? 0.f : -top);  // nothing but -inf in this warp: a sum of 0
+      float2 s = both(0.f);
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) {
+        const uint4 x = held[i * kWorkers];
 #pragma unroll
-    for (int i = 0; i < kMaxPacks; ++i) {
-      if (p_lo + (int)threadIdx.x + i * kBlock >= p_hi) break;
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        s0 += exp2_ftz((P::value(x[i], e) - at) * by);
-        s1 += exp2_ftz((P::value(x[i], e + 1) - at) * by);
+        for (int e = 0; e < E; e += 2) {
+          const float2 y = mul2(add2(pair_of<T>(x, e), at), both(by));
+          s = add2(s, make_float2(exp2_ftz(y.x), exp2_ftz(y.y)));
+        }
       }
+      sum = warp_sum(s.x + s.y);
     }
-    const float sum = warp_sum(s0 + s1);
+  }
+  if (kStats) {
     if (pieces == 1) {
-      if (lane == 0) pairs[warp] = make_float2(top, sum);
+      if (works && lane == 0) pairs[warp] = make_float2(top, sum);
       __syncthreads();
     } else {
-      if (lane < pieces) {
+      if (works && lane < pieces) {
         const uint32_t mine = smem_addr(pairs + piece * kWarps + warp);
         uint32_t there;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
         asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(top), "f"(sum) : "memory");
       }
+      __syncwarp();
       asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
       asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
     // every warp joins the pairs, in the same order
-    const int n = pieces * kWarps;
+    const int all = pieces * kWarps;
     float most = -INFINITY;
-    for (int i = lane; i < n; i += 32) most = fmaxf(most, pairs[i].x);
+    for (int i = lane; i < all; i += 32) most = fmaxf(most, pairs[i].x);
     top = warp_max(most);
     float total = 0.f;
-    for (int i = lane; i < n; i += 32) {
+    for (int i = lane; i < all; i += 32) {
       const float2 pair = pairs[i];
       // a sum of 0 stays out: its maximum is -inf; a NaN goes in
       if (pair.y != 0.f) total = fmaf(pair.y, exp2_ftz((pair.x - top) * by), total);
@@ -432,7 +468,7 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(Dis
   }
   const float mass = mass_of_row;
 
-  if (kStats && piece == 0 && warp == 0) {
+  if (kStats && piece == 0 && !works) {
     float loss = 0.f;
     if (mass > 0.f)
       for (int k = lane; k < a.k; k += 32) {
@@ -450,53 +486,55 @@ __global__ void __launch_bounds__(kBlock, 1024 / kBlock) distillation_kernel(Dis
 
   const float factor = a.scale * c * a.temperature, coef = factor * mass * inv_sum;
   const bool none = !(mass > 0.f);
-#pragma unroll
-  for (int i = 0; i < kMaxPacks; ++i) {
-    const int p = p_lo + (int)threadIdx.x + i * kBlock;
-    if (p >= p_hi) break;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (!none) {
-      T* e = reinterpret_cast<T*>(&v);
-#pragma unroll
-      for (int j = 0; j < E; ++j) e[j] = from_float<T>(exp2_ftz(fmaf(P::value(x[i], j), mul, add) * by) * coef);
-    }
-    put(p, v);
+  if (none) {
+    put_all([](int) { return make_uint4(0, 0, 0, 0); });
+    return;
   }
-  if (none) return;
+  put_all([&](int i) {
+    uint4 v = held[i * kWorkers];
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+      const float2 y = mul2(fma2(pair_of<T>(v, e), both(mul), both(add)), both(by));
+      set_pair<T>(v, e, mul2(make_float2(exp2_ftz(y.x), exp2_ftz(y.y)), both(coef)));
+    }
+    return v;
+  });
   __syncthreads();  // the entries' own gradients over what was written there
-  for (int k = threadIdx.x; k < a.k; k += kBlock)
+  for (int k = threadIdx.x; k < a.k; k += kWorkers + 32)
     if (t.at[k] >= 0)
       dz[t.at[k]] = from_float<T>(fmaf(exp2_ftz(fmaf(t.z[k], mul, add) * by), coef, -factor * t.sum[k]));
 }
 
-template <typename T, DistillationWay kWay, int kBlock>
-cudaError_t launch_held(const DistillationArgs& a, int pieces, cudaStream_t stream) {
+template <typename T, DistillationWay kWay, int kWorkers>
+cudaError_t launch_held(const DistillationArgs& a, int packs, int pieces, cudaStream_t stream) {
+  static std::atomic<int> kept[kKeptDevices];
+  const int shared = teacher_bytes(a.k) + 16 * (packs / pieces + 1);
+  int resident = 0;
+  const cudaError_t st =
+      resident_ctas(distillation_kernel<T, kWay, kWorkers>, kWorkers + 32, shared, kMostShared, kept, &resident);
+  if (st != cudaSuccess) return st;
   const bool cluster = kWay != DistillationWay::kBackward;
-  return launch_pdl_cluster(distillation_kernel<T, kWay, kBlock>, cluster ? pieces : 1,
-                            dim3((unsigned)(a.rows * pieces)), dim3(kBlock), (size_t)teacher_bytes(a.k), stream, a,
-                            pieces);
+  return launch_pdl_cluster(distillation_kernel<T, kWay, kWorkers>, cluster ? pieces : 1,
+                            dim3((unsigned)(a.rows * pieces)), dim3(kWorkers + 32), (size_t)shared, stream, a, pieces);
 }
 
 template <typename T, DistillationWay kWay>
 cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
-  constexpr int64_t E = 16 / (int64_t)sizeof(T);
-  const int64_t packs = a.vocab / E + 2;  // at most, with the row's first and last in part
-  // the smallest block that holds a row; above 512 threads, more blocks
-  int block = 64, pieces = 1;
-  while (block < 512 && packs > (int64_t)block * kMaxPacks) block *= 2;
-  while (pieces < 8 && packs > (int64_t)block * kMaxPacks * pieces) pieces *= 2;
-  if (packs > (int64_t)block * kMaxPacks * pieces) block = 1024;
-  if (packs > (int64_t)block * kMaxPacks * pieces)
+  constexpr int E = 16 / (int)sizeof(T);
+  const int packs = (int)(a.vocab / E + 2);  // at most, with the row's first and last in part
+  int workers = 32, pieces = 1;
+  while (workers < kMostWorkers && packs > workers * kPacksPerThread) workers *= 2;
+  while (pieces < 8 && packs * 16 > pieces * kPieceBytes) ++pieces;
+  if (16 * (packs / pieces + 1) + teacher_bytes(a.k) > kMostShared)
     return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle
-  while (pieces < 8 && a.rows * pieces * 2 <= device_sms() && packs > (int64_t)block * pieces) pieces *= 2;
-  switch (block) {
-    case 64: return launch_held<T, kWay, 64>(a, pieces, stream);
-    case 128: return launch_held<T, kWay, 128>(a, pieces, stream);
-    case 256: return launch_held<T, kWay, 256>(a, pieces, stream);
-    case 512: return launch_held<T, kWay, 512>(a, pieces, stream);
+  while (pieces < 8 && a.rows * (pieces + 1) <= device_sms() && packs > workers * pieces) ++pieces;
+  switch (workers) {
+    case 32: return launch_held<T, kWay, 32>(a, packs, pieces, stream);
+    case 64: return launch_held<T, kWay, 64>(a, packs, pieces, stream);
+    case 128: return launch_held<T, kWay, 128>(a, packs, pieces, stream);
   }
-  return launch_held<T, kWay, 1024>(a, pieces, stream);
+  return launch_held<T, kWay, kMostWorkers>(a, packs, pieces, stream);
 }
 
 }  // namespace

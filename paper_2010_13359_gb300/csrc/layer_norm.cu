@@ -19,75 +19,6 @@ namespace {
 constexpr int kPerThread = 16;  // values of a row in one thread
 constexpr int kMaxOnChip = 1024 * kPerThread;
 
-// Two fp32 operations in one instruction, each rounded as the single one.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<uint64_t&>(d))
-      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)),
-        "l"(reinterpret_cast<const uint64_t&>(c)));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("add.rn.f32x2 %0, %1, %2;"
-      : "=l"(reinterpret_cast<uint64_t&>(d))
-      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
-  return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;"
-      : "=l"(reinterpret_cast<uint64_t&>(d))
-      : "l"(reinterpret_cast<const uint64_t&>(a)), "l"(reinterpret_cast<const uint64_t&>(b)));
-  return d;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
-// Elements (e, e + 1) of a pack, and back.
-template <typename T>
-__device__ __forceinline__ float2 pair_of(const uint4& p, int e);
-template <>
-__device__ __forceinline__ float2 pair_of<float>(const uint4& p, int e) {
-  const float* v = reinterpret_cast<const float*>(&p);
-  return make_float2(v[e], v[e + 1]);
-}
-template <>
-__device__ __forceinline__ float2 pair_of<__nv_bfloat16>(const uint4& p, int e) {
-  const uint32_t v = reinterpret_cast<const uint32_t*>(&p)[e / 2];  // a bf16 is the upper half of an fp32
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-template <>
-__device__ __forceinline__ float2 pair_of<__half>(const uint4& p, int e) {
-  return __half22float2(reinterpret_cast<const __half2*>(&p)[e / 2]);
-}
-
-template <typename T>
-__device__ __forceinline__ void set_pair(uint4& p, int e, float2 v);
-template <>
-__device__ __forceinline__ void set_pair<float>(uint4& p, int e, float2 v) {
-  float* to = reinterpret_cast<float*>(&p);
-  to[e] = v.x;
-  to[e + 1] = v.y;
-}
-template <>
-__device__ __forceinline__ void set_pair<__nv_bfloat16>(uint4& p, int e, float2 v) {
-  reinterpret_cast<__nv_bfloat162*>(&p)[e / 2] = __float22bfloat162_rn(v);
-}
-template <>
-__device__ __forceinline__ void set_pair<__half>(uint4& p, int e, float2 v) {
-  reinterpret_cast<__half2*>(&p)[e / 2] = __float22half2_rn(v);
-}
-
-__device__ __forceinline__ void copy16_async(void* to, const void* from, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to)), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void wait_copies() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
-}
-
 // A thread's share of a row: N packs of E values.  kVec: pack i of lane t holds
 // values (i * kLanes + t) * E and the E - 1 after it; else (rows that do not
 // start on 16-byte boundaries) value e of pack i is (i * E + e) * kLanes + t, so
