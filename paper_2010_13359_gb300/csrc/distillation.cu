@@ -159,9 +159,11 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 // thread the packs that it copied there itself.  A warp takes its own maximum and
 // sum of exponentials and writes the pair to every block of the cluster; one
 // cluster barrier later each block joins all pairs and turns its packs into the
-// gradient.  One more warp prepares the teacher's entries meanwhile (as a
-// worker's extra task that took half of the block's time at the barrier).  Three
-// blocks or more share an SM, so one's loads overlap another's arithmetic.
+// gradient.  Clusters stay on the GPU and take row after row: as a thread has used
+// a pack for the last time it copies the next row's into its place.  One more warp
+// a block prepares the teacher's entries of the next row meanwhile (as a worker's
+// extra task that took half of the block's time at the barrier), and writes the
+// entries' own gradients when the workers are through.
 //
 // Rows need not start on 16-byte boundaries: packs are aligned ones, the first and
 // last of a row partly its neighbours', whose values are masked and not written.
@@ -318,204 +320,321 @@ __device__ __forceinline__ float prepare_teacher(const DistillationArgs& a, int6
   return warp_sum(mass);
 }
 
+// A block's part of a row.
+template <typename T, int kWorkers>
+struct Part {
+  static constexpr int E = 16 / (int)sizeof(T);
+  const T* z;
+  int shift;       // values of the row's first pack before the row
+  int p_lo, p_hi;  // the part's packs
+  int n;           // this thread's: p_lo + threadIdx.x, + kWorkers, ...
+
+  __device__ __forceinline__ Part(const DistillationArgs& a, int64_t row, int piece, int pieces) {
+    z = static_cast<const T*>(a.logits) + row * a.ld;
+    shift = (int)((uintptr_t)z % 16 / sizeof(T));
+    const int packs = (shift + (int)a.vocab + E - 1) / E;
+    p_lo = packs / pieces * piece + min(piece, packs % pieces);
+    p_hi = packs / pieces * (piece + 1) + min(piece + 1, packs % pieces);
+    const int left = p_hi - p_lo - (int)threadIdx.x;
+    n = threadIdx.x < kWorkers && left > 0 ? (left + kWorkers - 1) / kWorkers : 0;
+  }
+  __device__ __forceinline__ int pack(int i) const { return p_lo + (int)threadIdx.x + i * kWorkers; }
+  __device__ __forceinline__ const uint4* from() const { return reinterpret_cast<const uint4*>(z - shift) + pack(0); }
+  __device__ __forceinline__ int first_value() const { return max(p_lo * E - shift, 0); }
+  __device__ __forceinline__ int end_value(int vocab) const { return min(p_hi * E - shift, vocab); }
+  // packs that are the row's alone
+  __device__ __forceinline__ int full_lo() const { return p_lo * E < shift ? p_lo + 1 : p_lo; }
+  __device__ __forceinline__ int full_hi(int vocab) const { return p_hi * E - shift > vocab ? p_hi - 1 : p_hi; }
+};
+
+// Writes gradient_of(i), this thread's pack i, for every i.
+template <typename T, int kWorkers, typename F>
+__device__ __forceinline__ void put_all(const Part<T, kWorkers>& part, T* dz, int vocab, F&& gradient_of) {
+  constexpr int E = Part<T, kWorkers>::E;
+  const auto put_values = [&](int i, const uint4& v) {
+    const int first = part.pack(i) * E - part.shift;
+    const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+      if (first + j >= 0 && first + j < vocab) dz[first + j] = e[j];
+  };
+  if (((uintptr_t)dz ^ (uintptr_t)part.z) % 16 != 0) {
+    for (int i = 0; i < part.n; ++i) put_values(i, gradient_of(i));
+    return;
+  }
+  const int f_lo = part.full_lo(), f_hi = part.full_hi(vocab);
+  uint4* to = reinterpret_cast<uint4*>(dz - part.shift) + part.pack(0);
+#pragma unroll 4
+  for (int i = 0; i < part.n; ++i) {
+    const uint4 v = gradient_of(i);
+    const int p = part.pack(i);
+    if (p >= f_lo && p < f_hi) __stcs(to + i * kWorkers, v);
+    else put_values(i, v);
+  }
+}
+
+template <int kWorkers>
+constexpr int held_blocks() {  // on an SM, by registers
+  return 1024 / (kWorkers + 32);
+}
+
 template <typename T, DistillationWay kWay, int kWorkers>
-__global__ void __launch_bounds__(kWorkers + 32, 1536 / (kWorkers + 32))
+__global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
     distillation_kernel(DistillationArgs a, int pieces) {
   dq_pdl_enter();
   using P = Packs<T>;
+  using Mine = Part<T, kWorkers>;
   constexpr int E = P::E, kWarps = kWorkers / 32;
-  constexpr bool kStats = kWay != DistillationWay::kBackward;
+  constexpr bool kStats = kWay != DistillationWay::kBackward, kGradient = kWay != DistillationWay::kForward;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ float2 pairs[kStats ? 8 * kWarps : 1];  // (maximum, sum) of every worker warp of the cluster
-  __shared__ float mass_of_row;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  // (maximum, sum) of every worker warp of the cluster; a block may write a row's while another reads the row before's
+  __shared__ float2 pairs[2][kStats ? 8 * kWarps : 1];
+  __shared__ float masses[2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, vocab = (int)a.vocab;
   const bool works = warp < kWarps;
   const int piece = blockIdx.x % pieces;
-  const int64_t row = blockIdx.x / pieces;
-  const T* z = static_cast<const T*>(a.logits) + row * a.ld;
-  T* dz = kWay == DistillationWay::kForward ? nullptr : static_cast<T*>(a.dlogits) + row * a.dld;
-  const int shift = (int)((uintptr_t)z % 16 / sizeof(T));  // values of the first pack before the row
-  const int vocab = (int)a.vocab, packs = (shift + vocab + E - 1) / E;
-  const int p_lo = packs / pieces * piece + min(piece, packs % pieces);
-  const int p_hi = packs / pieces * (piece + 1) + min(piece + 1, packs % pieces);
-  const int lo = max(p_lo * E - shift, 0), hi = min(p_hi * E - shift, vocab);
-  const bool same_shift = (uintptr_t)z % 16 == (uintptr_t)dz % 16;
-  // a worker's packs: p_mine, p_mine + kWorkers, ... (n of them)
-  const int p_mine = p_lo + (int)threadIdx.x;
-  const int n = works && p_mine < p_hi ? (p_hi - p_mine + kWorkers - 1) / kWorkers : 0;
-  // packs that are the row's alone; the others are its first and last
-  const int f_lo = piece == 0 && shift > 0 ? p_lo + 1 : p_lo;
-  const int f_hi = piece == pieces - 1 && (shift + vocab) % E != 0 ? p_hi - 1 : p_hi;
-  const auto put_values = [&](int pack, const uint4& v) {
-    const int first = pack * E - shift;
-    const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (first + i >= 0 && first + i < vocab) dz[first + i] = e[i];
+  const int64_t first_row = blockIdx.x / pieces, stride = gridDim.x / pieces;
+  const auto teacher = [&](int parity) {
+    Teacher t;
+    t.table_size = table_size(a.k);
+    t.table = reinterpret_cast<int32_t*>(dynamic + parity * teacher_bytes(a.k));
+    t.logp = reinterpret_cast<float*>(t.table + t.table_size);
+    t.z = t.logp + a.k;
+    t.sum = t.z + a.k;
+    t.at = reinterpret_cast<int32_t*>(t.sum + a.k);
+    return t;
   };
-  // writes gradient_of(i) at this thread's pack i for every i
-  const auto put_all = [&](auto&& gradient_of) {
-    if (!same_shift) {
-      for (int i = 0; i < n; ++i) put_values(p_mine + i * kWorkers, gradient_of(i));
-      return;
-    }
-    uint4* to = reinterpret_cast<uint4*>(dz - shift) + p_mine;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const uint4 v = gradient_of(i);
-      if ((unsigned)(p_mine + i * kWorkers - f_lo) < (unsigned)(f_hi - f_lo)) __stcs(to + i * kWorkers, v);
-    }
-    if (n > 0 && p_mine < f_lo) put_values(p_mine, gradient_of(0));
-    if (n > 0 && p_mine + (n - 1) * kWorkers >= max(f_hi, f_lo)) put_values(p_mine + (n - 1) * kWorkers, gradient_of(n - 1));
-  };
-
-  const float c = a.weights ? a.weights[row] : 1.f;
-  if (c == 0.f) {
-    if (kStats && piece == 0 && threadIdx.x == 0) {
-      a.loss[row] = 0.f;
-      if (a.lse) a.lse[row] = 0.f;
-    }
-    if (kWay != DistillationWay::kForward)
-      put_all([](int) { return make_uint4(0, 0, 0, 0); });
-    return;
-  }
-
-  Teacher t;
-  t.table_size = table_size(a.k);
-  t.table = reinterpret_cast<int32_t*>(dynamic);
-  t.logp = reinterpret_cast<float*>(t.table + t.table_size);
-  t.z = t.logp + a.k;
-  t.sum = t.z + a.k;
-  t.at = reinterpret_cast<int32_t*>(t.sum + a.k);
-  uint4* const held = reinterpret_cast<uint4*>(dynamic + teacher_bytes(a.k)) + threadIdx.x;  // this thread's packs
-  const uint4* from = reinterpret_cast<const uint4*>(z - shift) + p_mine;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) copy16_async(held + i * kWorkers, from + i * kWorkers, 16);
-
-  // a value's q: exp2((v * mul + add) * by) * (1 / sum), in that order: the difference first, so that
-  // the type's lowest values do not overflow
+  uint4* const held = reinterpret_cast<uint4*>(dynamic + 2 * teacher_bytes(a.k)) + threadIdx.x;  // this thread's packs
   const float inv_t = 1.f / a.temperature;
-  float mul = 1.f, add = 0.f, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f, top = -INFINITY, sum = 0.f;
-  if (!works) {
-    const float mass = prepare_teacher(a, row, t, lo, hi, kStats && piece == 0, z);
-    if (lane == 0) mass_of_row = mass;
+
+  // the weights of this cluster's next 32 rows, a lane each
+  float some_weights = 0.f;
+  int64_t weights_at = -1;  // the first of those rows, by the cluster's count
+  const auto weight_of = [&](int64_t turn) {
+    if (!a.weights) return 1.f;
+    if (weights_at < 0 || turn - weights_at >= 32) {
+      weights_at = turn;
+      const int64_t row = first_row + (turn + lane) * stride;
+      some_weights = row < a.rows ? a.weights[row] : 0.f;
+    }
+    return __shfl_sync(kFullMask, some_weights, (int)(turn - weights_at));
+  };
+  // the next row from `turn` on that counts; those before it get their zeros
+  float next_c = 1.f;
+  const auto advance = [&](int64_t turn) {
+    for (;; ++turn) {
+      const int64_t row = first_row + turn * stride;
+      if (row >= a.rows) return turn;
+      next_c = weight_of(turn);
+      if (next_c != 0.f) return turn;
+      if (kStats && piece == 0 && threadIdx.x == 0) {
+        a.loss[row] = 0.f;
+        if (a.lse) a.lse[row] = 0.f;
+      }
+      if (kGradient)
+        put_all(Mine(a, row, piece, pieces), static_cast<T*>(a.dlogits) + row * a.dld, vocab,
+                [](int) { return make_uint4(0, 0, 0, 0); });
+    }
+  };
+  const auto prepare = [&](const Mine& part, int64_t row, int parity) {
+    const float mass = prepare_teacher(a, row, teacher(parity), part.first_value(), part.end_value(vocab),
+                                       kStats && piece == 0, part.z);
+    if (lane == 0) masses[parity] = mass;
+  };
+
+  int64_t turn = advance(0);
+  if (first_row + turn * stride >= a.rows) return;  // as the whole cluster does
+  Mine part(a, first_row + turn * stride, piece, pieces);
+  if (works) {
+#pragma unroll 4
+    for (int i = 0; i < part.n; ++i) copy16_async(held + i * kWorkers, part.from() + i * kWorkers, 16);
   } else {
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    // neighbours' values in the row's first and last packs
-    const auto mask = [&](int i) {
-      const int first = (p_mine + i * kWorkers) * E - shift;
-      T* e = reinterpret_cast<T*>(held + i * kWorkers);
-#pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
+    prepare(part, first_row + turn * stride, 0);
+  }
+  for (int parity = 0;; parity ^= 1) {
+    const int64_t row = first_row + turn * stride;
+    const float c = next_c;
+    T* const dz = kGradient ? static_cast<T*>(a.dlogits) + row * a.dld : nullptr;
+    // the row after this one: its packs follow into this one's places
+    const int64_t next_turn = advance(turn + 1);
+    const bool last = first_row + next_turn * stride >= a.rows;
+    const Mine next(a, last ? row : first_row + next_turn * stride, piece, pieces);
+    const int next_n = last ? 0 : next.n;
+    const uint4* const next_from = next.from();
+    const auto follow = [&](int i) {
+      if (i < next_n) copy16_async(held + i * kWorkers, next_from + i * kWorkers, 16);
     };
-    if (n > 0 && p_mine < f_lo) mask(0);
-    if (n > 0 && p_mine + (n - 1) * kWorkers >= f_hi) mask(n - 1);
-    if (kStats) {
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) top = fmaxf(top, P::max_of(held[i * kWorkers]));
-      top = warp_max(top);
-      const float2 at = both(top == -INFINITY ? 0.f : -top);  // nothing but -inf in this warp: a sum of 0
-      float2 s = both(0.f);
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const uint4 x = held[i * kWorkers];
+
+    // a value's q: exp2((v * mul + add) * by) * (1 / sum), in that order: the difference first, so that
+    // the type's lowest values do not overflow
+    float mul = 1.f, add = 0.f, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f, top = -INFINITY, sum = 0.f;
+    if (works) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      const auto mask = [&](int i) {  // neighbours' values in the row's first and last packs
+        const int first = part.pack(i) * E - part.shift;
+        T* e = reinterpret_cast<T*>(held + i * kWorkers);
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const float2 y = mul2(add2(pair_of<T>(x, e), at), both(by));
-          s = add2(s, make_float2(exp2_ftz(y.x), exp2_ftz(y.y)));
+        for (int j = 0; j < E; ++j)
+          if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
+      };
+      if (part.n > 0 && part.pack(0) < part.full_lo()) mask(0);
+      if (part.n > 0 && part.pack(part.n - 1) >= part.full_hi(vocab)) mask(part.n - 1);
+      if (kStats) {
+#pragma unroll 4
+        for (int i = 0; i < part.n; ++i) top = fmaxf(top, P::max_of(held[i * kWorkers]));
+        top = warp_max(top);
+        const float2 at = both(top == -INFINITY ? 0.f : -top);  // nothing but -inf in this warp: a sum of 0
+        float2 s = both(0.f);
+#pragma unroll 4
+        for (int i = 0; i < part.n; ++i) {
+          const uint4 x = held[i * kWorkers];
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const float2 y = mul2(add2(pair_of<T>(x, e), at), both(by));
+            s = add2(s, make_float2(exp2_ftz(y.x), exp2_ftz(y.y)));
+          }
+          if (!kGradient) follow(i);
+        }
+        sum = warp_sum(s.x + s.y);
+      }
+    }
+    if (kStats) {
+      if (pieces == 1) {
+        if (works && lane == 0) pairs[parity][warp] = make_float2(top, sum);
+        __syncthreads();
+      } else {
+        if (works && lane < pieces) {
+          const uint32_t mine = smem_addr(&pairs[parity][piece * kWarps + warp]);
+          uint32_t there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
+          asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(top), "f"(sum) : "memory");
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+      }
+      // every warp joins the pairs, in the same order
+      const int all = pieces * kWarps;
+      float most = -INFINITY;
+      for (int i = lane; i < all; i += 32) most = fmaxf(most, pairs[parity][i].x);
+      top = warp_max(most);
+      float total = 0.f;
+      for (int i = lane; i < all; i += 32) {
+        const float2 pair = pairs[parity][i];
+        // a sum of 0 stays out: its maximum is -inf; a NaN goes in
+        if (pair.y != 0.f) total = fmaf(pair.y, exp2_ftz((pair.x - top) * by), total);
+      }
+      total = warp_sum(total);
+      add = -top;
+      inv_sum = 1.f / total;
+      log_sum = logf(total);
+      if (top == -INFINITY) inv_sum = log_sum = NAN;
+    } else {
+      __syncthreads();
+      mul = inv_t;
+      add = -a.lse[row];
+      by = kLog2e;
+    }
+    const float mass = masses[parity];
+    const bool none = !(mass > 0.f);  // no entry
+    const float factor = a.scale * c * a.temperature, coef = factor * mass * inv_sum;
+    if (works) {
+      if (kGradient) {
+        if (none) {
+          put_all(part, dz, vocab, [](int) { return make_uint4(0, 0, 0, 0); });
+          for (int i = 0; i < part.n; ++i) follow(i);
+        } else {
+          put_all(part, dz, vocab, [&](int i) {
+            uint4 v = held[i * kWorkers];
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              const float2 y = mul2(fma2(pair_of<T>(v, e), both(mul), both(add)), both(by));
+              set_pair<T>(v, e, mul2(make_float2(exp2_ftz(y.x), exp2_ftz(y.y)), both(coef)));
+            }
+            follow(i);
+            return v;
+          });
+        }
+        asm volatile("bar.arrive 1, %0;" ::"n"(kWorkers + 32) : "memory");
+      }
+      for (int i = part.n; i < next_n; ++i) follow(i);
+    } else {
+      const Teacher t = teacher(parity);
+      if (kStats && piece == 0) {
+        float loss = 0.f;
+        if (!none)
+          for (int k = lane; k < a.k; k += 32) {
+            const float logp = t.logp[k];
+            const float p = exp2_ftz(logp * kLog2e);
+            if (p > 0.f) loss = fmaf(p, logp - ((t.z[k] - top) * inv_t - log_sum), loss);
+          }
+        loss = warp_sum(loss);
+        if (lane == 0) {
+          a.loss[row] = none ? 0.f : c * a.temperature * a.temperature * loss;
+          if (a.lse) a.lse[row] = none ? 0.f : fmaf(top, inv_t, log_sum);
         }
       }
-      sum = warp_sum(s.x + s.y);
-    }
-  }
-  if (kStats) {
-    if (pieces == 1) {
-      if (works && lane == 0) pairs[warp] = make_float2(top, sum);
-      __syncthreads();
-    } else {
-      if (works && lane < pieces) {
-        const uint32_t mine = smem_addr(pairs + piece * kWarps + warp);
-        uint32_t there;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
-        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(top), "f"(sum) : "memory");
+      if (!last) prepare(next, first_row + next_turn * stride, parity ^ 1);
+      if (kGradient) {
+        // the entries' own gradients over what the workers wrote there
+        asm volatile("bar.sync 1, %0;" ::"n"(kWorkers + 32) : "memory");
+        if (!none)
+          for (int k = lane; k < a.k; k += 32)
+            if (t.at[k] >= 0)
+              dz[t.at[k]] = from_float<T>(fmaf(exp2_ftz(fmaf(t.z[k], mul, add) * by), coef, -factor * t.sum[k]));
       }
-      __syncwarp();
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
-    // every warp joins the pairs, in the same order
-    const int all = pieces * kWarps;
-    float most = -INFINITY;
-    for (int i = lane; i < all; i += 32) most = fmaxf(most, pairs[i].x);
-    top = warp_max(most);
-    float total = 0.f;
-    for (int i = lane; i < all; i += 32) {
-      const float2 pair = pairs[i];
-      // a sum of 0 stays out: its maximum is -inf; a NaN goes in
-      if (pair.y != 0.f) total = fmaf(pair.y, exp2_ftz((pair.x - top) * by), total);
-    }
-    total = warp_sum(total);
-    add = -top;
-    inv_sum = 1.f / total;
-    log_sum = logf(total);
-    if (top == -INFINITY) inv_sum = log_sum = NAN;
-  } else {
-    __syncthreads();
-    mul = inv_t;
-    add = -a.lse[row];
-    by = kLog2e;
+    if (last) return;
+    turn = next_turn;
+    part = next;
   }
-  const float mass = mass_of_row;
+}
 
-  if (kStats && piece == 0 && !works) {
-    float loss = 0.f;
-    if (mass > 0.f)
-      for (int k = lane; k < a.k; k += 32) {
-        const float logp = t.logp[k];
-        const float p = exp2_ftz(logp * kLog2e);
-        if (p > 0.f) loss = fmaf(p, logp - ((t.z[k] - top) * inv_t - log_sum), loss);
-      }
-    loss = warp_sum(loss);
-    if (lane == 0) {
-      a.loss[row] = mass > 0.f ? c * a.temperature * a.temperature * loss : 0.f;
-      if (a.lse) a.lse[row] = mass > 0.f ? fmaf(top, inv_t, log_sum) : 0.f;
-    }
+// Clusters of `pieces` blocks that fit on the GPU at once.  Asked of the runtime
+// when the sizes differ from the last call's (a few microseconds).
+template <typename K>
+cudaError_t resident_clusters(K kern, int threads, int shared, int pieces, std::atomic<uint64_t> (&kept)[kKeptDevices],
+                              int* clusters) {
+  int dev = 0;
+  cudaError_t st = cudaGetDevice(&dev);
+  if (st != cudaSuccess) return st;
+  if (dev < 0 || dev >= kKeptDevices) return cudaErrorInvalidDevice;
+  const uint64_t key = (uint64_t)shared << 8 | (uint64_t)pieces, seen = kept[dev].load(std::memory_order_acquire);
+  if (seen >> 24 == key) {
+    *clusters = (int)(seen & 0xffffffu);
+    return cudaSuccess;
   }
-  if (kWay == DistillationWay::kForward) return;
-
-  const float factor = a.scale * c * a.temperature, coef = factor * mass * inv_sum;
-  const bool none = !(mass > 0.f);
-  if (none) {
-    put_all([](int) { return make_uint4(0, 0, 0, 0); });
-    return;
-  }
-  put_all([&](int i) {
-    uint4 v = held[i * kWorkers];
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      const float2 y = mul2(fma2(pair_of<T>(v, e), both(mul), both(add)), both(by));
-      set_pair<T>(v, e, mul2(make_float2(exp2_ftz(y.x), exp2_ftz(y.y)), both(coef)));
-    }
-    return v;
-  });
-  __syncthreads();  // the entries' own gradients over what was written there
-  for (int k = threadIdx.x; k < a.k; k += kWorkers + 32)
-    if (t.at[k] >= 0)
-      dz[t.at[k]] = from_float<T>(fmaf(exp2_ftz(fmaf(t.z[k], mul, add) * by), coef, -factor * t.sum[k]));
+  if ((st = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared)) != cudaSuccess)
+    return st;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)pieces;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3((unsigned)pieces);
+  lc.blockDim = dim3((unsigned)threads);
+  lc.dynamicSmemBytes = (size_t)shared;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  int n = 0;
+  if ((st = cudaOccupancyMaxActiveClusters(&n, kern, &lc)) != cudaSuccess) return st;
+  *clusters = n > 0 ? n : 1;
+  kept[dev].store(key << 24 | (uint64_t)*clusters, std::memory_order_release);
+  return cudaSuccess;
 }
 
 template <typename T, DistillationWay kWay, int kWorkers>
 cudaError_t launch_held(const DistillationArgs& a, int packs, int pieces, cudaStream_t stream) {
-  static std::atomic<int> kept[kKeptDevices];
-  const int shared = teacher_bytes(a.k) + 16 * (packs / pieces + 1);
-  int resident = 0;
-  const cudaError_t st =
-      resident_ctas(distillation_kernel<T, kWay, kWorkers>, kWorkers + 32, shared, kMostShared, kept, &resident);
+  static std::atomic<uint64_t> kept[kKeptDevices];
+  const int shared = 2 * teacher_bytes(a.k) + 16 * (packs / pieces + 1);
+  const int cluster = kWay == DistillationWay::kBackward ? 1 : pieces;  // its pieces exchange nothing
+  int clusters = 0;
+  const cudaError_t st = resident_clusters(distillation_kernel<T, kWay, kWorkers>, kWorkers + 32, shared, cluster, kept,
+                                           &clusters);
   if (st != cudaSuccess) return st;
-  const bool cluster = kWay != DistillationWay::kBackward;
-  return launch_pdl_cluster(distillation_kernel<T, kWay, kWorkers>, cluster ? pieces : 1,
-                            dim3((unsigned)(a.rows * pieces)), dim3(kWorkers + 32), (size_t)shared, stream, a, pieces);
+  const int64_t at_once = min64(a.rows, max64((int64_t)clusters * cluster / pieces, 1));
+  return launch_pdl_cluster(distillation_kernel<T, kWay, kWorkers>, cluster, dim3((unsigned)(at_once * pieces)),
+                            dim3(kWorkers + 32), (size_t)shared, stream, a, pieces);
 }
 
 template <typename T, DistillationWay kWay>
@@ -525,7 +644,7 @@ cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
   int workers = 32, pieces = 1;
   while (workers < kMostWorkers && packs > workers * kPacksPerThread) workers *= 2;
   while (pieces < 8 && packs * 16 > pieces * kPieceBytes) ++pieces;
-  if (16 * (packs / pieces + 1) + teacher_bytes(a.k) > kMostShared)
+  if (16 * (packs / pieces + 1) + 2 * teacher_bytes(a.k) > kMostShared)
     return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle
   while (pieces < 8 && a.rows * (pieces + 1) <= device_sms() && packs > workers * pieces) ++pieces;
