@@ -160,16 +160,16 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 // sum of exponentials and writes the pair to every block of the cluster; one
 // cluster barrier later each block joins all pairs and turns its packs into the
 // gradient.  Clusters stay on the GPU and take row after row: as a thread has used
-// a pack for the last time it copies the next row's into its place.  One more warp
-// a block prepares the teacher's entries of the next row meanwhile (as a worker's
-// extra task that took half of the block's time at the barrier), and writes the
-// entries' own gradients when the workers are through.
+// a pack for the last time it copies the next row's into its place.  Helper warps
+// (a quarter as many as workers, one at least) prepare the teacher's entries of the next row meanwhile, and write the
+// entries' own gradients when the workers are through: a single warp's latency on
+// 128 entries came close to the time of a row.
 //
-// Rows need not start on 16-byte boundaries: packs are aligned ones, the first and
-// last of a row partly its neighbours', whose values are masked and not written.
-constexpr int kPacksPerThread = 16;  // about: what a warp does once a row costs it as much as 6 packs
+// Rows need not start on 16-byte boundaries: packs are aligned ones that lie in the
+// row, and the values before the first and after the last pack belong to the first
+// helper warp, a lane each.
 constexpr int kMostWorkers = 256;
-constexpr int kPieceBytes = kMostWorkers * kPacksPerThread * 16;
+constexpr int kPieceBytes = 64 << 10;
 constexpr int kMostShared = 220 << 10;
 
 template <typename T>
@@ -211,113 +211,143 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
-// What a block's extra warp makes of the teacher's entries, for the block's piece
-// [lo, hi) of the vocabulary.  Arrays of k: logp (log p, or -inf where there is no entry), z (the logits at the
-// ids), at (the id where this entry is the first with it and in the piece, else
-// -1), sum (p summed over the id's entries, at its first).
+// What a block's helpers make of the teacher's entries, for the block's part
+// [lo, hi) of the vocabulary.  Arrays of k: t (an entry's t / T, or -inf where there
+// is none), z (the logits at the ids), at (the id where this entry stands for it and it is in the part, else
+// -1), sum (p summed over the id's entries, where `at` has it).
 struct Teacher {
-  float* logp;
+  float* t;
   float* z;
   int32_t* at;
   float* sum;
-  int32_t* table;  // table_size slots: entry + 1, or 0
-  int32_t table_size;
 };
-__host__ __device__ constexpr int32_t table_size(int32_t k) {
-  int32_t n = 32;
-  while (n < 2 * k) n *= 2;
-  return n;
-}
-__host__ __device__ constexpr int32_t teacher_bytes(int32_t k) { return 16 * k + 4 * table_size(k); }
+__host__ __device__ constexpr int32_t teacher_bytes(int32_t k) { return 16 * ((4 * k + 3) / 4); }
 
-// Returns sum p_k (the same in every lane; 0 where the row has no entry).
-template <typename T>
-__device__ __forceinline__ float prepare_teacher(const DistillationArgs& a, int64_t row, const Teacher& t, int lo,
-                                                 int hi, bool want_all, const T* z) {
-  const int lane = threadIdx.x & 31;
+template <int kHelpers>
+constexpr int helper_warps() {
+  return kHelpers / 32;
+}
+// What the helpers leave for a row beside the arrays.
+template <int kHelpers>
+struct TeacherTotals {
+  float lse;                                // L
+  float mass[helper_warps<kHelpers>()];     // sums of p of each helper warp
+  int32_t any[helper_warps<kHelpers>()];    // whether it had entries
+  float most[helper_warps<kHelpers>()], exps[helper_warps<kHelpers>()];  // on the way to L
+  int32_t twice;                            // whether an id of the part came more than once
+};
+
+template <int kHelpers>
+__device__ __forceinline__ void helpers_wait() {
+  __syncwarp();
+  if constexpr (kHelpers > 32) asm volatile("bar.sync 2, %0;" ::"n"(kHelpers) : "memory");
+}
+
+// seen: a bit for every value of the part.
+template <typename T, int kHelpers>
+__device__ __forceinline__ void prepare_teacher(const DistillationArgs& a, int64_t row, const Teacher& t,
+                                                TeacherTotals<kHelpers>& totals, uint4* seen, int me, int lo, int hi, bool want_all,
+                                                const T* z) {
+  const int lane = me & 31, warp = me / 32;
   const float inv_t = 1.f / a.temperature;
+  constexpr int kBatch = 2;  // loads of each kind on their way at once
   float most = -INFINITY;
-  for (int k0 = lane; k0 < a.k; k0 += 128) {  // four loads of each kind on their way at once
-    int32_t id[4];
-    float v[4], x[4];
+  bool any = false;
+  for (int k0 = me; k0 < a.k; k0 += kBatch * kHelpers) {
+    int32_t id[kBatch];
+    float v[kBatch], x[kBatch];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = k0 + 32 * i;
+    for (int i = 0; i < kBatch; ++i) {
+      const int k = k0 + kHelpers * i;
       id[i] = k < a.k ? a.ids[row * a.teacher_ld + k] : -1;
       v[i] = k < a.k ? teacher_value(a, row, k) * inv_t : -INFINITY;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kBatch; ++i) {
       if (id[i] >= a.vocab || v[i] == -INFINITY) id[i] = -1;
       const bool mine = id[i] >= lo && id[i] < hi;
       x[i] = id[i] >= 0 && (mine || want_all) ? to_float(z[id[i]]) : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int k = k0 + 32 * i;
+    for (int i = 0; i < kBatch; ++i) {
+      const int k = k0 + kHelpers * i;
       if (id[i] < 0) v[i] = -INFINITY;
+      else any = true;
       most = fmaxf(most, v[i]);
       if (k >= a.k) continue;
-      t.logp[k] = v[i];
+      t.t[k] = v[i];
       t.at[k] = id[i] >= lo && id[i] < hi ? id[i] : -1;
       t.z[k] = x[i];
     }
   }
-  for (int i = lane; i < t.table_size; i += 32) t.table[i] = 0;
-  most = warp_max(most);
-  if (most == -INFINITY) return 0.f;
+  for (int i = me; i < (hi - lo + 127) / 128; i += kHelpers) seen[i] = make_uint4(0, 0, 0, 0);
+  any = __any_sync(kFullMask, any);
+  if (!a.teacher_lse) most = warp_max(most);
+  if (lane == 0) {
+    totals.any[warp] = any;
+    totals.most[warp] = most;
+  }
+  if (me == 0) totals.twice = 0;
+  helpers_wait<kHelpers>();
+  // an id's entries are joined at whichever of them comes first here
+  for (int k = me; k < a.k; k += kHelpers) {
+    const int at = t.at[k] - lo;
+    if (at < 0) continue;
+    if (atomicOr(reinterpret_cast<uint32_t*>(seen) + at / 32, 1u << at % 32) >> at % 32 & 1u) {
+      t.at[k] = -1;
+      totals.twice = 1;
+    }
+  }
   float lse;
   if (a.teacher_lse) {
     lse = a.teacher_lse[row];
+    helpers_wait<kHelpers>();
   } else {
+    most = totals.most[0];
+#pragma unroll
+    for (int i = 1; i < helper_warps<kHelpers>(); ++i) most = fmaxf(most, totals.most[i]);
+    if (most == -INFINITY) most = 0.f;  // no entry: L is not used
     float s = 0.f;
-    for (int k = lane; k < a.k; k += 32) s += exp2_ftz((t.logp[k] - most) * kLog2e);
-    lse = most + logf(warp_sum(s));
+    for (int k = me; k < a.k; k += kHelpers) s += exp2_ftz((t.t[k] - most) * kLog2e);
+    s = warp_sum(s);
+    if (lane == 0) totals.exps[warp] = s;
+    helpers_wait<kHelpers>();
+    s = totals.exps[0];
+#pragma unroll
+    for (int i = 1; i < helper_warps<kHelpers>(); ++i) s += totals.exps[i];
+    lse = most + logf(s);
   }
-  __syncwarp();
+  if (me == 0) totals.lse = lse;
+  const auto p_of = [&](int k) { return t.t[k] == -INFINITY ? 0.f : exp2_ftz((t.t[k] - lse) * kLog2e); };
+  const bool twice = totals.twice != 0;
   float mass = 0.f;
-  for (int k0 = 0; k0 < a.k; k0 += 32) {
-    const int k = k0 + lane;
-    const float logp = k < a.k ? t.logp[k] - lse : -INFINITY;
-    const float p = exp2_ftz(logp * kLog2e);
+  for (int k = me; k < a.k; k += kHelpers) {
+    const float p = p_of(k);
     mass += p;
-    if (k < a.k) t.logp[k] = logp;
-    // an id's entries are joined at the first: within these 32 by lane, with
-    // earlier ones through the table (one lane an id at a time, so that its sum has one order)
-    const int32_t id = k < a.k ? t.at[k] : -1;
-    const unsigned same = __match_any_sync(kFullMask, id);
-    const bool leads = id >= 0 && __ffs(same) - 1 == lane;
-    float joined = p;
-    if (__any_sync(kFullMask, id >= 0 && (same & (same - 1)) != 0))
-      for (int l = 0; l < 32; ++l) {
-        const float other = __shfl_sync(kFullMask, p, l);
-        if (l != lane && (same >> l & 1u)) joined += other;
-      }
-    int first = -1;
-    if (leads) {
-      unsigned slot = (unsigned)id * 2654435761u >> 16;
-      for (;;) {
-        slot &= (unsigned)t.table_size - 1u;
-        int32_t found = t.table[slot];
-        if (found == 0) found = atomicCAS(t.table + slot, 0, k + 1);
-        if (found == 0) {
-          first = k;
-          break;
-        }
-        if (t.at[found - 1] == id) {
-          first = found - 1;
-          break;
-        }
-        ++slot;
-      }
+    float sum = p;
+    if (twice && t.at[k] >= 0) {  // in the entries' order, whichever stands for them
+      sum = 0.f;
+      for (int j = 0; j < a.k; ++j)
+        if (a.ids[row * a.teacher_ld + j] == t.at[k]) sum += p_of(j);
     }
-    __syncwarp();
-    if (leads && first == k) t.sum[k] = joined;
-    if (leads && first != k) t.sum[first] += joined;
-    if (k < a.k && !(leads && first == k)) t.at[k] = -1;
-    __syncwarp();
+    t.sum[k] = sum;
   }
-  return warp_sum(mass);
+  mass = warp_sum(mass);
+  if (lane == 0) totals.mass[warp] = mass;
+}
+
+// 16-byte packs of shared memory for a part's values, and for a bit for each of them and of a row's edges.
+template <typename T>
+__host__ __device__ constexpr int held_packs(int64_t vocab, int pieces) {
+  return (int)(vocab * (int64_t)sizeof(T) / 16) / pieces + 1;
+}
+template <typename T>
+__host__ __device__ constexpr int seen_packs(int held) {
+  return (held * (16 / (int)sizeof(T)) + 32 + 127) / 128;
+}
+template <typename T>
+__host__ __device__ constexpr int held_shared(int32_t k, int64_t vocab, int pieces) {
+  return 2 * teacher_bytes(k) + 16 * (held_packs<T>(vocab, pieces) + seen_packs<T>(held_packs<T>(vocab, pieces)));
 }
 
 // A block's part of a row.
@@ -325,86 +355,85 @@ template <typename T, int kWorkers>
 struct Part {
   static constexpr int E = 16 / (int)sizeof(T);
   const T* z;
-  int shift;       // values of the row's first pack before the row
-  int p_lo, p_hi;  // the part's packs
-  int n;           // this thread's: p_lo + threadIdx.x, + kWorkers, ...
+  int head;        // values of the row before its first whole pack
+  int p_lo, p_hi;  // the part's packs: pack p holds values head + p E and the E - 1 after it
+  int lo, hi;      // the part's values, the row's edges included
+  int n;           // this thread's packs: p_lo + threadIdx.x, + kWorkers, ...
 
   __device__ __forceinline__ Part(const DistillationArgs& a, int64_t row, int piece, int pieces) {
+    const int vocab = (int)a.vocab;
     z = static_cast<const T*>(a.logits) + row * a.ld;
-    shift = (int)((uintptr_t)z % 16 / sizeof(T));
-    const int packs = (shift + (int)a.vocab + E - 1) / E;
+    head = min((int)((16 - (uintptr_t)z % 16) % 16 / sizeof(T)), vocab);
+    const int packs = (vocab - head) / E;
     p_lo = packs / pieces * piece + min(piece, packs % pieces);
     p_hi = packs / pieces * (piece + 1) + min(piece + 1, packs % pieces);
+    lo = piece == 0 ? 0 : head + p_lo * E;
+    hi = piece == pieces - 1 ? vocab : head + p_hi * E;
     const int left = p_hi - p_lo - (int)threadIdx.x;
     n = threadIdx.x < kWorkers && left > 0 ? (left + kWorkers - 1) / kWorkers : 0;
   }
-  __device__ __forceinline__ int pack(int i) const { return p_lo + (int)threadIdx.x + i * kWorkers; }
-  __device__ __forceinline__ const uint4* from() const { return reinterpret_cast<const uint4*>(z - shift) + pack(0); }
-  __device__ __forceinline__ int first_value() const { return max(p_lo * E - shift, 0); }
-  __device__ __forceinline__ int end_value(int vocab) const { return min(p_hi * E - shift, vocab); }
-  // packs that are the row's alone
-  __device__ __forceinline__ int full_lo() const { return p_lo * E < shift ? p_lo + 1 : p_lo; }
-  __device__ __forceinline__ int full_hi(int vocab) const { return p_hi * E - shift > vocab ? p_hi - 1 : p_hi; }
+  __device__ __forceinline__ int first_value() const { return head + (p_lo + (int)threadIdx.x) * E; }
+  // the value at the part's edges that this lane of the first helper warp holds, or -1
+  __device__ __forceinline__ int edge_value() const {
+    const int lane = threadIdx.x & 31, before = head + p_lo * E - lo, after = hi - (head + p_hi * E);
+    if (lane < 16) return lane < before ? lane : -1;
+    return lane - 16 < after ? hi - after + lane - 16 : -1;
+  }
 };
 
 // Writes gradient_of(i), this thread's pack i, for every i.
 template <typename T, int kWorkers, typename F>
-__device__ __forceinline__ void put_all(const Part<T, kWorkers>& part, T* dz, int vocab, F&& gradient_of) {
+__device__ __forceinline__ void put_all(const Part<T, kWorkers>& part, T* dz, F&& gradient_of) {
   constexpr int E = Part<T, kWorkers>::E;
-  const auto put_values = [&](int i, const uint4& v) {
-    const int first = part.pack(i) * E - part.shift;
-    const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-      if (first + j >= 0 && first + j < vocab) dz[first + j] = e[j];
-  };
-  if (((uintptr_t)dz ^ (uintptr_t)part.z) % 16 != 0) {
-    for (int i = 0; i < part.n; ++i) put_values(i, gradient_of(i));
+  T* to = dz + part.first_value();
+  if (((uintptr_t)dz ^ (uintptr_t)part.z) % 16 == 0) {
+#pragma unroll 4
+    for (int i = 0; i < part.n; ++i) __stcs(reinterpret_cast<uint4*>(to) + i * kWorkers, gradient_of(i));
     return;
   }
-  const int f_lo = part.full_lo(), f_hi = part.full_hi(vocab);
-  uint4* to = reinterpret_cast<uint4*>(dz - part.shift) + part.pack(0);
-#pragma unroll 4
   for (int i = 0; i < part.n; ++i) {
     const uint4 v = gradient_of(i);
-    const int p = part.pack(i);
-    if (p >= f_lo && p < f_hi) __stcs(to + i * kWorkers, v);
-    else put_values(i, v);
+#pragma unroll
+    for (int j = 0; j < E; ++j) to[i * kWorkers * E + j] = reinterpret_cast<const T*>(&v)[j];
   }
 }
 
 template <int kWorkers>
-constexpr int held_blocks() {  // on an SM, by registers
-  return 1024 / (kWorkers + 32);
+constexpr int helpers() {
+  return kWorkers >= 128 ? kWorkers / 4 : 32;
+}
+template <int kWorkers>
+constexpr int held_threads() {
+  return kWorkers + helpers<kWorkers>();
 }
 
 template <typename T, DistillationWay kWay, int kWorkers>
-__global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
+__global__ void __launch_bounds__(held_threads<kWorkers>(), 1024 / held_threads<kWorkers>())
     distillation_kernel(DistillationArgs a, int pieces) {
   dq_pdl_enter();
   using P = Packs<T>;
   using Mine = Part<T, kWorkers>;
-  constexpr int E = P::E, kWarps = kWorkers / 32;
+  constexpr int E = P::E, kWarps = kWorkers / 32;  // of workers
   constexpr bool kStats = kWay != DistillationWay::kBackward, kGradient = kWay != DistillationWay::kForward;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  // (maximum, sum) of every worker warp of the cluster; a block may write a row's while another reads the row before's
-  __shared__ float2 pairs[2][kStats ? 8 * kWarps : 1];
-  __shared__ float masses[2];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, vocab = (int)a.vocab;
-  const bool works = warp < kWarps;
+  // (maximum, sum) of every warp of the cluster; a block may write a row's while another reads the row before's
+  __shared__ float2 pairs[2][kStats ? 8 * (kWarps + 1) : 1];
+  constexpr int kHelpers = helpers<kWorkers>();
+  __shared__ TeacherTotals<kHelpers> totals[2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const bool works = warp < kWarps, first_helper = warp == kWarps;
   const int piece = blockIdx.x % pieces;
   const int64_t first_row = blockIdx.x / pieces, stride = gridDim.x / pieces;
   const auto teacher = [&](int parity) {
     Teacher t;
-    t.table_size = table_size(a.k);
-    t.table = reinterpret_cast<int32_t*>(dynamic + parity * teacher_bytes(a.k));
-    t.logp = reinterpret_cast<float*>(t.table + t.table_size);
-    t.z = t.logp + a.k;
+    t.t = reinterpret_cast<float*>(dynamic + parity * teacher_bytes(a.k));
+    t.z = t.t + a.k;
     t.sum = t.z + a.k;
     t.at = reinterpret_cast<int32_t*>(t.sum + a.k);
     return t;
   };
-  uint4* const held = reinterpret_cast<uint4*>(dynamic + 2 * teacher_bytes(a.k)) + threadIdx.x;  // this thread's packs
+  uint4* const seen = reinterpret_cast<uint4*>(dynamic + 2 * teacher_bytes(a.k));
+  uint4* const held = seen + seen_packs<T>(held_packs<T>(a.vocab, pieces)) + threadIdx.x;  // this thread's packs
   const float inv_t = 1.f / a.temperature;
 
   // the weights of this cluster's next 32 rows, a lane each
@@ -431,15 +460,19 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
         a.loss[row] = 0.f;
         if (a.lse) a.lse[row] = 0.f;
       }
-      if (kGradient)
-        put_all(Mine(a, row, piece, pieces), static_cast<T*>(a.dlogits) + row * a.dld, vocab,
-                [](int) { return make_uint4(0, 0, 0, 0); });
+      if (kGradient) {
+        const Mine part(a, row, piece, pieces);
+        T* const dz = static_cast<T*>(a.dlogits) + row * a.dld;
+        put_all(part, dz, [](int) { return make_uint4(0, 0, 0, 0); });
+        if (first_helper && part.edge_value() >= 0) dz[part.edge_value()] = from_float<T>(0.f);
+      }
     }
   };
+  float edge = 0.f, next_edge = 0.f;  // first helper warp: the lane's value at the part's edges
   const auto prepare = [&](const Mine& part, int64_t row, int parity) {
-    const float mass = prepare_teacher(a, row, teacher(parity), part.first_value(), part.end_value(vocab),
-                                       kStats && piece == 0, part.z);
-    if (lane == 0) masses[parity] = mass;
+    next_edge = part.edge_value() >= 0 ? to_float(part.z[part.edge_value()]) : -INFINITY;
+    prepare_teacher<T, kHelpers>(a, row, teacher(parity), totals[parity], seen, (int)threadIdx.x - kWorkers, part.lo, part.hi,
+                                 kStats && piece == 0, part.z);
   };
 
   int64_t turn = advance(0);
@@ -447,7 +480,8 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
   Mine part(a, first_row + turn * stride, piece, pieces);
   if (works) {
 #pragma unroll 4
-    for (int i = 0; i < part.n; ++i) copy16_async(held + i * kWorkers, part.from() + i * kWorkers, 16);
+    for (int i = 0; i < part.n; ++i)
+      copy16_async(held + i * kWorkers, reinterpret_cast<const uint4*>(part.z + part.first_value()) + i * kWorkers, 16);
   } else {
     prepare(part, first_row + turn * stride, 0);
   }
@@ -460,7 +494,7 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
     const bool last = first_row + next_turn * stride >= a.rows;
     const Mine next(a, last ? row : first_row + next_turn * stride, piece, pieces);
     const int next_n = last ? 0 : next.n;
-    const uint4* const next_from = next.from();
+    const uint4* const next_from = reinterpret_cast<const uint4*>(next.z + next.first_value());
     const auto follow = [&](int i) {
       if (i < next_n) copy16_async(held + i * kWorkers, next_from + i * kWorkers, 16);
     };
@@ -470,15 +504,6 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
     float mul = 1.f, add = 0.f, by = inv_t * kLog2e, inv_sum = 1.f, log_sum = 0.f, top = -INFINITY, sum = 0.f;
     if (works) {
       asm volatile("cp.async.wait_all;" ::: "memory");
-      const auto mask = [&](int i) {  // neighbours' values in the row's first and last packs
-        const int first = part.pack(i) * E - part.shift;
-        T* e = reinterpret_cast<T*>(held + i * kWorkers);
-#pragma unroll
-        for (int j = 0; j < E; ++j)
-          if (first + j < 0 || first + j >= vocab) e[j] = from_float<T>(-INFINITY);
-      };
-      if (part.n > 0 && part.pack(0) < part.full_lo()) mask(0);
-      if (part.n > 0 && part.pack(part.n - 1) >= part.full_hi(vocab)) mask(part.n - 1);
       if (kStats) {
 #pragma unroll 4
         for (int i = 0; i < part.n; ++i) top = fmaxf(top, P::max_of(held[i * kWorkers]));
@@ -497,14 +522,20 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
         }
         sum = warp_sum(s.x + s.y);
       }
+    } else if (kStats) {
+      edge = next_edge;
+      top = warp_max(edge);
+      sum = warp_sum(exp2_ftz((edge - (top == -INFINITY ? 0.f : top)) * by));
+    } else {
+      edge = next_edge;
     }
     if (kStats) {
       if (pieces == 1) {
-        if (works && lane == 0) pairs[parity][warp] = make_float2(top, sum);
+        if (lane == 0 && warp <= kWarps) pairs[parity][warp] = make_float2(top, sum);
         __syncthreads();
       } else {
-        if (works && lane < pieces) {
-          const uint32_t mine = smem_addr(&pairs[parity][piece * kWarps + warp]);
+        if (lane < pieces && warp <= kWarps) {
+          const uint32_t mine = smem_addr(&pairs[parity][piece * (kWarps + 1) + warp]);
           uint32_t there;
           asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(mine), "r"(lane));
           asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(top), "f"(sum) : "memory");
@@ -514,7 +545,7 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
       }
       // every warp joins the pairs, in the same order
-      const int all = pieces * kWarps;
+      const int all = pieces * (kWarps + 1);
       float most = -INFINITY;
       for (int i = lane; i < all; i += 32) most = fmaxf(most, pairs[parity][i].x);
       top = warp_max(most);
@@ -535,16 +566,22 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
       add = -a.lse[row];
       by = kLog2e;
     }
-    const float mass = masses[parity];
-    const bool none = !(mass > 0.f);  // no entry
+    float mass = totals[parity].mass[0];
+    int any = totals[parity].any[0];
+#pragma unroll
+    for (int i = 1; i < helper_warps<kHelpers>(); ++i) {
+      mass += totals[parity].mass[i];
+      any |= totals[parity].any[i];
+    }
+    const bool none = any == 0;
     const float factor = a.scale * c * a.temperature, coef = factor * mass * inv_sum;
     if (works) {
       if (kGradient) {
         if (none) {
-          put_all(part, dz, vocab, [](int) { return make_uint4(0, 0, 0, 0); });
+          put_all(part, dz, [](int) { return make_uint4(0, 0, 0, 0); });
           for (int i = 0; i < part.n; ++i) follow(i);
         } else {
-          put_all(part, dz, vocab, [&](int i) {
+          put_all(part, dz, [&](int i) {
             uint4 v = held[i * kWorkers];
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
@@ -555,18 +592,20 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
             return v;
           });
         }
-        asm volatile("bar.arrive 1, %0;" ::"n"(kWorkers + 32) : "memory");
+        __syncwarp();
+        asm volatile("bar.arrive 1, %0;" ::"n"(held_threads<kWorkers>()) : "memory");
       }
       for (int i = part.n; i < next_n; ++i) follow(i);
     } else {
       const Teacher t = teacher(parity);
-      if (kStats && piece == 0) {
+      if (kStats && piece == 0 && first_helper) {
         float loss = 0.f;
+        const float lse_t = totals[parity].lse;
         if (!none)
           for (int k = lane; k < a.k; k += 32) {
-            const float logp = t.logp[k];
+            const float logp = t.t[k] - lse_t;
             const float p = exp2_ftz(logp * kLog2e);
-            if (p > 0.f) loss = fmaf(p, logp - ((t.z[k] - top) * inv_t - log_sum), loss);
+            if (p != 0.f) loss = fmaf(p, logp - ((t.z[k] - top) * inv_t - log_sum), loss);
           }
         loss = warp_sum(loss);
         if (lane == 0) {
@@ -574,12 +613,16 @@ __global__ void __launch_bounds__(kWorkers + 32, held_blocks<kWorkers>())
           if (a.lse) a.lse[row] = none ? 0.f : fmaf(top, inv_t, log_sum);
         }
       }
+      const int at_edge = first_helper ? part.edge_value() : -1;
+      if (kGradient && at_edge >= 0)
+        dz[at_edge] = from_float<T>(none ? 0.f : exp2_ftz(fmaf(edge, mul, add) * by) * coef);
       if (!last) prepare(next, first_row + next_turn * stride, parity ^ 1);
       if (kGradient) {
         // the entries' own gradients over what the workers wrote there
-        asm volatile("bar.sync 1, %0;" ::"n"(kWorkers + 32) : "memory");
+        __syncwarp();
+        asm volatile("bar.sync 1, %0;" ::"n"(held_threads<kWorkers>()) : "memory");
         if (!none)
-          for (int k = lane; k < a.k; k += 32)
+          for (int k = (int)threadIdx.x - kWorkers; k < a.k; k += kHelpers)
             if (t.at[k] >= 0)
               dz[t.at[k]] = from_float<T>(fmaf(exp2_ftz(fmaf(t.z[k], mul, add) * by), coef, -factor * t.sum[k]));
       }
@@ -624,36 +667,37 @@ cudaError_t resident_clusters(K kern, int threads, int shared, int pieces, std::
 }
 
 template <typename T, DistillationWay kWay, int kWorkers>
-cudaError_t launch_held(const DistillationArgs& a, int packs, int pieces, cudaStream_t stream) {
+cudaError_t launch_held(const DistillationArgs& a, int pieces, cudaStream_t stream) {
   static std::atomic<uint64_t> kept[kKeptDevices];
-  const int shared = 2 * teacher_bytes(a.k) + 16 * (packs / pieces + 1);
+  const int shared = held_shared<T>(a.k, a.vocab, pieces);
   const int cluster = kWay == DistillationWay::kBackward ? 1 : pieces;  // its pieces exchange nothing
   int clusters = 0;
-  const cudaError_t st = resident_clusters(distillation_kernel<T, kWay, kWorkers>, kWorkers + 32, shared, cluster, kept,
-                                           &clusters);
+  const cudaError_t st = resident_clusters(distillation_kernel<T, kWay, kWorkers>, held_threads<kWorkers>(), shared,
+                                           cluster, kept, &clusters);
   if (st != cudaSuccess) return st;
   const int64_t at_once = min64(a.rows, max64((int64_t)clusters * cluster / pieces, 1));
   return launch_pdl_cluster(distillation_kernel<T, kWay, kWorkers>, cluster, dim3((unsigned)(at_once * pieces)),
-                            dim3(kWorkers + 32), (size_t)shared, stream, a, pieces);
+                            dim3(held_threads<kWorkers>()), (size_t)shared, stream, a, pieces);
 }
 
 template <typename T, DistillationWay kWay>
 cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
-  constexpr int E = 16 / (int)sizeof(T);
-  const int packs = (int)(a.vocab / E + 2);  // at most, with the row's first and last in part
+  const int packs = held_packs<T>(a.vocab, 1);
   int workers = 32, pieces = 1;
-  while (workers < kMostWorkers && packs > workers * kPacksPerThread) workers *= 2;
+  // 4096 bf16 rows, us with 8 | 16 packs a worker: 16,000 values 69 | 55, 8000 values 38 | 36, 4000 values
+  // (64 workers | 32) 28 | 38
+  while (workers < kMostWorkers && packs > workers * (workers == 32 ? 8 : 16)) workers *= 2;
   while (pieces < 8 && packs * 16 > pieces * kPieceBytes) ++pieces;
-  if (16 * (packs / pieces + 1) + 2 * teacher_bytes(a.k) > kMostShared)
+  if (held_shared<T>(a.k, a.vocab, pieces) > kMostShared)
     return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle
   while (pieces < 8 && a.rows * (pieces + 1) <= device_sms() && packs > workers * pieces) ++pieces;
   switch (workers) {
-    case 32: return launch_held<T, kWay, 32>(a, packs, pieces, stream);
-    case 64: return launch_held<T, kWay, 64>(a, packs, pieces, stream);
-    case 128: return launch_held<T, kWay, 128>(a, packs, pieces, stream);
+    case 32: return launch_held<T, kWay, 32>(a, pieces, stream);
+    case 64: return launch_held<T, kWay, 64>(a, pieces, stream);
+    case 128: return launch_held<T, kWay, 128>(a, pieces, stream);
   }
-  return launch_held<T, kWay, kMostWorkers>(a, packs, pieces, stream);
+  return launch_held<T, kWay, kMostWorkers>(a, pieces, stream);
 }
 
 }  // namespace
