@@ -1,114 +1,506 @@
 // Embedding lookup with scaling, and its gradient over the tokens sorted by id.
+//
+//   y_i = scale table[id_i];   dtable[v] = scale sum over i with id_i = v of dy_i
+//
+// Both are bound by memory: a row of the table (or of dy) read and one written
+// per token, one operation a value; the gradient also writes every row of
+// the table's gradient that no token fell on, which is most of its traffic
+// where the vocabulary is larger than the batch.
 #include "device_common.cuh"
 #include "operators.cuh"
 
 namespace dq {
 namespace {
 
-constexpr int kThreads = 256;
-
-// The place's id, or -1 where it holds no token.
+// The place's id, or the vocabulary where it holds no token.
 __device__ __forceinline__ int32_t token_at(const EmbeddingArgs& a, int64_t i) {
-  const int64_t id = a.token_bits == 32 ? static_cast<const int32_t*>(a.ids)[i] : static_cast<const int64_t*>(a.ids)[i];
-  return id >= 0 && id < a.vocab ? (int32_t)id : -1;
+  if (a.token_bits == 32) {
+    const int32_t id = static_cast<const int32_t*>(a.ids)[i];
+    return (uint32_t)id < (uint32_t)a.vocab ? id : (int32_t)a.vocab;
+  }
+  const int64_t id = static_cast<const int64_t*>(a.ids)[i];
+  return (uint64_t)id < (uint64_t)a.vocab ? (int32_t)id : (int32_t)a.vocab;
 }
 
-// One block per place.
-template <typename E, typename T>
-__global__ void __launch_bounds__(kThreads) embedding_forward_kernel(EmbeddingArgs a) {
+// ---------------------------------------------------------------------------
+// Forward: `lanes` threads take a row, 16 bytes of y each at a time (kVec: rows
+// of table and y are aligned for that), kRows rows of one thread on their way at
+// once.
+// ---------------------------------------------------------------------------
+constexpr int kForwardThreads = 256, kRows = 4;
+
+template <typename E, typename T, bool kVec>
+__global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(EmbeddingArgs a, int lanes) {
   dq_pdl_enter();
-  const int64_t i = blockIdx.x;
-  const int32_t id = token_at(a, i);
-  T* y = static_cast<T*>(a.y) + i * a.ld;
-  const E* row = static_cast<const E*>(a.table) + i / a.tokens * a.p_stride + (int64_t)max(id, 0) * a.width;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads)
-    y[c] = from_float<T>(id < 0 ? 0.f : to_float(row[c]) * a.scale);
+  constexpr int N = kVec ? 16 / (int)sizeof(T) : 1;  // values a thread takes of a row
+  const int lane = threadIdx.x % lanes, groups = kForwardThreads / lanes;
+  const int64_t all = a.tokens * a.workers;
+  const int64_t first = ((int64_t)blockIdx.x * kRows) * groups + threadIdx.x / lanes;
+  const E* row[kRows];
+  bool live[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    const int64_t i = first + r * groups;
+    const int32_t id = i < all ? token_at(a, i) : (int32_t)a.vocab;
+    live[r] = id < a.vocab;
+    row[r] = static_cast<const E*>(a.table) +
+             (live[r] ? (int64_t)((uint32_t)i / (uint32_t)a.tokens) * a.p_stride + (int64_t)id * a.width : 0);
+  }
+  for (int c = lane * N; c < a.width; c += lanes * N) {
+    float v[kRows][N];
+    if constexpr (kVec) {
+      constexpr int kBytes = N * (int)sizeof(E);  // of the table: 8, 16 or 32
+      uint2 p[kRows][kBytes / 8];
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int k = 0; k < kBytes / 8; k += 2) {
+          if constexpr (kBytes >= 16) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (live[r]) q = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row[r] + c) + 8 * k);
+            p[r][k] = make_uint2(q.x, q.y);
+            p[r][k + 1] = make_uint2(q.z, q.w);
+          } else {
+            p[r][k] = make_uint2(0, 0);
+            if (live[r]) p[r][k] = *reinterpret_cast<const uint2*>(row[r] + c);
+          }
+        }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[r][e] = to_float(reinterpret_cast<const E*>(p[r])[e]) * a.scale;
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) v[r][0] = live[r] ? to_float(row[r][c]) * a.scale : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int64_t i = first + r * groups;
+      if (i >= all) continue;
+      T* y = static_cast<T*>(a.y) + i * a.ld + c;
+      if constexpr (kVec) {
+        uint4 q;
+#pragma unroll
+        for (int e = 0; e < N; ++e) reinterpret_cast<T*>(&q)[e] = from_float<T>(v[r][e]);
+        __stcs(reinterpret_cast<uint4*>(y), q);
+      } else {
+        *y = from_float<T>(v[r][0]);
+      }
+    }
+  }
 }
 
-// Scratch, per worker: vocab + 1 starts of the ids' runs, then the places
-// sorted by id (and by place within an id).
+// ---------------------------------------------------------------------------
+// Backward, in three kernels:
+//   1. a cluster of blocks per worker sorts its places by id, the places of an id in
+//      order, while the other blocks write zeros to the rows that no token fell on
+//      (the sort takes 10 to 30 us on a few SMs, and hides behind them);
+//   2. the sorted places are cut into chunks; a chunk's rows of dy are read
+//      once and summed id by id.  A run of one id that lies in the chunk is the result;
+//      what a run that crosses into other chunks has there goes to the scratch space;
+//   3. such runs' parts are added up in order.
+// Nothing is added atomically, so the same call gives the same bits.
+// ---------------------------------------------------------------------------
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kSortMost = 20480;  // places of one block: two buffers of them in shared memory
+constexpr int kSection = 8 * kSortMost;  // places that are sorted at once; more are taken in turn, and added
+constexpr int kMostBins = 512;
+constexpr int kFillRows = 1 << 16;  // rows of one filling block, a bit each
+
+// Scratch: per worker the sorted ids and places of a section; then the chunks' parts.
 struct Sorted {
-  int32_t* starts;
+  int32_t* ids;
   int32_t* places;
 };
+__host__ __device__ inline int64_t section_of(int64_t tokens) { return tokens < kSection ? tokens : kSection; }
 __host__ __device__ inline Sorted sorted_of(const EmbeddingArgs& a, int64_t m) {
-  int32_t* base = static_cast<int32_t*>(a.scratch) + m * (a.vocab + 1 + a.tokens);
-  return {base, base + a.vocab + 1};
+  const int64_t n = section_of(a.tokens);
+  int32_t* base = static_cast<int32_t*>(a.scratch) + m * 2 * n;
+  return {base, base + n};
 }
 
-__global__ void __launch_bounds__(kThreads) embedding_clear_kernel(EmbeddingArgs a) {
-  dq_pdl_enter();
-  const int64_t v = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (v <= a.vocab) sorted_of(a, blockIdx.y).starts[v] = 0;
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_block(const void* p, int rank) {  // the same place in another block of the cluster
+  uint32_t there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_addr(p)), "r"(rank));
+  return there;
 }
 
-__global__ void __launch_bounds__(kThreads) embedding_count_kernel(EmbeddingArgs a) {
-  dq_pdl_enter();
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= a.tokens) return;
-  const int32_t id = token_at(a, blockIdx.y * a.tokens + i);
-  if (id >= 0) atomicAdd(sorted_of(a, blockIdx.y).starts + id, 1);
-}
-
-// Counts to starts: one warp per worker.
-__global__ void __launch_bounds__(32) embedding_scan_kernel(EmbeddingArgs a) {
-  dq_pdl_enter();
-  int32_t* starts = sorted_of(a, blockIdx.x).starts;
-  const int lane = threadIdx.x;
-  int32_t before = 0;
-  for (int64_t v0 = 0; v0 <= a.vocab; v0 += 32) {
-    const int64_t v = v0 + lane;
-    const int32_t n = v <= a.vocab ? starts[v] : 0;
-    int32_t s = n;
+// Sorts the n places from `begin` on of worker m by id, `share` of them to each
+// of the cluster's blocks: passes of up to 9 bits from the lowest, each of which keeps
+// the order within a digit.  A warp counts the digits of its part of the block's places, the counts are
+// added up over warps, blocks and digits, and every place goes to where its digit's
+// earlier ones end, in the shared memory of the block that holds that position.
+__device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, int n, int share, int rank, int ranks,
+                             unsigned char* dynamic) {
+  uint32_t* from = reinterpret_cast<uint32_t*>(dynamic);
+  uint32_t* to = from + share;
+  uint16_t* counts = reinterpret_cast<uint16_t*>(to + share);  // [warp][bin]
+  __shared__ uint32_t totals[kMostBins], bases[kMostBins], warp_sums[kSortWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const int mine = max(0, min(share, n - rank * share));
+  const int part = (mine + kSortThreads - 1) / kSortThreads * 32;  // places of a warp
+  const int lo = min(warp * part, mine), hi = min(lo + part, mine);
+  const int bits = 32 - __clz((int)a.vocab), passes = (bits + 8) / 9, width = (bits + passes - 1) / passes;
+  const int bins = 1 << width;
+  const int64_t at = m * a.tokens;
+  const Sorted out = sorted_of(a, m);
+  for (int i = threadIdx.x; i < mine; i += kSortThreads) from[i] = (uint32_t)(begin + rank * share + i);
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * width;
+    for (int i = threadIdx.x; i < kSortWarps * bins / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
+    __syncthreads();
+    uint16_t* const mine_counts = counts + warp * bins;
+    constexpr int kBatch = 4;  // ids on their way at once
+    for (int i0 = lo; i0 < hi; i0 += 32 * kBatch) {
+      int32_t id[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = i0 + 32 * k + lane;
+        id[k] = i < hi ? token_at(a, at + from[i]) : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
+        const unsigned same = __match_any_sync(kFullMask, digit);
+        if (digit >= 0 && __ffs(same) - 1 == lane) mine_counts[digit] += (uint16_t)__popc(same);
+        __syncwarp();
+      }
+    }
+    __syncthreads();
+    // counts: the block's places of the digit in earlier warps; totals: in the block
+    if (threadIdx.x < bins) {
+      uint32_t sum = 0;
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = counts[w * bins + threadIdx.x];
+        counts[w * bins + threadIdx.x] = (uint16_t)sum;
+        sum += c;
+      }
+      totals[threadIdx.x] = sum;
+    }
+    if (ranks > 1) cluster_wait();
+    else __syncthreads();
+    uint32_t all = 0, earlier = 0;
+    if (threadIdx.x < bins)
+      for (int r = 0; r < ranks; ++r) {
+        uint32_t c;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(in_block(totals + threadIdx.x, r)) : "memory");
+        if (r < rank) earlier += c;
+        all += c;
+      }
+    // bases: the section's places of lower digits, and of this one in earlier blocks
+    uint32_t scan = all;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int32_t up = __shfl_up_sync(kFullMask, s, o);
-      if (lane >= o) s += up;
+      const uint32_t up = __shfl_up_sync(kFullMask, scan, o);
+      if (lane >= o) scan += up;
     }
-    if (v <= a.vocab) starts[v] = before + s - n;
-    before += __shfl_sync(kFullMask, s, 31);
+    if (lane == 31) warp_sums[warp] = scan;
+    __syncthreads();
+    if (threadIdx.x < bins) {
+      for (int w = 0; w < warp; ++w) scan += warp_sums[w];
+      bases[threadIdx.x] = scan - all + earlier;
+    }
+    __syncthreads();
+    const bool last = pass == passes - 1;
+    for (int i0 = lo; i0 < hi; i0 += 32 * kBatch) {
+      uint32_t place[kBatch];
+      int32_t id[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int i = i0 + 32 * k + lane;
+        place[k] = i < hi ? from[i] : 0;
+        id[k] = i < hi ? token_at(a, at + place[k]) : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
+        const unsigned same = __match_any_sync(kFullMask, digit);
+        uint32_t before = 0;
+        if (digit >= 0) before = mine_counts[digit];
+        __syncwarp();
+        if (digit >= 0) {
+          if (__ffs(same) - 1 == lane) mine_counts[digit] = (uint16_t)(before + __popc(same));
+          const uint32_t where = bases[digit] + before + __popc(same & ((1u << lane) - 1u));
+          if (last) {
+            out.places[where] = (int32_t)place[k];
+            out.ids[where] = id[k];
+          } else {
+            const int r = (int)(where / (uint32_t)share);
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_block(to + (where - r * (uint32_t)share), r)),
+                         "r"(place[k])
+                         : "memory");
+          }
+        }
+        __syncwarp();
+      }
+    }
+    // the other blocks' places have come, and nobody needs these totals any more
+    if (ranks > 1) cluster_wait();
+    else __syncthreads();
+    uint32_t* const t = from;
+    from = to;
+    to = t;
   }
 }
 
-// A place's rank within its id's run: the earlier places with the same id.
-__global__ void __launch_bounds__(kThreads) embedding_place_kernel(EmbeddingArgs a) {
-  dq_pdl_enter();
-  __shared__ int32_t tile[kThreads];
-  const int64_t first = blockIdx.y * a.tokens, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int32_t id = i < a.tokens ? token_at(a, first + i) : -1;
-  int32_t rank = 0;
-  for (int64_t j0 = 0; j0 <= (int64_t)blockIdx.x * kThreads; j0 += kThreads) {
+// Zeros to rows [v0, v1) of worker m's gradient that none of its n places from `begin` on holds
+// (skip: look for those; else to all).
+__device__ void fill_rows(const EmbeddingArgs& a, int64_t m, int64_t begin, int n, int64_t v0, int64_t v1, bool skip,
+                          unsigned char* dynamic) {
+  uint32_t* held = reinterpret_cast<uint32_t*>(dynamic);  // a bit a row
+  const int rows = (int)(v1 - v0), lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  if (skip) {
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) held[i] = 0;
     __syncthreads();
-    tile[threadIdx.x] = j0 + threadIdx.x < a.tokens ? token_at(a, first + j0 + threadIdx.x) : -1;
+    constexpr int kBatch = 8;
+    const int64_t at = m * a.tokens + begin;
+    for (int i0 = threadIdx.x; i0 < n; i0 += kSortThreads * kBatch) {
+      int32_t id[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) id[k] = i0 + k * kSortThreads < n ? token_at(a, at + i0 + k * kSortThreads) : -1;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (id[k] >= v0 && id[k] < v1) atomicOr(held + (int)(id[k] - v0) / 32, 1u << (int)(id[k] - v0) % 32);
+    }
     __syncthreads();
-    for (int j = 0; j < kThreads; ++j) rank += tile[j] == id && j0 + j < i ? 1 : 0;
   }
-  const Sorted s = sorted_of(a, blockIdx.y);
-  if (id >= 0) s.places[s.starts[id] + rank] = (int32_t)i;
+  float* const table = a.dtable + m * a.g_stride;
+  for (int r = warp; r < rows; r += kSortWarps) {
+    if (skip && (held[r / 32] >> r % 32 & 1u)) continue;
+    float* row = table + (v0 + r) * a.width;
+    // up to 3 values before the first 16-byte boundary, then 16 bytes at a time
+    const int head = min((int)((16 - (uintptr_t)row % 16) % 16 / 4), (int)a.width), packs = ((int)a.width - head) / 4;
+    const int tail = head + 4 * packs;
+    if (lane < head) row[lane] = 0.f;
+    if (tail + lane < a.width) row[tail + lane] = 0.f;
+    float4* to = reinterpret_cast<float4*>(row + head);
+    for (int i = lane; i < packs; i += 32) __stcs(to + i, make_float4(0.f, 0.f, 0.f, 0.f));
+  }
 }
 
-// One block per row of a worker's table.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) embedding_gradient_kernel(EmbeddingArgs a) {
+// Blocks [0, workers * ranks) sort, the others fill `rows` rows each, `fills` blocks to a worker.
+__global__ void __launch_bounds__(kSortThreads, 2)
+    embedding_sort_kernel(EmbeddingArgs a, int64_t begin, int n, int share, int ranks, int rows, int fills, int skip) {
   dq_pdl_enter();
-  const int64_t v = blockIdx.x, m = blockIdx.y;
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  const int sorters = n > 0 ? a.workers * ranks : 0;
+  if ((int)blockIdx.x < sorters) {
+    sort_section(a, blockIdx.x / ranks, begin, n, share, blockIdx.x % ranks, ranks, dynamic);
+    return;
+  }
+  const int64_t fill = blockIdx.x - sorters;
+  if (fill >= (int64_t)fills * a.workers) return;  // the cluster's spare blocks
+  const int64_t v0 = fill % fills * rows;
+  fill_rows(a, fill / fills, begin, n, v0, min64(v0 + rows, a.vocab), skip != 0, dynamic);
+}
+
+// A thread of the second and third kernel takes kCols columns: one 16-byte pack
+// of dy (two in 32 bits), or (kVec false) columns `lanes` apart.
+constexpr int kSumThreads = 128, kCols = 8, kSlice = kSumThreads * kCols;
+
+struct Chunks {
+  int32_t size;   // places of a chunk
+  int32_t count;  // chunks of a worker
+  int32_t lanes;  // threads that take a chunk's columns, at most kSumThreads
+};
+
+// A worker's chunk's two parts, each a row of `width` sums: 0: of the run that comes
+// from the chunk before; 1: of one that begins here and goes on.
+__device__ __forceinline__ float* part_of(const EmbeddingArgs& a, const Chunks& ch, int64_t m, int64_t chunk, int which) {
+  float* parts = reinterpret_cast<float*>(static_cast<int32_t*>(a.scratch) +
+                                          (2 * section_of(a.tokens) * a.workers + 3) / 4 * 4);
+  return parts + ((m * ch.count + chunk) * 2 + which) * ((a.width + 3) / 4 * 4);
+}
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArgs a, int n, Chunks ch) {
+  dq_pdl_enter();
+  constexpr int E = 16 / (int)sizeof(T), P = kCols / E;
+  constexpr int kAhead = kVec ? (sizeof(T) == 4 ? 4 : 8) : 2;  // rows of dy on their way at once
+  const int lane = threadIdx.x % ch.lanes, groups = kSumThreads / ch.lanes;
+  const int64_t which = (int64_t)blockIdx.x * groups + threadIdx.x / ch.lanes;
+  if (which >= (int64_t)a.workers * ch.count) return;
+  const int64_t m = which / ch.count, chunk = which % ch.count;
   const Sorted s = sorted_of(a, m);
-  const int32_t begin = s.starts[v], end = s.starts[v + 1];
-  if (begin == end && a.accumulate) return;
-  float* out = a.dtable + m * a.g_stride + v * a.width;
-  for (int64_t c = threadIdx.x; c < a.width; c += kThreads) {
-    float sum = 0.f;
-    for (int32_t j = begin; j < end; ++j)
-      sum += to_float(static_cast<const T*>(a.dy)[(m * a.tokens + s.places[j]) * a.ld + c]);
-    sum *= a.scale;
-    out[c] = a.accumulate ? out[c] + sum : sum;
+  const int lo = (int)chunk * ch.size, hi = min(lo + ch.size, n);
+  const int c0 = (int)blockIdx.y * kSlice + (kVec ? lane * kCols : lane);
+  const auto column = [&](int k) { return kVec ? c0 + k : c0 + k * ch.lanes; };
+  if (c0 >= a.width) return;
+  const T* dy = static_cast<const T*>(a.dy) + m * a.tokens * a.ld;
+  float* const table = a.dtable + m * a.g_stride;
+
+  float sum[kCols];
+#pragma unroll
+  for (int k = 0; k < kCols; ++k) sum[k] = 0.f;
+  bool came = lo > 0 && s.ids[lo - 1] == s.ids[lo];  // the run at hand began in an earlier chunk
+  const auto flush = [&](int32_t id, bool goes) {
+    if (came || goes) {
+      float* out = part_of(a, ch, m, chunk, came ? 0 : 1);
+#pragma unroll
+      for (int k = 0; k < kCols; k += kVec ? 4 : 1) {
+        if constexpr (kVec) {
+          if (column(k) < a.width)
+            *reinterpret_cast<float4*>(out + column(k)) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+        } else if (column(k) < a.width) {
+          out[column(k)] = sum[k];
+        }
+      }
+    } else {
+      float* out = table + (int64_t)id * a.width;
+#pragma unroll
+      for (int k = 0; k < kCols; k += kVec ? 4 : 1) {
+        if (column(k) >= a.width) continue;
+        if constexpr (kVec) {
+          float4* q = reinterpret_cast<float4*>(out + column(k));
+          float4 v = make_float4(sum[k] * a.scale, sum[k + 1] * a.scale, sum[k + 2] * a.scale, sum[k + 3] * a.scale);
+          if (a.accumulate) {
+            const float4 old = *q;
+            v = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
+          }
+          __stcs(q, v);
+        } else {
+          const float v = sum[k] * a.scale;
+          out[column(k)] = a.accumulate ? out[column(k)] + v : v;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) sum[k] = 0.f;
+    came = false;
+  };
+
+  for (int j0 = lo; j0 < hi; j0 += kAhead) {
+    int32_t id[kAhead + 1];
+    int32_t place[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      id[j] = j0 + j < hi ? s.ids[j0 + j] : (int32_t)a.vocab;
+      place[j] = j0 + j < hi ? s.places[j0 + j] : 0;
+    }
+    // of the place after these, wherever it lies
+    id[kAhead] = j0 + kAhead < n ? s.ids[j0 + kAhead] : (int32_t)a.vocab;
+    const int32_t after = hi < n ? s.ids[hi] : (int32_t)a.vocab;  // of the next chunk's first
+    uint4 x[kAhead][P];
+    T y[kVec ? 1 : kAhead][kVec ? 1 : kCols];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (id[j] < a.vocab) {
+        if constexpr (kVec) {
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+            if (column(p * E) < a.width)
+              x[j][p] = __ldcs(reinterpret_cast<const uint4*>(dy + (int64_t)place[j] * a.ld + column(p * E)));
+        } else {
+#pragma unroll
+          for (int k = 0; k < kCols; ++k)
+            if (column(k) < a.width) y[j][k] = dy[(int64_t)place[j] * a.ld + column(k)];
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (j0 + j >= hi || id[j] >= a.vocab) break;  // the places without a token come last
+      if constexpr (kVec) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          if (column(p * E) < a.width)
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+              const float2 v = pair_of<T>(x[j][p], e);
+              sum[p * E + e] += v.x;
+              sum[p * E + e + 1] += v.y;
+            }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k)
+          if (column(k) < a.width) sum[k] += to_float(y[j][k]);
+      }
+      const bool ends_chunk = j0 + j + 1 == hi;
+      const int32_t next = ends_chunk ? after : id[j + 1];
+      if (next != id[j]) flush(id[j], false);
+      else if (ends_chunk) flush(id[j], true);
+    }
   }
+}
+
+// The parts of the run that begins in chunk `which` and goes on, if one does.
+constexpr int kJoinThreads = 256, kJoinSlice = 512;
+
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingArgs a, int n, Chunks ch) {
+  dq_pdl_enter();
+  __shared__ float4 shared[kJoinThreads / 2];
+  const int64_t m = blockIdx.x / ch.count, chunk = blockIdx.x % ch.count;
+  const Sorted s = sorted_of(a, m);
+  const int lo = (int)chunk * ch.size, hi = lo + ch.size;
+  if (hi >= n) return;  // nothing after it
+  const int32_t id = s.ids[hi];
+  if (id >= a.vocab || s.ids[hi - 1] != id) return;
+  if (s.ids[lo] == id && lo > 0 && s.ids[lo - 1] == id) return;  // it began earlier
+  // the run's last chunk: the first whose next one starts with another id
+  const int lane = threadIdx.x & 31;
+  int64_t last = chunk + 1;
+  for (;;) {
+    const int64_t next = (last + lane + 1) * ch.size;
+    const unsigned ends = __ballot_sync(kFullMask, next >= n || s.ids[next] != id);
+    if (ends != 0) {
+      last += __ffs(ends) - 1;
+      break;
+    }
+    last += 32;
+  }
+  // two halves of the block take half of the parts each
+  const int half = threadIdx.x / (kJoinThreads / 2), t = threadIdx.x % (kJoinThreads / 2);
+  const int64_t count = last - chunk + 1, mid = (count + 1) / 2;
+  const int64_t first = half == 0 ? 0 : mid, end = half == 0 ? mid : count;
+  const int c = (int)blockIdx.y * kJoinSlice + 4 * t;  // the parts' rows are padded to whole packs
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < a.width)
+#pragma unroll 8
+    for (int64_t i = first; i < end; ++i) {
+      const float4 v = *reinterpret_cast<const float4*>(part_of(a, ch, m, chunk + i, i == 0 ? 1 : 0) + c);
+      sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+  if (half == 1) shared[t] = sum;
+  __syncthreads();
+  if (half == 1 || c >= a.width) return;
+  const float4 v = shared[t];
+  const float total[4] = {(sum.x + v.x) * a.scale, (sum.y + v.y) * a.scale, (sum.z + v.z) * a.scale, (sum.w + v.w) * a.scale};
+  float* out = a.dtable + m * a.g_stride + (int64_t)id * a.width + c;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (c + k < a.width) out[k] = a.accumulate ? out[k] + total[k] : total[k];
+}
+
+int lanes_for(int64_t width, int per_thread, int most) {
+  int lanes = 1;
+  while (lanes < most && (int64_t)lanes * per_thread < width) lanes *= 2;
+  return lanes;
+}
+
+// Chunks small enough for 32 blocks of the second kernel on every SM, of at least 16 places.
+constexpr int64_t kSumBlocks = 152 * 32;
+
+Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
+  Chunks ch;
+  ch.lanes = lanes_for(width, kCols, kSumThreads);
+  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
+  ch.size = (int32_t)max64(16, ceil_div(n * workers * slices, kSumBlocks * groups));
+  ch.count = (int32_t)max64(1, ceil_div(n, ch.size));
+  return ch;
 }
 
 }  // namespace
 
-size_t embedding_scratch_bytes(int64_t vocab, int64_t, int64_t max_tokens, int32_t workers) {
-  return 4 * (size_t)workers * (size_t)(vocab + 1 + max_tokens);
+size_t embedding_scratch_bytes(int64_t, int64_t width, int64_t max_tokens, int32_t workers) {
+  const int64_t n = section_of(max_tokens);
+  // the most chunks that any smaller number of tokens makes: n workers slices / size <= blocks groups
+  const Chunks ch = chunks_of(n, width, workers);
+  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
+  const int64_t chunks = min64(workers * ceil_div(n, 16), kSumBlocks * groups / slices + workers);
+  return 4 * (size_t)((2 * n * workers + 3) / 4 * 4) + 8 * (size_t)chunks * (size_t)((width + 3) / 4 * 4);
 }
 
 cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t stream, uint64_t* launches) {
@@ -117,28 +509,79 @@ cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t stream
   ++*launches;
   return with_dtype(a.table_dtype, [&](auto e) {
     return with_dtype(a.dtype, [&](auto t) {
-      return launch_pdl(embedding_forward_kernel<decltype(e), decltype(t)>, dim3((unsigned)n), dim3(kThreads), 0,
-                        stream, a);
+      using E = decltype(e);
+      using T = decltype(t);
+      constexpr int N = 16 / (int)sizeof(T), kBytes = N * (int)sizeof(E), kAlign = kBytes < 16 ? kBytes : 16;
+      const bool vec = a.width % N == 0 && (uintptr_t)a.y % 16 == 0 && a.ld % N == 0 &&
+                       (uintptr_t)a.table % kAlign == 0 && a.width * (int64_t)sizeof(E) % kAlign == 0 &&
+                       a.p_stride * (int64_t)sizeof(E) % kAlign == 0;
+      const int lanes = lanes_for(a.width, vec ? N : 1, kForwardThreads);
+      const dim3 grid((unsigned)ceil_div(n, kRows * (kForwardThreads / lanes)));
+      return vec ? launch_pdl(embedding_forward_kernel<E, T, true>, grid, dim3(kForwardThreads), 0, stream, a, lanes)
+                 : launch_pdl(embedding_forward_kernel<E, T, false>, grid, dim3(kForwardThreads), 0, stream, a, lanes);
     });
   });
 }
 
-cudaError_t launch_embedding_backward(const EmbeddingArgs& a, cudaStream_t stream, uint64_t* launches) {
-  const dim3 block(kThreads), by_token((unsigned)ceil_div(a.tokens, kThreads), a.workers);
-  cudaError_t st = launch_pdl(embedding_clear_kernel, dim3((unsigned)ceil_div(a.vocab + 1, kThreads), a.workers), block,
-                              0, stream, a);
-  ++*launches;
-  if (st == cudaSuccess && a.tokens > 0) {
-    *launches += 3;
-    if ((st = launch_pdl(embedding_count_kernel, by_token, block, 0, stream, a)) == cudaSuccess &&
-        (st = launch_pdl(embedding_scan_kernel, dim3(a.workers), dim3(32), 0, stream, a)) == cudaSuccess)
-      st = launch_pdl(embedding_place_kernel, by_token, block, 0, stream, a);
-  }
-  if (st != cudaSuccess) return st;
-  ++*launches;
-  return with_dtype(a.dtype, [&](auto t) {
-    return launch_pdl(embedding_gradient_kernel<decltype(t)>, dim3((unsigned)a.vocab, a.workers), block, 0, stream, a);
-  });
+cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t stream, uint64_t* launches) {
+  EmbeddingArgs a = args;
+  int64_t begin = 0;
+  do {
+    const int n = (int)min64(a.tokens - begin, kSection);
+    // 1. sort and fill
+    int ranks = 1;
+    while (ranks < 8 && ceil_div(n, ranks) > 4096) ranks *= 2;
+    const int share = (int)max64(ceil_div(n, ranks), 1);
+    int64_t rows = 1, fills = 0;
+    bool skip = false;
+    if (!a.accumulate) {
+      // rows of a filling block: at least a 16th MB, about a 4th of what falls to an SM up to 1 MB, and
+      // four times the bytes of the ids that it looks through
+      const int64_t row = 4 * a.width, least = max64(64 << 10, min64(1 << 20, a.workers * a.vocab * row / (152 * 4)));
+      const int64_t bytes = max64(least, 4 * (int64_t)n * a.token_bits / 8);
+      skip = n > 0 && a.vocab * row >= bytes;
+      rows = min64(max64((skip ? bytes : least) / row, 1), kFillRows);
+      fills = ceil_div(a.vocab, rows);
+    }
+    const int64_t sorters = n > 0 ? (int64_t)a.workers * ranks : 0;
+    const int64_t blocks = ceil_div(sorters + fills * a.workers, ranks) * ranks;
+    const int shared = (int)max64(n > 0 ? 8 * (int64_t)share + 2 * kSortWarps * kMostBins : 0, skip ? kFillRows / 8 : 0);
+    static std::atomic<int> kept[kKeptDevices];
+    int resident = 0;
+    cudaError_t st = resident_ctas(embedding_sort_kernel, kSortThreads, 8 * kSortMost + 2 * kSortWarps * kMostBins,
+                                   8 * kSortMost + 2 * kSortWarps * kMostBins, kept, &resident);
+    if (st != cudaSuccess) return st;
+    if (blocks > 0) {
+      ++*launches;
+      st = launch_pdl_cluster(embedding_sort_kernel, ranks, dim3((unsigned)blocks), dim3(kSortThreads), (size_t)shared,
+                              stream, a, begin, n, share, ranks, (int)rows, (int)fills, skip ? 1 : 0);
+      if (st != cudaSuccess) return st;
+    }
+    if (n == 0) return cudaSuccess;
+    // 2. and 3. sum
+    const Chunks ch = chunks_of(n, a.width, a.workers);
+    const int64_t slices = ceil_div(a.width, kSlice), groups = kSumThreads / ch.lanes;
+    ++*launches;
+    st = with_dtype(a.dtype, [&](auto t) {
+      using T = decltype(t);
+      const bool vec = a.width % kCols == 0 && (uintptr_t)a.dy % 16 == 0 && a.ld * (int64_t)sizeof(T) % 16 == 0 &&
+                       (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
+      const dim3 grid((unsigned)ceil_div((int64_t)a.workers * ch.count, groups), (unsigned)slices);
+      return vec ? launch_pdl(embedding_sum_kernel<T, true>, grid, dim3(kSumThreads), 0, stream, a, n, ch)
+                 : launch_pdl(embedding_sum_kernel<T, false>, grid, dim3(kSumThreads), 0, stream, a, n, ch);
+    });
+    if (st != cudaSuccess) return st;
+    if (ch.count > 1) {
+      ++*launches;
+      st = launch_pdl(embedding_join_kernel,
+                      dim3((unsigned)(a.workers * ch.count), (unsigned)ceil_div(a.width, kJoinSlice)), dim3(kJoinThreads),
+                      0, stream, a, n, ch);
+      if (st != cudaSuccess) return st;
+    }
+    begin += n;
+    a.accumulate = 1;
+  } while (begin < a.tokens);
+  return cudaSuccess;
 }
 
 }  // namespace dq
