@@ -34,57 +34,65 @@ __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(Embe
   dq_pdl_enter();
   constexpr int N = kVec ? 16 / (int)sizeof(T) : 1;  // values a thread takes of a row
   const int lane = threadIdx.x % lanes, groups = kForwardThreads / lanes;
-  const int64_t all = a.tokens * a.workers;
-  const int64_t first = ((int64_t)blockIdx.x * kRows) * groups + threadIdx.x / lanes;
-  const E* row[kRows];
-  bool live[kRows];
+  const int64_t all = a.tokens * a.workers, stride = (int64_t)gridDim.x * kRows * groups;
+  int64_t first = ((int64_t)blockIdx.x * kRows) * groups + threadIdx.x / lanes;
+  int32_t id[kRows];
+  const auto ids_at = [&](int64_t at) {
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    const int64_t i = first + r * groups;
-    const int32_t id = i < all ? token_at(a, i) : (int32_t)a.vocab;
-    live[r] = id < a.vocab;
-    row[r] = static_cast<const E*>(a.table) +
-             (live[r] ? (int64_t)((uint32_t)i / (uint32_t)a.tokens) * a.p_stride + (int64_t)id * a.width : 0);
-  }
-  for (int c = lane * N; c < a.width; c += lanes * N) {
-    float v[kRows][N];
-    if constexpr (kVec) {
-      constexpr int kBytes = N * (int)sizeof(E);  // of the table: 8, 16 or 32
-      uint2 p[kRows][kBytes / 8];
-#pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int k = 0; k < kBytes / 8; k += 2) {
-          if constexpr (kBytes >= 16) {
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (live[r]) q = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row[r] + c) + 8 * k);
-            p[r][k] = make_uint2(q.x, q.y);
-            p[r][k + 1] = make_uint2(q.z, q.w);
-          } else {
-            p[r][k] = make_uint2(0, 0);
-            if (live[r]) p[r][k] = *reinterpret_cast<const uint2*>(row[r] + c);
-          }
-        }
-#pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[r][e] = to_float(reinterpret_cast<const E*>(p[r])[e]) * a.scale;
-    } else {
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) v[r][0] = live[r] ? to_float(row[r][c]) * a.scale : 0.f;
-    }
+    for (int r = 0; r < kRows; ++r) id[r] = at + r * groups < all ? token_at(a, at + r * groups) : (int32_t)a.vocab;
+  };
+  ids_at(first);
+  for (; first < all; first += stride) {
+    const E* row[kRows];
+    bool live[kRows];
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
-      const int64_t i = first + r * groups;
-      if (i >= all) continue;
-      T* y = static_cast<T*>(a.y) + i * a.ld + c;
+      const uint32_t i = (uint32_t)(first + r * groups);
+      live[r] = id[r] < a.vocab;
+      row[r] = static_cast<const E*>(a.table) +
+               (live[r] ? (int64_t)(i / (uint32_t)a.tokens) * a.p_stride + (int64_t)id[r] * a.width : 0);
+    }
+    ids_at(first + stride);  // on their way while these rows are
+    for (int c = lane * N; c < a.width; c += lanes * N) {
+      float v[kRows][N];
       if constexpr (kVec) {
-        uint4 q;
+        constexpr int kBytes = N * (int)sizeof(E);  // of the table: 8, 16 or 32
+        uint2 p[kRows][kBytes / 8];
 #pragma unroll
-        for (int e = 0; e < N; ++e) reinterpret_cast<T*>(&q)[e] = from_float<T>(v[r][e]);
-        __stcs(reinterpret_cast<uint4*>(y), q);
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+          for (int k = 0; k < kBytes / 8; k += 2) {
+            if constexpr (kBytes >= 16) {
+              uint4 q = make_uint4(0, 0, 0, 0);
+              if (live[r]) q = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row[r] + c) + 8 * k);
+              p[r][k] = make_uint2(q.x, q.y);
+              p[r][k + 1] = make_uint2(q.z, q.w);
+            } else {
+              p[r][k] = make_uint2(0, 0);
+              if (live[r]) p[r][k] = *reinterpret_cast<const uint2*>(row[r] + c);
+            }
+          }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[r][e] = to_float(reinterpret_cast<const E*>(p[r])[e]) * a.scale;
       } else {
-        *y = from_float<T>(v[r][0]);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) v[r][0] = live[r] ? to_float(row[r][c]) * a.scale : 0.f;
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const int64_t i = first + r * groups;
+        if (i >= all) continue;
+        T* y = static_cast<T*>(a.y) + i * a.ld + c;
+        if constexpr (kVec) {
+          uint4 q;
+#pragma unroll
+          for (int e = 0; e < N; ++e) reinterpret_cast<T*>(&q)[e] = from_float<T>(live[r] ? v[r][e] : 0.f);
+          __stcs(reinterpret_cast<uint4*>(y), q);
+        } else {
+          *y = from_float<T>(v[r][0]);
+        }
       }
     }
   }
@@ -286,6 +294,7 @@ __device__ void fill_rows(const EmbeddingArgs& a, int64_t m, int64_t begin, int 
 __global__ void __launch_bounds__(kSortThreads, 2)
     embedding_sort_kernel(EmbeddingArgs a, int64_t begin, int n, int share, int ranks, int rows, int fills, int skip) {
   dq_pdl_enter();
+  dq_pdl_release();  // the sums' blocks may take up places as this grid's last ones come free
   extern __shared__ __align__(16) unsigned char dynamic[];
   const int sorters = n > 0 ? a.workers * ranks : 0;
   if ((int)blockIdx.x < sorters) {
@@ -298,9 +307,10 @@ __global__ void __launch_bounds__(kSortThreads, 2)
   fill_rows(a, fill / fills, begin, n, v0, min64(v0 + rows, a.vocab), skip != 0, dynamic);
 }
 
-// A thread of the second and third kernel takes kCols columns: one 16-byte pack
-// of dy (two in 32 bits), or (kVec false) columns `lanes` apart.
-constexpr int kSumThreads = 128, kCols = 8, kSlice = kSumThreads * kCols;
+// A thread of the second kernel takes 8 columns: one 16-byte pack of dy (two in
+// 32 bits), or (kVec false) 2 columns, `lanes` apart.
+constexpr int kSumThreads = 128;
+__host__ __device__ constexpr int columns_of(bool vec) { return vec ? 8 : 2; }
 
 struct Chunks {
   int32_t size;   // places of a chunk
@@ -319,15 +329,16 @@ __device__ __forceinline__ float* part_of(const EmbeddingArgs& a, const Chunks& 
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArgs a, int n, Chunks ch) {
   dq_pdl_enter();
-  constexpr int E = 16 / (int)sizeof(T), P = kCols / E;
-  constexpr int kAhead = kVec ? (sizeof(T) == 4 ? 4 : 8) : 2;  // rows of dy on their way at once
+  dq_pdl_release();
+  constexpr int kCols = columns_of(kVec), E = 16 / (int)sizeof(T), P = kVec ? kCols / E : 1;
+  constexpr int kAhead = kVec && sizeof(T) == 4 ? 4 : 8;  // rows of dy on their way at once
   const int lane = threadIdx.x % ch.lanes, groups = kSumThreads / ch.lanes;
   const int64_t which = (int64_t)blockIdx.x * groups + threadIdx.x / ch.lanes;
   if (which >= (int64_t)a.workers * ch.count) return;
   const int64_t m = which / ch.count, chunk = which % ch.count;
   const Sorted s = sorted_of(a, m);
   const int lo = (int)chunk * ch.size, hi = min(lo + ch.size, n);
-  const int c0 = (int)blockIdx.y * kSlice + (kVec ? lane * kCols : lane);
+  const int c0 = (int)blockIdx.y * kSumThreads * kCols + (kVec ? lane * kCols : lane);
   const auto column = [&](int k) { return kVec ? c0 + k : c0 + k * ch.lanes; };
   if (c0 >= a.width) return;
   const T* dy = static_cast<const T*>(a.dy) + m * a.tokens * a.ld;
@@ -373,17 +384,25 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
     came = false;
   };
 
-  for (int j0 = lo; j0 < hi; j0 += kAhead) {
-    int32_t id[kAhead + 1];
-    int32_t place[kAhead];
+  const int32_t after = hi < n ? s.ids[hi] : (int32_t)a.vocab;  // of the next chunk's first place
+  int32_t next_id[kAhead + 1], next_place[kAhead];
+  const auto places_at = [&](int j0) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      id[j] = j0 + j < hi ? s.ids[j0 + j] : (int32_t)a.vocab;
-      place[j] = j0 + j < hi ? s.places[j0 + j] : 0;
+      next_id[j] = j0 + j < hi ? s.ids[j0 + j] : (int32_t)a.vocab;
+      next_place[j] = j0 + j < hi ? s.places[j0 + j] : 0;
     }
-    // of the place after these, wherever it lies
-    id[kAhead] = j0 + kAhead < n ? s.ids[j0 + kAhead] : (int32_t)a.vocab;
-    const int32_t after = hi < n ? s.ids[hi] : (int32_t)a.vocab;  // of the next chunk's first
+    next_id[kAhead] = j0 + kAhead < hi ? s.ids[j0 + kAhead] : after;
+  };
+  places_at(lo);
+  for (int j0 = lo; j0 < hi; j0 += kAhead) {
+    int32_t id[kAhead + 1], place[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      id[j] = next_id[j];
+      place[j] = next_place[j];
+    }
+    id[kAhead] = next_id[kAhead];
     uint4 x[kAhead][P];
     T y[kVec ? 1 : kAhead][kVec ? 1 : kCols];
 #pragma unroll
@@ -400,6 +419,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
             if (column(k) < a.width) y[j][k] = dy[(int64_t)place[j] * a.ld + column(k)];
         }
       }
+    places_at(j0 + kAhead);  // on their way while these rows are
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (j0 + j >= hi || id[j] >= a.vocab) break;  // the places without a token come last
@@ -436,21 +456,21 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingA
   const Sorted s = sorted_of(a, m);
   const int lo = (int)chunk * ch.size, hi = lo + ch.size;
   if (hi >= n) return;  // nothing after it
-  const int32_t id = s.ids[hi];
-  if (id >= a.vocab || s.ids[hi - 1] != id) return;
-  if (s.ids[lo] == id && lo > 0 && s.ids[lo - 1] == id) return;  // it began earlier
-  // the run's last chunk: the first whose next one starts with another id
   const int lane = threadIdx.x & 31;
+  const int64_t after = hi + (int64_t)(lane + 1) * ch.size;  // the first place of the chunk after chunk + 1 + lane
+  const int32_t id = s.ids[hi], id_last = s.ids[hi - 1], id_first = s.ids[lo], id_before = lo > 0 ? s.ids[lo - 1] : -1;
+  const int32_t id_after = after < n ? s.ids[after] : -1;
+  if (id >= a.vocab || id_last != id) return;
+  if (id_first == id && id_before == id) return;  // it began earlier
+  // the run's last chunk: the first whose next one starts with another id
   int64_t last = chunk + 1;
-  for (;;) {
-    const int64_t next = (last + lane + 1) * ch.size;
-    const unsigned ends = __ballot_sync(kFullMask, next >= n || s.ids[next] != id);
-    if (ends != 0) {
-      last += __ffs(ends) - 1;
-      break;
-    }
+  unsigned ends = __ballot_sync(kFullMask, id_after != id);
+  while (ends == 0) {
     last += 32;
+    const int64_t next = (last + lane + 1) * ch.size;
+    ends = __ballot_sync(kFullMask, next >= n || s.ids[next] != id);
   }
+  last += __ffs(ends) - 1;
   // two halves of the block take half of the parts each
   const int half = threadIdx.x / (kJoinThreads / 2), t = threadIdx.x % (kJoinThreads / 2);
   const int64_t count = last - chunk + 1, mid = (count + 1) / 2;
@@ -483,10 +503,10 @@ int lanes_for(int64_t width, int per_thread, int most) {
 // Chunks small enough for 32 blocks of the second kernel on every SM, of at least 16 places.
 constexpr int64_t kSumBlocks = 152 * 32;
 
-Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
+Chunks chunks_of(int64_t n, int64_t width, int64_t workers, bool vec) {
   Chunks ch;
-  ch.lanes = lanes_for(width, kCols, kSumThreads);
-  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
+  ch.lanes = lanes_for(width, columns_of(vec), kSumThreads);
+  const int64_t slices = ceil_div(width, kSumThreads * columns_of(vec)), groups = kSumThreads / ch.lanes;
   ch.size = (int32_t)max64(16, ceil_div(n * workers * slices, kSumBlocks * groups));
   ch.count = (int32_t)max64(1, ceil_div(n, ch.size));
   return ch;
@@ -497,8 +517,8 @@ Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
 size_t embedding_scratch_bytes(int64_t, int64_t width, int64_t max_tokens, int32_t workers) {
   const int64_t n = section_of(max_tokens);
   // the most chunks that any smaller number of tokens makes: n workers slices / size <= blocks groups
-  const Chunks ch = chunks_of(n, width, workers);
-  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
+  const Chunks ch = chunks_of(n, width, workers, true);
+  const int64_t slices = ceil_div(width, kSumThreads * columns_of(true)), groups = kSumThreads / ch.lanes;
   const int64_t chunks = min64(workers * ceil_div(n, 16), kSumBlocks * groups / slices + workers);
   return 4 * (size_t)((2 * n * workers + 3) / 4 * 4) + 8 * (size_t)chunks * (size_t)((width + 3) / 4 * 4);
 }
@@ -516,9 +536,13 @@ cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t stream
                        (uintptr_t)a.table % kAlign == 0 && a.width * (int64_t)sizeof(E) % kAlign == 0 &&
                        a.p_stride * (int64_t)sizeof(E) % kAlign == 0;
       const int lanes = lanes_for(a.width, vec ? N : 1, kForwardThreads);
-      const dim3 grid((unsigned)ceil_div(n, kRows * (kForwardThreads / lanes)));
-      return vec ? launch_pdl(embedding_forward_kernel<E, T, true>, grid, dim3(kForwardThreads), 0, stream, a, lanes)
-                 : launch_pdl(embedding_forward_kernel<E, T, false>, grid, dim3(kForwardThreads), 0, stream, a, lanes);
+      const auto kern = vec ? embedding_forward_kernel<E, T, true> : embedding_forward_kernel<E, T, false>;
+      static std::atomic<int> kept[2][kKeptDevices];
+      int resident = 0;
+      const cudaError_t st = resident_ctas(kern, kForwardThreads, 0, 0, kept[vec ? 1 : 0], &resident);
+      if (st != cudaSuccess) return st;
+      const int64_t blocks = min64(ceil_div(n, kRows * (kForwardThreads / lanes)), resident);
+      return launch_pdl(kern, dim3((unsigned)blocks), dim3(kForwardThreads), 0, stream, a, lanes);
     });
   });
 }
@@ -532,20 +556,23 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     int ranks = 1;
     while (ranks < 8 && ceil_div(n, ranks) > 4096) ranks *= 2;
     const int share = (int)max64(ceil_div(n, ranks), 1);
+    const int64_t sorters = n > 0 ? (int64_t)a.workers * ranks : 0;
     int64_t rows = 1, fills = 0;
     bool skip = false;
+    int shared = (int)(n > 0 ? 8 * (int64_t)share + 2 * kSortWarps * kMostBins : 0);
     if (!a.accumulate) {
-      // rows of a filling block: at least a 16th MB, about a 4th of what falls to an SM up to 1 MB, and
-      // four times the bytes of the ids that it looks through
-      const int64_t row = 4 * a.width, least = max64(64 << 10, min64(1 << 20, a.workers * a.vocab * row / (152 * 4)));
-      const int64_t bytes = max64(least, 4 * (int64_t)n * a.token_bits / 8);
-      skip = n > 0 && a.vocab * row >= bytes;
-      rows = min64(max64((skip ? bytes : least) / row, 1), kFillRows);
+      // filling blocks for whole waves of the GPU, of at least a 16th MB each, and of four times the bytes
+      // of the ids that a block looks through to find the rows to leave alone
+      const int64_t all = 4 * a.width * a.vocab, ids = (int64_t)n * a.token_bits / 8;
+      skip = n > 0 && all >= max64(64 << 10, 4 * ids);
+      if (skip) shared = (int)max64(shared, kFillRows / 8);
+      const int64_t at_once = max64(1, device_sms()) * (shared <= (100 << 10) ? 2 : 1);
+      const int64_t waves = max64(1, min64(8, a.workers * all / (at_once * max64(64 << 10, skip ? 4 * ids : 0))));
+      fills = max64(1, (waves * at_once - sorters) / a.workers);
+      rows = min64(max64(ceil_div(a.vocab, fills), ceil_div(64 << 10, 4 * a.width)), kFillRows);
       fills = ceil_div(a.vocab, rows);
     }
-    const int64_t sorters = n > 0 ? (int64_t)a.workers * ranks : 0;
     const int64_t blocks = ceil_div(sorters + fills * a.workers, ranks) * ranks;
-    const int shared = (int)max64(n > 0 ? 8 * (int64_t)share + 2 * kSortWarps * kMostBins : 0, skip ? kFillRows / 8 : 0);
     static std::atomic<int> kept[kKeptDevices];
     int resident = 0;
     cudaError_t st = resident_ctas(embedding_sort_kernel, kSortThreads, 8 * kSortMost + 2 * kSortWarps * kMostBins,
@@ -559,13 +586,14 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     }
     if (n == 0) return cudaSuccess;
     // 2. and 3. sum
-    const Chunks ch = chunks_of(n, a.width, a.workers);
-    const int64_t slices = ceil_div(a.width, kSlice), groups = kSumThreads / ch.lanes;
+    const int size = a.dtype == DQGAN_F32 ? 4 : 2;
+    const bool vec = a.width % columns_of(true) == 0 && (uintptr_t)a.dy % 16 == 0 && a.ld * size % 16 == 0 &&
+                     (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
+    const Chunks ch = chunks_of(n, a.width, a.workers, vec);
+    const int64_t slices = ceil_div(a.width, kSumThreads * columns_of(vec)), groups = kSumThreads / ch.lanes;
     ++*launches;
     st = with_dtype(a.dtype, [&](auto t) {
       using T = decltype(t);
-      const bool vec = a.width % kCols == 0 && (uintptr_t)a.dy % 16 == 0 && a.ld * (int64_t)sizeof(T) % 16 == 0 &&
-                       (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
       const dim3 grid((unsigned)ceil_div((int64_t)a.workers * ch.count, groups), (unsigned)slices);
       return vec ? launch_pdl(embedding_sum_kernel<T, true>, grid, dim3(kSumThreads), 0, stream, a, n, ch)
                  : launch_pdl(embedding_sum_kernel<T, false>, grid, dim3(kSumThreads), 0, stream, a, n, ch);

@@ -390,6 +390,7 @@ __global__ void __launch_bounds__(backward_threads<T, kLanes>(), 1) layer_norm_b
     stage = stage + 1 == kStages ? 0 : stage + 1;
     parity ^= 1;
   }
+  dq_pdl_release();  // the join's blocks, if any, may take up places as this grid's come free
   if (!a.dweight && !a.dbias) return;
   // the groups' sums in order, through shared memory in the ring's place
   float* sums = reinterpret_cast<float*>(dynamic);
