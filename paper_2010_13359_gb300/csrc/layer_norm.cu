@@ -150,16 +150,14 @@ __device__ __forceinline__ void row_sum_collect(float (&v)[K], const float* shar
 }
 
 // A block's threads: one row for each kLanes of them.  Register use decides
-// (forward: three blocks of 256 on an SM; backward: one of 512, or of 256 in
-// 32 bits, whose rows take twice the shared memory).
+// (forward: three blocks of 256 on an SM; backward: one of 512).
 template <int kLanes>
 constexpr int forward_threads() {
   return kLanes > 256 ? kLanes : 256;
 }
-template <typename T, int kLanes>
+template <int kLanes>
 constexpr int backward_threads() {
-  constexpr int kLeast = sizeof(T) == 4 ? 256 : 512;
-  return kLanes > kLeast ? kLanes : kLeast;
+  return kLanes > 512 ? kLanes : 512;
 }
 
 // Rows on their way or at work in shared memory, `rows` vectors of them to a stage.
@@ -174,20 +172,22 @@ constexpr int forward_stages() {
 }
 template <typename T, int kLanes>
 constexpr int backward_stages() {
-  return stages_that_fit<T>(backward_threads<T, kLanes>(), 2, 200 << 10, 6);
+  return stages_that_fit<T>(backward_threads<kLanes>(), 2, 200 << 10, 6);
 }
 
 // Forward.  Blocks walk over a worker's rows, with its weight and bias in
 // registers.  The next rows are on their way while one is worked on: every
 // thread copies its own packs to its own places in shared memory, so no barrier
 // guards them.
-template <typename T, int kLanes, bool kVec>
+// kWhole: the width is a multiple of a pack, so no pack needs looking into.
+template <typename T, int kLanes, bool kVec, bool kWhole>
 __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : kLanes > 256 ? 2 : 3)
     layer_norm_forward_kernel(LayerNormArgs a) {
   dq_pdl_enter();
   using S = Slice<T, kLanes, kVec>;
   constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
   constexpr int kStages = forward_stages<T, kLanes>();
+  constexpr bool ragged = !kWhole;
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ float shared[2][kThreads / 32];
   uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][pack][thread]
@@ -234,25 +234,28 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
     row_sum_publish<kLanes, 1>(s, shared[0]);
     row_wait<kLanes>();
     row_sum_collect<kLanes, 1>(s, shared[0]);
-    const float mean = s[0] / (float)width;
+    const float mean = s[0] * inv_width;
     t = both(0.f);
 #pragma unroll
-    for (int i = 0; i < S::N; ++i)
+    for (int i = 0; i < S::N; ++i) {  // nothing past the row's end counts
+      float2 u = both(0.f);
 #pragma unroll
       for (int e = 0; e < S::E; e += 2) {
         float2 d = add2(x[i][e / 2], both(-mean));
         x[i][e / 2] = d;
-        if (!kVec || S::at(i, S::E - 1, lane) >= width) {  // nothing past the row's end counts
+        if (ragged) {
           if (S::at(i, e, lane) >= width) d.x = 0.f;
           if (S::at(i, e + 1, lane) >= width) d.y = 0.f;
         }
-        t = fma2(d, d, t);
+        u = fma2(d, d, u);
       }
+      if (ragged || S::at(i, 0, lane) < width) t = add2(t, u);
+    }
     s[0] = t.x + t.y;
     row_sum_publish<kLanes, 1>(s, shared[1]);
     row_wait<kLanes>();
     row_sum_collect<kLanes, 1>(s, shared[1]);
-    const float rstd = 1.f / sqrtf(fmaf(s[0], inv_width, a.eps));
+    const float rstd = rsqrtf(fmaf(s[0], inv_width, a.eps));  // 2 units at most, at a sixth of the division's instructions
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
 #pragma unroll
@@ -268,6 +271,9 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
   }
 }
 
+// A row of the scratch space, in floats: whole 16-byte packs.
+__host__ __device__ constexpr int64_t part_stride(int64_t width) { return (width + 3) / 4 * 4; }
+
 // Backward.  A block walks over rows of one worker, its rows ahead on their way
 // as above, and keeps each column's sums for dweight and dbias in registers; what
 // it has at the end goes to its row of the scratch space, and a second kernel
@@ -276,10 +282,10 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
 // packs in shared memory, which hides the exchange between the row's warps:
 // one barrier a row.
 template <typename T, int kLanes, bool kVec>
-__global__ void __launch_bounds__(backward_threads<T, kLanes>(), 1) layer_norm_backward_kernel(LayerNormArgs a) {
+__global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_backward_kernel(LayerNormArgs a) {
   dq_pdl_enter();
   using S = Slice<T, kLanes, kVec>;
-  constexpr int kThreads = backward_threads<T, kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kThreads = backward_threads<kLanes>(), kGroups = kThreads / kLanes;
   constexpr int kStages = backward_stages<T, kLanes>();
   constexpr bool kRing = kVec && kStages >= 3;  // else a row is read again from the caches
   extern __shared__ __align__(16) unsigned char dynamic[];
@@ -410,7 +416,7 @@ __global__ void __launch_bounds__(backward_threads<T, kLanes>(), 1) layer_norm_b
     if (!out) continue;
     out += m * a.g_stride;
     const bool whole = parts == 1;
-    float* part = a.scratch + ((m * parts + blockIdx.x) * 2 + which) * a.width;
+    float* part = a.scratch + ((m * parts + blockIdx.x) * 2 + which) * part_stride(a.width);
     const auto put = [&](int c, float v) {
       if (whole) out[c] = a.accumulate ? out[c] + v : v;
       else part[c] = v;
@@ -427,28 +433,37 @@ __global__ void __launch_bounds__(backward_threads<T, kLanes>(), 1) layer_norm_b
   }
 }
 
-// The blocks' rows of the scratch space, added up in order: a block takes 32
-// columns of one worker's dweight or dbias, its warps every kWarps-th row.
+// The blocks' rows of the scratch space, added up in order: a block takes 128
+// columns of one worker's dweight or dbias, its warps every kJoinWarps-th row.
 constexpr int kJoinWarps = 8;
 
 __global__ void __launch_bounds__(kJoinWarps * 32) layer_norm_join_kernel(LayerNormArgs a, int parts) {
   dq_pdl_enter();
-  __shared__ float shared[kJoinWarps][32];
+  __shared__ float4 shared[kJoinWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, which = blockIdx.z;
-  const int64_t m = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
+  const int64_t m = blockIdx.y, c = ((int64_t)blockIdx.x * 32 + lane) * 4;
   float* out = which == 0 ? a.dweight : a.dbias;
   if (!out) return;
-  float v = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < a.width)
 #pragma unroll 4
-    for (int p = warp; p < parts; p += kJoinWarps) v += a.scratch[((m * parts + p) * 2 + which) * a.width + c];
+    for (int p = warp; p < parts; p += kJoinWarps) {
+      const float4 w = *reinterpret_cast<const float4*>(a.scratch + ((m * parts + p) * 2 + which) * part_stride(a.width) + c);
+      v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+    }
   shared[warp][lane] = v;
   __syncthreads();
-  if (warp != 0 || c >= a.width) return;
+  if (warp != 0) return;
 #pragma unroll
-  for (int i = 1; i < kJoinWarps; ++i) v += shared[i][lane];
+  for (int i = 1; i < kJoinWarps; ++i) {
+    const float4 w = shared[i][lane];
+    v = make_float4(v.x + w.x, v.y + w.y, v.z + w.z, v.w + w.w);
+  }
   out += m * a.g_stride + c;
-  *out = a.accumulate ? *out + v : v;
+  const float sums[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (c + k < a.width) out[k] = a.accumulate ? out[k] + sums[k] : sums[k];
 }
 
 // Rows of more than kMaxOnChip values, one block each: further passes over the
@@ -570,23 +585,23 @@ bool rows_aligned(const void* p, int64_t ld, size_t size) {
   return ((uintptr_t)p & 15u) == 0 && ld * (int64_t)size % 16 == 0;
 }
 
-template <typename T, int kLanes, bool kVec>
+template <typename T, int kLanes, bool kVec, bool kWhole>
 cudaError_t forward(const LayerNormArgs& a, cudaStream_t stream) {
   constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
   constexpr int kShared = kVec ? forward_stages<T, kLanes>() * kThreads * kPerThread * (int)sizeof(T) : 0;
   static std::atomic<int> kept[kKeptDevices];
   int resident = 0;
   const cudaError_t st =
-      resident_ctas(layer_norm_forward_kernel<T, kLanes, kVec>, kThreads, kShared, kShared, kept, &resident);
+      resident_ctas(layer_norm_forward_kernel<T, kLanes, kVec, kWhole>, kThreads, kShared, kShared, kept, &resident);
   if (st != cudaSuccess) return st;
   const int64_t blocks = min64(max64(resident / a.workers, 1), ceil_div(a.rows, kGroups));
-  return launch_pdl(layer_norm_forward_kernel<T, kLanes, kVec>, dim3((unsigned)blocks, (unsigned)a.workers),
+  return launch_pdl(layer_norm_forward_kernel<T, kLanes, kVec, kWhole>, dim3((unsigned)blocks, (unsigned)a.workers),
                     dim3(kThreads), kShared, stream, a);
 }
 
 template <typename T, int kLanes, bool kVec>
 cudaError_t backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches) {
-  constexpr int kThreads = backward_threads<T, kLanes>(), kGroups = kThreads / kLanes;
+  constexpr int kThreads = backward_threads<kLanes>(), kGroups = kThreads / kLanes;
   constexpr int kStages = backward_stages<T, kLanes>();
   constexpr int kRing = kVec && kStages >= 3 ? kStages * 2 * kThreads * kPerThread * (int)sizeof(T) : 0;
   constexpr int kSums = kGroups > 1 ? kThreads * kPerThread * 4 : 0;
@@ -603,14 +618,14 @@ cudaError_t backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* laun
                   kShared, stream, a);
   if (st != cudaSuccess || !sums || parts == 1) return st;
   ++*launches;
-  return launch_pdl(layer_norm_join_kernel, dim3((unsigned)ceil_div(a.width, 32), (unsigned)a.workers, 2),
+  return launch_pdl(layer_norm_join_kernel, dim3((unsigned)ceil_div(a.width, 128), (unsigned)a.workers, 2),
                     dim3(kJoinWarps * 32), 0, stream, a, (int)parts);
 }
 
 }  // namespace
 
 size_t layer_norm_scratch_bytes(int64_t width, int32_t workers) {
-  return width <= kMaxOnChip ? 8 * (size_t)width * (size_t)backward_blocks(workers) : 0;
+  return width <= kMaxOnChip ? 8 * (size_t)part_stride(width) * (size_t)backward_blocks(workers) : 0;
 }
 
 cudaError_t launch_layer_norm_forward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches) {
@@ -624,7 +639,9 @@ cudaError_t launch_layer_norm_forward(const LayerNormArgs& a, cudaStream_t strea
     const bool vec = rows_aligned(a.x, a.x_ld, sizeof(T)) && rows_aligned(a.out, a.out_ld, sizeof(T));
     return with_lanes(a.width, [&](auto lanes) {
       constexpr int kLanes = decltype(lanes)::value;
-      return vec ? forward<T, kLanes, true>(a, stream) : forward<T, kLanes, false>(a, stream);
+      if (!vec) return forward<T, kLanes, false, false>(a, stream);
+      return a.width % (16 / (int64_t)sizeof(T)) == 0 ? forward<T, kLanes, true, true>(a, stream)
+                                                       : forward<T, kLanes, true, false>(a, stream);
     });
   });
 }
