@@ -169,7 +169,6 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 // row, and the values before the first and after the last pack belong to the first
 // helper warp, a lane each.
 constexpr int kMostWorkers = 256;
-constexpr int kPieceBytes = 64 << 10;
 constexpr int kMostShared = 220 << 10;
 
 template <typename T>
@@ -684,10 +683,27 @@ template <typename T, DistillationWay kWay>
 cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
   const int packs = held_packs<T>(a.vocab, 1);
   int workers = 32, pieces = 1;
-  // 4096 bf16 rows, us with 8 | 16 packs a worker: 16,000 values 69 | 55, 8000 values 38 | 36, 4000 values
-  // (64 workers | 32) 28 | 38
-  while (workers < kMostWorkers && packs > workers * (workers == 32 ? 8 : 16)) workers *= 2;
-  while (pieces < 8 && packs * 16 > pieces * kPieceBytes) ++pieces;
+  if (packs <= 64 * 16) {
+    // 4096 rows of 4000 bf16 values: 28 us with 64 workers, 38 with 32
+    if (packs > 32 * 8) workers = 64;
+  } else {
+    // What counts is the rows on their way on an SM, as far as registers (launch bounds) and shared memory let
+    // blocks onto it, and next the warps: 4096 rows, % of the measured copy bandwidth by (workers, pieces):
+    // 50,000 bf16 values (256, 1) 200 KB on an SM: 89, (256, 2) 150 KB: 72; 80,000 (128, 4) 200 KB: 78, (256, 3)
+    // 160 KB: 73; 128,000 (256, 4) 192 KB: 84, (128, 4) 192 KB: 79.
+    int64_t best = 0;
+    for (int w = 128; w <= kMostWorkers; w *= 2)
+      for (int p = 1; p <= 8; ++p) {
+        const int shared = held_shared<T>(a.k, a.vocab, p), threads = w + w / 4;
+        if (shared > kMostShared || packs < p * w * 8) continue;
+        const int64_t blocks = min64(1024 / threads, (226 << 10) / (shared + (3 << 10)));
+        const int64_t score = min64(blocks * (packs / p) * 16, 200 << 10) * (w == kMostWorkers ? 11 : 10);
+        if (score <= best) continue;
+        best = score;
+        workers = w;
+        pieces = p;
+      }
+  }
   if (held_shared<T>(a.k, a.vocab, pieces) > kMostShared)
     return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle

@@ -22,7 +22,8 @@ constexpr int kMaxOnChip = 1024 * kPerThread;
 // A thread's share of a row: N packs of E values.  kVec: pack i of lane t holds
 // values (i * kLanes + t) * E and the E - 1 after it; else (rows that do not
 // start on 16-byte boundaries) value e of pack i is (i * E + e) * kLanes + t, so
-// that single-element accesses of a warp are adjacent.
+// that single-element accesses of a warp are adjacent.  Such rows come into shared
+// memory as the aligned packs that hold them, copied by all of a row's threads.
 template <typename T, int kLanes, bool kVec>
 struct Slice {
   static constexpr int E = 16 / (int)sizeof(T);
@@ -46,14 +47,37 @@ struct Slice {
     }
   }
 
-  // The same into this thread's places of a ring stage (`stride` packs apart).
-  __device__ __forceinline__ static void fetch(const T* row, int width, int lane, uint4* to, int stride) {
+  // Packs of a row vector in the ring, and where this thread's row begins in them.
+  __host__ __device__ static constexpr int ring_packs(int threads) { return threads * N + (kVec ? 0 : threads / kLanes); }
+  __device__ __forceinline__ static int ring_at() { return kVec ? (int)threadIdx.x : (int)threadIdx.x / kLanes * (kLanes * N + 1); }
+
+  // The row into a ring stage, 0 past its end.
+  __device__ __forceinline__ static void fetch(const T* row, int width, int lane, uint4* to, int threads) {
+    const int shift = kVec ? 0 : (int)((uintptr_t)row & 15u);
+    const char* from = reinterpret_cast<const char*>(row) - shift;
+    to += ring_at();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int left = (width - at(i, 0, lane)) * (int)sizeof(T);
+    for (int i = 0; i < (kVec ? N : N + 1); ++i) {
+      if (i == N && lane > 0) break;  // one pack more than the threads' N
+      const int pack = i * kLanes + lane, left = shift + width * (int)sizeof(T) - 16 * pack;
       const int bytes = left >= 16 ? 16 : left > 0 ? left : 0;
-      copy16_async(to + i * stride, row + (bytes > 0 ? at(i, 0, lane) : 0), bytes);
+      copy16_async(kVec ? to + i * threads : to + pack, from + (bytes > 0 ? 16 * pack : 0), bytes);
     }
+  }
+
+  // What fetch brought.
+  __device__ __forceinline__ static void take(const uint4* from, const T* row, int lane, int threads, uint4 (&x)[N]) {
+    from += ring_at();
+    if (kVec) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = from[i * threads];
+      return;
+    }
+    const T* values = reinterpret_cast<const T*>(reinterpret_cast<const char*>(from) + ((uintptr_t)row & 15u));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&x[i])[e] = values[at(i, e, lane)];
   }
 
   __device__ __forceinline__ static void store(T* row, int width, int lane, const uint4 (&y)[N]) {
@@ -121,10 +145,11 @@ __device__ __forceinline__ void row_sum_publish(float (&v)[K], float* shared) {
       for (int k = 0; k < K; ++k) shared[threadIdx.x / 32 * K + k] = v[k];
 }
 
-// Waits for the other threads of this thread's row (nothing up to a warp).
+// Waits for the other threads of this thread's row.
 template <int kLanes>
 __device__ __forceinline__ void row_wait() {
-  if constexpr (kLanes > 32)
+  if constexpr (kLanes <= 32) __syncwarp();
+  else
     asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / kLanes), "n"(kLanes) : "memory");
 }
 
@@ -160,19 +185,16 @@ constexpr int backward_threads() {
   return kLanes > 512 ? kLanes : 512;
 }
 
-// Rows on their way or at work in shared memory, `rows` vectors of them to a stage.
-template <typename T>
-constexpr int stages_that_fit(int threads, int rows, int bytes, int most) {
-  const int fit = bytes / (rows * threads * kPerThread * (int)sizeof(T));
-  return fit > most ? most : fit;
-}
-template <typename T, int kLanes>
+// Rows on their way or at work in shared memory, as far as they fit.
+template <typename T, int kLanes, bool kVec>
 constexpr int forward_stages() {
-  return stages_that_fit<T>(forward_threads<kLanes>(), 1, (kLanes > 256 ? 128 : 64) << 10, 4);
+  constexpr int kFit = ((kLanes > 256 ? 132 : 68) << 10) / (16 * Slice<T, kLanes, kVec>::ring_packs(forward_threads<kLanes>()));
+  return kFit > 4 ? 4 : kFit;
 }
-template <typename T, int kLanes>
+template <typename T, int kLanes, bool kVec>
 constexpr int backward_stages() {
-  return stages_that_fit<T>(backward_threads<kLanes>(), 2, 200 << 10, 6);
+  constexpr int kFit = (208 << 10) / (32 * Slice<T, kLanes, kVec>::ring_packs(backward_threads<kLanes>()));
+  return kFit > 6 ? 6 : kFit;
 }
 
 // Forward.  Blocks walk over a worker's rows, with its weight and bias in
@@ -186,19 +208,18 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
   dq_pdl_enter();
   using S = Slice<T, kLanes, kVec>;
   constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
-  constexpr int kStages = forward_stages<T, kLanes>();
+  constexpr int kStages = forward_stages<T, kLanes, kVec>(), kPacks = S::ring_packs(kThreads);
   constexpr bool ragged = !kWhole;
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ float shared[2][kThreads / 32];
-  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][pack][thread]
+  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][packs]
   const int width = (int)a.width, lane = threadIdx.x % kLanes;
   const int64_t m = blockIdx.y, step = (int64_t)gridDim.x * kGroups;
   const int64_t first = (int64_t)blockIdx.x * kGroups;
   const T* xs = static_cast<const T*>(a.x) + m * a.rows * a.x_ld;
   T* ys = static_cast<T*>(a.out) + m * a.rows * a.out_ld;
   const auto fetch = [&](int64_t r, int stage) {
-    if (!kVec) return;
-    if (r < a.rows) S::fetch(xs + r * a.x_ld, width, lane, ring + stage * S::N * kThreads + threadIdx.x, kThreads);
+    if (r < a.rows) S::fetch(xs + r * a.x_ld, width, lane, ring + stage * kPacks, kThreads);
     copies_begun();
   };
   const int64_t mine = first + threadIdx.x / kLanes;
@@ -209,6 +230,10 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
   S::params(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, width, lane, b);
   const float inv_width = 1.f / (float)width;
   int stage = 0;
+  if (!kVec) {
+    wait_copies<kStages - 2>();
+    row_wait<kLanes>();
+  }
   for (int64_t r0 = first; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + threadIdx.x / kLanes;
     const bool live = r < a.rows;
@@ -216,12 +241,9 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
     if (kVec) {
       fetch(r + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
       wait_copies<kStages - 1>();
-#pragma unroll
-      for (int i = 0; i < S::N; ++i) p[i] = ring[(stage * S::N + i) * kThreads + threadIdx.x];
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-    } else if (live) {
-      S::load(xs + r * a.x_ld, width, lane, p);
     }
+    S::take(ring + stage * kPacks, xs + r * a.x_ld, lane, kThreads, p);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
     float2 x[S::N][S::E / 2], t = both(0.f);
 #pragma unroll
     for (int i = 0; i < S::N; ++i)
@@ -233,6 +255,10 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
     float s[1] = {t.x + t.y};
     row_sum_publish<kLanes, 1>(s, shared[0]);
     row_wait<kLanes>();
+    if (!kVec) {  // the row before was taken by all; the next one has come when they meet again
+      fetch(r + (kStages - 1) * step, stage >= 2 ? stage - 2 : stage + kStages - 2);
+      wait_copies<kStages - 2>();
+    }
     row_sum_collect<kLanes, 1>(s, shared[0]);
     const float mean = s[0] * inv_width;
     t = both(0.f);
@@ -286,11 +312,11 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
   dq_pdl_enter();
   using S = Slice<T, kLanes, kVec>;
   constexpr int kThreads = backward_threads<kLanes>(), kGroups = kThreads / kLanes;
-  constexpr int kStages = backward_stages<T, kLanes>();
-  constexpr bool kRing = kVec && kStages >= 3;  // else a row is read again from the caches
+  constexpr int kStages = backward_stages<T, kLanes, kVec>(), kPacks = S::ring_packs(kThreads);
+  constexpr bool kRing = kStages >= 3;  // else a row is read again from the caches
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ float shared[2][kThreads / 32 * 2];
-  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][x, dy][pack][thread]
+  uint4* ring = reinterpret_cast<uint4*>(dynamic);  // [stage][x, dy][packs]
   const int width = (int)a.width, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int64_t m = blockIdx.y, parts = gridDim.x, step = parts * kGroups;
   const int64_t first = (int64_t)blockIdx.x * kGroups;
@@ -300,20 +326,16 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
   const auto fetch = [&](int64_t r, int stage) {
     if (!kRing) return;
     if (r < a.rows) {
-      uint4* to = ring + stage * 2 * S::N * kThreads + threadIdx.x;
+      uint4* to = ring + stage * 2 * kPacks;
       S::fetch(xs + r * a.x_ld, width, lane, to, kThreads);
-      S::fetch(dys + r * a.dy_ld, width, lane, to + S::N * kThreads, kThreads);
+      S::fetch(dys + r * a.dy_ld, width, lane, to + kPacks, kThreads);
     }
     copies_begun();
   };
   const auto take = [&](int64_t r, int stage, uint4 (&x)[S::N], uint4 (&g)[S::N]) {
     if (kRing) {
-      const uint4* from = ring + stage * 2 * S::N * kThreads + threadIdx.x;
-#pragma unroll
-      for (int i = 0; i < S::N; ++i) {
-        x[i] = from[i * kThreads];
-        g[i] = from[(S::N + i) * kThreads];
-      }
+      S::take(ring + stage * 2 * kPacks, xs + r * a.x_ld, lane, kThreads, x);
+      S::take(ring + stage * 2 * kPacks + kPacks, dys + r * a.dy_ld, lane, kThreads, g);
     } else {
       S::load(xs + r * a.x_ld, width, lane, x);
       S::load(dys + r * a.dy_ld, width, lane, g);
@@ -337,6 +359,10 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
     next_rstd = a.rstd[m * a.rows + first + group];
   }
   int stage = 0, before = 0, parity = 0;
+  if (!kVec && kRing) {
+    wait_copies<kStages >= 3 ? kStages - 3 : 0>();
+    row_wait<kLanes>();
+  }
   int64_t last = -1;  // the row before
   for (int64_t r0 = first; r0 < a.rows + step; r0 += step) {
     const int64_t r = r0 + group;
@@ -344,7 +370,8 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
     const float new_mean = next_mean, new_rstd = next_rstd;
     if (kRing) {  // the stage of the row before last is free
       fetch(r + (kStages - 2) * step, stage + kStages - 2 >= kStages ? stage - 2 : stage + kStages - 2);
-      wait_copies<kStages - 2 >= 0 ? kStages - 2 : 0>();
+      // rows that all of their threads copy: the one after this has come when they meet at the turn's end
+      wait_copies<kVec ? (kStages >= 2 ? kStages - 2 : 0) : (kStages >= 3 ? kStages - 3 : 0)>();
     }
     if (r < a.rows) {
       if (r + step < a.rows) {
@@ -588,7 +615,7 @@ bool rows_aligned(const void* p, int64_t ld, size_t size) {
 template <typename T, int kLanes, bool kVec, bool kWhole>
 cudaError_t forward(const LayerNormArgs& a, cudaStream_t stream) {
   constexpr int kThreads = forward_threads<kLanes>(), kGroups = kThreads / kLanes;
-  constexpr int kShared = kVec ? forward_stages<T, kLanes>() * kThreads * kPerThread * (int)sizeof(T) : 0;
+  constexpr int kShared = forward_stages<T, kLanes, kVec>() * 16 * Slice<T, kLanes, kVec>::ring_packs(kThreads);
   static std::atomic<int> kept[kKeptDevices];
   int resident = 0;
   const cudaError_t st =
@@ -602,8 +629,8 @@ cudaError_t forward(const LayerNormArgs& a, cudaStream_t stream) {
 template <typename T, int kLanes, bool kVec>
 cudaError_t backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches) {
   constexpr int kThreads = backward_threads<kLanes>(), kGroups = kThreads / kLanes;
-  constexpr int kStages = backward_stages<T, kLanes>();
-  constexpr int kRing = kVec && kStages >= 3 ? kStages * 2 * kThreads * kPerThread * (int)sizeof(T) : 0;
+  constexpr int kStages = backward_stages<T, kLanes, kVec>();
+  constexpr int kRing = kStages >= 3 ? kStages * 32 * Slice<T, kLanes, kVec>::ring_packs(kThreads) : 0;
   constexpr int kSums = kGroups > 1 ? kThreads * kPerThread * 4 : 0;
   constexpr int kShared = kRing > kSums ? kRing : kSums;
   static std::atomic<int> kept[kKeptDevices];
