@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(Embe
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortMost = 20480;  // places of one block: two buffers of them in shared memory
+constexpr int kCarryMost = kSortMost / 2;  // up to here with their ids, which else are read again
 constexpr int kSection = 8 * kSortMost;  // places that are sorted at once; more are taken in turn, and added
 constexpr int kMostBins = 512;
 constexpr int kFillRows = 1 << 16;  // rows of one filling block, a bit each
@@ -141,12 +142,13 @@ __device__ __forceinline__ uint32_t in_block(const void* p, int rank) {  // the 
 // of the cluster's blocks: passes of up to 9 bits from the lowest, each of which keeps
 // the order within a digit.  A warp counts the digits of its part of the block's places, the counts are
 // added up over warps, blocks and digits, and every place goes to where its digit's
-// earlier ones end, in the shared memory of the block that holds that position.
+// earlier ones end, in the shared memory of the block that holds that position.  kCarry: its id goes with it.
+template <bool kCarry>
 __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, int n, int share, int rank, int ranks,
                              unsigned char* dynamic) {
-  uint32_t* from = reinterpret_cast<uint32_t*>(dynamic);
-  uint32_t* to = from + share;
-  uint16_t* counts = reinterpret_cast<uint16_t*>(to + share);  // [warp][bin]
+  uint32_t* from = reinterpret_cast<uint32_t*>(dynamic);  // places, then (kCarry) ids
+  uint32_t* to = from + (kCarry ? 2 : 1) * share;
+  uint16_t* counts = reinterpret_cast<uint16_t*>(to + (kCarry ? 2 : 1) * share);  // [warp][bin]
   __shared__ uint32_t totals[kMostBins], bases[kMostBins], warp_sums[kSortWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const int mine = max(0, min(share, n - rank * share));
@@ -156,22 +158,26 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
   const int bins = 1 << width;
   const int64_t at = m * a.tokens;
   const Sorted out = sorted_of(a, m);
-  for (int i = threadIdx.x; i < mine; i += kSortThreads) from[i] = (uint32_t)(begin + rank * share + i);
+  constexpr int kBatch = 4;  // ids on their way at once
+#pragma unroll 4
+  for (int i = threadIdx.x; i < mine; i += kSortThreads) {
+    const uint32_t place = (uint32_t)(begin + rank * share + i);
+    from[i] = place;
+    if (kCarry) from[share + i] = (uint32_t)token_at(a, at + place);
+  }
+  const auto id_of = [&](int i) { return kCarry ? (int32_t)from[share + i] : token_at(a, at + from[i]); };
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * width;
     for (int i = threadIdx.x; i < kSortWarps * bins / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
     __syncthreads();
     uint16_t* const mine_counts = counts + warp * bins;
-    constexpr int kBatch = 4;  // ids on their way at once
     for (int i0 = lo; i0 < hi; i0 += 32 * kBatch) {
       int32_t id[kBatch];
 #pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int i = i0 + 32 * k + lane;
-        id[k] = i < hi ? token_at(a, at + from[i]) : -1;
-      }
+      for (int k = 0; k < kBatch; ++k) id[k] = i0 + 32 * k + lane < hi ? id_of(i0 + 32 * k + lane) : -1;
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
+        if (i0 + 32 * k >= hi) break;
         const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
         const unsigned same = __match_any_sync(kFullMask, digit);
         if (digit >= 0 && __ffs(same) - 1 == lane) mine_counts[digit] += (uint16_t)__popc(same);
@@ -182,6 +188,7 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
     // counts: the block's places of the digit in earlier warps; totals: in the block
     if (threadIdx.x < bins) {
       uint32_t sum = 0;
+#pragma unroll 8
       for (int w = 0; w < kSortWarps; ++w) {
         const uint32_t c = counts[w * bins + threadIdx.x];
         counts[w * bins + threadIdx.x] = (uint16_t)sum;
@@ -192,13 +199,19 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
     if (ranks > 1) cluster_wait();
     else __syncthreads();
     uint32_t all = 0, earlier = 0;
-    if (threadIdx.x < bins)
-      for (int r = 0; r < ranks; ++r) {
-        uint32_t c;
-        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c) : "r"(in_block(totals + threadIdx.x, r)) : "memory");
-        if (r < rank) earlier += c;
-        all += c;
+    if (threadIdx.x < bins) {
+      uint32_t c[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {  // all on their way at once
+        c[r] = 0;
+        if (r < ranks) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(c[r]) : "r"(in_block(totals + threadIdx.x, r)));
       }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        all += c[r];
+        if (r < rank) earlier += c[r];
+      }
+    }
     // bases: the section's places of lower digits, and of this one in earlier blocks
     uint32_t scan = all;
 #pragma unroll
@@ -221,10 +234,11 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
       for (int k = 0; k < kBatch; ++k) {
         const int i = i0 + 32 * k + lane;
         place[k] = i < hi ? from[i] : 0;
-        id[k] = i < hi ? token_at(a, at + place[k]) : -1;
+        id[k] = i < hi ? id_of(i) : -1;
       }
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
+        if (i0 + 32 * k >= hi) break;
         const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
         const unsigned same = __match_any_sync(kFullMask, digit);
         uint32_t before = 0;
@@ -237,10 +251,11 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
             out.places[where] = (int32_t)place[k];
             out.ids[where] = id[k];
           } else {
-            const int r = (int)(where / (uint32_t)share);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_block(to + (where - r * (uint32_t)share), r)),
-                         "r"(place[k])
-                         : "memory");
+            const int r = ranks == 1 ? 0 : (int)(where / (uint32_t)share);
+            const uint32_t there = in_block(to + (where - r * (uint32_t)share), r);
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(place[k]) : "memory");
+            if (kCarry)
+              asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there + 4 * (uint32_t)share), "r"(id[k]) : "memory");
           }
         }
         __syncwarp();
@@ -298,7 +313,8 @@ __global__ void __launch_bounds__(kSortThreads, 2)
   extern __shared__ __align__(16) unsigned char dynamic[];
   const int sorters = n > 0 ? a.workers * ranks : 0;
   if ((int)blockIdx.x < sorters) {
-    sort_section(a, blockIdx.x / ranks, begin, n, share, blockIdx.x % ranks, ranks, dynamic);
+    if (share <= kCarryMost) sort_section<true>(a, blockIdx.x / ranks, begin, n, share, blockIdx.x % ranks, ranks, dynamic);
+    else sort_section<false>(a, blockIdx.x / ranks, begin, n, share, blockIdx.x % ranks, ranks, dynamic);
     return;
   }
   const int64_t fill = blockIdx.x - sorters;
@@ -307,10 +323,9 @@ __global__ void __launch_bounds__(kSortThreads, 2)
   fill_rows(a, fill / fills, begin, n, v0, min64(v0 + rows, a.vocab), skip != 0, dynamic);
 }
 
-// A thread of the second kernel takes 8 columns: one 16-byte pack of dy (two in
-// 32 bits), or (kVec false) 2 columns, `lanes` apart.
-constexpr int kSumThreads = 128;
-__host__ __device__ constexpr int columns_of(bool vec) { return vec ? 8 : 2; }
+// A thread of the second kernel takes 8 columns: one 16-byte pack of dy, two in 32
+// bits; where rows of dy are not aligned, shifted out of the aligned packs that hold them.
+constexpr int kSumThreads = 128, kCols = 8, kSlice = kSumThreads * kCols;
 
 struct Chunks {
   int32_t size;   // places of a chunk
@@ -326,21 +341,21 @@ __device__ __forceinline__ float* part_of(const EmbeddingArgs& a, const Chunks& 
   return parts + ((m * ch.count + chunk) * 2 + which) * ((a.width + 3) / 4 * 4);
 }
 
-template <typename T, bool kVec>
+// kIn: rows of dy start on 16-byte boundaries; kOut: the table's gradient's do.
+template <typename T, bool kIn, bool kOut>
 __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArgs a, int n, Chunks ch) {
   dq_pdl_enter();
   dq_pdl_release();
-  constexpr int kCols = columns_of(kVec), E = 16 / (int)sizeof(T), P = kVec ? kCols / E : 1;
-  constexpr int kAhead = kVec && sizeof(T) == 4 ? 4 : 8;  // rows of dy on their way at once
+  constexpr int E = 16 / (int)sizeof(T), P = kCols / E, Q = kIn ? P : P + 1;  // packs of a row: its own, read
+  constexpr int kAhead = Q * (kIn ? 2 : 1) <= 2 ? 8 : 4;                      // rows of dy on their way at once
+  __shared__ float turned[kOut ? 1 : kSumThreads * kCols];
   const int lane = threadIdx.x % ch.lanes, groups = kSumThreads / ch.lanes;
   const int64_t which = (int64_t)blockIdx.x * groups + threadIdx.x / ch.lanes;
   if (which >= (int64_t)a.workers * ch.count) return;
   const int64_t m = which / ch.count, chunk = which % ch.count;
   const Sorted s = sorted_of(a, m);
-  const int lo = (int)chunk * ch.size, hi = min(lo + ch.size, n);
-  const int c0 = (int)blockIdx.y * kSumThreads * kCols + (kVec ? lane * kCols : lane);
-  const auto column = [&](int k) { return kVec ? c0 + k : c0 + k * ch.lanes; };
-  if (c0 >= a.width) return;
+  const int lo = (int)chunk * ch.size, hi = min(lo + ch.size, n), width = (int)a.width;
+  const int c0 = (int)blockIdx.y * kSlice + lane * kCols;
   const T* dy = static_cast<const T*>(a.dy) + m * a.tokens * a.ld;
   float* const table = a.dtable + m * a.g_stride;
 
@@ -352,32 +367,41 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
     if (came || goes) {
       float* out = part_of(a, ch, m, chunk, came ? 0 : 1);
 #pragma unroll
-      for (int k = 0; k < kCols; k += kVec ? 4 : 1) {
-        if constexpr (kVec) {
-          if (column(k) < a.width)
-            *reinterpret_cast<float4*>(out + column(k)) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
-        } else if (column(k) < a.width) {
-          out[column(k)] = sum[k];
+      for (int k = 0; k < kCols; k += 4)
+        if (c0 + k < width)  // up to whole packs
+          *reinterpret_cast<float4*>(out + c0 + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+    } else if (kOut) {
+      float* out = table + (int64_t)id * width + c0;
+#pragma unroll
+      for (int k = 0; k < kCols; k += 4) {
+        if (c0 + k >= width) continue;
+        float4* q = reinterpret_cast<float4*>(out + k);
+        float4 v = make_float4(sum[k] * a.scale, sum[k + 1] * a.scale, sum[k + 2] * a.scale, sum[k + 3] * a.scale);
+        if (a.accumulate) {
+          const float4 old = *q;
+          v = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
         }
+        __stcs(q, v);
       }
     } else {
-      float* out = table + (int64_t)id * a.width;
+      // the lanes' columns turned, so that neighbouring lanes write neighbouring columns
+      const int seg = min(ch.lanes, 32), l = lane % seg;
+      float* mine = turned + (threadIdx.x - l) * kCols;  // of this warp, or group
+      const unsigned mask = seg == 32 ? kFullMask : ((1u << seg) - 1u) << (threadIdx.x % 32 - l);
 #pragma unroll
-      for (int k = 0; k < kCols; k += kVec ? 4 : 1) {
-        if (column(k) >= a.width) continue;
-        if constexpr (kVec) {
-          float4* q = reinterpret_cast<float4*>(out + column(k));
-          float4 v = make_float4(sum[k] * a.scale, sum[k + 1] * a.scale, sum[k + 2] * a.scale, sum[k + 3] * a.scale);
-          if (a.accumulate) {
-            const float4 old = *q;
-            v = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
-          }
-          __stcs(q, v);
-        } else {
-          const float v = sum[k] * a.scale;
-          out[column(k)] = a.accumulate ? out[column(k)] + v : v;
-        }
+      for (int k = 0; k < kCols; k += 4)
+        *reinterpret_cast<float4*>(mine + l * kCols + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+      __syncwarp(mask);
+      const int first = c0 - l * kCols;
+      float* out = table + (int64_t)id * width + first;
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) {
+        const int c = l + k * seg;
+        if (first + c >= width) continue;
+        const float v = mine[c] * a.scale;
+        out[c] = a.accumulate ? out[c] + v : v;
       }
+      __syncwarp(mask);
     }
 #pragma unroll
     for (int k = 0; k < kCols; ++k) sum[k] = 0.f;
@@ -396,47 +420,37 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
   };
   places_at(lo);
   for (int j0 = lo; j0 < hi; j0 += kAhead) {
-    int32_t id[kAhead + 1], place[kAhead];
+    int32_t id[kAhead + 1];
+    uint4 x[kAhead][Q];
+    int shift[kIn ? 1 : kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       id[j] = next_id[j];
-      place[j] = next_place[j];
+      const T* row = dy + (int64_t)next_place[j] * a.ld + c0;
+      const int s16 = kIn ? 0 : (int)((uintptr_t)row & 15u);
+      if (!kIn) shift[j] = s16;
+      const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) - s16);
+      const int bytes = (width - c0) * (int)sizeof(T) + s16;  // before the row's end
+      if (id[j] < a.vocab) {
+#pragma unroll
+        for (int p = 0; p < Q; ++p)
+          if (16 * p < bytes) x[j][p] = kIn ? __ldcs(from + p) : from[p];
+      }
     }
     id[kAhead] = next_id[kAhead];
-    uint4 x[kAhead][P];
-    T y[kVec ? 1 : kAhead][kVec ? 1 : kCols];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (id[j] < a.vocab) {
-        if constexpr (kVec) {
-#pragma unroll
-          for (int p = 0; p < P; ++p)
-            if (column(p * E) < a.width)
-              x[j][p] = __ldcs(reinterpret_cast<const uint4*>(dy + (int64_t)place[j] * a.ld + column(p * E)));
-        } else {
-#pragma unroll
-          for (int k = 0; k < kCols; ++k)
-            if (column(k) < a.width) y[j][k] = dy[(int64_t)place[j] * a.ld + column(k)];
-        }
-      }
     places_at(j0 + kAhead);  // on their way while these rows are
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (j0 + j >= hi || id[j] >= a.vocab) break;  // the places without a token come last
-      if constexpr (kVec) {
 #pragma unroll
-        for (int p = 0; p < P; ++p)
-          if (column(p * E) < a.width)
+      for (int p = 0; p < P; ++p) {
+        const uint4 y = kIn ? x[j][p] : funnel16(x[j][p], x[j][kIn ? p : p + 1], shift[kIn ? 0 : j]);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) {
-              const float2 v = pair_of<T>(x[j][p], e);
-              sum[p * E + e] += v.x;
-              sum[p * E + e + 1] += v.y;
-            }
-      } else {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k)
-          if (column(k) < a.width) sum[k] += to_float(y[j][k]);
+        for (int e = 0; e < E; e += 2) {
+          const float2 v = pair_of<T>(y, e);
+          sum[p * E + e] += v.x;
+          sum[p * E + e + 1] += v.y;
+        }
       }
       const bool ends_chunk = j0 + j + 1 == hi;
       const int32_t next = ends_chunk ? after : id[j + 1];
@@ -446,13 +460,19 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
   }
 }
 
-// The parts of the run that begins in chunk `which` and goes on, if one does.
+// The parts of the run that begins in a chunk and goes on, if one does: `lanes`
+// threads (32, 64 or 128) take 4 columns each; with 128 the block's two halves take
+// half of the parts each.
 constexpr int kJoinThreads = 256, kJoinSlice = 512;
 
-__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingArgs a, int n, Chunks ch) {
+__global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingArgs a, int n, Chunks ch, int lanes) {
   dq_pdl_enter();
   __shared__ float4 shared[kJoinThreads / 2];
-  const int64_t m = blockIdx.x / ch.count, chunk = blockIdx.x % ch.count;
+  const bool halves = lanes == kJoinThreads / 2;
+  const int group = threadIdx.x / lanes, t = threadIdx.x % lanes;
+  const int64_t which = halves ? blockIdx.x : (int64_t)blockIdx.x * (kJoinThreads / lanes) + group;
+  if (which >= (int64_t)a.workers * ch.count) return;
+  const int64_t m = which / ch.count, chunk = which % ch.count;
   const Sorted s = sorted_of(a, m);
   const int lo = (int)chunk * ch.size, hi = lo + ch.size;
   if (hi >= n) return;  // nothing after it
@@ -471,10 +491,8 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingA
     ends = __ballot_sync(kFullMask, next >= n || s.ids[next] != id);
   }
   last += __ffs(ends) - 1;
-  // two halves of the block take half of the parts each
-  const int half = threadIdx.x / (kJoinThreads / 2), t = threadIdx.x % (kJoinThreads / 2);
-  const int64_t count = last - chunk + 1, mid = (count + 1) / 2;
-  const int64_t first = half == 0 ? 0 : mid, end = half == 0 ? mid : count;
+  const int64_t count = last - chunk + 1, mid = halves ? (count + 1) / 2 : count;
+  const int64_t first = group == 0 || !halves ? 0 : mid, end = group == 0 || !halves ? mid : count;
   const int c = (int)blockIdx.y * kJoinSlice + 4 * t;  // the parts' rows are padded to whole packs
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   if (c < a.width)
@@ -483,11 +501,15 @@ __global__ void __launch_bounds__(kJoinThreads) embedding_join_kernel(EmbeddingA
       const float4 v = *reinterpret_cast<const float4*>(part_of(a, ch, m, chunk + i, i == 0 ? 1 : 0) + c);
       sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
     }
-  if (half == 1) shared[t] = sum;
-  __syncthreads();
-  if (half == 1 || c >= a.width) return;
-  const float4 v = shared[t];
-  const float total[4] = {(sum.x + v.x) * a.scale, (sum.y + v.y) * a.scale, (sum.z + v.z) * a.scale, (sum.w + v.w) * a.scale};
+  if (halves) {
+    if (group == 1) shared[t] = sum;
+    __syncthreads();
+    if (group == 1) return;
+    const float4 v = shared[t];
+    sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+  }
+  if (c >= a.width) return;
+  const float total[4] = {sum.x * a.scale, sum.y * a.scale, sum.z * a.scale, sum.w * a.scale};
   float* out = a.dtable + m * a.g_stride + (int64_t)id * a.width + c;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
@@ -500,14 +522,15 @@ int lanes_for(int64_t width, int per_thread, int most) {
   return lanes;
 }
 
-// Chunks small enough for 32 blocks of the second kernel on every SM, of at least 16 places.
+// Chunks small enough for 32 blocks of the second kernel on every SM, of at least 16 places; at most 1024 to a
+// worker, so that a run through many of them is soon joined.
 constexpr int64_t kSumBlocks = 152 * 32;
 
-Chunks chunks_of(int64_t n, int64_t width, int64_t workers, bool vec) {
+Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
   Chunks ch;
-  ch.lanes = lanes_for(width, columns_of(vec), kSumThreads);
-  const int64_t slices = ceil_div(width, kSumThreads * columns_of(vec)), groups = kSumThreads / ch.lanes;
-  ch.size = (int32_t)max64(16, ceil_div(n * workers * slices, kSumBlocks * groups));
+  ch.lanes = lanes_for(width, kCols, kSumThreads);
+  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
+  ch.size = (int32_t)max64(max64(16, ceil_div(n, 1024)), ceil_div(n * workers * slices, kSumBlocks * groups));
   ch.count = (int32_t)max64(1, ceil_div(n, ch.size));
   return ch;
 }
@@ -517,8 +540,8 @@ Chunks chunks_of(int64_t n, int64_t width, int64_t workers, bool vec) {
 size_t embedding_scratch_bytes(int64_t, int64_t width, int64_t max_tokens, int32_t workers) {
   const int64_t n = section_of(max_tokens);
   // the most chunks that any smaller number of tokens makes: n workers slices / size <= blocks groups
-  const Chunks ch = chunks_of(n, width, workers, true);
-  const int64_t slices = ceil_div(width, kSumThreads * columns_of(true)), groups = kSumThreads / ch.lanes;
+  const Chunks ch = chunks_of(n, width, workers);
+  const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
   const int64_t chunks = min64(workers * ceil_div(n, 16), kSumBlocks * groups / slices + workers);
   return 4 * (size_t)((2 * n * workers + 3) / 4 * 4) + 8 * (size_t)chunks * (size_t)((width + 3) / 4 * 4);
 }
@@ -559,7 +582,7 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     const int64_t sorters = n > 0 ? (int64_t)a.workers * ranks : 0;
     int64_t rows = 1, fills = 0;
     bool skip = false;
-    int shared = (int)(n > 0 ? 8 * (int64_t)share + 2 * kSortWarps * kMostBins : 0);
+    int shared = n > 0 ? (share <= kCarryMost ? 16 : 8) * share + 2 * kSortWarps * kMostBins : 0;
     if (!a.accumulate) {
       // filling blocks for whole waves of the GPU, of at least a 16th MB each, and of four times the bytes
       // of the ids that a block looks through to find the rows to leave alone
@@ -587,23 +610,27 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     if (n == 0) return cudaSuccess;
     // 2. and 3. sum
     const int size = a.dtype == DQGAN_F32 ? 4 : 2;
-    const bool vec = a.width % columns_of(true) == 0 && (uintptr_t)a.dy % 16 == 0 && a.ld * size % 16 == 0 &&
-                     (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
-    const Chunks ch = chunks_of(n, a.width, a.workers, vec);
-    const int64_t slices = ceil_div(a.width, kSumThreads * columns_of(vec)), groups = kSumThreads / ch.lanes;
+    const bool in = (uintptr_t)a.dy % 16 == 0 && a.ld * size % 16 == 0;
+    const bool out = a.width % 4 == 0 && (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
+    const Chunks ch = chunks_of(n, a.width, a.workers);
+    const dim3 grid((unsigned)ceil_div((int64_t)a.workers * ch.count, kSumThreads / ch.lanes),
+                    (unsigned)ceil_div(a.width, kSlice));
     ++*launches;
     st = with_dtype(a.dtype, [&](auto t) {
       using T = decltype(t);
-      const dim3 grid((unsigned)ceil_div((int64_t)a.workers * ch.count, groups), (unsigned)slices);
-      return vec ? launch_pdl(embedding_sum_kernel<T, true>, grid, dim3(kSumThreads), 0, stream, a, n, ch)
-                 : launch_pdl(embedding_sum_kernel<T, false>, grid, dim3(kSumThreads), 0, stream, a, n, ch);
+      const auto kern = in ? (out ? embedding_sum_kernel<T, true, true> : embedding_sum_kernel<T, true, false>)
+                           : (out ? embedding_sum_kernel<T, false, true> : embedding_sum_kernel<T, false, false>);
+      return launch_pdl(kern, grid, dim3(kSumThreads), 0, stream, a, n, ch);
     });
     if (st != cudaSuccess) return st;
     if (ch.count > 1) {
+      const int lanes = (int)max64(32, lanes_for(a.width, 4, kJoinThreads / 2));
+      const int chunks_a_block = lanes == kJoinThreads / 2 ? 1 : kJoinThreads / lanes;
       ++*launches;
       st = launch_pdl(embedding_join_kernel,
-                      dim3((unsigned)(a.workers * ch.count), (unsigned)ceil_div(a.width, kJoinSlice)), dim3(kJoinThreads),
-                      0, stream, a, n, ch);
+                      dim3((unsigned)ceil_div((int64_t)a.workers * ch.count, chunks_a_block),
+                           (unsigned)ceil_div(a.width, kJoinSlice)),
+                      dim3(kJoinThreads), 0, stream, a, n, ch, lanes);
       if (st != cudaSuccess) return st;
     }
     begin += n;

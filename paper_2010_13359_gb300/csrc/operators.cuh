@@ -169,6 +169,19 @@ __device__ __forceinline__ void set_pair<__half>(uint4& p, int e, float2 v) {
   reinterpret_cast<__half2*>(&p)[e / 2] = __float22half2_rn(v);
 }
 
+// Bytes [s, s + 16) of the 32 in (a, b); s < 16, a multiple of 2.
+__device__ __forceinline__ uint4 funnel16(const uint4& a, const uint4& b, int s) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint32_t t[6], u[5];
+#pragma unroll
+  for (int k = 0; k < 6; ++k) t[k] = s & 8 ? w[k + 2] : w[k];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) u[k] = s & 4 ? t[k + 1] : t[k];
+  const int bits = (s & 3) * 8;
+  return make_uint4(__funnelshift_r(u[0], u[1], bits), __funnelshift_r(u[1], u[2], bits),
+                    __funnelshift_r(u[2], u[3], bits), __funnelshift_r(u[3], u[4], bits));
+}
+
 // Copies `bytes` (at most 16) bytes and zeros the rest of the 16, asynchronously.
 __device__ __forceinline__ void copy16_async(void* to, const void* from, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
