@@ -114,6 +114,7 @@ constexpr int kSortMost = 20480;  // places of one block: two buffers of them in
 constexpr int kCarryMost = kSortMost / 2;  // up to here with their ids, which else are read again
 constexpr int kSection = 8 * kSortMost;  // places that are sorted at once; more are taken in turn, and added
 constexpr int kMostBins = 512;
+constexpr int kSortShared = 8 * kSortMost + 2 * kSortWarps * kMostBins;  // at most
 constexpr int kFillRows = 1 << 16;  // rows of one filling block, a bit each
 
 // Scratch: per worker the sorted ids and places of a section; then the chunks' parts.
@@ -138,6 +139,19 @@ __device__ __forceinline__ uint32_t in_block(const void* p, int rank) {  // the 
   return there;
 }
 
+// The lanes whose digit of `width` bits is this lane's (-1: none), a bit at a time: a
+// warp's match instruction takes several times as long.
+__device__ __forceinline__ unsigned lanes_with(int digit, int width) {
+  unsigned same = __ballot_sync(kFullMask, digit >= 0);
+#pragma unroll
+  for (int b = 0; b < 9; ++b)
+    if (b < width) {
+      const unsigned set = __ballot_sync(kFullMask, digit >> b & 1);
+      same &= digit >> b & 1 ? set : ~set;
+    }
+  return digit >= 0 ? same : 0u;
+}
+
 // Sorts the n places from `begin` on of worker m by id, `share` of them to each
 // of the cluster's blocks: passes of up to 9 bits from the lowest, each of which keeps
 // the order within a digit.  A warp counts the digits of its part of the block's places, the counts are
@@ -146,7 +160,11 @@ __device__ __forceinline__ uint32_t in_block(const void* p, int rank) {  // the 
 template <bool kCarry>
 __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, int n, int share, int rank, int ranks,
                              unsigned char* dynamic) {
-  uint32_t* from = reinterpret_cast<uint32_t*>(dynamic);  // places, then (kCarry) ids
+  // places, counted from `begin`, and above kPlaceBits a place's rank among its warp's with the digit; then (kCarry) ids
+  constexpr int kPlaceBits = 18;
+  static_assert(kSection <= 1 << kPlaceBits && kSortMost / kSortWarps + 32 < 1 << (32 - kPlaceBits), "packed places");
+  constexpr uint32_t kPlace = (1u << kPlaceBits) - 1u;
+  uint32_t* from = reinterpret_cast<uint32_t*>(dynamic);
   uint32_t* to = from + (kCarry ? 2 : 1) * share;
   uint16_t* counts = reinterpret_cast<uint16_t*>(to + (kCarry ? 2 : 1) * share);  // [warp][bin]
   __shared__ uint32_t totals[kMostBins], bases[kMostBins], warp_sums[kSortWarps];
@@ -156,16 +174,16 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
   const int lo = min(warp * part, mine), hi = min(lo + part, mine);
   const int bits = 32 - __clz((int)a.vocab), passes = (bits + 8) / 9, width = (bits + passes - 1) / passes;
   const int bins = 1 << width;
-  const int64_t at = m * a.tokens;
+  const int64_t at = m * a.tokens + begin;
   const Sorted out = sorted_of(a, m);
   constexpr int kBatch = 4;  // ids on their way at once
 #pragma unroll 4
   for (int i = threadIdx.x; i < mine; i += kSortThreads) {
-    const uint32_t place = (uint32_t)(begin + rank * share + i);
+    const uint32_t place = (uint32_t)(rank * share + i);
     from[i] = place;
     if (kCarry) from[share + i] = (uint32_t)token_at(a, at + place);
   }
-  const auto id_of = [&](int i) { return kCarry ? (int32_t)from[share + i] : token_at(a, at + from[i]); };
+  const auto id_of = [&](int i) { return kCarry ? (int32_t)from[share + i] : token_at(a, at + (from[i] & kPlace)); };
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * width;
     for (int i = threadIdx.x; i < kSortWarps * bins / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
@@ -179,8 +197,14 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
       for (int k = 0; k < kBatch; ++k) {
         if (i0 + 32 * k >= hi) break;
         const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
-        const unsigned same = __match_any_sync(kFullMask, digit);
-        if (digit >= 0 && __ffs(same) - 1 == lane) mine_counts[digit] += (uint16_t)__popc(same);
+        const unsigned same = lanes_with(digit, width);
+        uint32_t earlier = 0;
+        if (digit >= 0) earlier = mine_counts[digit];
+        __syncwarp();
+        if (digit >= 0) {
+          if (__ffs(same) - 1 == lane) mine_counts[digit] = (uint16_t)(earlier + __popc(same));
+          from[i0 + 32 * k + lane] |= (earlier + __popc(same & ((1u << lane) - 1u))) << kPlaceBits;
+        }
         __syncwarp();
       }
     }
@@ -227,38 +251,20 @@ __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, i
     }
     __syncthreads();
     const bool last = pass == passes - 1;
-    for (int i0 = lo; i0 < hi; i0 += 32 * kBatch) {
-      uint32_t place[kBatch];
-      int32_t id[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int i = i0 + 32 * k + lane;
-        place[k] = i < hi ? from[i] : 0;
-        id[k] = i < hi ? id_of(i) : -1;
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        if (i0 + 32 * k >= hi) break;
-        const int digit = id[k] >= 0 ? id[k] >> shift & (bins - 1) : -1;
-        const unsigned same = __match_any_sync(kFullMask, digit);
-        uint32_t before = 0;
-        if (digit >= 0) before = mine_counts[digit];
-        __syncwarp();
-        if (digit >= 0) {
-          if (__ffs(same) - 1 == lane) mine_counts[digit] = (uint16_t)(before + __popc(same));
-          const uint32_t where = bases[digit] + before + __popc(same & ((1u << lane) - 1u));
-          if (last) {
-            out.places[where] = (int32_t)place[k];
-            out.ids[where] = id[k];
-          } else {
-            const int r = ranks == 1 ? 0 : (int)(where / (uint32_t)share);
-            const uint32_t there = in_block(to + (where - r * (uint32_t)share), r);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(place[k]) : "memory");
-            if (kCarry)
-              asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there + 4 * (uint32_t)share), "r"(id[k]) : "memory");
-          }
-        }
-        __syncwarp();
+#pragma unroll 4
+    for (int i = lo + lane; i < hi; i += 32) {
+      const uint32_t place = from[i] & kPlace;
+      const int32_t id = id_of(i);
+      const int digit = id >> shift & (bins - 1);
+      const uint32_t where = bases[digit] + mine_counts[digit] + (from[i] >> kPlaceBits);
+      if (last) {
+        out.places[where] = (int32_t)(begin + place);
+        out.ids[where] = id;
+      } else {
+        const int r = ranks == 1 ? 0 : (int)(where / (uint32_t)share);
+        const uint32_t there = in_block(to + (where - r * (uint32_t)share), r);
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(place) : "memory");
+        if (kCarry) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there + 4 * (uint32_t)share), "r"(id) : "memory");
       }
     }
     // the other blocks' places have come, and nobody needs these totals any more
@@ -577,7 +583,7 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     const int n = (int)min64(a.tokens - begin, kSection);
     // 1. sort and fill
     int ranks = 1;
-    while (ranks < 8 && ceil_div(n, ranks) > 4096) ranks *= 2;
+    while (ranks < 8 && ceil_div(n, ranks) > 1024) ranks *= 2;  // 32,768 places: 27 us in one block, 20 in eight
     const int share = (int)max64(ceil_div(n, ranks), 1);
     const int64_t sorters = n > 0 ? (int64_t)a.workers * ranks : 0;
     int64_t rows = 1, fills = 0;
@@ -598,8 +604,7 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     const int64_t blocks = ceil_div(sorters + fills * a.workers, ranks) * ranks;
     static std::atomic<int> kept[kKeptDevices];
     int resident = 0;
-    cudaError_t st = resident_ctas(embedding_sort_kernel, kSortThreads, 8 * kSortMost + 2 * kSortWarps * kMostBins,
-                                   8 * kSortMost + 2 * kSortWarps * kMostBins, kept, &resident);
+    cudaError_t st = resident_ctas(embedding_sort_kernel, kSortThreads, kSortShared, kSortShared, kept, &resident);
     if (st != cudaSuccess) return st;
     if (blocks > 0) {
       ++*launches;
