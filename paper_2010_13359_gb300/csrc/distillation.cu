@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 // sum of exponentials and writes the pair to every block of the cluster; one
 // cluster barrier later each block joins all pairs and turns its packs into the
 // gradient.  Clusters stay on the GPU and take row after row: as a thread has used
-// a pack for the last time it copies the next row's into its place.  Helper warps
-// (a quarter as many as workers, one at least) prepare the teacher's entries of the next row meanwhile, and write the
+// a pack for the last time it copies the next row's into its place.  Helper warps prepare
+// the teacher's entries of the next row meanwhile, and write the
 // entries' own gradients when the workers are through: a single warp's latency on
 // 128 entries came close to the time of a row.
 //
@@ -397,17 +397,11 @@ __device__ __forceinline__ void put_all(const Part<T, kWorkers>& part, T* dz, F&
   }
 }
 
-template <int kWorkers>
-constexpr int helpers() {
-  return kWorkers >= 128 ? kWorkers / 4 : 32;
-}
-template <int kWorkers>
-constexpr int held_threads() {
-  return kWorkers + helpers<kWorkers>();
-}
+// Helper threads of a block: twice as many for many teacher entries.
+constexpr int helpers(int workers, bool many) { return (workers == 256 ? 64 : 32) * (many ? 2 : 1); }
 
-template <typename T, DistillationWay kWay, int kWorkers>
-__global__ void __launch_bounds__(held_threads<kWorkers>(), 1024 / held_threads<kWorkers>())
+template <typename T, DistillationWay kWay, int kWorkers, bool kMany>
+__global__ void __launch_bounds__(kWorkers + helpers(kWorkers, kMany), 1024 / (kWorkers + helpers(kWorkers, kMany)))
     distillation_kernel(DistillationArgs a, int pieces) {
   dq_pdl_enter();
   using P = Packs<T>;
@@ -417,7 +411,7 @@ __global__ void __launch_bounds__(held_threads<kWorkers>(), 1024 / held_threads<
   extern __shared__ __align__(16) unsigned char dynamic[];
   // (maximum, sum) of every warp of the cluster; a block may write a row's while another reads the row before's
   __shared__ float2 pairs[2][kStats ? 8 * (kWarps + 1) : 1];
-  constexpr int kHelpers = helpers<kWorkers>();
+  constexpr int kHelpers = helpers(kWorkers, kMany);
   __shared__ TeacherTotals<kHelpers> totals[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   const bool works = warp < kWarps, first_helper = warp == kWarps;
@@ -592,7 +586,7 @@ __global__ void __launch_bounds__(held_threads<kWorkers>(), 1024 / held_threads<
           });
         }
         __syncwarp();
-        asm volatile("bar.arrive 1, %0;" ::"n"(held_threads<kWorkers>()) : "memory");
+        asm volatile("bar.arrive 1, %0;" ::"n"(kWorkers + kHelpers) : "memory");
       }
       for (int i = part.n; i < next_n; ++i) follow(i);
     } else {
@@ -619,7 +613,7 @@ __global__ void __launch_bounds__(held_threads<kWorkers>(), 1024 / held_threads<
       if (kGradient) {
         // the entries' own gradients over what the workers wrote there
         __syncwarp();
-        asm volatile("bar.sync 1, %0;" ::"n"(held_threads<kWorkers>()) : "memory");
+        asm volatile("bar.sync 1, %0;" ::"n"(kWorkers + kHelpers) : "memory");
         if (!none)
           for (int k = (int)threadIdx.x - kWorkers; k < a.k; k += kHelpers)
             if (t.at[k] >= 0)
@@ -665,23 +659,27 @@ cudaError_t resident_clusters(K kern, int threads, int shared, int pieces, std::
   return cudaSuccess;
 }
 
-template <typename T, DistillationWay kWay, int kWorkers>
+template <typename T, DistillationWay kWay, int kWorkers, bool kMany>
 cudaError_t launch_held(const DistillationArgs& a, int pieces, cudaStream_t stream) {
+  constexpr int kThreadsHeld = kWorkers + helpers(kWorkers, kMany);
+  const auto kern = distillation_kernel<T, kWay, kWorkers, kMany>;
   static std::atomic<uint64_t> kept[kKeptDevices];
   const int shared = held_shared<T>(a.k, a.vocab, pieces);
   const int cluster = kWay == DistillationWay::kBackward ? 1 : pieces;  // its pieces exchange nothing
   int clusters = 0;
-  const cudaError_t st = resident_clusters(distillation_kernel<T, kWay, kWorkers>, held_threads<kWorkers>(), shared,
-                                           cluster, kept, &clusters);
+  const cudaError_t st = resident_clusters(kern, kThreadsHeld, shared, cluster, kept, &clusters);
   if (st != cudaSuccess) return st;
   const int64_t at_once = min64(a.rows, max64((int64_t)clusters * cluster / pieces, 1));
-  return launch_pdl_cluster(distillation_kernel<T, kWay, kWorkers>, cluster, dim3((unsigned)(at_once * pieces)),
-                            dim3(held_threads<kWorkers>()), (size_t)shared, stream, a, pieces);
+  return launch_pdl_cluster(kern, cluster, dim3((unsigned)(at_once * pieces)), dim3(kThreadsHeld), (size_t)shared, stream,
+                            a, pieces);
 }
 
 template <typename T, DistillationWay kWay>
 cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
   const int packs = held_packs<T>(a.vocab, 1);
+  // 2300 bf16 values, 8000 rows, us with the lesser and the greater number of helpers: 8 entries 37 | 39, 184
+  // entries 72 | 54
+  const auto many = [&](int w) { return a.k > (w == kMostWorkers ? 128 : 64); };
   int workers = 32, pieces = 1;
   if (packs <= 64 * 16) {
     // 4096 rows of 4000 bf16 values: 28 us with 64 workers, 38 with 32
@@ -694,7 +692,7 @@ cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
     int64_t best = 0;
     for (int w = 128; w <= kMostWorkers; w *= 2)
       for (int p = 1; p <= 8; ++p) {
-        const int shared = held_shared<T>(a.k, a.vocab, p), threads = w + w / 4;
+        const int shared = held_shared<T>(a.k, a.vocab, p), threads = w + helpers(w, many(w));
         if (shared > kMostShared || packs < p * w * 8) continue;
         const int64_t blocks = min64(1024 / threads, (226 << 10) / (shared + (3 << 10)));
         const int64_t score = min64(blocks * (packs / p) * 16, 200 << 10) * (w == kMostWorkers ? 11 : 10);
@@ -708,12 +706,17 @@ cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
     return launch_pdl(distillation_long_kernel<T, kWay>, dim3((unsigned)a.rows), dim3(kThreads), 0, stream, a);
   // few rows: more, smaller pieces, down to a pack a thread, while SMs are idle
   while (pieces < 8 && a.rows * (pieces + 1) <= device_sms() && packs > workers * pieces) ++pieces;
+  const auto go = [&](auto of) {
+    constexpr int kWorkers = decltype(of)::value;
+    return many(kWorkers) ? launch_held<T, kWay, kWorkers, true>(a, pieces, stream)
+                          : launch_held<T, kWay, kWorkers, false>(a, pieces, stream);
+  };
   switch (workers) {
-    case 32: return launch_held<T, kWay, 32>(a, pieces, stream);
-    case 64: return launch_held<T, kWay, 64>(a, pieces, stream);
-    case 128: return launch_held<T, kWay, 128>(a, pieces, stream);
+    case 32: return go(std::integral_constant<int, 32>{});
+    case 64: return go(std::integral_constant<int, 64>{});
+    case 128: return go(std::integral_constant<int, 128>{});
   }
-  return launch_held<T, kWay, kMostWorkers>(a, pieces, stream);
+  return go(std::integral_constant<int, kMostWorkers>{});
 }
 
 }  // namespace

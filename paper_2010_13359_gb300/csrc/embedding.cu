@@ -23,75 +23,62 @@ __device__ __forceinline__ int32_t token_at(const EmbeddingArgs& a, int64_t i) {
 }
 
 // ---------------------------------------------------------------------------
-// Forward: `lanes` threads take a row, 16 bytes of y each at a time (kVec: rows
-// of table and y are aligned for that), kRows rows of one thread on their way at
-// once.
+// Forward: `lanes` threads take a row, each kAtOnce pieces of it at once: 16 bytes
+// of y (kVec: rows of table and y are aligned for that) or one value.
 // ---------------------------------------------------------------------------
-constexpr int kForwardThreads = 256, kRows = 4;
+constexpr int kForwardThreads = 256;
+// 16,384 rows of 1023 values: 49 us with 8 single fp32 values at once, 57 with 4; bf16 ones 76 and 61
+constexpr int at_once(bool vec, int size) { return vec || size == 2 ? 4 : 8; }
 
 template <typename E, typename T, bool kVec>
 __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(EmbeddingArgs a, int lanes) {
   dq_pdl_enter();
-  constexpr int N = kVec ? 16 / (int)sizeof(T) : 1;  // values a thread takes of a row
+  constexpr int N = kVec ? 16 / (int)sizeof(T) : 1, kAtOnce = at_once(kVec, (int)sizeof(E));  // values of a piece, pieces
+  constexpr int kWords = (N * (int)sizeof(E) + 7) / 8;                       // of the table, in 8 bytes
   const int lane = threadIdx.x % lanes, groups = kForwardThreads / lanes;
-  const int64_t all = a.tokens * a.workers, stride = (int64_t)gridDim.x * kRows * groups;
-  int64_t first = ((int64_t)blockIdx.x * kRows) * groups + threadIdx.x / lanes;
-  int32_t id[kRows];
-  const auto ids_at = [&](int64_t at) {
+  const int64_t all = a.tokens * a.workers, stride = (int64_t)gridDim.x * groups;
+  const auto id_at = [&](int64_t i) { return i < all ? token_at(a, i) : (int32_t)a.vocab; };
+  int64_t i = (int64_t)blockIdx.x * groups + threadIdx.x / lanes;
+  int32_t next_id = id_at(i);
+  for (; i < all; i += stride) {
+    const int32_t id = next_id;
+    const bool live = id < a.vocab;
+    next_id = id_at(i + stride);  // on its way while this row is
+    const E* row = static_cast<const E*>(a.table) +
+                   (live ? (int64_t)((uint32_t)i / (uint32_t)a.tokens) * a.p_stride + (int64_t)id * a.width : 0);
+    T* y = static_cast<T*>(a.y) + i * a.ld;
+    for (int c0 = lane * N; c0 < a.width; c0 += lanes * N * kAtOnce) {
+      uint2 p[kAtOnce][kWords];
+      float single[kAtOnce];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) id[r] = at + r * groups < all ? token_at(a, at + r * groups) : (int32_t)a.vocab;
-  };
-  ids_at(first);
-  for (; first < all; first += stride) {
-    const E* row[kRows];
-    bool live[kRows];
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int c = c0 + k * lanes * N;
+        if (!live || c >= a.width) continue;
+        if constexpr (!kVec) {
+          single[k] = to_float(row[c]);
+        } else if constexpr (kWords == 1) {
+          p[k][0] = *reinterpret_cast<const uint2*>(row + c);
+        } else {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      const uint32_t i = (uint32_t)(first + r * groups);
-      live[r] = id[r] < a.vocab;
-      row[r] = static_cast<const E*>(a.table) +
-               (live[r] ? (int64_t)(i / (uint32_t)a.tokens) * a.p_stride + (int64_t)id[r] * a.width : 0);
-    }
-    ids_at(first + stride);  // on their way while these rows are
-    for (int c = lane * N; c < a.width; c += lanes * N) {
-      float v[kRows][N];
-      if constexpr (kVec) {
-        constexpr int kBytes = N * (int)sizeof(E);  // of the table: 8, 16 or 32
-        uint2 p[kRows][kBytes / 8];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
-#pragma unroll
-          for (int k = 0; k < kBytes / 8; k += 2) {
-            if constexpr (kBytes >= 16) {
-              uint4 q = make_uint4(0, 0, 0, 0);
-              if (live[r]) q = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row[r] + c) + 8 * k);
-              p[r][k] = make_uint2(q.x, q.y);
-              p[r][k + 1] = make_uint2(q.z, q.w);
-            } else {
-              p[r][k] = make_uint2(0, 0);
-              if (live[r]) p[r][k] = *reinterpret_cast<const uint2*>(row[r] + c);
-            }
+          for (int w = 0; w < kWords; w += 2) {
+            const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row + c) + 8 * w);
+            p[k][w] = make_uint2(q.x, q.y);
+            p[k][w + 1] = make_uint2(q.z, q.w);
           }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
-#pragma unroll
-          for (int e = 0; e < N; ++e) v[r][e] = to_float(reinterpret_cast<const E*>(p[r])[e]) * a.scale;
-      } else {
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) v[r][0] = live[r] ? to_float(row[r][c]) * a.scale : 0.f;
+        }
       }
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        const int64_t i = first + r * groups;
-        if (i >= all) continue;
-        T* y = static_cast<T*>(a.y) + i * a.ld + c;
-        if constexpr (kVec) {
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int c = c0 + k * lanes * N;
+        if (c >= a.width) continue;
+        if constexpr (!kVec) {
+          y[c] = from_float<T>(live ? single[k] * a.scale : 0.f);
+        } else {
           uint4 q;
 #pragma unroll
-          for (int e = 0; e < N; ++e) reinterpret_cast<T*>(&q)[e] = from_float<T>(live[r] ? v[r][e] : 0.f);
-          __stcs(reinterpret_cast<uint4*>(y), q);
-        } else {
-          *y = from_float<T>(v[r][0]);
+          for (int e = 0; e < N; ++e)
+            reinterpret_cast<T*>(&q)[e] = from_float<T>(live ? to_float(reinterpret_cast<const E*>(p[k])[e]) * a.scale : 0.f);
+          __stcs(reinterpret_cast<uint4*>(y + c), q);
         }
       }
     }
@@ -564,13 +551,13 @@ cudaError_t launch_embedding_forward(const EmbeddingArgs& a, cudaStream_t stream
       const bool vec = a.width % N == 0 && (uintptr_t)a.y % 16 == 0 && a.ld % N == 0 &&
                        (uintptr_t)a.table % kAlign == 0 && a.width * (int64_t)sizeof(E) % kAlign == 0 &&
                        a.p_stride * (int64_t)sizeof(E) % kAlign == 0;
-      const int lanes = lanes_for(a.width, vec ? N : 1, kForwardThreads);
+      const int lanes = lanes_for(a.width, (vec ? N : 1) * at_once(vec, (int)sizeof(E)), kForwardThreads);
       const auto kern = vec ? embedding_forward_kernel<E, T, true> : embedding_forward_kernel<E, T, false>;
       static std::atomic<int> kept[2][kKeptDevices];
       int resident = 0;
       const cudaError_t st = resident_ctas(kern, kForwardThreads, 0, 0, kept[vec ? 1 : 0], &resident);
       if (st != cudaSuccess) return st;
-      const int64_t blocks = min64(ceil_div(n, kRows * (kForwardThreads / lanes)), resident);
+      const int64_t blocks = min64(ceil_div(n, kForwardThreads / lanes), resident);
       return launch_pdl(kern, dim3((unsigned)blocks), dim3(kForwardThreads), 0, stream, a, lanes);
     });
   });
