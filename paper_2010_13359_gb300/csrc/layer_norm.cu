@@ -159,7 +159,7 @@ template <int kLanes, int K>
 __device__ __forceinline__ void row_sum_collect(float (&v)[K], const float* shared) {
   if constexpr (kLanes > 32) {
     constexpr int kWarps = kLanes / 32;
-    const float* mine = shared + ((int)threadIdx.x / 32 & ~(kWarps - 1)) * K;
+    const float* mine = shared + (int)threadIdx.x / kLanes * kWarps * K;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float s[kWarps];
@@ -178,11 +178,11 @@ __device__ __forceinline__ void row_sum_collect(float (&v)[K], const float* shar
 // (forward: three blocks of 256 on an SM; backward: one of 512).
 template <int kLanes>
 constexpr int forward_threads() {
-  return kLanes > 256 ? kLanes : 256;
+  return kLanes > 256 ? kLanes : 256 / kLanes * kLanes;
 }
 template <int kLanes>
 constexpr int backward_threads() {
-  return kLanes > 512 ? kLanes : 512;
+  return kLanes > 512 ? kLanes : 512 / kLanes * kLanes;
 }
 
 // Rows on their way or at work in shared memory, as far as they fit.
@@ -602,9 +602,13 @@ cudaError_t with_lanes(int64_t width, F&& f) {
   if (width <= 16 * kPerThread) return f(Lanes<16>{});
   if (width <= 32 * kPerThread) return f(Lanes<32>{});
   if (width <= 64 * kPerThread) return f(Lanes<64>{});
+  if (width <= 96 * kPerThread) return f(Lanes<96>{});
   if (width <= 128 * kPerThread) return f(Lanes<128>{});
+  if (width <= 192 * kPerThread) return f(Lanes<192>{});
   if (width <= 256 * kPerThread) return f(Lanes<256>{});
+  if (width <= 384 * kPerThread) return f(Lanes<384>{});
   if (width <= 512 * kPerThread) return f(Lanes<512>{});
+  if (width <= 768 * kPerThread) return f(Lanes<768>{});
   return f(Lanes<1024>{});
 }
 
