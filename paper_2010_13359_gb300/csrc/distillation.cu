@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 
   // the teacher's entries: p holds t / T, then the probabilities
   float most = -INFINITY;
+  bool some = false;
   for (int k = threadIdx.x; k < a.k; k += kThreads) {
     const int32_t v = a.ids[row * a.teacher_ld + k];
     const float t = teacher_value(a, row, k) * inv_t;
@@ -70,8 +71,9 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
     id[k] = there ? v : -1;
     p[k] = there ? t : -INFINITY;
     if (there) most = fmaxf(most, t);
+    some = some || there;
   }
-  const bool any = __syncthreads_or(most > -INFINITY ? 1 : 0);
+  const bool any = __syncthreads_or(some ? 1 : 0);
   if (!any || c == 0.f) {
     if (threadIdx.x == 0 && kWay != DistillationWay::kBackward) {
       a.loss[row] = 0.f;
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
     if (id[k] >= 0) {
       const float logp = p[k] - lse_t;
       const float pk = expf(logp);
-      if (pk > 0.f) loss += pk * (logp - ((to_float(z[id[k]]) - top) * inv_t - log_sum));
+      if (pk != 0.f) loss += pk * (logp - ((to_float(z[id[k]]) - top) * inv_t - log_sum));
       mass += pk;
       p[k] = pk;
     }
@@ -690,12 +692,19 @@ cudaError_t launch(const DistillationArgs& a, cudaStream_t stream) {
     // 50,000 bf16 values (256, 1) 200 KB on an SM: 89, (256, 2) 150 KB: 72; 80,000 (128, 4) 200 KB: 78, (256, 3)
     // 160 KB: 73; 128,000 (256, 4) 192 KB: 84, (128, 4) 192 KB: 79.
     int64_t best = 0;
+    const int64_t sms = device_sms();
     for (int w = 128; w <= kMostWorkers; w *= 2)
       for (int p = 1; p <= 8; ++p) {
         const int shared = held_shared<T>(a.k, a.vocab, p), threads = w + helpers(w, many(w));
         if (shared > kMostShared || packs < p * w * 8) continue;
+        // the gradient alone, whose pieces exchange nothing: 1023 x 50,001 fp32 values in 4 pieces 67 us, in 2 74
+        if (kWay == DistillationWay::kBackward && packs > p * 4096 && p < 8) continue;
         const int64_t blocks = min64(1024 / threads, (226 << 10) / (shared + (3 << 10)));
-        const int64_t score = min64(blocks * (packs / p) * 16, 200 << 10) * (w == kMostWorkers ? 11 : 10);
+        // (one block alone has nothing to do between its phases); the last turn may leave clusters idle
+        const int64_t at_once = max64(blocks * sms / p, 1), turns = ceil_div(a.rows, at_once);
+        const int64_t busy = a.rows <= at_once ? 100 : 100 * a.rows / (turns * at_once);
+        const int64_t score =
+            min64(blocks * (packs / p) * 16, 200 << 10) * (w == kMostWorkers ? 11 : 10) * (blocks > 1 ? 10 : 7) * busy + blocks;
         if (score <= best) continue;
         best = score;
         workers = w;

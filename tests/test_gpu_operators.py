@@ -376,6 +376,57 @@ def test_embedding_offsets_past_32_bits(P):
     op.destroy()
 
 
+@pytest.mark.parametrize("in_shift,out_shift,width,dtype", [(0, 0, 64, 1), (3, 0, 64, 1), (0, 1, 64, 1), (5, 2, 64, 2),
+                                                            (0, 0, 41, 0), (1, 3, 41, 0), (7, 1, 300, 1), (0, 1, 1032, 0),
+                                                            (1, 0, 1032, 1), (2, 2, 7, 1)])
+def test_embedding_backward_alignments(P, in_shift, out_shift, width, dtype):
+    """Rows of dy and of the table's gradient that start anywhere, with unused values between them."""
+    tokens, vocab, pad = 700, 60, 5
+    ids = tokens_of(1, tokens, vocab, 32, "zipf", width)
+    dy, _ = rows_of(torch.randn((tokens, width), generator=gen(21), device="cuda"), pad, DTYPES[dtype], in_shift)
+    op = P.Embedding(vocab=vocab, width=width, max_tokens=tokens, dtype=dtype, scale=0.5, cuda_stream=stream())
+    flat = torch.full((out_shift + vocab * width + 3,), math.nan, device="cuda")
+    g = flat[out_shift:out_shift + vocab * width]
+    op.backward(tokens, ids, dy, dy.stride(0), g, 0)
+    there = (ids[0] >= 0) & (ids[0] < vocab)
+    at, values = ids[0].long()[there], dy[there].double()
+    want, size = torch.zeros((2, vocab, width), dtype=torch.float64, device="cuda")
+    want.index_add_(0, at, values)
+    size.index_add_(0, at, values.abs())
+    count = torch.bincount(at, minlength=vocab).double()[:, None]
+    within(g.view(vocab, width), want * 0.5, 0.5 * (count + 2) * U * size, "dtable")
+    assert flat[:out_shift].isnan().all() and flat[out_shift + vocab * width:].isnan().all()
+    base = torch.randn(vocab * width, generator=gen(22), device="cuda")
+    added = torch.full_like(flat, math.nan)
+    added[out_shift:out_shift + vocab * width] = base
+    op.backward(tokens, ids, dy, dy.stride(0), added[out_shift:], 0, accumulate=True)
+    assert torch.equal(added[out_shift:out_shift + vocab * width], base + g)
+    op.destroy()
+
+
+def test_embedding_backward_of_more_places_than_are_sorted_at_once(P):
+    """Written and added to, each over several sections; no places at all in a worker's later ones."""
+    workers, tokens, vocab, width = 2, 400_001, 5003, 12
+    ids = tokens_of(workers, tokens, vocab, 64, "zipf", 31)
+    ids[1, 170_000:] = -1
+    dy = torch.randn((workers * tokens, width), generator=gen(32), device="cuda")
+    op = P.Embedding(vocab=vocab, width=width, max_tokens=tokens, workers=workers, token_bits=64, cuda_stream=stream())
+    g = torch.full((workers, vocab * width), math.nan, device="cuda")
+    op.backward(tokens, ids, dy, width, g, vocab * width)
+    there = (ids >= 0) & (ids < vocab)
+    at, values = (ids + vocab * torch.arange(workers, device="cuda")[:, None])[there], dy[there.view(-1)].double()
+    want, size = torch.zeros((2, workers * vocab, width), dtype=torch.float64, device="cuda")
+    want.index_add_(0, at, values)
+    size.index_add_(0, at, values.abs())
+    count = torch.bincount(at, minlength=workers * vocab).double()[:, None]
+    within(g.view(workers * vocab, width), want, (count + 2) * U * size, "dtable")
+    added = torch.ones_like(g)
+    op.backward(tokens, ids, dy, width, added, vocab * width, accumulate=True)
+    within(added.view(workers * vocab, width), want + 1, (count + 8) * U * (size + 1), "dtable added to")
+    assert torch.equal(added.view(-1, width)[count[:, 0] == 0], torch.ones_like(added).view(-1, width)[count[:, 0] == 0])
+    op.destroy()
+
+
 # ---------------------------------------------------------------------------
 # distillation
 # ---------------------------------------------------------------------------
@@ -467,6 +518,26 @@ def test_distillation(P, case):
     assert torch.equal(loss3, loss2)
     op.backward(rows, z, z.stride(0), lse, *args, scale, z, z.stride(0))
     assert torch.equal(z.contiguous().view(torch.uint8), dz.contiguous().view(torch.uint8))
+    op.destroy()
+
+
+@pytest.mark.parametrize("rows,vocab,k,dtype", [(6, 1003, 40, 1), (3, 40_001, 65, 0), (700, 333, 5, 2), (5, 129, 200, 1)])
+def test_distillation_ids_in_steps_and_other_alignments(P, rows, vocab, k, dtype):
+    """Ids a fixed step apart, all the same id, and a gradient whose rows are aligned differently from the logits'."""
+    T = DTYPES[dtype]
+    z = torch.randn((rows, vocab), generator=gen(41), device="cuda")
+    steps = torch.tensor([1, 2, 3, 0, 16, 128, 64], device="cuda")[torch.arange(rows, device="cuda") % 7]
+    ids = (5 + steps[:, None] * torch.arange(k, device="cuda")) % vocab
+    values = torch.randn((rows, k), generator=gen(42), device="cuda")
+    z, _ = rows_of(z, 1, T, 1)
+    dz, flat = rows_of(torch.full((rows, vocab), math.nan), 4, T, 2)
+    loss, lse = torch.full((2, rows), math.nan, device="cuda")
+    op = P.Distillation(vocab=vocab, k=k, dtype=dtype, cuda_stream=stream())
+    op.step(rows, z, z.stride(0), ids.int(), values, k, None, None, 1.0, loss, lse, dz, dz.stride(0))
+    ref = distillation(z.double(), ids, values.double(), None, torch.ones(rows, device="cuda").double(), 1.0, 1.0)
+    within(loss, ref[0], ref[3] + 4 * U * ref[0].abs(), "loss")
+    within(dz, ref[2], ref[5] + rounded(ref[2].abs() + ref[5], T), "dlogits")
+    assert untouched(flat, rows, vocab, 4, 2)
     op.destroy()
 
 
@@ -642,3 +713,10 @@ def test_other_stream_and_graph(P):
             for a, b in zip(replayed, (x, mean, loss, dx, g)):
                 assert torch.equal(a, b)
     assert norm.launch_count() > 0 and embed.launch_count() > 0 and distill.launch_count() > 0
+
+
+@pytest.mark.parametrize("shape", [(2, 150, 1500, 1, 0, 0, False), (1, 77, 2999, 0, 1, 1, False), (3, 40, 6000, 1, 0, 0, True),
+                                   (1, 30, 12000, 2, 0, 3, False), (1, 200, 5120, 1, 0, 0, False)], ids=str)
+def test_layer_norm_between_powers_of_two(P, shape):
+    test_layer_norm_forward(P, shape)
+    test_layer_norm_backward(P, shape)
