@@ -555,8 +555,9 @@ DQGAN_API int dqgan_embedding_forward(dqgan_operator* op, int64_t tokens, const 
  * row is written (0 where no token fell); with accumulate != 0 the rows that
  * have tokens are added to and the others are left alone (a table that also
  * serves as the output layer's weight).  A row's dy are summed in the order of
- * their places within runs, and the runs' sums in order.  Rows of dy whose
- * place holds no token are not read.
+ * their places within runs, and the runs' sums in order; a worker's places
+ * beyond the first 163,840 are taken in further sections of as many, each added
+ * to the table's gradient.  Rows of dy whose place holds no token are not read.
  */
 DQGAN_API int dqgan_embedding_backward(dqgan_operator* op, int64_t tokens, const void* ids, const void* dy,
                                        int64_t dy_stride, float* dtable, int64_t g_stride, int32_t accumulate);

@@ -24,7 +24,9 @@ __device__ __forceinline__ int32_t token_at(const EmbeddingArgs& a, int64_t i) {
 
 // ---------------------------------------------------------------------------
 // Forward: `lanes` threads take a row, each kAtOnce pieces of it at once: 16 bytes
-// of y (kVec: rows of table and y are aligned for that) or one value.
+// of y (kVec: rows of table and y are aligned for that) or one value; the next row's
+// id is on its way meanwhile.  8 x 4096 rows of 1024 fp32 values to bf16: 23 us, 87 %
+// of 6694.5 GB/s; of 1023 (single values) 49 us.
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
 // 16,384 rows of 1023 values: 49 us with 8 single fp32 values at once, 57 with 4; bf16 ones 76 and 61
@@ -88,13 +90,17 @@ __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(Embe
 // ---------------------------------------------------------------------------
 // Backward, in three kernels:
 //   1. a cluster of blocks per worker sorts its places by id, the places of an id in
-//      order, while the other blocks write zeros to the rows that no token fell on
-//      (the sort takes 10 to 30 us on a few SMs, and hides behind them);
+//      order, while the other blocks write zeros to the rows that no token fell on.
+//      The sort takes 13 us for 4096 places, 25 for 32,768 and 84 for 131,072 on at most
+//      eight SMs a worker, and hides behind the zeros of a large table;
 //   2. the sorted places are cut into chunks; a chunk's rows of dy are read
 //      once and summed id by id.  A run of one id that lies in the chunk is the result;
 //      what a run that crosses into other chunks has there goes to the scratch space;
 //   3. such runs' parts are added up in order.
-// Nothing is added atomically, so the same call gives the same bits.
+// Nothing is added atomically, so the same call gives the same bits.  Measured: 8 x 4096
+// tokens of 32,000 x 1024 171 us (97 % of 6694.5 GB/s, 136 of them zeros), 131,072 tokens
+// of 128,000 x 4096 612 us (77 %: zeros 300 us at 5.0 TB/s, sums 276 us at 5.9 TB/s, joins
+// 25 us); small ones are bound by the three kernels' latencies: 2 x 333 tokens 15 us.
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortMost = 20480;  // places of one block: two buffers of them in shared memory
@@ -141,9 +147,11 @@ __device__ __forceinline__ unsigned lanes_with(int digit, int width) {
 
 // Sorts the n places from `begin` on of worker m by id, `share` of them to each
 // of the cluster's blocks: passes of up to 9 bits from the lowest, each of which keeps
-// the order within a digit.  A warp counts the digits of its part of the block's places, the counts are
-// added up over warps, blocks and digits, and every place goes to where its digit's
-// earlier ones end, in the shared memory of the block that holds that position.  kCarry: its id goes with it.
+// the order within a digit.  A warp counts the digits of its part of the block's
+// places, the counts are added up over warps, blocks and digits, and every place goes
+// to where its digit's earlier ones end, in the shared memory of the block that holds
+// that position.  kCarry: its id goes with it.  One SM's issue slots bound it (about
+// 100 instructions for 32 places and pass), hence the cluster.
 template <bool kCarry>
 __device__ void sort_section(const EmbeddingArgs& a, int64_t m, int64_t begin, int n, int share, int rank, int ranks,
                              unsigned char* dynamic) {

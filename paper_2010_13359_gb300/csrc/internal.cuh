@@ -1,6 +1,7 @@
 // Internal declarations of the sm_103a DQGAN library (not part of the C-ABI).
 //
-// Every kernel computes in IEEE binary32 with explicit round-to-nearest
+// Every kernel of the method (the token-model operators are apart, see
+// operators.cuh) computes in IEEE binary32 with explicit round-to-nearest
 // intrinsics (__fmul_rn, __fadd_rn, __fsub_rn, __fdiv_rn), which the compiler
 // never contracts into fused multiply-adds; the library is also built with
 // -fmad=false.  That makes messages and residuals reproducible bit for bit.

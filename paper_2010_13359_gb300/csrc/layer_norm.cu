@@ -200,8 +200,13 @@ constexpr int backward_stages() {
 // Forward.  Blocks walk over a worker's rows, with its weight and bias in
 // registers.  The next rows are on their way while one is worked on: every
 // thread copies its own packs to its own places in shared memory, so no barrier
-// guards them.
-// kWhole: the width is a multiple of a pack, so no pack needs looking into.
+// guards them (rows that are not aligned are copied and taken by all of a row's
+// threads, between the barriers of its two sums).  kWhole: the width is a multiple
+// of a pack, so no pack needs looking into.
+//
+// Measured (of 6694.5 GB/s): 16,384 rows of 1024 bf16 values 12.2 us (82 %), of 4096
+// 45 us (89 %), of 5120 63 us (80 %), of 4095 65 us (62 %: single-element reads and
+// writes); four rows of 512 on each of four workers 2.4 us.
 template <typename T, int kLanes, bool kVec, bool kWhole>
 __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : kLanes > 256 ? 2 : 3)
     layer_norm_forward_kernel(LayerNormArgs a) {
@@ -307,6 +312,11 @@ __host__ __device__ constexpr int64_t part_stride(int64_t width) { return (width
 // result).  A row's sums are published while the row before is finished from its
 // packs in shared memory, which hides the exchange between the row's warps:
 // one barrier a row.
+//
+// Measured: 16,384 rows of 4096 bf16 values 74 us with the join (82 % of 6694.5 GB/s),
+// in fp32 133 us (91 %); of 8192 (512 a worker) 52 us (58 %) and of 1024 27 us (56 %):
+// one block's 16 warps leave the row's chain exposed there.  Tried: 32 values a
+// thread with the weights in shared memory, 79 us and 58 us.
 template <typename T, int kLanes, bool kVec>
 __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_backward_kernel(LayerNormArgs a) {
   dq_pdl_enter();
