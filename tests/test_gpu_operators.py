@@ -720,3 +720,40 @@ def test_other_stream_and_graph(P):
 def test_layer_norm_between_powers_of_two(P, shape):
     test_layer_norm_forward(P, shape)
     test_layer_norm_backward(P, shape)
+
+
+@pytest.mark.parametrize("width", [64, 1537, 20_000])
+def test_layer_norm_gradient_of_no_rows(P, width):
+    """Zeros, or what was there; the rows' pointers are not looked at."""
+    op = P.LayerNorm(width=width, workers=3, cuda_stream=stream())
+    g = torch.full((3, 2 * width), math.nan, device="cuda")
+    op.backward(0, None, width, None, width, None, 0, None, None, None, width, g, g[:, width:], 2 * width)
+    assert not g.any()
+    g.fill_(2.5)
+    op.backward(0, None, width, None, width, None, 0, None, None, None, width, g, g[:, width:], 2 * width, accumulate=True)
+    assert (g == 2.5).all()
+    op.destroy()
+
+
+@pytest.mark.parametrize("rows", [1, 5, 400])
+def test_distillation_of_rows_that_do_not_count(P, rows):
+    """All weights 0, no entries, and every second row: zeros where nothing counts, the others as alone."""
+    vocab, k = 9000, 12
+    z = torch.randn((rows, vocab), generator=gen(51), device="cuda").bfloat16()
+    ids = torch.randint(0, vocab, (rows, k), generator=gen(52), device="cuda").int()
+    values = torch.randn((rows, k), generator=gen(53), device="cuda")
+    op = P.Distillation(vocab=vocab, k=k, dtype=1, cuda_stream=stream())
+
+    def step(ids, weights):
+        loss, lse = torch.full((2, rows), math.nan, device="cuda")
+        dz = torch.full_like(z, math.nan)
+        op.step(rows, z, vocab, ids, values, k, None, weights, 1.0, loss, lse, dz, vocab)
+        return loss, lse, dz
+
+    for got in step(ids, torch.zeros(rows, device="cuda")) + step(torch.full_like(ids, -1), None):
+        assert not got.any()
+    weights = torch.ones(rows, device="cuda")
+    weights[::2] = 0
+    for part, whole in zip(step(ids, weights), step(ids, None)):
+        assert not part[::2].any() and torch.equal(part[1::2], whole[1::2])
+    op.destroy()
