@@ -99,8 +99,8 @@ __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(Embe
 //   3. such runs' parts are added up in order.
 // Nothing is added atomically, so the same call gives the same bits.  Measured: 8 x 4096
 // tokens of 32,000 x 1024 171 us (97 % of 6694.5 GB/s, 136 of them zeros), 131,072 tokens
-// of 128,000 x 4096 612 us (77 %: zeros 300 us at 5.0 TB/s, sums 276 us at 5.9 TB/s, joins
-// 25 us); small ones are bound by the three kernels' latencies: 2 x 333 tokens 15 us.
+// of 128,000 x 4096 602 us (79 %: zeros 300 us at 5.0 TB/s, sums 276 us at 5.9 TB/s, joins
+// about 20 us); small ones are bound by the three kernels' latencies: 2 x 333 tokens 15 us.
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortMost = 20480;  // places of one block: two buffers of them in shared memory
@@ -523,9 +523,10 @@ int lanes_for(int64_t width, int per_thread, int most) {
   return lanes;
 }
 
-// Chunks small enough for 32 blocks of the second kernel on every SM, of at least 16 places; at most 1024 to a
-// worker, so that a run through many of them is soon joined.
-constexpr int64_t kSumBlocks = 152 * 32;
+// Chunks small enough for 16 blocks of the second kernel on every SM (four at once: 131,072 tokens of 128,000 x
+// 4096 602 us, with 32 blocks and as many more parts to join 611), of at least 16 places; at most 1024 to a worker,
+// so that a run through many of them is soon joined.
+constexpr int64_t kSumBlocks = 152 * 16;
 
 Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
   Chunks ch;
