@@ -204,9 +204,9 @@ constexpr int backward_stages() {
 // threads, between the barriers of its two sums).  kWhole: the width is a multiple
 // of a pack, so no pack needs looking into.
 //
-// Measured (of 6694.5 GB/s): 16,384 rows of 1024 bf16 values 12.2 us (82 %), of 4096
+// Measured (of 6694.5 GB/s): 16,384 rows of 1024 bf16 values 12.7 us (79 %), of 4096
 // 45 us (89 %), of 5120 63 us (80 %), of 4095 65 us (62 %: single-element reads and
-// writes); four rows of 512 on each of four workers 2.4 us.
+// writes); four rows of 512 on each of four workers 2.5 us.
 template <typename T, int kLanes, bool kVec, bool kWhole>
 __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : kLanes > 256 ? 2 : 3)
     layer_norm_forward_kernel(LayerNormArgs a) {
