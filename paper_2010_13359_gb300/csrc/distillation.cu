@@ -414,6 +414,9 @@ template <typename T, DistillationWay kWay, int kWorkers, bool kMany>
 __global__ void __launch_bounds__(kWorkers + helpers(kWorkers, kMany), 1024 / (kWorkers + helpers(kWorkers, kMany)))
     distillation_kernel(DistillationArgs a, int pieces) {
   dq_pdl_enter();
+  // this block runs: others of its cluster wait for that before they write into its shared memory
+  const bool exchanges = kWay != DistillationWay::kBackward && pieces > 1;
+  if (exchanges) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   using P = Packs<T>;
   using Mine = Part<T, kWorkers>;
   constexpr int E = P::E, kWarps = kWorkers / 32;  // of workers
@@ -478,8 +481,15 @@ __global__ void __launch_bounds__(kWorkers + helpers(kWorkers, kMany), 1024 / (k
                                  kStats && piece == 0, part.z);
   };
 
+  const auto all_run = [&] {
+    __syncwarp();
+    if (exchanges) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
   int64_t turn = advance(0);
-  if (first_row + turn * stride >= a.rows) return;  // as the whole cluster does
+  if (first_row + turn * stride >= a.rows) {  // as the whole cluster does
+    all_run();
+    return;
+  }
   Mine part(a, first_row + turn * stride, piece, pieces);
   if (works) {
 #pragma unroll 4
@@ -488,6 +498,7 @@ __global__ void __launch_bounds__(kWorkers + helpers(kWorkers, kMany), 1024 / (k
   } else {
     prepare(part, first_row + turn * stride, 0);
   }
+  all_run();
   for (int parity = 0;; parity ^= 1) {
     const int64_t row = first_row + turn * stride;
     const float c = next_c;
