@@ -203,9 +203,9 @@ class Handle:
 
     # -- lifetime -------------------------------------------------------------
     def destroy(self) -> None:
-        if self._h is not None and self._h.value:
-            _check(load_library().dqgan_destroy(self._h))
-        self._h = None
+        h, self._h = self._h, None  # freed even where an error of earlier work is returned
+        if h is not None and h.value:
+            _check(load_library().dqgan_destroy(h))
 
     def __del__(self):
         try:

@@ -74,9 +74,9 @@ class Operator:
         self._h = h
 
     def destroy(self) -> None:
-        if self._h is not None and self._h.value:
-            _check(load_library().dqgan_operator_destroy(self._h))
-        self._h = None
+        h, self._h = self._h, None  # freed even where an error of earlier work is returned
+        if h is not None and h.value:
+            _check(load_library().dqgan_operator_destroy(h))
 
     def __del__(self):
         try:

@@ -83,3 +83,32 @@ def test_null_handles(P):
     assert L.dqgan_embedding_backward(None, 1, None, None, 1, None, 1, 0) == P.dqgan.ERR_INVALID_ARG
     assert L.dqgan_distillation_forward(None, 1, None, 1, None, None, 1, None, None, None, None) == P.dqgan.ERR_INVALID_ARG
     assert b"NULL" in L.dqgan_operator_last_error(None)
+
+
+@pytest.mark.parametrize("owner,call", [("Operator", "dqgan_operator_destroy"), ("Handle", "dqgan_destroy")])
+def test_a_destroy_that_fails_is_not_repeated(P, monkeypatch, owner, call):
+    """The library frees the object whatever it returns: an error of earlier work that shows there is raised once, and
+    the owner lets go of the object."""
+    from paper_2010_13359_gb300 import dqgan, operators
+    destroyed = []
+
+    class Library:
+        def dqgan_operator_last_error(self, op):
+            return b"destroy: an earlier error"
+
+        dqgan_last_error = dqgan_operator_last_error
+
+    def destroy(self, h):
+        destroyed.append(h.value)
+        return P.dqgan.ERR_CUDA
+
+    setattr(Library, call, destroy)
+    module, cls = (operators, operators.Operator) if owner == "Operator" else (dqgan, dqgan.Handle)
+    monkeypatch.setattr(module, "load_library", lambda: Library())
+    o = object.__new__(cls)
+    o._h = ctypes.c_void_p(1234)
+    with pytest.raises(P.DqganError, match="earlier error"):
+        o.destroy()
+    o.destroy()
+    del o
+    assert destroyed == [1234]
