@@ -4,13 +4,15 @@ A worker's gradient F(w; xi) comes from the caller's model; these are the ends
 of that gradient that a matrix product does not cover, batched over the
 workers.  As in ``dqgan``, the classes only marshal arguments: pointers are
 ``torch.Tensor``s, integer addresses or None where the header allows NULL, and
-strides are in elements.
+strides are in elements.  A tensor has to be of the type that the operator was
+made for (ids as torch.topk gives them are int64, the distillation's int32);
+memory that a tensor of another type holds is given by its address, or as bytes.
 """
 from __future__ import annotations
 
 import ctypes
 
-from .dqgan import F32, OK, DqganError, _ptr, load_library
+from .dqgan import BF16, ERR_INVALID_ARG, F16, F32, OK, DqganError, _ptr, load_library
 
 
 class LayerNormConfig(ctypes.Structure):
@@ -62,6 +64,34 @@ def _check(status: int, op=None):
         raise DqganError(status, load_library().dqgan_operator_last_error(op).decode())
 
 
+def _types(*names: str):
+    """torch's types of these names; None where torch is not there to make tensors."""
+    try:
+        import torch
+    except ImportError:
+        return (None,) * len(names)
+    return tuple(getattr(torch, name) for name in names)
+
+
+_NAMES = {F32: "float32", BF16: "bfloat16", F16: "float16"}
+
+
+def _at(x, dtype) -> int | None:
+    """Address of x, whose elements are read or written as `dtype`."""
+    if x is None:
+        return None
+    try:
+        if x.dtype is dtype:
+            return x.data_ptr()
+    except AttributeError:
+        return _ptr(x)
+    if dtype is not None and hasattr(x, "data_ptr"):
+        got = str(x.dtype)
+        if got != "torch.uint8" and got.replace("torch.u", "torch.") != str(dtype):
+            raise DqganError(ERR_INVALID_ARG, f"a tensor of {got} where the operator has {dtype}")
+    return _ptr(x)
+
+
 class Operator:
     """Owner of one ``dqgan_operator``."""
 
@@ -107,6 +137,7 @@ class LayerNorm(Operator):
                  cuda_stream: int | None = None):
         super().__init__("dqgan_layer_norm_create",
                          LayerNormConfig(width=width, workers=workers, dtype=dtype, eps=eps, cuda_stream=cuda_stream))
+        self._f32, self._rows = _types("float32", _NAMES[dtype])
         L = load_library()
         self._forward = L.dqgan_layer_norm_forward
         self._backward = L.dqgan_layer_norm_backward
@@ -114,17 +145,19 @@ class LayerNorm(Operator):
     def forward(self, rows: int, x, x_stride: int, weight, bias, p_stride: int, y, y_stride: int, mean=None,
                 rstd=None) -> None:
         """`rows` rows per worker; worker m's weight and bias p_stride * m floats after worker 0's."""
-        status = self._forward(self._h, rows, _ptr(x), x_stride, _ptr(weight), _ptr(bias), p_stride, _ptr(y), y_stride,
-                               _ptr(mean), _ptr(rstd))
+        T, f32 = self._rows, self._f32
+        status = self._forward(self._h, rows, _at(x, T), x_stride, _at(weight, f32), _at(bias, f32), p_stride,
+                               _at(y, T), y_stride, _at(mean, f32), _at(rstd, f32))
         if status:
             _check(status, self._h)
 
     def backward(self, rows: int, dy, dy_stride: int, x, x_stride: int, weight, p_stride: int, mean, rstd, dx,
                  dx_stride: int, dweight, dbias, g_stride: int, accumulate: bool = False) -> None:
         """dx, and each worker's dweight and dbias, g_stride floats apart."""
-        status = self._backward(self._h, rows, _ptr(dy), dy_stride, _ptr(x), x_stride, _ptr(weight), p_stride,
-                                _ptr(mean), _ptr(rstd), _ptr(dx), dx_stride, _ptr(dweight), _ptr(dbias), g_stride,
-                                accumulate)
+        T, f32 = self._rows, self._f32
+        status = self._backward(self._h, rows, _at(dy, T), dy_stride, _at(x, T), x_stride, _at(weight, f32), p_stride,
+                                _at(mean, f32), _at(rstd, f32), _at(dx, T), dx_stride, _at(dweight, f32),
+                                _at(dbias, f32), g_stride, accumulate)
         if status:
             _check(status, self._h)
 
@@ -138,19 +171,24 @@ class Embedding(Operator):
                          EmbeddingConfig(vocab=vocab, width=width, max_tokens=max_tokens, workers=workers,
                                          table_dtype=table_dtype, dtype=dtype, token_bits=token_bits, scale=scale,
                                          cuda_stream=cuda_stream))
+        self._f32, self._rows, self._table, self._ids = _types("float32", _NAMES[dtype], _NAMES[table_dtype],
+                                                               f"int{token_bits}")
         L = load_library()
         self._forward = L.dqgan_embedding_forward
         self._backward = L.dqgan_embedding_backward
 
     def forward(self, tokens: int, ids, table, p_stride: int, y, y_stride: int) -> None:
         """`tokens` tokens per worker; worker m's table p_stride * m elements after worker 0's."""
-        status = self._forward(self._h, tokens, _ptr(ids), _ptr(table), p_stride, _ptr(y), y_stride)
+        T, E, I = self._rows, self._table, self._ids
+        status = self._forward(self._h, tokens, _at(ids, I), _at(table, E), p_stride, _at(y, T), y_stride)
         if status:
             _check(status, self._h)
 
     def backward(self, tokens: int, ids, dy, dy_stride: int, dtable, g_stride: int, accumulate: bool = False) -> None:
         """Each worker's gradient of its table, g_stride floats apart."""
-        status = self._backward(self._h, tokens, _ptr(ids), _ptr(dy), dy_stride, _ptr(dtable), g_stride, accumulate)
+        T, I, f32 = self._rows, self._ids, self._f32
+        status = self._backward(self._h, tokens, _at(ids, I), _at(dy, T), dy_stride, _at(dtable, f32), g_stride,
+                                accumulate)
         if status:
             _check(status, self._h)
 
@@ -163,6 +201,7 @@ class Distillation(Operator):
         super().__init__("dqgan_distillation_create",
                          DistillationConfig(vocab=vocab, k=k, dtype=dtype, teacher_dtype=teacher_dtype,
                                             temperature=temperature, cuda_stream=cuda_stream))
+        self._f32, self._i32, self._rows, self._values = _types("float32", "int32", _NAMES[dtype], _NAMES[teacher_dtype])
         L = load_library()
         self._forward = L.dqgan_distillation_forward
         self._backward = L.dqgan_distillation_backward
@@ -170,23 +209,27 @@ class Distillation(Operator):
 
     def forward(self, rows: int, logits, logits_stride: int, ids, values, teacher_stride: int, teacher_lse, weights,
                 loss, lse=None) -> None:
-        status = self._forward(self._h, rows, _ptr(logits), logits_stride, _ptr(ids), _ptr(values), teacher_stride,
-                               _ptr(teacher_lse), _ptr(weights), _ptr(loss), _ptr(lse))
+        T, I, V, f32 = self._rows, self._i32, self._values, self._f32
+        status = self._forward(self._h, rows, _at(logits, T), logits_stride, _at(ids, I), _at(values, V),
+                               teacher_stride, _at(teacher_lse, f32), _at(weights, f32), _at(loss, f32), _at(lse, f32))
         if status:
             _check(status, self._h)
 
     def backward(self, rows: int, logits, logits_stride: int, lse, ids, values, teacher_stride: int, teacher_lse,
                  weights, scale: float, dlogits, dlogits_stride: int) -> None:
-        status = self._backward(self._h, rows, _ptr(logits), logits_stride, _ptr(lse), _ptr(ids), _ptr(values),
-                                teacher_stride, _ptr(teacher_lse), _ptr(weights), scale, _ptr(dlogits), dlogits_stride)
+        T, I, V, f32 = self._rows, self._i32, self._values, self._f32
+        status = self._backward(self._h, rows, _at(logits, T), logits_stride, _at(lse, f32), _at(ids, I),
+                                _at(values, V), teacher_stride, _at(teacher_lse, f32), _at(weights, f32), scale,
+                                _at(dlogits, T), dlogits_stride)
         if status:
             _check(status, self._h)
 
     def step(self, rows: int, logits, logits_stride: int, ids, values, teacher_stride: int, teacher_lse, weights,
              scale: float, loss, lse, dlogits, dlogits_stride: int) -> None:
         """The forward and the backward pass in one call."""
-        status = self._step(self._h, rows, _ptr(logits), logits_stride, _ptr(ids), _ptr(values), teacher_stride,
-                            _ptr(teacher_lse), _ptr(weights), scale, _ptr(loss), _ptr(lse), _ptr(dlogits),
-                            dlogits_stride)
+        T, I, V, f32 = self._rows, self._i32, self._values, self._f32
+        status = self._step(self._h, rows, _at(logits, T), logits_stride, _at(ids, I), _at(values, V), teacher_stride,
+                            _at(teacher_lse, f32), _at(weights, f32), scale, _at(loss, f32), _at(lse, f32),
+                            _at(dlogits, T), dlogits_stride)
         if status:
             _check(status, self._h)

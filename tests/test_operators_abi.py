@@ -112,3 +112,67 @@ def test_a_destroy_that_fails_is_not_repeated(P, monkeypatch, owner, call):
     o.destroy()
     del o
     assert destroyed == [1234]
+
+
+def fake_operators(P, monkeypatch):
+    """The three operators over a library that only records its calls."""
+    from paper_2010_13359_gb300 import operators
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith(("create", "destroy")):
+                return lambda *args: 0
+            return lambda *args: calls.append(name) or 0
+
+    monkeypatch.setattr(operators, "load_library", lambda: Library())
+    return (P.LayerNorm(width=8, dtype=P.BF16), P.Embedding(vocab=4, width=8, max_tokens=2, table_dtype=P.F16, token_bits=64),
+            P.Distillation(vocab=8, k=2, teacher_dtype=P.BF16)), calls
+
+
+def operator_calls(torch, ops):
+    """Every call with tensors of the right types: (call, arguments, which of them are tensors)."""
+    norm, embed, distill = ops
+    half, f16, f32 = (torch.zeros(16, dtype=t) for t in (torch.bfloat16, torch.float16, torch.float32))
+    ids32, ids64 = torch.zeros(4, dtype=torch.int32), torch.zeros(4, dtype=torch.int64)
+    return [
+        (norm.forward, [1, half, 8, f32, f32, 8, half, 8, f32, f32]),
+        (norm.backward, [1, half, 8, half, 8, f32, 8, f32, f32, half, 8, f32, f32, 8]),
+        (embed.forward, [1, ids64, f16, 32, f32, 8]),
+        (embed.backward, [1, ids64, f32, 8, f32, 32]),
+        (distill.forward, [1, f32, 8, ids32, half, 2, f32, f32, f32, f32]),
+        (distill.backward, [1, f32, 8, f32, ids32, half, 2, f32, f32, 1.0, f32, 8]),
+        (distill.step, [1, f32, 8, ids32, half, 2, f32, f32, 1.0, f32, f32, f32, 8]),
+    ]
+
+
+def test_tensors_of_another_type_are_refused(P, monkeypatch):
+    """torch.topk and torch's default integers give int64 ids: read as 32-bit ones every second is the upper half."""
+    torch = pytest.importorskip("torch")
+    ops, calls = fake_operators(P, monkeypatch)
+    types = (torch.float32, torch.bfloat16, torch.float16, torch.float64, torch.int32, torch.int64, torch.int8)
+    for call, args in operator_calls(torch, ops):
+        for i, right in enumerate(args):
+            if not isinstance(right, torch.Tensor):
+                continue
+            for t in types:
+                if t is right.dtype:
+                    continue
+                with pytest.raises(P.DqganError) as ei:
+                    call(*args[:i], right.to(t), *args[i + 1:])
+                assert ei.value.status == P.dqgan.ERR_INVALID_ARG
+                assert str(t) in str(ei.value) and str(right.dtype) in str(ei.value)
+    assert calls == []
+
+
+def test_what_the_types_let_through(P, monkeypatch):
+    """The config's types, addresses, None, raw bytes and unsigned ids of the same size."""
+    torch = pytest.importorskip("torch")
+    ops, calls = fake_operators(P, monkeypatch)
+    for call, args in operator_calls(torch, ops):
+        call(*args)
+        tensors = [i for i, a in enumerate(args) if isinstance(a, torch.Tensor)]
+        for other in (lambda x: None, lambda x: x.data_ptr(), lambda x: x.view(torch.uint8),
+                      lambda x: x.view({torch.int32: torch.uint32, torch.int64: torch.uint64}.get(x.dtype, x.dtype))):
+            call(*[other(a) if i in tensors else a for i, a in enumerate(args)])
+    assert len(calls) == 5 * 7
