@@ -44,12 +44,28 @@ class TokenModel:
         b |= {name: torch.empty(rows[0], device=device) for name in ("mean", "rstd", "loss")}
         return b
 
+    def _check_batch(self, params, ids, teacher_ids, teacher_values, weights, g) -> None:
+        """The kernels take addresses, and one row stride for both teacher tensors."""
+        M, rows, k = self.workers, self.workers * self.tokens, self.k
+        for name, t in (("params", params), ("g", g)):
+            if t.dim() != 2 or t.shape[0] != M or t.shape[1] < self.d or t.stride(1) != 1:
+                raise ValueError(f"{name}: {M} rows of at least {self.d} values are needed")
+        for name, t in (("ids", ids), ("weights", weights)):
+            if t is not None and not (t.is_contiguous() and (t.numel() == rows or t.dim() == 1 and t.numel() > rows)):
+                raise ValueError(f"{name}: {rows} values without gaps are needed")
+        for name, t in (("teacher_ids", teacher_ids), ("teacher_values", teacher_values)):
+            if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < k or k > 1 and t.stride(1) != 1:
+                raise ValueError(f"{name}: {rows} rows of at least {k} values are needed")
+        if rows > 1 and teacher_ids.stride(0) != teacher_values.stride(0):
+            raise ValueError("teacher_ids and teacher_values: rows of one stride are needed")
+
     def operator(self, params, ids, teacher_ids, teacher_values, weights, g, b) -> None:
         """g[m] = F(params[m]) for every worker m, and b["loss"] each token's loss.  params: (workers, d) fp32,
-        its rows p_stride floats apart; ids: (workers, tokens) int32, -1 for no token; teacher_ids and
-        teacher_values: (workers * tokens, k); weights: a token's weight, 0 where it does not count; g: rows
-        of at least d floats."""
+        its rows p_stride floats apart; ids: (workers, tokens) int32, -1 for no token; teacher_ids (int32) and
+        teacher_values: (workers * tokens, k), rows of one stride; weights: a token's weight, 0 where it does
+        not count, or None; g: rows of at least d floats."""
         import torch
+        self._check_batch(params, ids, teacher_ids, teacher_values, weights, g)
         M, n, V, C = self.workers, self.tokens, self.vocab, self.width
         p_stride, g_stride = params.stride(0), g.stride(0)
         table = params[:, :V * C].view(M, V, C)
