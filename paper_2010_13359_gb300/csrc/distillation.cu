@@ -61,12 +61,13 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
   const float c = a.weights ? a.weights[row] : 1.f;
   const float inv_t = 1.f / a.temperature;
 
-  // the teacher's entries: p holds t / T, then the probabilities
+  // the teacher's entries: p holds t, then the probabilities.  log p = (t - most) / T - lse_t, the difference first,
+  // so that the type's lowest values do not overflow (most: 0 where L is given)
   float most = -INFINITY;
   bool some = false;
   for (int k = threadIdx.x; k < a.k; k += kThreads) {
     const int32_t v = a.ids[row * a.teacher_ld + k];
-    const float t = teacher_value(a, row, k) * inv_t;
+    const float t = teacher_value(a, row, k);
     const bool there = v >= 0 && v < a.vocab && t != -INFINITY;
     id[k] = there ? v : -1;
     p[k] = there ? t : -INFINITY;
@@ -85,13 +86,14 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
   }
   float lse_t;
   if (a.teacher_lse) {
+    most = 0.f;
     lse_t = a.teacher_lse[row];
   } else {
     most = block_max(most, shared);
     float s = 0.f;
     for (int k = threadIdx.x; k < a.k; k += kThreads)
-      if (id[k] >= 0) s += expf(p[k] - most);
-    lse_t = most + logf(block_sum(s, shared));
+      if (id[k] >= 0) s += expf((p[k] - most) * inv_t);
+    lse_t = logf(block_sum(s, shared));
   }
 
   // q_v = exp((z_v - top) / T) / sum; in the gradient alone exp(z_v / T - lse)
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
   float loss = 0.f, mass = 0.f;
   for (int k = threadIdx.x; k < a.k; k += kThreads)
     if (id[k] >= 0) {
-      const float logp = p[k] - lse_t;
+      const float logp = (p[k] - most) * inv_t - lse_t;
       const float pk = expf(logp);
       if (pk != 0.f) loss += pk * (logp - ((to_float(z[id[k]]) - top) * inv_t - log_sum));
       mass += pk;
@@ -219,10 +221,12 @@ __device__ __forceinline__ float warp_max(float x) {
   return x;
 }
 
-// What a block's helpers make of the teacher's entries, for the block's part
-// [lo, hi) of the vocabulary.  Arrays of k: t (an entry's t / T, or -inf where there
-// is none), z (the logits at the ids), at (the id where this entry stands for it and
-// it is in the part, else -1), sum (p summed over the id's entries, where `at` has it).
+// What a block's helpers make of the teacher's entries, for the block's part [lo, hi) of
+// the vocabulary.  Arrays of k: t ((value - the greatest) / T, the difference first, so
+// that the type's lowest values do not overflow and large ones keep their digits, or
+// value / T where L is given; -inf where there is no entry), z (the logits at the ids), at
+// (the id where this entry stands for it and it is in the part, else -1), sum (p summed
+// over the id's entries, where `at` has it).
 struct Teacher {
   float* t;
   float* z;
@@ -238,7 +242,7 @@ constexpr int helper_warps() {
 // What the helpers leave for a row beside the arrays.
 template <int kHelpers>
 struct TeacherTotals {
-  float lse;                                // L
+  float lse;                                // log p = t - lse: log sum exp t, or L
   float mass[helper_warps<kHelpers>()];     // sums of p of each helper warp
   int32_t any[helper_warps<kHelpers>()];    // whether it had entries
   float most[helper_warps<kHelpers>()], exps[helper_warps<kHelpers>()];  // on the way to L
@@ -269,7 +273,7 @@ __device__ __forceinline__ void prepare_teacher(const DistillationArgs& a, int64
     for (int i = 0; i < kBatch; ++i) {
       const int k = k0 + kHelpers * i;
       id[i] = k < a.k ? a.ids[row * a.teacher_ld + k] : -1;
-      v[i] = k < a.k ? teacher_value(a, row, k) * inv_t : -INFINITY;
+      v[i] = k < a.k ? teacher_value(a, row, k) : -INFINITY;
     }
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
@@ -284,7 +288,7 @@ __device__ __forceinline__ void prepare_teacher(const DistillationArgs& a, int64
       else any = true;
       most = fmaxf(most, v[i]);
       if (k >= a.k) continue;
-      t.t[k] = v[i];
+      t.t[k] = a.teacher_lse ? v[i] * inv_t : v[i];
       t.at[k] = id[i] >= lo && id[i] < hi ? id[i] : -1;
       t.z[k] = x[i];
     }
@@ -317,14 +321,18 @@ __device__ __forceinline__ void prepare_teacher(const DistillationArgs& a, int64
     for (int i = 1; i < helper_warps<kHelpers>(); ++i) most = fmaxf(most, totals.most[i]);
     if (most == -INFINITY) most = 0.f;  // no entry: L is not used
     float s = 0.f;
-    for (int k = me; k < a.k; k += kHelpers) s += exp2_ftz((t.t[k] - most) * kLog2e);
+    for (int k = me; k < a.k; k += kHelpers) {
+      const float x = (t.t[k] - most) * inv_t;
+      t.t[k] = x;
+      s += exp2_ftz(x * kLog2e);
+    }
     s = warp_sum(s);
     if (lane == 0) totals.exps[warp] = s;
     helpers_wait<kHelpers>();
     s = totals.exps[0];
 #pragma unroll
     for (int i = 1; i < helper_warps<kHelpers>(); ++i) s += totals.exps[i];
-    lse = most + logf(s);
+    lse = logf(s);
   }
   if (me == 0) totals.lse = lse;
   const auto p_of = [&](int k) { return t.t[k] == -INFINITY ? 0.f : exp2_ftz((t.t[k] - lse) * kLog2e); };

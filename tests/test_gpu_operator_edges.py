@@ -1,0 +1,53 @@
+"""The token-model operators at the ends of their types' ranges, against the definitions in 64 bits."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+
+from operator_references import U, distillation, rounded, within
+from test_gpu_operators import DTYPES, P, gen, stream  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("vocab", [300, 40_000, 1_000_003])  # one block a row, a cluster, rows that do not fit on chip
+@pytest.mark.parametrize("teacher", [0, 1])
+@pytest.mark.parametrize("temperature", [0.5, 1.0, 2.0])
+def test_distillation_of_extreme_teacher_values(P, vocab, teacher, temperature):  # noqa: F811
+    """The type's lowest value is a number: entries of nothing else share the mass, whatever t / T overflows to.  The
+    probabilities depend on differences, so the definition is evaluated at values moved to where they can be written."""
+    least = torch.finfo(DTYPES[teacher]).min
+    rows = [  # values as given, and with the same differences where those count
+        ([least] * 4, [0.0] * 4),
+        ([-least] * 4, [0.0] * 4),
+        ([least, -least, 0.0, least], [-1e4, 0.0, -1e4, -1e4]),
+        ([0.5 * -least, 0.5 * -least, least, -math.inf], [0.0, 0.0, -1e4, -math.inf]),
+        ([least, 0.5, 0.25, -math.inf], [-1e4, 0.5, 0.25, -math.inf]),
+        ([least, -math.inf, -math.inf, -math.inf], [0.0, -math.inf, -math.inf, -math.inf]),
+        ([0.5, 1.0, -2.0, 3.0], [0.5, 1.0, -2.0, 3.0]),
+    ]
+    R, T32 = len(rows), float(np.float32(temperature))
+    values = torch.tensor([r[0] for r in rows], device="cuda").to(DTYPES[teacher])
+    moved = torch.tensor([r[1] for r in rows], device="cuda", dtype=torch.float64)
+    ids = torch.tensor([[7, 250, 11, 0]] * R, dtype=torch.int32, device="cuda")
+    z = torch.randn((R, vocab), generator=gen(vocab), device="cuda")
+    op = P.Distillation(vocab=vocab, k=4, teacher_dtype=teacher, temperature=temperature, cuda_stream=stream())
+    loss, lse, loss2, lse2 = torch.full((4, R), math.nan, device="cuda")
+    dz, back = torch.full((2, R, vocab), math.nan, device="cuda")
+    op.forward(R, z, vocab, ids, values, 4, None, None, loss, lse)
+    op.step(R, z, vocab, ids, values, 4, None, None, 1.0, loss2, lse2, dz, vocab)
+    op.backward(R, z, vocab, lse, ids, values, 4, None, None, 1.0, back, vocab)
+    ones = torch.ones(R, dtype=torch.float64, device="cuda")
+    ref = distillation(z.double(), ids, moved, None, ones, T32, 1.0)
+    for got in (loss, loss2):
+        within(got, ref[0], ref[3] + 4 * U * ref[0].abs(), "loss")
+    for got in (lse, lse2):
+        within(got, ref[1], ref[4], "lse")
+    within(dz, ref[2], ref[5] + rounded(ref[2].abs() + ref[5], torch.float32), "dlogits of the step")
+    want = distillation(z.double(), ids, moved, None, ones, T32, 1.0, lse=lse.double())
+    within(back, want[2], want[5] + rounded(want[2].abs() + want[5], torch.float32), "dlogits")
+    op.destroy()
