@@ -483,7 +483,7 @@ typedef struct dqgan_embedding_config {
  *   k              teacher entries a row, 1 <= k <= 1024;
  *   dtype          of the student's logits and their gradient;
  *   teacher_dtype  of the teacher's logits;
- *   temperature    > 0, finite;  reserved  0. */
+ *   temperature    > 0, finite, not subnormal;  reserved  0. */
 typedef struct dqgan_distillation_config {
   int64_t vocab;
   int32_t k;

@@ -141,8 +141,8 @@ int dqgan_distillation_create(const dqgan_distillation_config* cfg, dqgan_operat
   if (cfg->vocab < 1 || cfg->vocab > kMaxVocab) return invalid(nullptr, "vocab outside [1, 2^24]");
   if (cfg->k < 1 || cfg->k > kMaxEntries) return invalid(nullptr, "k outside [1, 1024]");
   if (!known_dtype(cfg->dtype) || !known_dtype(cfg->teacher_dtype)) return invalid(nullptr, "unknown dtype");
-  if (!std::isfinite(cfg->temperature) || !(cfg->temperature > 0.f))
-    return invalid(nullptr, "temperature is not positive and finite");
+  if (!std::isnormal(cfg->temperature) || !(cfg->temperature > 0.f))  // of a subnormal one 1 / T overflows
+    return invalid(nullptr, "temperature is not a positive normal number");
   if (cfg->reserved[0] != 0 || cfg->reserved[1] != 0) return invalid(nullptr, "reserved is not 0");
   const int st = create(Kind::kDistillation, cfg->cuda_stream, 0, out);
   if (st == DQGAN_OK) (*out)->distillation = *cfg;

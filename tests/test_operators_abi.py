@@ -176,3 +176,13 @@ def test_what_the_types_let_through(P, monkeypatch):
                       lambda x: x.view({torch.int32: torch.uint32, torch.int64: torch.uint64}.get(x.dtype, x.dtype))):
             call(*[other(a) if i in tensors else a for i, a in enumerate(args)])
     assert len(calls) == 5 * 7
+
+
+def test_temperatures_whose_reciprocal_overflows_are_refused(P):
+    """The kernels multiply by 1 / T: infinite for a subnormal T, and every result NaN."""
+    least = 2.0 ** -126
+    P.Distillation(vocab=8, k=1, temperature=least)._h = None  # kept from a destroy, which needs a GPU
+    for t in (least / 2, least / 8, 2.0 ** -149):
+        with pytest.raises(P.DqganError, match="temperature") as ei:
+            P.Distillation(vocab=8, k=1, temperature=t)
+        assert ei.value.status == P.dqgan.ERR_INVALID_ARG
