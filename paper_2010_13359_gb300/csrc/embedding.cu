@@ -349,7 +349,7 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
   dq_pdl_release();
   constexpr int E = 16 / (int)sizeof(T), P = kCols / E, Q = kIn ? P : P + 1;  // packs of a row: its own, read
   constexpr int kAhead = Q * (kIn ? 2 : 1) <= 2 ? 8 : 4;                      // rows of dy on their way at once
-  __shared__ float turned[kOut ? 1 : kSumThreads * kCols];
+  __shared__ __align__(16) float turned[kOut ? 1 : kSumThreads * kCols];
   const int lane = threadIdx.x % ch.lanes, groups = kSumThreads / ch.lanes;
   const int64_t which = (int64_t)blockIdx.x * groups + threadIdx.x / ch.lanes;
   if (which >= (int64_t)a.workers * ch.count) return;
