@@ -433,6 +433,9 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *     at a stride of at least that many elements; worker m's rows follow
  *     worker m - 1's.  Pointers need the alignment of their element only;
  *     rows that start on 16-byte boundaries are read and written fastest.
+ *     Where a row's ends are not on such boundaries, up to 14 bytes beside it
+ *     may be read along (not written, and their values do not matter), but
+ *     nothing before the first row's first value or after the last row's last.
  *   - Parameters, gradients, statistics and losses are fp32, and so is all
  *     arithmetic: sums, softmax statistics and norms are held in 32 bits
  *     and a 16-bit result is rounded once.  Every sum has a fixed order, so the

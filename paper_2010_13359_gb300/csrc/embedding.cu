@@ -332,6 +332,7 @@ struct Chunks {
   int32_t size;   // places of a chunk
   int32_t count;  // chunks of a worker
   int32_t lanes;  // threads that take a chunk's columns, at most kSumThreads
+  int32_t near;   // rows_near of dy
 };
 
 // A worker's chunk's two parts, each a row of `width` sums: 0: of the run that comes
@@ -342,9 +343,12 @@ __device__ __forceinline__ float* part_of(const EmbeddingArgs& a, const Chunks& 
   return parts + ((m * ch.count + chunk) * 2 + which) * ((a.width + 3) / 4 * 4);
 }
 
+// Blocks on an SM: three to five as registers come out; one instance would miss its fourth by 10 registers.
+constexpr int sum_blocks(bool in, bool out, int size) { return in && !out && size == 2 ? 4 : 0; }
+
 // kIn: rows of dy start on 16-byte boundaries; kOut: the table's gradient's do.
 template <typename T, bool kIn, bool kOut>
-__global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArgs a, int n, Chunks ch) {
+__global__ void __launch_bounds__(kSumThreads, sum_blocks(kIn, kOut, sizeof(T))) embedding_sum_kernel(EmbeddingArgs a, int n, Chunks ch) {
   dq_pdl_enter();
   dq_pdl_release();
   constexpr int E = 16 / (int)sizeof(T), P = kCols / E, Q = kIn ? P : P + 1;  // packs of a row: its own, read
@@ -410,12 +414,16 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
   };
 
   const int32_t after = hi < n ? s.ids[hi] : (int32_t)a.vocab;  // of the next chunk's first place
+  // Batches with a row whose packs might reach beyond dy are read by single values.
+  constexpr bool kWhole = kIn && kOut && E == 4;  // rows end with a pack
+  const Rows inside = rows_inside((int)a.tokens, a.workers, (int)m, ch.near, !kIn && c0 == 0,
+                                  c0 + 2 * kCols > width && !(kIn && width % E == 0));
   int32_t next_id[kAhead + 1], next_place[kAhead];
   const auto places_at = [&](int j0) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       next_id[j] = j0 + j < hi ? s.ids[j0 + j] : (int32_t)a.vocab;
-      next_place[j] = j0 + j < hi ? s.places[j0 + j] : 0;
+      next_place[j] = j0 + j < hi ? s.places[j0 + j] : inside.begin;
     }
     next_id[kAhead] = j0 + kAhead < hi ? s.ids[j0 + kAhead] : after;
   };
@@ -424,18 +432,36 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(EmbeddingArg
     int32_t id[kAhead + 1];
     uint4 x[kAhead][Q];
     int shift[kIn ? 1 : kAhead];
+    int first = next_place[0], last = next_place[0];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      id[j] = next_id[j];
-      const T* row = dy + (int64_t)next_place[j] * a.ld + c0;
-      const int s16 = kIn ? 0 : (int)((uintptr_t)row & 15u);
-      if (!kIn) shift[j] = s16;
-      const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) - s16);
-      const int bytes = (width - c0) * (int)sizeof(T) + s16;  // before the row's end
-      if (id[j] < a.vocab) {
+    for (int j = 1; j < kAhead; ++j) {
+      first = min(first, next_place[j]);
+      last = max(last, next_place[j]);
+    }
+    if (!kWhole && (first < inside.begin || last >= inside.end)) {
 #pragma unroll
-        for (int p = 0; p < Q; ++p)
-          if (16 * p < bytes) x[j][p] = kIn ? __ldcs(from + p) : from[p];
+      for (int j = 0; j < kAhead; ++j) {
+        id[j] = next_id[j];
+        const T* row = dy + (int64_t)next_place[j] * a.ld + c0;
+        if (!kIn) shift[j] = 0;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+          reinterpret_cast<T*>(&x[j][c / E])[c % E] = id[j] < a.vocab && c0 + c < width ? row[c] : from_float<T>(0.f);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        id[j] = next_id[j];
+        const T* row = dy + (int64_t)next_place[j] * a.ld + c0;
+        const int s16 = kIn ? 0 : (int)((uintptr_t)row & 15u);
+        if (!kIn) shift[j] = s16;
+        const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(row) - s16);
+        const int bytes = (width - c0) * (int)sizeof(T) + s16;  // before the row's end
+        if (id[j] < a.vocab) {
+#pragma unroll
+          for (int p = 0; p < Q; ++p)
+            if (16 * p < bytes) x[j][p] = kIn ? __ldcs(from + p) : from[p];
+        }
       }
     }
     id[kAhead] = next_id[kAhead];
@@ -529,7 +555,7 @@ int lanes_for(int64_t width, int per_thread, int most) {
 constexpr int64_t kSumBlocks = 152 * 16;
 
 Chunks chunks_of(int64_t n, int64_t width, int64_t workers) {
-  Chunks ch;
+  Chunks ch{};
   ch.lanes = lanes_for(width, kCols, kSumThreads);
   const int64_t slices = ceil_div(width, kSlice), groups = kSumThreads / ch.lanes;
   ch.size = (int32_t)max64(max64(16, ceil_div(n, 1024)), ceil_div(n * workers * slices, kSumBlocks * groups));
@@ -613,7 +639,8 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& args, cudaStream_t st
     const int size = a.dtype == DQGAN_F32 ? 4 : 2;
     const bool in = (uintptr_t)a.dy % 16 == 0 && a.ld * size % 16 == 0;
     const bool out = a.width % 4 == 0 && (uintptr_t)a.dtable % 16 == 0 && a.g_stride % 4 == 0;
-    const Chunks ch = chunks_of(n, a.width, a.workers);
+    Chunks ch = chunks_of(n, a.width, a.workers);
+    ch.near = rows_near(a.ld * size);
     const dim3 grid((unsigned)ceil_div((int64_t)a.workers * ch.count, kSumThreads / ch.lanes),
                     (unsigned)ceil_div(a.width, kSlice));
     ++*launches;

@@ -51,8 +51,11 @@ struct Slice {
   __host__ __device__ static constexpr int ring_packs(int threads) { return threads * N + (kVec ? 0 : threads / kLanes); }
   __device__ __forceinline__ static int ring_at() { return kVec ? (int)threadIdx.x : (int)threadIdx.x / kLanes * (kLanes * N + 1); }
 
-  // The row into a ring stage, 0 past its end.
-  __device__ __forceinline__ static void fetch(const T* row, int width, int lane, uint4* to, int threads) {
+  // The row into a ring stage, 0 past its end.  all: where the tensor begins, if the row may be so near to that that
+  // its first pack begins before; nothing there is read.  (Only a group's first row may: rows of less than 16 bytes, of
+  // which several are, have a group of 8 threads each.)
+  __device__ __forceinline__ static void fetch(const T* row, int width, int lane, uint4* to, int threads,
+                                               const T* all = nullptr) {
     const int shift = kVec ? 0 : (int)((uintptr_t)row & 15u);
     const char* from = reinterpret_cast<const char*>(row) - shift;
     to += ring_at();
@@ -61,6 +64,12 @@ struct Slice {
       if (i == N && lane > 0) break;  // one pack more than the threads' N
       const int pack = i * kLanes + lane, left = shift + width * (int)sizeof(T) - 16 * pack;
       const int bytes = left >= 16 ? 16 : left > 0 ? left : 0;
+      if (!kVec && i == 0 && lane == 0 && all && (uintptr_t)from < (uintptr_t)all) {
+#pragma unroll 1
+        for (int e = 0; e < (16 - shift) / (int)sizeof(T); ++e)
+          reinterpret_cast<T*>(to)[shift / (int)sizeof(T) + e] = e < width ? row[e] : from_float<T>(0.f);
+        continue;
+      }
       copy16_async(kVec ? to + i * threads : to + pack, from + (bytes > 0 ? 16 * pack : 0), bytes);
     }
   }
@@ -223,13 +232,13 @@ __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : 
   const int64_t first = (int64_t)blockIdx.x * kGroups;
   const T* xs = static_cast<const T*>(a.x) + m * a.rows * a.x_ld;
   T* ys = static_cast<T*>(a.out) + m * a.rows * a.out_ld;
-  const auto fetch = [&](int64_t r, int stage) {
-    if (r < a.rows) S::fetch(xs + r * a.x_ld, width, lane, ring + stage * kPacks, kThreads);
+  const auto fetch = [&](int64_t r, int stage, const T* all = nullptr) {
+    if (r < a.rows) S::fetch(xs + r * a.x_ld, width, lane, ring + stage * kPacks, kThreads, all);
     copies_begun();
   };
   const int64_t mine = first + threadIdx.x / kLanes;
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) fetch(mine + s * step, s);
+  for (int s = 0; s < kStages - 1; ++s) fetch(mine + s * step, s, s == 0 ? static_cast<const T*>(a.x) : nullptr);
   float2 w[S::N][S::E / 2], b[S::N][S::E / 2];
   S::params(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, width, lane, w);
   S::params(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, width, lane, b);
@@ -333,12 +342,12 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
   const T* xs = static_cast<const T*>(a.x) + m * a.rows * a.x_ld;
   const T* dys = static_cast<const T*>(a.dy) + m * a.rows * a.dy_ld;
 
-  const auto fetch = [&](int64_t r, int stage) {
+  const auto fetch = [&](int64_t r, int stage, bool begins = false) {
     if (!kRing) return;
     if (r < a.rows) {
       uint4* to = ring + stage * 2 * kPacks;
-      S::fetch(xs + r * a.x_ld, width, lane, to, kThreads);
-      S::fetch(dys + r * a.dy_ld, width, lane, to + kPacks, kThreads);
+      S::fetch(xs + r * a.x_ld, width, lane, to, kThreads, begins ? static_cast<const T*>(a.x) : nullptr);
+      S::fetch(dys + r * a.dy_ld, width, lane, to + kPacks, kThreads, begins ? static_cast<const T*>(a.dy) : nullptr);
     }
     copies_begun();
   };
@@ -352,7 +361,7 @@ __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_back
     }
   };
 #pragma unroll
-  for (int s = 0; s < kStages - 2; ++s) fetch(first + group + s * step, s);
+  for (int s = 0; s < kStages - 2; ++s) fetch(first + group + s * step, s, s == 0);
 
   float2 w[S::N][S::E / 2], sw[S::N][S::E / 2], sb[S::N][S::E / 2];
   S::params(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, width, lane, w);

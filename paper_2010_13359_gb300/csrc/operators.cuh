@@ -182,6 +182,21 @@ __device__ __forceinline__ uint4 funnel16(const uint4& a, const uint4& b, int s)
                     __funnelshift_r(u[2], u[3], bits), __funnelshift_r(u[3], u[4], bits));
 }
 
+// Rows that do not start or end on 16-byte boundaries are read as the aligned packs of 16 bytes that hold them.  Gaps
+// between rows may be read along, but nothing before the first row's first value or after the last row's last: those of
+// worker m's rows whose packs stay clear of that.  near: the rows from either end whose packs may not; heads: a pack
+// may begin before its row does; tails: it may end after it.
+struct Rows {
+  int begin, end;
+};
+__host__ __device__ constexpr int rows_near(int64_t ld_bytes) { return ld_bytes < 16 ? (int)ceil_div(16, ld_bytes) : 1; }
+__host__ __device__ constexpr Rows rows_inside(int rows, int workers, int m, int near, bool heads, bool tails) {
+  const int64_t before = near - (int64_t)m * rows, after = near - (int64_t)(workers - 1 - m) * rows;
+  const int begin = !heads || before < 0 ? 0 : before < rows ? (int)before : rows;
+  const int end = rows - (!tails || after < 0 ? 0 : after < rows - begin ? (int)after : rows - begin);
+  return {begin, end};
+}
+
 // Copies `bytes` (at most 16) bytes and zeros the rest of the 16, asynchronously.
 __device__ __forceinline__ void copy16_async(void* to, const void* from, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");

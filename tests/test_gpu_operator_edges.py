@@ -7,7 +7,9 @@ import numpy as np
 import pytest
 
 from operator_references import U, distillation, rounded, within
-from test_gpu_operators import DTYPES, P, gen, stream  # noqa: F401
+from test_gpu_operators import DTYPES, P, gen, rows_of, stream  # noqa: F401
+from test_gpu_operators import test_layer_norm_backward as norm_backward_case
+from test_gpu_operators import test_layer_norm_forward as norm_forward_case
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +53,26 @@ def test_distillation_of_extreme_teacher_values(P, vocab, teacher, temperature):
     want = distillation(z.double(), ids, moved, None, ones, T32, 1.0, lse=lse.double())
     within(back, want[2], want[5] + rounded(want[2].abs() + want[5], torch.float32), "dlogits")
     op.destroy()
+
+
+@pytest.mark.parametrize("width,pad,shift,dtype", [(1, 0, 1, 1), (1, 2, 7, 2), (2, 0, 3, 0), (3, 0, 5, 1), (3, 1, 1, 0), (5, 0, 6, 2),
+                                                   (7, 1, 0, 1), (9, 7, 0, 1), (6, 2, 0, 0), (21, 0, 3, 1)])
+@pytest.mark.parametrize("workers,tokens", [(1, 1), (2, 3), (3, 40)])
+def test_narrow_rows_at_both_ends_of_a_tensor(P, width, pad, shift, dtype, workers, tokens):  # noqa: F811
+    """Rows whose first or last pack of 16 bytes reaches beyond the tensor, into memory that holds NaN."""
+    n, vocab = workers * tokens, 4
+    dy, _ = rows_of(torch.randn((n, width), generator=gen(width), device="cuda"), pad, DTYPES[dtype], shift)
+    ids = torch.randint(0, vocab, (workers, tokens), generator=gen(tokens), device="cuda").int()
+    op = P.Embedding(vocab=vocab, width=width, max_tokens=tokens, workers=workers, dtype=dtype, cuda_stream=stream())
+    g = torch.full((workers, vocab * width), math.nan, device="cuda")
+    op.backward(tokens, ids, dy, dy.stride(0), g, vocab * width)
+    want, size = torch.zeros((2, workers * vocab, width), dtype=torch.float64, device="cuda")
+    at = (ids.long() + vocab * torch.arange(workers, device="cuda")[:, None]).view(-1)
+    want.index_add_(0, at, dy.double())
+    size.index_add_(0, at, dy.double().abs())
+    count = torch.bincount(at, minlength=workers * vocab).double()[:, None]
+    within(g.view(workers * vocab, width), want, (count + 2) * U * size, "dtable")
+    op.destroy()
+    shape = (workers, tokens, width, dtype, pad, shift, False)
+    norm_forward_case(P, shape)
+    norm_backward_case(P, shape)
