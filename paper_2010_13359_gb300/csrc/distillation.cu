@@ -191,10 +191,6 @@ struct Packs {
     else return to_float(reinterpret_cast<const T*>(&p)[e]);
   }
 
-  static __device__ __forceinline__ uint32_t lowest() {  // -inf, in every element of a word
-    return sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
-  }
-
   static __device__ __forceinline__ float max_of(const uint4& p) {  // NaN where nothing else
     if constexpr (sizeof(T) == 4) {
       return fmaxf(fmaxf(value(p, 0), value(p, 1)), fmaxf(value(p, 2), value(p, 3)));
