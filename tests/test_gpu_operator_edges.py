@@ -76,3 +76,56 @@ def test_narrow_rows_at_both_ends_of_a_tensor(P, width, pad, shift, dtype, worke
     shape = (workers, tokens, width, dtype, pad, shift, False)
     norm_forward_case(P, shape)
     norm_backward_case(P, shape)
+
+
+@pytest.mark.parametrize("vocab,k", [(500, 300), (32_000, 1024), (130_000, 200)])
+def test_distillation_of_ids_that_come_again(P, vocab, k):  # noqa: F811
+    """One id twice, pairs, ids of many entries, all the same: summed over their entries, and one of them does not make
+    every other entry of the row dear (it did 20-fold; a few looks at k ids each cost a small part of the row)."""
+    rows = 1024
+    z = torch.randn((rows, vocab), generator=gen(k), device="cuda").bfloat16()
+    step = vocab // k
+    unique = (torch.randint(0, vocab, (rows, 1), generator=gen(vocab), device="cuda") + step * torch.arange(k, device="cuda")) % vocab
+    one = unique.clone()
+    one[:, k - 1] = one[:, 0]
+    many = one.clone()
+    many[0::4, 1::2] = many[0::4, 0::2]
+    many[1::4] = many[1::4, k // 2:k // 2 + 1]
+    many[2::4] = many[2::4, torch.arange(k, device="cuda") % 7]
+    many[3::8, 5] = -1
+    values = torch.randn((rows, k), generator=gen(63), device="cuda")
+    op = P.Distillation(vocab=vocab, k=k, dtype=1, temperature=1.5, cuda_stream=stream())
+    loss, lse = torch.full((2, rows), math.nan, device="cuda")
+    dz = torch.full_like(z, math.nan)
+
+    def call(ids):
+        op.step(rows, z, vocab, ids, values, k, None, None, 1.0, loss, lse, dz, vocab)
+
+    ones = torch.ones(rows, dtype=torch.float64, device="cuda")
+    for ids in (one, many):
+        call(ids.int())
+        first = dz.clone()
+        for at in range(0, rows, 256):
+            part = slice(at, at + 256)
+            ref = distillation(z[part].double(), ids[part], values[part].double(), None, ones[part], 1.5, 1.0)
+            within(loss[part], ref[0], ref[3] + 4 * U * ref[0].abs(), "loss")
+            within(dz[part], ref[2], ref[5] + rounded(ref[2].abs() + ref[5], torch.bfloat16), "dlogits")
+        call(ids.int())
+        assert torch.equal(first.view(torch.int16), dz.view(torch.int16))
+
+    def time_of(ids):
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            for _ in range(4):
+                call(ids)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    if k > 1000:
+        assert time_of(one.int()) < 4 * time_of(unique.int())
+    op.destroy()
