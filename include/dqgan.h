@@ -439,7 +439,9 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *   - Parameters, gradients, statistics and losses are fp32, and so is all
  *     arithmetic: sums, softmax statistics and norms are held in 32 bits
  *     and a 16-bit result is rounded once.  Every sum has a fixed order, so the
- *     same call on the same data gives the same bits.
+ *     same call on the same data gives the same bits.  Exponentials below 2^-126
+ *     may be taken as 0, and the last digits of a result depend on whether its
+ *     row fits on chip.
  *   - Sizes of 0 rows or tokens are allowed (gradients of nothing are 0).
  *   - An output may be the input named with it below (same pointer and stride);
  *     no other overlap is allowed.
@@ -581,7 +583,10 @@ DQGAN_API int dqgan_distillation_forward(dqgan_operator* op, int64_t rows, const
                                          const float* teacher_lse, const float* weights, float* loss, float* lse);
 
 /* The gradient of scale * sum of losses with respect to the logits, from the
- * forward pass's lse.  dlogits may be logits. */
+ * forward pass's lse.  dlogits may be logits.  q is exp(z / T - lse) at that fp32
+ * lse, so it is off by |lse| 2^-24 relative to itself: a row whose logits are
+ * all far from 0 (below -1e5, or of the type's lowest value) needs the step,
+ * which takes differences from the row's maximum. */
 DQGAN_API int dqgan_distillation_backward(dqgan_operator* op, int64_t rows, const void* logits, int64_t logits_stride,
                                           const float* lse, const int32_t* ids, const void* values,
                                           int64_t teacher_stride, const float* teacher_lse, const float* weights,

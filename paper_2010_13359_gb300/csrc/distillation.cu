@@ -48,7 +48,8 @@ __device__ __forceinline__ float block_max(float x, float* shared) {
 
 // Rows that do not fit on chip: one block each, which reads its row once for the
 // maximum, once for the sum and once for the gradient, the later times out of the
-// L2 as far as that holds them.
+// L2 as far as that holds them, a value at a time: 256 rows of 1,000,003 bf16 values
+// 3.97 ms, 4 % of 6694.5 GB/s.
 template <typename T, DistillationWay kWay>
 __global__ void __launch_bounds__(kThreads) distillation_long_kernel(DistillationArgs a) {
   dq_pdl_enter();
@@ -170,8 +171,8 @@ __global__ void __launch_bounds__(kThreads) distillation_long_kernel(Distillatio
 // they took half of the block's time at the barrier.
 //
 // Measured (of 6694.5 GB/s): both passes over 8192 x 128,000 bf16 761 us (82 %),
-// over 4096 x 32,000 89 us (86 %); the gradient alone of 1023 x 50,001 fp32 70 us
-// (88 %).  Issue slots are 63 % used and the rest goes to the row's two exchanges
+// over 4096 x 32,000 89 us (86 %), in fp32 191 us (82 %), in place 206 us; the loss alone
+// 438 us (72 %) and 54 us (69 %); the gradient alone of 1023 x 50,001 fp32 70 us (88 %).  Issue slots are 63 % used and the rest goes to the row's two exchanges
 // (cluster barrier, join) and to the start of each row's loads.  Rows of a few
 // thousand values are bound by the latency of a row's chain: 8000 x 2300 with 8
 // entries 37 us, a quarter of the bandwidth.
@@ -409,7 +410,8 @@ struct Part {
   }
 };
 
-// Writes gradient_of(i), this thread's pack i, for every i.
+// Writes gradient_of(i), this thread's pack i, for every i: value by value where the gradient's rows are aligned
+// otherwise than the logits' (4096 x 32,000 bf16 306 us, 89 where they are alike).
 template <typename T, int kWorkers, typename F>
 __device__ __forceinline__ void put_all(const Part<T, kWorkers>& part, T* dz, F&& gradient_of) {
   constexpr int E = Part<T, kWorkers>::E;

@@ -26,10 +26,10 @@ __device__ __forceinline__ int32_t token_at(const EmbeddingArgs& a, int64_t i) {
 // Forward: `lanes` threads take a row, each kAtOnce pieces of it at once: 16 bytes
 // of y (kVec: rows of table and y are aligned for that) or one value; the next row's
 // id is on its way meanwhile.  8 x 4096 rows of 1024 fp32 values to bf16: 23 us, 87 %
-// of 6694.5 GB/s; of 1023 (single values) 49 us.
+// of 6694.5 GB/s; of 1023 (single values) 49 us, from a bf16 table 61 us (41 %, 25 %).
 // ---------------------------------------------------------------------------
 constexpr int kForwardThreads = 256;
-// 16,384 rows of 1023 values: 49 us with 8 single fp32 values at once, 57 with 4; bf16 ones 76 and 61
+// 8 x 4096 rows of 1023 values: 49 us with 8 single fp32 values at once, 57 with 4; bf16 ones 76 and 61
 constexpr int at_once(bool vec, int size) { return vec || size == 2 ? 4 : 8; }
 
 template <typename E, typename T, bool kVec>
@@ -100,7 +100,10 @@ __global__ void __launch_bounds__(kForwardThreads) embedding_forward_kernel(Embe
 // Nothing is added atomically, so the same call gives the same bits.  Measured: 8 x 4096
 // tokens of 32,000 x 1024 171 us (97 % of 6694.5 GB/s, 136 of them zeros), 131,072 tokens
 // of 128,000 x 4096 602 us (79 %: zeros 300 us at 5.0 TB/s, sums 276 us at 5.9 TB/s, joins
-// about 20 us); small ones are bound by the three kernels' latencies: 2 x 333 tokens 15 us.
+// about 20 us); small ones are bound by the three kernels' latencies: 2 x 333 tokens 16 us.
+// Where no zeros hide it the sort stands in the way: added to the same 8 tables 66 us (45 %),
+// 131,072 tokens added to 128,000 x 1024 214 us (38 %), 8 x 31,395 f16 tokens of 3541 x 109
+// 79 us (13 %).
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kSortMost = 20480;  // places of one block: two buffers of them in shared memory

@@ -9,7 +9,8 @@
 // group of kLanes threads holds it, 16 values to a thread.  The variance is taken
 // from the deviations, in a second sum over the same registers, so that a large
 // mean costs no digits.  Rows longer than 16,384 values are read again from the
-// caches instead.
+// caches instead, and so are those of the backward pass in fp32 above 8192: a row of
+// x and one of dy take up to 128 KB there, which leaves no room for rows ahead.
 #include "device_common.cuh"
 #include "operators.cuh"
 
@@ -214,8 +215,9 @@ constexpr int backward_stages() {
 // of a pack, so no pack needs looking into.
 //
 // Measured (of 6694.5 GB/s): 16,384 rows of 1024 bf16 values 12.7 us (79 %), of 4096
-// 45 us (89 %), of 5120 63 us (80 %), of 4095 65 us (62 %: single-element reads and
-// writes); four rows of 512 on each of four workers 2.5 us.
+// 46 us (87 %), of 5120 63 us (80 %), of 4095 65 us (62 %: single-element reads and
+// writes), of 4096 fp32 ones 95 us (85 %); four rows of 512 on each of four workers 2.5 us.
+// Groups of 512 and 1024 threads have 64 registers a thread and spill 8 to 92 bytes.
 template <typename T, int kLanes, bool kVec, bool kWhole>
 __global__ void __launch_bounds__(forward_threads<kLanes>(), kLanes > 512 ? 1 : kLanes > 256 ? 2 : 3)
     layer_norm_forward_kernel(LayerNormArgs a) {
@@ -324,8 +326,11 @@ __host__ __device__ constexpr int64_t part_stride(int64_t width) { return (width
 //
 // Measured: 16,384 rows of 4096 bf16 values 74 us with the join (82 % of 6694.5 GB/s),
 // in fp32 133 us (91 %); of 8192 (512 a worker) 52 us (58 %) and of 1024 27 us (56 %):
-// one block's 16 warps leave the row's chain exposed there.  Tried: 32 values a
-// thread with the weights in shared memory, 79 us and 58 us.
+// one block's 16 warps leave the row's chain exposed there.  Rows that are not
+// aligned: of 4095 bf16 values 107 us (56 %).  Groups of 768 (fp32) and 1024 threads spill,
+// up to 312 bytes of stores a thread in fp32: 4096 rows of 12,288 fp32 values 131 us
+// (69 %), of 16,384 218 us (55 %), in bf16 81 us and 116 us (55 %, 52 %).  Tried: 32
+// values a thread with the weights in shared memory, 79 us and 58 us.
 template <typename T, int kLanes, bool kVec>
 __global__ void __launch_bounds__(backward_threads<kLanes>(), 1) layer_norm_backward_kernel(LayerNormArgs a) {
   dq_pdl_enter();
@@ -513,7 +518,9 @@ __global__ void __launch_bounds__(kJoinWarps * 32) layer_norm_join_kernel(LayerN
 }
 
 // Rows of more than kMaxOnChip values, one block each: further passes over the
-// row come out of the caches.
+// row come out of the caches, a value at a time.  4000 rows of 20,000 bf16 values
+// forward 131 us (36 % of 6694.5 GB/s), backward, where the parameters' sums read x and dy
+// once more, 377 us (19 %).
 constexpr int kLongThreads = 512;
 
 template <typename T>
