@@ -424,6 +424,13 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *                 q = softmax(z / T); loss = c T^2 sum_k p_k (log p_k - log q_id_k);
  *                 dz = scale c T (q sum_k p_k - sum_k p_k at id_k).
  *                 One entry a row with t = 0, T = 1 is cross entropy.
+ *   linear        u = x W^T + b, y = act(u) + r; du = dy act'(u): dx = du W,
+ *                 dW = du^T x, db = sum over rows of du (dr = dy).
+ *   token loss    the output layer with its cross entropy: z = x W^T,
+ *                 loss = c (log sum_v exp z_v - z_target); dz = scale c (softmax(z)
+ *                 - 1 at the target): dx = dz W, dW = dz^T x.
+ *   clipping      n the norm of a worker's gradient over many tensors; the tensors
+ *                 times min(1, max_norm / (n + eps)), into the worker's row.
  *
  * Conventions, where they differ from or add to the ones above:
  *   - An operator handle has its own stream, scratch and error text.  It keeps
@@ -449,6 +456,12 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
 #define DQGAN_F32 0
 #define DQGAN_BF16 1
 #define DQGAN_F16 2
+
+/* Activations of a linear layer. */
+#define DQGAN_NONE 0
+#define DQGAN_RELU 1
+#define DQGAN_GELU 2 /* u times the normal distribution function of u */
+#define DQGAN_SILU 3 /* u times the logistic function of u */
 
 /* Layer norm.  32 bytes, no implicit padding.
  *   width  1 <= width <= 65536;  workers  1 <= workers <= 4096;
@@ -499,21 +512,89 @@ typedef struct dqgan_distillation_config {
   void* cuda_stream;
 } dqgan_distillation_config;
 
+/* Linear layer.  56 bytes, no implicit padding.
+ *   inputs, outputs  1 <= inputs, outputs <= 65536;
+ *   max_rows         largest number of rows a worker of a call has, in [1, 2^24];
+ *                    workers * max_rows at most 2^28;
+ *   workers          1 <= workers <= 4096;
+ *   dtype            of x, y, u, r, dy, dx;
+ *   weight_dtype     of the weights: dtype, or DQGAN_F32;
+ *   activation       DQGAN_NONE / RELU / GELU / SILU;  reserved  0. */
+typedef struct dqgan_linear_config {
+  int64_t inputs;
+  int64_t outputs;
+  int64_t max_rows;
+  int32_t workers;
+  int32_t dtype;
+  int32_t weight_dtype;
+  int32_t activation;
+  uint32_t reserved[2];
+  void* cuda_stream;
+} dqgan_linear_config;
+
+/* Token loss.  56 bytes, no implicit padding.
+ *   vocab         1 <= vocab <= 2^24;
+ *   width         1 <= width <= 65536;
+ *   max_rows      largest number of rows a worker of a call has, in [1, 2^24];
+ *                 workers * max_rows at most 2^28;
+ *   workers       1 <= workers <= 4096;
+ *   dtype         of x and dx;
+ *   weight_dtype  of the weights: dtype, or DQGAN_F32;
+ *   token_bits    of the targets, 32 or 64, signed;  reserved  0. */
+typedef struct dqgan_token_loss_config {
+  int64_t vocab;
+  int64_t width;
+  int64_t max_rows;
+  int32_t workers;
+  int32_t dtype;
+  int32_t weight_dtype;
+  int32_t token_bits;
+  uint32_t reserved[2];
+  void* cuda_stream;
+} dqgan_token_loss_config;
+
+/* Gradient clipping.  32 bytes, no implicit padding.
+ *   workers    1 <= workers <= 4096;
+ *   dtype      of the tensors;  out_dtype  of their places: dtype, or DQGAN_F32;
+ *   eps        >= 0, finite;  reserved  0. */
+typedef struct dqgan_gradient_clip_config {
+  int32_t workers;
+  int32_t dtype;
+  int32_t out_dtype;
+  float eps;
+  uint32_t reserved[2];
+  void* cuda_stream;
+} dqgan_gradient_clip_config;
+
+/* One tensor of every worker: worker m's `size` values, without gaps, at
+ * data + m * stride elements.  24 bytes, no implicit padding. */
+typedef struct dqgan_tensor {
+  void* data;
+  int64_t size;
+  int64_t stride;
+} dqgan_tensor;
+
 typedef struct dqgan_operator dqgan_operator;
 
 /* Create an operator on the current device, with its scratch space (layer
- * norm and embedding: for the gradients; distillation has none).  On error
+ * norm and embedding: for the gradients; distillation has none; linear: its operands as the
+ * tensor cores read them; token loss: besides those a piece of the logits' gradient, up to
+ * 512 MB; clipping: the blocks' sums).  On error
  * *out is NULL, dqgan_operator_last_error(NULL) holds the reason and nothing
  * stays allocated.  The test hook DQGAN_TEST_FAIL_ALLOC of dqgan_create
  * applies here too. */
 DQGAN_API int dqgan_layer_norm_create(const dqgan_layer_norm_config* cfg, dqgan_operator** out);
 DQGAN_API int dqgan_embedding_create(const dqgan_embedding_config* cfg, dqgan_operator** out);
 DQGAN_API int dqgan_distillation_create(const dqgan_distillation_config* cfg, dqgan_operator** out);
+DQGAN_API int dqgan_linear_create(const dqgan_linear_config* cfg, dqgan_operator** out);
+DQGAN_API int dqgan_token_loss_create(const dqgan_token_loss_config* cfg, dqgan_operator** out);
+DQGAN_API int dqgan_gradient_clip_create(const dqgan_gradient_clip_config* cfg, dqgan_operator** out);
 
 /* Release the operator (synchronises its stream first).  NULL is a no-op. */
 DQGAN_API int dqgan_operator_destroy(dqgan_operator* op);
 
-/* Wait for the operator's stream; DQGAN_ERR_CUDA if enqueued work failed. */
+/* Wait for the operator's stream; DQGAN_ERR_CUDA if enqueued work failed, DQGAN_ERR_TIMEOUT
+ * if a bounded wait in one of its kernels gave up. */
 DQGAN_API int dqgan_operator_synchronize(dqgan_operator* op);
 
 /* Kernels the operator has launched so far. */
@@ -597,6 +678,76 @@ DQGAN_API int dqgan_distillation_step(dqgan_operator* op, int64_t rows, const vo
                                       const int32_t* ids, const void* values, int64_t teacher_stride,
                                       const float* teacher_lse, const float* weights, float scale, float* loss,
                                       float* lse, void* dlogits, int64_t dlogits_stride);
+
+/*
+ * Linear layer of workers * rows rows (rows <= max_rows): y = act(x W^T + b) + r.
+ * weight: outputs rows of inputs values, contiguous, worker m's at
+ * weight + m * p_stride elements of weight_dtype (0: shared, else >= inputs *
+ * outputs).  bias: fp32, worker m's at bias + m * b_stride (0: shared), or NULL.
+ * residual: r, rows of outputs values, or NULL; y may be residual.  pre: receives
+ * u = x W^T + b, which the backward pass of an activation needs, or NULL.
+ * Products of 16-bit rows with fp32 weights take the weights rounded to bf16
+ * (bf16 rows), or with 16 of their bits (f16 rows).
+ */
+DQGAN_API int dqgan_linear_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
+                                   const void* weight, int64_t p_stride, const float* bias, int64_t b_stride,
+                                   const void* residual, int64_t residual_stride, void* y, int64_t y_stride, void* pre,
+                                   int64_t pre_stride);
+
+/*
+ * Its gradient, from the forward pass's x and pre (not read where the activation
+ * is DQGAN_NONE).  dx, dweight and dbias may each be NULL; x is needed for
+ * dweight, weight for dx.  dweight, dbias: worker m's at + m * g_stride floats,
+ * written, or added to with accumulate != 0.  The residual's gradient is dy.
+ */
+DQGAN_API int dqgan_linear_backward(dqgan_operator* op, int64_t rows, const void* dy, int64_t dy_stride, const void* x,
+                                    int64_t x_stride, const void* weight, int64_t p_stride, const void* pre,
+                                    int64_t pre_stride, void* dx, int64_t dx_stride, float* dweight, float* dbias,
+                                    int64_t g_stride, int32_t accumulate);
+
+/*
+ * Cross entropy of workers * rows rows (rows <= max_rows) of the output layer
+ * z = x W^T, whose logits are nowhere kept.  weight: vocab rows of width values,
+ * contiguous, worker m's at weight + m * p_stride elements of weight_dtype (0:
+ * shared, else >= vocab * width).  targets: one a row, worker m's at + m * rows.
+ * weights: c of each row, or NULL (ones).  A row whose target is outside
+ * [0, vocab) or whose weight is 0 does not count: its loss, lse and gradient are
+ * 0, and what x holds there does not matter.  loss: one a row.
+ * lse: log sum_v exp(z_v), one a row, or NULL.
+ */
+DQGAN_API int dqgan_token_loss_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
+                                       const void* weight, int64_t p_stride, const void* targets, const float* weights,
+                                       float* loss, float* lse);
+
+/*
+ * The gradient of scale * sum of losses with respect to x and the weights, from
+ * the forward pass's lse.  dx and dweight may each be NULL.  dweight: worker m's
+ * vocab * width floats at + m * g_stride, written, or added to with accumulate != 0.
+ */
+DQGAN_API int dqgan_token_loss_backward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
+                                        const void* weight, int64_t p_stride, const void* targets,
+                                        const float* weights, const float* lse, float scale, void* dx,
+                                        int64_t dx_stride, float* dweight, int64_t g_stride, int32_t accumulate);
+
+/* Both in one call.  lse may be NULL. */
+DQGAN_API int dqgan_token_loss_step(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
+                                    const void* weight, int64_t p_stride, const void* targets, const float* weights,
+                                    float scale, float* loss, float* lse, void* dx, int64_t dx_stride, float* dweight,
+                                    int64_t g_stride, int32_t accumulate);
+
+/*
+ * norms[m] = the 2-norm of worker m's values in all `count` tensors (at most
+ * 4096; sizes may be 0).  The list is read during the call only.
+ */
+DQGAN_API int dqgan_gradient_norm(dqgan_operator* op, int64_t count, const dqgan_tensor* tensors, float* norms);
+
+/*
+ * Writes min(1, max_norm / (norm + eps)) times each tensor to its place (of the
+ * same size), worker by worker.  max_norm >= 0.  A worker whose norm is not finite
+ * is passed on as it is.  norms: as above, or NULL.  A place may be its tensor (same address, type and stride).
+ */
+DQGAN_API int dqgan_gradient_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* tensors,
+                                  const dqgan_tensor* places, float max_norm, float* norms);
 
 /* Text of the last error on this handle, or of the last failed
  * create / validate / layout call in this thread when h is NULL.

@@ -118,6 +118,13 @@ struct SignServerExtras {
   int64_t seg_nslices;
 };
 
+// cuTensorMapEncodeTiled through the runtime's driver entry point (no link
+// against libcuda); nullptr if it is unavailable.
+using TensorMapEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+TensorMapEncoder tensor_map_encoder();
+
 // TMA tensor map over the payload words of M messages: a 2-D array of u32,
 // rows = workers (M), columns = message words up to the end of the payload;
 // boxes of box_words words (a multiple of 4; 32 with the 128-byte swizzle)

@@ -1,0 +1,291 @@
+// Linear layers of the workers: y = act(x W^T + b) + r, and the gradients of x, W and b.
+//
+//   u = x W^T + b;  y = act(u) + r
+//   du = dy act'(u);  dx = du W;  dW = du^T x;  db = sum over rows of du   (dr = dy)
+//
+// Three products a layer (2 rows inputs outputs operations each), bound by the
+// tensor cores where there are some hundred rows, by the weights' bytes below.
+// How many 16-bit parts an operand has follows from the result's type: results
+// of 16 bits take one part of each operand in that type (a second rounding of the
+// size of the result's own); what is summed into fp32 gradients, and all of fp32
+// layers, takes as many as keep the products' error near 2^-17 (two parts) or
+// 2^-24 (three).  f16 values that do not lie as f16 in memory are two bf16 parts
+// (all of their 11 bits, at any exponent).
+#include "device_common.cuh"
+#include "products.cuh"
+
+namespace dq {
+
+namespace {
+
+int act_parts(int dtype) { return dtype == DQGAN_F32 ? 3 : dtype == DQGAN_F16 ? 2 : 1; }
+int weight_parts(const LinearShape& s) { return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 ? 2 : 1; }
+bool exact_slope(int activation) { return activation == DQGAN_NONE || activation == DQGAN_RELU; }  // du has dy's values
+int grad_parts(const LinearShape& s) {
+  return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 || !exact_slope(s.activation) ? 2 : 1;
+}
+bool half_forward(const LinearShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
+bool half_backward(const LinearShape& s) { return half_forward(s) && exact_slope(s.activation); }
+
+constexpr int kGradRows = 64;  // least rows of a block of slope_kernel
+constexpr int kGradColumns = 256;
+
+struct Scratch {
+  uint32_t* err;
+  void* products;
+  void *x, *w, *d;
+  float* sums;
+  size_t bytes;
+};
+
+Scratch scratch_of(const LinearShape& s, void* base) {
+  Scratch c{};
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    void* p = static_cast<char*>(base) + at;
+    at += (size_t)ceil_div(bytes, 1024) * 1024;
+    return p;
+  };
+  c.err = static_cast<uint32_t*>(take(1024));
+  c.products = take(kProductScratch);
+  const int64_t rows = (int64_t)s.workers * s.max_rows;
+  c.x = take(rows * round8(s.inputs) * 2 * act_parts(s.dtype));
+  c.w = take((int64_t)s.workers * s.outputs * round8(s.inputs) * 2 * weight_parts(s));
+  c.d = take(rows * round8(s.outputs) * 2 * grad_parts(s));
+  c.sums = static_cast<float*>(take((int64_t)s.workers * ceil_div(s.max_rows, kGradRows) * s.outputs * 4));
+  c.bytes = at;
+  return c;
+}
+
+struct SlopeArgs {
+  const void* dy;
+  int64_t dy_ld;
+  const void* pre;
+  int64_t pre_ld;
+  void* to;  // du in parts, or nullptr
+  int64_t ld, part;
+  int32_t parts;
+  bool half;
+  float* sums;  // [worker][block of rows][outputs], or nullptr
+  int64_t rows, columns;
+  int32_t block_rows;
+  int32_t activation;
+  bool dy_packs, pre_packs;
+};
+
+__device__ __forceinline__ float activation_slope(float u, int activation) {
+  switch (activation) {
+    case DQGAN_RELU: return u > 0.f ? 1.f : (u != u ? u : 0.f);
+    case DQGAN_GELU: return fmaf(u * 0.39894228040143268f, expf(-0.5f * u * u), gelu_cdf(u));
+    case DQGAN_SILU: {
+      const float s = sigmoid(u);
+      return s * fmaf(u, 1.f - s, 1.f);
+    }
+  }
+  return 1.f;
+}
+
+// du of a block of rows and 256 columns, in parts, and the columns' sums.
+template <typename T>
+__global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
+  dq_pdl_enter();
+  __shared__ float turn[8][kGradColumns];
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int64_t column = (int64_t)blockIdx.x * kGradColumns + lane * 8;
+  const int64_t worker = blockIdx.z;
+  const int64_t first = (int64_t)blockIdx.y * a.block_rows, last = min(first + a.block_rows, a.rows);
+  const int count = (int)max((int64_t)0, min((int64_t)8, a.columns - column));
+  float sum[8] = {};
+  if (count > 0)
+    for (int64_t r = first + warp; r < last; r += 8) {
+      const int64_t row = worker * a.rows + r;
+      float x[8];
+      read8(static_cast<const T*>(a.dy) + row * a.dy_ld + column, count, a.dy_packs, x);
+      if (a.pre) {
+        float u[8];
+        read8(static_cast<const T*>(a.pre) + row * a.pre_ld + column, count, a.pre_packs, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= activation_slope(u[i], a.activation);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i >= count) x[i] = 0.f;
+        sum[i] += x[i];
+      }
+      if (a.to) write_parts(x, a.to, row * a.ld + column, a.part, a.parts, a.half);
+    }
+  if (a.sums) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn[warp][lane * 8 + i] = sum[i];
+    __syncthreads();
+    const int64_t j = (int64_t)blockIdx.x * kGradColumns + threadIdx.x;
+    if (j < a.columns) {
+      float s = 0.f;
+      for (int w = 0; w < 8; ++w) s += turn[w][threadIdx.x];
+      a.sums[((worker * gridDim.y) + blockIdx.y) * a.columns + j] = s;
+    }
+  }
+}
+
+// db: the blocks' sums in order.
+__global__ void __launch_bounds__(256) bias_kernel(const float* sums, int blocks, int64_t columns, float* dbias,
+                                                   int64_t g_stride, int accumulate) {
+  dq_pdl_enter();
+  const int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, worker = blockIdx.y;
+  if (j >= columns) return;
+  double s = 0.;
+  for (int b = 0; b < blocks; ++b) s += sums[(worker * blocks + b) * columns + j];
+  float* const to = dbias + worker * g_stride + j;
+  *to = accumulate ? *to + (float)s : (float)s;
+}
+
+}  // namespace
+
+size_t linear_scratch_bytes(const LinearShape& s) { return scratch_of(s, nullptr).bytes; }
+
+cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint64_t* launches) {
+  const LinearShape& s = a.shape;
+  const Scratch c = scratch_of(s, a.scratch);
+  const bool half = half_forward(s);
+  Product p;
+  p.rows = a.rows;
+  p.columns = s.outputs;
+  p.depth = s.inputs;
+  p.workers = s.workers;
+  const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+  const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
+  cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.a);
+  if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
+  if (st != cudaSuccess) return st;
+  p.terms = product_terms(p.a.parts, p.b.parts);
+  StoreArgs out{};
+  out.out = a.y;
+  out.out_ld = a.y_ld;
+  out.out_batch = a.rows * a.y_ld;
+  out.out_dtype = s.dtype;
+  out.pre = a.pre_out;
+  out.pre_ld = a.pre_ld;
+  out.pre_batch = a.rows * a.pre_ld;
+  out.residual = a.residual;
+  out.residual_ld = a.residual_ld;
+  out.residual_batch = a.rows * a.residual_ld;
+  out.bias = a.bias;
+  out.bias_batch = a.b_stride;
+  out.activation = s.activation;
+  return launch_product_store(p, out, c.products, c.err, stream, launches);
+}
+
+cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uint64_t* launches) {
+  const LinearShape& s = a.shape;
+  const Scratch c = scratch_of(s, a.scratch);
+  cudaError_t st = cudaSuccess;
+  if (a.rows == 0) {  // gradients of nothing
+    if (a.accumulate) return st;
+    for (int m = 0; m < s.workers && st == cudaSuccess; ++m) {
+      if (a.dweight) st = cudaMemsetAsync(a.dweight + m * a.g_stride, 0, (size_t)s.outputs * s.inputs * 4, stream);
+      if (a.dbias && st == cudaSuccess) st = cudaMemsetAsync(a.dbias + m * a.g_stride, 0, (size_t)s.outputs * 4, stream);
+    }
+    return st;
+  }
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  const bool half = half_backward(s);
+  const int parts = half ? 1 : grad_parts(s);
+  const MatrixArgs dy{a.dy, a.dy_ld, a.rows * a.dy_ld, s.dtype, a.rows, s.outputs, s.workers};
+  const bool direct = s.activation == DQGAN_NONE && (half || (s.dtype == DQGAN_BF16 && parts == 1)) &&
+                      operand_in_place(a.dy, a.dy_ld, a.rows * a.dy_ld);
+  ProductOperand d;
+  if (direct) st = make_operand(dy, parts, half, c.d, stream, launches, &d);
+  if (st == cudaSuccess && (!direct || a.dbias)) {
+    const int size = s.dtype == DQGAN_F32 ? 4 : 2;
+    SlopeArgs k{};
+    k.dy = a.dy;
+    k.dy_ld = a.dy_ld;
+    k.dy_packs = ((uintptr_t)a.dy & 15) == 0 && a.dy_ld * size % 16 == 0;
+    if (s.activation != DQGAN_NONE) {
+      k.pre = a.pre;
+      k.pre_ld = a.pre_ld;
+      k.pre_packs = ((uintptr_t)a.pre & 15) == 0 && a.pre_ld * size % 16 == 0;
+    }
+    k.ld = round8(s.outputs);
+    k.part = k.ld * a.rows * s.workers;
+    k.parts = parts;
+    k.half = half;
+    k.rows = a.rows;
+    k.columns = s.outputs;
+    k.activation = s.activation;
+    k.to = direct ? nullptr : c.d;
+    k.sums = a.dbias ? c.sums : nullptr;
+    const int64_t wide = ceil_div(s.outputs, kGradColumns);
+    // four blocks an SM, of 64 rows at least
+    int64_t blocks = ceil_div((int64_t)sms * 4, wide * s.workers);
+    k.block_rows = (int32_t)(ceil_div(ceil_div(a.rows, blocks), kGradRows) * kGradRows);
+    blocks = ceil_div(a.rows, k.block_rows);
+    ++*launches;
+    st = blocks > 65535 ? cudaErrorInvalidValue : with_dtype(s.dtype, [&](auto t) {
+      return launch_pdl(slope_kernel<decltype(t)>, dim3((unsigned)wide, (unsigned)blocks, (unsigned)s.workers), dim3(256), 0,
+                        stream, k);
+    });
+    if (st == cudaSuccess && a.dbias) {
+      ++*launches;
+      st = launch_pdl(bias_kernel, dim3((unsigned)ceil_div(s.outputs, 256), (unsigned)s.workers), dim3(256), 0, stream,
+                      (const float*)c.sums, (int)blocks, s.outputs, a.dbias, a.g_stride, a.accumulate);
+    }
+    if (!direct) {
+      d.data = c.d;
+      d.ld = k.ld;
+      d.batch = k.ld * a.rows;
+      d.part = k.part;
+      d.parts = parts;
+      d.half = half;
+    }
+  }
+  if (st != cudaSuccess) return st;
+  if (a.dx) {
+    Product p;
+    p.rows = a.rows;
+    p.columns = s.inputs;
+    p.depth = s.outputs;
+    p.workers = s.workers;
+    p.a = d;
+    if (s.dtype == DQGAN_BF16) p.a.parts = 1;
+    const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
+    st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
+    if (st != cudaSuccess) return st;
+    p.b.across = true;
+    p.terms = product_terms(p.a.parts, p.b.parts);
+    StoreArgs out{};
+    out.out = a.dx;
+    out.out_ld = a.dx_ld;
+    out.out_batch = a.rows * a.dx_ld;
+    out.out_dtype = s.dtype;
+    st = launch_product_store(p, out, c.products, c.err, stream, launches);
+  }
+  if (st == cudaSuccess && a.dweight) {
+    Product p;
+    p.rows = s.outputs;
+    p.columns = s.inputs;
+    p.depth = a.rows;
+    p.workers = s.workers;
+    p.a = d;
+    const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+    st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.b);
+    if (st != cudaSuccess) return st;
+    p.a.across = p.b.across = true;
+    p.terms = product_terms(p.a.parts, p.b.parts);
+    StoreArgs out{};
+    out.out = a.dweight;
+    out.out_ld = s.inputs;
+    out.out_batch = a.g_stride;
+    out.out_dtype = DQGAN_F32;
+    if (a.accumulate) {
+      out.add = a.dweight;
+      out.add_ld = s.inputs;
+      out.add_batch = a.g_stride;
+    }
+    st = launch_product_store(p, out, c.products, c.err, stream, launches);
+  }
+  return st;
+}
+
+}  // namespace dq

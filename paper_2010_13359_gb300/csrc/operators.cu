@@ -11,7 +11,7 @@
 
 namespace {
 
-enum class Kind { kLayerNorm, kEmbedding, kDistillation };
+enum class Kind { kLayerNorm, kEmbedding, kDistillation, kLinear, kTokenLoss, kGradientClip };
 
 }  // namespace
 
@@ -20,6 +20,10 @@ struct dqgan_operator {
   dqgan_layer_norm_config norm{};
   dqgan_embedding_config embedding{};
   dqgan_distillation_config distillation{};
+  dqgan_linear_config linear{};
+  dqgan_token_loss_config token_loss{};
+  dqgan_gradient_clip_config clip{};
+  uint32_t* waits = nullptr;  // error word of the kernels that wait, at the start of their scratch
   cudaStream_t stream = nullptr;
   void* scratch = nullptr;
   uint64_t launches = 0;
@@ -33,6 +37,7 @@ constexpr int64_t kMaxBatch = 1 << 28;          // workers * tokens, workers * v
 constexpr int64_t kMaxRows = (int64_t)1 << 30;  // rows of one call, over all workers
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
 constexpr int kMaxEntries = 1024;
+constexpr int64_t kMaxTensors = 4096;
 
 struct NvtxRange {
   explicit NvtxRange(const char* name) { nvtxRangePushA(name); }
@@ -96,6 +101,45 @@ int check_rows(dqgan_operator* op, const char* what, int64_t rows, int64_t worke
   return DQGAN_OK;
 }
 
+// As create, for operators whose kernels wait: scratch that begins with a zeroed error word.
+int create_waiting(Kind kind, void* stream, size_t scratch_bytes, dqgan_operator** out) {
+  const int r = create(kind, stream, scratch_bytes, out);
+  if (r != DQGAN_OK) return r;
+  dqgan_operator* op = *out;
+  cudaError_t st = cudaMemsetAsync(op->scratch, 0, 4, op->stream);
+  if (st == cudaSuccess) st = cudaStreamSynchronize(op->stream);
+  if (st != cudaSuccess) {
+    cudaFree(op->scratch);
+    cudaGetLastError();
+    delete op;
+    *out = nullptr;
+    return fail(nullptr, DQGAN_ERR_CUDA, "clearing scratch: %s", cudaGetErrorString(st));
+  }
+  op->waits = static_cast<uint32_t*>(op->scratch);
+  return DQGAN_OK;
+}
+
+int check_batch(int64_t max_rows, int32_t workers) {
+  if (max_rows < 1 || max_rows > kMaxTokens) return invalid(nullptr, "max_rows outside [1, 2^24]");
+  if (workers < 1 || workers > kMaxWorkers) return invalid(nullptr, "workers outside [1, 4096]");
+  if (workers * max_rows > kMaxBatch) return invalid(nullptr, "workers * max_rows above 2^28");
+  return DQGAN_OK;
+}
+
+int check_weight_dtype(int32_t dtype, int32_t weight_dtype) {
+  if (!known_dtype(dtype) || !known_dtype(weight_dtype)) return invalid(nullptr, "unknown dtype");
+  if (weight_dtype != dtype && weight_dtype != DQGAN_F32) return invalid(nullptr, "weight_dtype is neither dtype nor F32");
+  return DQGAN_OK;
+}
+
+dq::LinearShape shape(const dqgan_linear_config& c) {
+  return {c.inputs, c.outputs, c.max_rows, c.workers, c.dtype, c.weight_dtype, c.activation};
+}
+dq::TokenLossShape shape(const dqgan_token_loss_config& c) {
+  return {c.vocab, c.width, c.max_rows, c.workers, c.dtype, c.weight_dtype, c.token_bits};
+}
+dq::ClipShape shape(const dqgan_gradient_clip_config& c) { return {c.workers, c.dtype, c.out_dtype, c.eps}; }
+
 }  // namespace
 
 extern "C" {
@@ -149,6 +193,50 @@ int dqgan_distillation_create(const dqgan_distillation_config* cfg, dqgan_operat
   return st;
 }
 
+int dqgan_linear_create(const dqgan_linear_config* cfg, dqgan_operator** out) {
+  if (!out) return invalid(nullptr, "out is NULL");
+  *out = nullptr;
+  if (!cfg) return invalid(nullptr, "config is NULL");
+  if (cfg->inputs < 1 || cfg->inputs > kMaxWidth) return invalid(nullptr, "inputs outside [1, 65536]");
+  if (cfg->outputs < 1 || cfg->outputs > kMaxWidth) return invalid(nullptr, "outputs outside [1, 65536]");
+  if (int r = check_batch(cfg->max_rows, cfg->workers)) return r;
+  if (int r = check_weight_dtype(cfg->dtype, cfg->weight_dtype)) return r;
+  if (cfg->activation < DQGAN_NONE || cfg->activation > DQGAN_SILU) return invalid(nullptr, "unknown activation");
+  if (cfg->reserved[0] != 0 || cfg->reserved[1] != 0) return invalid(nullptr, "reserved is not 0");
+  const int st = create_waiting(Kind::kLinear, cfg->cuda_stream, dq::linear_scratch_bytes(shape(*cfg)), out);
+  if (st == DQGAN_OK) (*out)->linear = *cfg;
+  return st;
+}
+
+int dqgan_token_loss_create(const dqgan_token_loss_config* cfg, dqgan_operator** out) {
+  if (!out) return invalid(nullptr, "out is NULL");
+  *out = nullptr;
+  if (!cfg) return invalid(nullptr, "config is NULL");
+  if (cfg->vocab < 1 || cfg->vocab > kMaxVocab) return invalid(nullptr, "vocab outside [1, 2^24]");
+  if (cfg->width < 1 || cfg->width > kMaxWidth) return invalid(nullptr, "width outside [1, 65536]");
+  if (int r = check_batch(cfg->max_rows, cfg->workers)) return r;
+  if (int r = check_weight_dtype(cfg->dtype, cfg->weight_dtype)) return r;
+  if (cfg->token_bits != 32 && cfg->token_bits != 64) return invalid(nullptr, "token_bits not in {32, 64}");
+  if (cfg->reserved[0] != 0 || cfg->reserved[1] != 0) return invalid(nullptr, "reserved is not 0");
+  const int st = create_waiting(Kind::kTokenLoss, cfg->cuda_stream, dq::token_loss_scratch_bytes(shape(*cfg)), out);
+  if (st == DQGAN_OK) (*out)->token_loss = *cfg;
+  return st;
+}
+
+int dqgan_gradient_clip_create(const dqgan_gradient_clip_config* cfg, dqgan_operator** out) {
+  if (!out) return invalid(nullptr, "out is NULL");
+  *out = nullptr;
+  if (!cfg) return invalid(nullptr, "config is NULL");
+  if (cfg->workers < 1 || cfg->workers > kMaxWorkers) return invalid(nullptr, "workers outside [1, 4096]");
+  if (!known_dtype(cfg->dtype) || !known_dtype(cfg->out_dtype)) return invalid(nullptr, "unknown dtype");
+  if (cfg->out_dtype != cfg->dtype && cfg->out_dtype != DQGAN_F32) return invalid(nullptr, "out_dtype is neither dtype nor F32");
+  if (!std::isfinite(cfg->eps) || cfg->eps < 0.f) return invalid(nullptr, "eps is negative or not finite");
+  if (cfg->reserved[0] != 0 || cfg->reserved[1] != 0) return invalid(nullptr, "reserved is not 0");
+  const int st = create(Kind::kGradientClip, cfg->cuda_stream, dq::clip_scratch_bytes(shape(*cfg)), out);
+  if (st == DQGAN_OK) (*out)->clip = *cfg;
+  return st;
+}
+
 int dqgan_operator_destroy(dqgan_operator* op) {
   if (!op) return DQGAN_OK;
   cudaStreamSynchronize(op->stream);
@@ -163,6 +251,14 @@ int dqgan_operator_synchronize(dqgan_operator* op) {
   if (!op) return invalid(nullptr, "operator is NULL");
   const cudaError_t st = cudaStreamSynchronize(op->stream);
   if (st != cudaSuccess) return fail(op, DQGAN_ERR_CUDA, "synchronize: %s", cudaGetErrorString(st));
+  if (op->waits) {
+    uint32_t word = 0;
+    cudaError_t read = cudaMemcpyAsync(&word, op->waits, 4, cudaMemcpyDeviceToHost, op->stream);
+    if (read == cudaSuccess) read = cudaStreamSynchronize(op->stream);
+    if (read == cudaSuccess && word) read = cudaMemsetAsync(op->waits, 0, 4, op->stream);
+    if (read != cudaSuccess) return fail(op, DQGAN_ERR_CUDA, "synchronize: %s", cudaGetErrorString(read));
+    if (word) return fail(op, DQGAN_ERR_TIMEOUT, "a wait on the device gave up: what was computed since the last synchronize is not valid");
+  }
   return DQGAN_OK;
 }
 
@@ -385,6 +481,219 @@ int dqgan_distillation_step(dqgan_operator* op, int64_t rows, const void* logits
                             int64_t dlogits_stride) {
   return distillation(op, dq::DistillationWay::kStep, rows, logits, logits_stride, ids, values, teacher_stride,
                       teacher_lse, weights, scale, loss, lse, dlogits, dlogits_stride);
+}
+
+}  // extern "C"
+
+extern "C" {
+
+int dqgan_linear_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride, const void* weight,
+                         int64_t p_stride, const float* bias, int64_t b_stride, const void* residual,
+                         int64_t residual_stride, void* y, int64_t y_stride, void* pre, int64_t pre_stride) {
+  if (int r = check(op, Kind::kLinear, "a linear layer")) return r;
+  const dqgan_linear_config& c = op->linear;
+  if (rows < 0 || rows > c.max_rows) return invalid(op, "rows outside [0, max_rows]");
+  if (rows == 0) return DQGAN_OK;
+  if (!x || !weight || !y) return invalid(op, "NULL x, weight or y");
+  if (!stride_ok(x_stride, c.inputs) || !stride_ok(y_stride, c.outputs) ||
+      (residual && !stride_ok(residual_stride, c.outputs)) || (pre && !stride_ok(pre_stride, c.outputs)))
+    return invalid(op, "a row stride is below the width");
+  if (p_stride != 0 && !stride_ok(p_stride, c.inputs * c.outputs))
+    return invalid(op, "p_stride is neither 0 nor at least inputs * outputs");
+  if (bias && b_stride != 0 && !stride_ok(b_stride, c.outputs)) return invalid(op, "b_stride is neither 0 nor at least the outputs");
+  const uintptr_t size = dtype_size(c.dtype);
+  if (!aligned(x, size) || !aligned(weight, dtype_size(c.weight_dtype)) || !aligned(bias, 4) || !aligned(residual, size) ||
+      !aligned(y, size) || !aligned(pre, size))
+    return invalid(op, "a pointer is not aligned to its element");
+  NvtxRange range("dqgan linear forward");
+  dq::LinearArgs a{};
+  a.shape = shape(c);
+  a.x = x;
+  a.x_ld = x_stride;
+  a.weight = weight;
+  a.p_stride = p_stride;
+  a.bias = bias;
+  a.b_stride = b_stride;
+  a.residual = residual;
+  a.residual_ld = residual_stride;
+  a.y = y;
+  a.y_ld = y_stride;
+  a.pre_out = pre;
+  a.pre_ld = pre_stride;
+  a.rows = rows;
+  a.scratch = op->scratch;
+  return launched(op, dq::launch_linear_forward(a, op->stream, &op->launches), "linear forward");
+}
+
+int dqgan_linear_backward(dqgan_operator* op, int64_t rows, const void* dy, int64_t dy_stride, const void* x,
+                          int64_t x_stride, const void* weight, int64_t p_stride, const void* pre, int64_t pre_stride,
+                          void* dx, int64_t dx_stride, float* dweight, float* dbias, int64_t g_stride,
+                          int32_t accumulate) {
+  if (int r = check(op, Kind::kLinear, "a linear layer")) return r;
+  const dqgan_linear_config& c = op->linear;
+  if (rows < 0 || rows > c.max_rows) return invalid(op, "rows outside [0, max_rows]");
+  if (!dx && !dweight && !dbias) return DQGAN_OK;
+  const bool slope = c.activation != DQGAN_NONE;
+  if (rows > 0) {
+    if (!dy || (dweight && !x) || (dx && !weight) || (slope && !pre)) return invalid(op, "NULL dy, x, weight or pre");
+    if (!stride_ok(dy_stride, c.outputs) || (dweight && !stride_ok(x_stride, c.inputs)) ||
+        (dx && !stride_ok(dx_stride, c.inputs)) || (slope && !stride_ok(pre_stride, c.outputs)))
+      return invalid(op, "a row stride is below the width");
+  }
+  if (p_stride != 0 && !stride_ok(p_stride, c.inputs * c.outputs))
+    return invalid(op, "p_stride is neither 0 nor at least inputs * outputs");
+  if (c.workers > 1 && ((dweight && !stride_ok(g_stride, c.inputs * c.outputs)) || (dbias && !stride_ok(g_stride, c.outputs))))
+    return invalid(op, "g_stride is below the parameters");
+  const uintptr_t size = dtype_size(c.dtype);
+  if (!aligned(dy, size) || !aligned(x, size) || !aligned(weight, dtype_size(c.weight_dtype)) || !aligned(pre, size) ||
+      !aligned(dx, size) || !aligned(dweight, 4) || !aligned(dbias, 4))
+    return invalid(op, "a pointer is not aligned to its element");
+  NvtxRange range("dqgan linear backward");
+  dq::LinearArgs a{};
+  a.shape = shape(c);
+  a.dy = dy;
+  a.dy_ld = dy_stride;
+  a.x = x;
+  a.x_ld = x_stride;
+  a.weight = weight;
+  a.p_stride = p_stride;
+  a.pre = pre;
+  a.pre_ld = pre_stride;
+  a.dx = dx;
+  a.dx_ld = dx_stride;
+  a.dweight = dweight;
+  a.dbias = dbias;
+  a.g_stride = c.workers > 1 ? g_stride : 0;
+  a.accumulate = accumulate != 0;
+  a.rows = rows;
+  a.scratch = op->scratch;
+  return launched(op, dq::launch_linear_backward(a, op->stream, &op->launches), "linear backward");
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the three token-loss calls share.
+int token_loss(dqgan_operator* op, bool forward, bool backward, int64_t rows, const void* x, int64_t x_stride,
+               const void* weight, int64_t p_stride, const void* targets, const float* weights, float scale,
+               float* loss, float* lse, void* dx, int64_t dx_stride, float* dweight, int64_t g_stride,
+               int32_t accumulate) {
+  if (int r = check(op, Kind::kTokenLoss, "a token loss")) return r;
+  const dqgan_token_loss_config& c = op->token_loss;
+  if (rows < 0 || rows > c.max_rows) return invalid(op, "rows outside [0, max_rows]");
+  if (!forward && !dx && !dweight) return DQGAN_OK;
+  if (rows > 0) {
+    if (!x || !weight || !targets) return invalid(op, "NULL x, weight or targets");
+    if (forward && !loss) return invalid(op, "NULL loss");
+    if (!forward && !lse) return invalid(op, "NULL lse");
+    if (!stride_ok(x_stride, c.width) || (dx && !stride_ok(dx_stride, c.width)))
+      return invalid(op, "a row stride is below the width");
+  }
+  if (p_stride != 0 && !stride_ok(p_stride, c.vocab * c.width))
+    return invalid(op, "p_stride is neither 0 nor at least vocab * width");
+  if (dweight && c.workers > 1 && !stride_ok(g_stride, c.vocab * c.width)) return invalid(op, "g_stride is below vocab * width");
+  if (!std::isfinite(scale)) return invalid(op, "scale is not finite");
+  const uintptr_t size = dtype_size(c.dtype);
+  if (!aligned(x, size) || !aligned(weight, dtype_size(c.weight_dtype)) || !aligned(targets, c.token_bits / 8) ||
+      !aligned(weights, 4) || !aligned(loss, 4) || !aligned(lse, 4) || !aligned(dx, size) || !aligned(dweight, 4))
+    return invalid(op, "a pointer is not aligned to its element");
+  NvtxRange range(!backward ? "dqgan token loss forward" : forward ? "dqgan token loss step" : "dqgan token loss backward");
+  dq::TokenLossArgs a{};
+  a.shape = shape(c);
+  a.x = x;
+  a.x_ld = x_stride;
+  a.weight = weight;
+  a.p_stride = p_stride;
+  a.targets = targets;
+  a.weights = weights;
+  a.loss = loss;
+  a.lse = lse;
+  a.scale = scale;
+  a.dx = dx;
+  a.dx_ld = dx_stride;
+  a.dweight = dweight;
+  a.g_stride = c.workers > 1 ? g_stride : 0;
+  a.accumulate = accumulate != 0;
+  a.forward = forward;
+  a.backward = backward;
+  a.rows = rows;
+  a.scratch = op->scratch;
+  return launched(op, dq::launch_token_loss(a, op->stream, &op->launches), "token loss");
+}
+
+// A list of tensors on its own.
+int check_tensors(dqgan_operator* op, int64_t count, const dqgan_tensor* t, int32_t dtype, const char* what) {
+  for (int64_t i = 0; i < count; ++i) {
+    if (t[i].size < 0 || t[i].size > kMaxStride)
+      return fail(op, DQGAN_ERR_INVALID_ARG, "%s %lld: size outside [0, 2^40]", what, (long long)i);
+    if (t[i].size == 0) continue;
+    if (!t[i].data) return fail(op, DQGAN_ERR_INVALID_ARG, "%s %lld: NULL", what, (long long)i);
+    if (!aligned(t[i].data, dtype_size(dtype)))
+      return fail(op, DQGAN_ERR_INVALID_ARG, "%s %lld: not aligned to its element", what, (long long)i);
+    if (op->clip.workers > 1 && !stride_ok(t[i].stride, t[i].size))
+      return fail(op, DQGAN_ERR_INVALID_ARG, "%s %lld: stride below the size", what, (long long)i);
+  }
+  return DQGAN_OK;
+}
+
+int check_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* from) {
+  if (int r = check(op, Kind::kGradientClip, "a gradient clipping")) return r;
+  if (count < 0 || count > kMaxTensors) return invalid(op, "count outside [0, 4096]");
+  if (count > 0 && !from) return invalid(op, "NULL tensors");
+  return check_tensors(op, count, from, op->clip.dtype, "tensor");
+}
+
+}  // namespace
+
+extern "C" {
+
+int dqgan_token_loss_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride, const void* weight,
+                             int64_t p_stride, const void* targets, const float* weights, float* loss, float* lse) {
+  return token_loss(op, true, false, rows, x, x_stride, weight, p_stride, targets, weights, 0.f, loss, lse, nullptr, 0,
+                    nullptr, 0, 0);
+}
+
+int dqgan_token_loss_backward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride, const void* weight,
+                              int64_t p_stride, const void* targets, const float* weights, const float* lse, float scale,
+                              void* dx, int64_t dx_stride, float* dweight, int64_t g_stride, int32_t accumulate) {
+  return token_loss(op, false, true, rows, x, x_stride, weight, p_stride, targets, weights, scale, nullptr,
+                    const_cast<float*>(lse), dx, dx_stride, dweight, g_stride, accumulate);
+}
+
+int dqgan_token_loss_step(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride, const void* weight,
+                          int64_t p_stride, const void* targets, const float* weights, float scale, float* loss,
+                          float* lse, void* dx, int64_t dx_stride, float* dweight, int64_t g_stride,
+                          int32_t accumulate) {
+  return token_loss(op, true, true, rows, x, x_stride, weight, p_stride, targets, weights, scale, loss, lse, dx,
+                    dx_stride, dweight, g_stride, accumulate);
+}
+
+int dqgan_gradient_norm(dqgan_operator* op, int64_t count, const dqgan_tensor* tensors, float* norms) {
+  if (int r = check_clip(op, count, tensors)) return r;
+  if (!norms) return invalid(op, "NULL norms");
+  if (!aligned(norms, 4)) return invalid(op, "a pointer is not aligned to its element");
+  NvtxRange range("dqgan gradient norm");
+  return launched(op, dq::launch_gradient_clip(shape(op->clip), count, tensors, nullptr, 0.f, norms, op->scratch, op->stream,
+                                               &op->launches), "gradient norm");
+}
+
+int dqgan_gradient_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* tensors, const dqgan_tensor* places,
+                        float max_norm, float* norms) {
+  if (int r = check_clip(op, count, tensors)) return r;
+  if (count > 0 && !places) return invalid(op, "NULL places");
+  if (int r = check_tensors(op, count, places, op->clip.out_dtype, "place")) return r;
+  for (int64_t i = 0; i < count; ++i) {
+    if (places[i].size != tensors[i].size) return fail(op, DQGAN_ERR_INVALID_ARG, "place %lld: not the tensor's size", (long long)i);
+    if (places[i].size > 0 && places[i].data == tensors[i].data &&
+        (op->clip.dtype != op->clip.out_dtype || (op->clip.workers > 1 && places[i].stride != tensors[i].stride)))
+      return fail(op, DQGAN_ERR_INVALID_ARG, "place %lld: the tensor itself in another type or stride", (long long)i);
+  }
+  if (!(max_norm >= 0.f)) return invalid(op, "max_norm is negative or NaN");
+  if (!aligned(norms, 4)) return invalid(op, "a pointer is not aligned to its element");
+  NvtxRange range("dqgan gradient clip");
+  return launched(op, dq::launch_gradient_clip(shape(op->clip), count, tensors, places, max_norm, norms, op->scratch,
+                                               op->stream, &op->launches), "gradient clip");
 }
 
 }  // extern "C"

@@ -77,6 +77,74 @@ struct DistillationArgs {
 
 enum class DistillationWay { kForward, kBackward, kStep };
 
+struct LinearShape {
+  int64_t inputs, outputs, max_rows;
+  int32_t workers;
+  int32_t dtype, weight_dtype;
+  int32_t activation;
+};
+
+struct LinearArgs {
+  LinearShape shape;
+  const void* x;         // worker m's row r at x + (m * rows + r) * x_ld
+  int64_t x_ld;
+  const void* weight;    // worker m's at + m * p_stride elements, outputs x inputs
+  int64_t p_stride;
+  const float* bias;     // forward; worker m's at + m * b_stride, or nullptr
+  int64_t b_stride;
+  const void* residual;  // forward; or nullptr
+  int64_t residual_ld;
+  void* y;               // forward
+  int64_t y_ld;
+  void* pre_out;         // forward; u, or nullptr
+  const void* pre;       // backward; u, unless the activation is none
+  int64_t pre_ld;
+  const void* dy;        // backward
+  int64_t dy_ld;
+  void* dx;              // backward; or nullptr
+  int64_t dx_ld;
+  float* dweight;        // backward; worker m's at + m * g_stride, or nullptr
+  float* dbias;
+  int64_t g_stride;
+  int32_t accumulate;
+  int64_t rows;          // per worker
+  void* scratch;         // linear_scratch_bytes
+};
+
+struct TokenLossShape {
+  int64_t vocab, width, max_rows;
+  int32_t workers;
+  int32_t dtype, weight_dtype;
+  int32_t token_bits;
+};
+
+struct TokenLossArgs {
+  TokenLossShape shape;
+  const void* x;         // worker m's row r at x + (m * rows + r) * x_ld
+  int64_t x_ld;
+  const void* weight;    // worker m's at + m * p_stride elements, vocab x width
+  int64_t p_stride;
+  const void* targets;   // one a row
+  const float* weights;  // or nullptr
+  float* loss;           // forward and step
+  float* lse;            // forward and step: written, or nullptr; backward: read
+  float scale;
+  void* dx;              // backward and step; or nullptr
+  int64_t dx_ld;
+  float* dweight;        // backward and step; worker m's at + m * g_stride, or nullptr
+  int64_t g_stride;
+  int32_t accumulate;
+  bool forward, backward;
+  int64_t rows;          // per worker
+  void* scratch;         // token_loss_scratch_bytes
+};
+
+struct ClipShape {
+  int32_t workers;
+  int32_t dtype, out_dtype;
+  float eps;
+};
+
 size_t layer_norm_scratch_bytes(int64_t width, int32_t workers);
 cudaError_t launch_layer_norm_forward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches);
 cudaError_t launch_layer_norm_backward(const LayerNormArgs& a, cudaStream_t stream, uint64_t* launches);
@@ -88,7 +156,20 @@ cudaError_t launch_embedding_backward(const EmbeddingArgs& a, cudaStream_t strea
 cudaError_t launch_distillation(const DistillationArgs& a, DistillationWay way, cudaStream_t stream,
                                 uint64_t* launches);
 
+size_t linear_scratch_bytes(const LinearShape& s);
+cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint64_t* launches);
+cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uint64_t* launches);
+
+size_t token_loss_scratch_bytes(const TokenLossShape& s);
+cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint64_t* launches);
+
+size_t clip_scratch_bytes(const ClipShape& s);
+// to: the tensors' places, or nullptr (norms alone).
+cudaError_t launch_gradient_clip(const ClipShape& s, int64_t count, const dqgan_tensor* from, const dqgan_tensor* to,
+                                 float max_norm, float* norms, void* scratch, cudaStream_t stream, uint64_t* launches);
+
 __host__ __device__ constexpr int64_t ceil_div(int64_t x, int64_t m) { return (x + m - 1) / m; }
+__host__ __device__ constexpr int64_t round8(int64_t n) { return ceil_div(n, 8) * 8; }
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }

@@ -1,0 +1,307 @@
+// The kernel of the matrix products: tcgen05 with both operands brought to
+// shared memory by TMA and the sums in tensor memory.
+//
+// One block an SM walks over tiles of 128 x BN results.  One warp's thread
+// loads blocks of 64 of the contracted index into a ring of stages, another's
+// multiplies them, and eight warps take the sums out of tensor memory, two
+// accumulators in turn, so that an epilogue runs beside the next tile's
+// products.
+//
+// The tensor cores' own sums are rounded towards zero, by up to one unit in the
+// last place each 16 products: over thousands of them the error grows past that
+// of fp32 sums.  So an accumulator takes `chunk` blocks only; the eight warps
+// add it to sums in registers (128 a thread), rounded to nearest, while the
+// other accumulator fills.
+#pragma once
+
+#include "device_common.cuh"
+#include "products.cuh"
+
+namespace dq {
+
+constexpr int kProductThreads = 384;  // 4 warps that load and multiply, 8 that take the sums
+constexpr int kTileRows = 128;
+constexpr int kBlockDepth = 64;       // 128 bytes: a row of the 128-byte swizzle
+constexpr int kStageRow = 33;         // floats: rows of the transposing buffers
+
+template <int BN>
+struct ProductShape {
+  static constexpr int kABytes = kTileRows * kBlockDepth * 2;
+  static constexpr int kBBytes = BN * kBlockDepth * 2;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+  static constexpr int kTurnBytes = 8 * 32 * kStageRow * 4;
+  // stages, transposing buffers, barriers; and what it takes to start on a boundary of 1024 bytes
+  static constexpr int kSmem = kStages * kStageBytes + kTurnBytes + 256 + 1024;
+};
+
+// ---- tcgen05 ----
+__device__ __forceinline__ void tensor_memory_allocate(uint32_t* to, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tensor_memory_free(uint32_t at, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+__device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+               : "memory");
+}
+__device__ __forceinline__ void tensor_multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+      : "memory");
+}
+// 32 columns of this warp's 32 lanes: lane l gets row l.
+__device__ __forceinline__ void tensor_load32(uint32_t at, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(at));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d(void* dst_smem, const void* tmap, int32_t x, int32_t y, int32_t z, int32_t w,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_addr(dst_smem)),
+      "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
+      : "memory");
+}
+
+// Shared-memory descriptor of an operand's 16 (contracted) x 64... slice with the 128-byte swizzle.  Rows along the
+// contracted index: 8 rows are 1024 bytes apart from the next 8.  Rows across it: 8 of the contracted index are 1024
+// bytes apart from the next 8, and 64 of the other index 64 * 128 bytes from the next 64.
+__device__ __forceinline__ uint64_t operand_descriptor(uint32_t at, bool across) {
+  const uint64_t lead = across ? (kBlockDepth * 128) >> 4 : 1;
+  return (uint64_t)((at & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+struct ProductTile {
+  int worker, split;
+  int64_t row, column;  // of the tile's first result
+  int begin, end;       // blocks of the contracted index
+};
+
+template <int BN>
+__device__ __forceinline__ ProductTile product_tile(const ProductArgs& p, int64_t t) {
+  ProductTile tile;
+  const int per_split = p.tiles_m * p.tiles_n;
+  const int64_t which = t / per_split;
+  const int in = (int)(t - which * per_split);
+  tile.split = (int)(which % p.splits);
+  tile.worker = (int)(which / p.splits);
+  // eight rows of tiles at a time: what runs at once shares operands in L2
+  constexpr int kGroup = 8;
+  const int group = in / (kGroup * p.tiles_n), left = in - group * kGroup * p.tiles_n;
+  const int high = p.tiles_m - group * kGroup < kGroup ? p.tiles_m - group * kGroup : kGroup;
+  tile.row = (int64_t)(group * kGroup + left % high) * kTileRows;
+  tile.column = (int64_t)(left / high) * BN;
+  tile.begin = (int)((int64_t)p.kblocks * tile.split / p.splits);
+  tile.end = (int)((int64_t)p.kblocks * (tile.split + 1) / p.splits);
+  return tile;
+}
+
+// The sums of one warp: row `row` of this lane, columns [column, column + BN / 2).
+template <int BN, typename Epilogue>
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductArgs p) {
+  dq_pdl_enter();
+  using S = ProductShape<BN>;
+  extern __shared__ __align__(1024) uint8_t raw[];
+  uint8_t* const smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+  float* const turn = reinterpret_cast<float*>(smem + S::kStages * S::kStageBytes);
+  uint64_t* const full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStageBytes + S::kTurnBytes);
+  uint64_t* const empty = full + S::kStages;
+  uint64_t* const sum_full = empty + S::kStages;
+  uint64_t* const sum_empty = sum_full + 2;
+  uint32_t* const at_shared = reinterpret_cast<uint32_t*>(sum_empty + 2);
+  static_assert((2 * S::kStages + 4) * 8 + 4 <= 256, "barriers");
+  constexpr uint32_t kColumns = 2 * BN;
+
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(sum_full + s, 1);
+      mbar_init(sum_empty + s, 8);
+    }
+    mbar_fence_init();
+  }
+  if (warp == 2) tensor_memory_allocate(at_shared, kColumns);
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  const uint32_t sums = *at_shared;
+
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
+  const int terms = p.terms.count;
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == 0 && lane == 0) {
+      uint32_t n = 0;  // stages filled so far
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        const ProductTile tile = product_tile<BN>(p, t);
+        const int wa = p.a_shared ? 0 : tile.worker, wb = p.b_shared ? 0 : tile.worker;
+        for (int k = tile.begin; ok && k < tile.end; ++k)
+          for (int term = 0; term < terms; ++term, ++n) {
+            const int s = n % S::kStages;
+            if (!(ok = mbar_wait_bounded(empty + s, (n / S::kStages & 1) ^ 1, p.err))) break;
+            mbar_arrive_expect_tx(full + s, S::kStageBytes);
+            uint8_t* const a = smem + s * S::kStageBytes;
+            uint8_t* const b = a + S::kABytes;
+            const int pa = p.terms.a[term], pb = p.terms.b[term];
+            if (p.a_across)
+              for (int i = 0; i < kTileRows / 64; ++i)
+                tma_load_4d(a + i * 8192, &p.a, (int)tile.row + 64 * i, k * kBlockDepth, wa, pa, full + s);
+            else
+              tma_load_4d(a, &p.a, k * kBlockDepth, (int)tile.row, wa, pa, full + s);
+            if (p.b_across)
+              for (int i = 0; i < BN / 64; ++i)
+                tma_load_4d(b + i * 8192, &p.b, (int)tile.column + 64 * i, k * kBlockDepth, wb, pb, full + s);
+            else
+              tma_load_4d(b, &p.b, k * kBlockDepth, (int)tile.column, wb, pb, full + s);
+          }
+      }
+      // what is still on its way into shared memory arrives before the block ends
+      for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
+        mbar_wait_bounded(full + i % S::kStages, i / S::kStages & 1, p.err);
+    } else if (warp == 1 && lane == 0) {
+      // D in fp32 | type and direction of A and B | N / 8 | M / 16
+      const uint32_t kind = 1u << 4 | (p.half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)p.a_across << 15 |
+                            (uint32_t)p.b_across << 16 | (uint32_t)(BN / 8) << 17 | (uint32_t)(kTileRows / 16) << 24;
+      const uint64_t da = operand_descriptor(smem_addr(smem), p.a_across);
+      const uint64_t db = operand_descriptor(smem_addr(smem + S::kABytes), p.b_across);
+      const uint32_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
+      uint32_t n = 0, c = 0;  // stages used, accumulators filled
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        const ProductTile tile = product_tile<BN>(p, t);
+        const int total = (tile.end - tile.begin) * terms;
+        for (int done = 0; ok && done < total; done += p.chunk, ++c) {
+          const uint32_t d = sums + (c & 1) * BN;
+          if (!(ok = mbar_wait_bounded(sum_empty + (c & 1), (c / 2 & 1) ^ 1, p.err))) break;
+          tensor_fence_after();
+          const int count = total - done < p.chunk ? total - done : p.chunk;
+          for (int i = 0; i < count; ++i, ++n) {
+            const uint32_t s = n % S::kStages;
+            if (!(ok = mbar_wait_bounded(full + s, n / S::kStages & 1, p.err))) break;
+            tensor_fence_after();
+            const uint64_t at = (uint64_t)(s * (S::kStageBytes >> 4));
+#pragma unroll
+            for (int k = 0; k < kBlockDepth / 16; ++k)
+              tensor_multiply(d, da + at + k * step_a, db + at + k * step_b, kind, i > 0 || k > 0);
+            tensor_commit(empty + s);
+          }
+          if (ok) tensor_commit(sum_full + (c & 1));
+        }
+      }
+      // the products end before the block does
+      for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
+        mbar_wait_bounded(empty + i % S::kStages, i / S::kStages & 1, p.err);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int sub = warp & 3, half = (warp - 4) / 4;
+    float* const buffer = turn + (warp - 4) * 32 * kStageRow;
+    uint32_t c = 0;
+    bool ok = true;
+    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      const ProductTile tile = product_tile<BN>(p, t);
+      const int total = (tile.end - tile.begin) * terms;
+      float v[BN / 2];
+#pragma unroll
+      for (int i = 0; i < BN / 2; ++i) v[i] = 0.f;
+      for (int done = 0; done < total; done += p.chunk, ++c) {
+        if (!(ok = mbar_wait_bounded(sum_full + (c & 1), c / 2 & 1, p.err))) break;
+        tensor_fence_after();
+        const uint32_t from = sums + ((uint32_t)(32 * sub) << 16) + (c & 1) * BN + half * (BN / 2);
+#pragma unroll
+        for (int i = 0; i < BN / 2; i += 32) {
+          uint32_t x[32];
+          tensor_load32(from + i, x);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[i + j] = __fadd_rn(v[i + j], __uint_as_float(x[j]));
+        }
+        tensor_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sum_empty + (c & 1));
+      }
+      if (ok) Epilogue::template run<BN>(p, tile, tile.row + 32 * sub, tile.column + half * (BN / 2), v, buffer, lane);
+    }
+  }
+  tensor_fence_before();
+  __syncthreads();
+  tensor_fence_after();
+  if (warp == 2) tensor_memory_free(sums, kColumns);
+}
+
+// Host: the tensor map of an operand.  `box`: rows of the tile along the operand's own index.
+inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth, int32_t workers, int box, CUtensorMap* out) {
+  const TensorMapEncoder encode = tensor_map_encoder();
+  if (!encode) return false;
+  const int batches = o.shared ? 1 : workers;
+  const auto stride = [&](int64_t s, int count) { return (cuuint64_t)(count > 1 ? s : o.ld) * 2; };
+  const cuuint64_t dims[4] = {(cuuint64_t)(o.across ? rows : depth), (cuuint64_t)(o.across ? depth : rows),
+                              (cuuint64_t)batches, (cuuint64_t)o.parts};
+  const cuuint64_t strides[3] = {(cuuint64_t)o.ld * 2, stride(o.batch, batches), stride(o.part, o.parts)};
+  const cuuint32_t boxes[4] = {64u, (cuuint32_t)(o.across ? kBlockDepth : box), 1u, 1u};
+  const cuuint32_t steps[4] = {1u, 1u, 1u, 1u};
+  return encode(out, o.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                const_cast<void*>(o.data), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Fills what the kernel needs of a product; false where its sizes are beyond the kernel's.
+template <int BN>
+inline bool product_args(const Product& p, uint32_t* err, ProductArgs* out) {
+  out->rows = p.rows;
+  out->columns = p.columns;
+  out->workers = p.workers;
+  out->kblocks = (int32_t)ceil_div(p.depth, kBlockDepth);
+  out->chunk = 8;
+  out->splits = 1;
+  out->tiles_m = (int32_t)ceil_div(p.rows, kTileRows);
+  out->tiles_n = (int32_t)ceil_div(p.columns, BN);
+  out->terms = p.terms;
+  out->a_across = p.a.across;
+  out->b_across = p.b.across;
+  out->a_shared = p.a.shared;
+  out->b_shared = p.b.shared;
+  out->half = p.a.half;
+  out->err = err;
+  return p.rows <= INT32_MAX && p.columns <= INT32_MAX && p.depth <= INT32_MAX &&
+         (int64_t)out->tiles_m * out->tiles_n <= INT32_MAX &&
+         encode_operand(p.a, p.rows, p.depth, p.workers, kTileRows, &out->a) &&
+         encode_operand(p.b, p.columns, p.depth, p.workers, BN, &out->b);
+}
+
+template <int BN, typename Epilogue>
+inline cudaError_t launch_product(const ProductArgs& p, cudaStream_t stream, uint64_t* launches) {
+  static std::atomic<int> kept[kKeptDevices];
+  int ctas = 0;
+  const cudaError_t st = resident_ctas(product_kernel<BN, Epilogue>, kProductThreads, ProductShape<BN>::kSmem,
+                                       ProductShape<BN>::kSmem, kept, &ctas);
+  if (st != cudaSuccess) return st;
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
+  const int grid = (int)(tiles < ctas ? tiles : ctas);
+  ++*launches;
+  return launch_pdl(product_kernel<BN, Epilogue>, dim3(grid), dim3(kProductThreads), ProductShape<BN>::kSmem, stream, p);
+}
+
+}  // namespace dq

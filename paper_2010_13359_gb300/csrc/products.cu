@@ -1,0 +1,201 @@
+// Matrix products that are stored: with bias, activation, residual, or added to
+// what is there; and the splitting of operands into 16-bit parts.
+#include "product_kernel.cuh"
+
+namespace dq {
+
+ProductTerms product_terms(int a_parts, int b_parts) {
+  ProductTerms t;
+  t.count = 0;
+  const int parts = a_parts > b_parts ? a_parts : b_parts;
+  for (int order = parts - 1; order >= 0; --order)  // the smallest first
+    for (int i = 0; i <= order; ++i)
+      if (i < a_parts && order - i < b_parts) {
+        t.a[t.count] = (uint8_t)i;
+        t.b[t.count++] = (uint8_t)(order - i);
+      }
+  return t;
+}
+
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void store_value(const StoreArgs& s, int worker, int64_t row, int64_t column, float x, float bias) {
+  if (s.add) x += s.add[worker * s.add_batch + row * s.add_ld + column];
+  x += bias;
+  if (s.pre) static_cast<T*>(s.pre)[worker * s.pre_batch + row * s.pre_ld + column] = from_float<T>(x);
+  x = activate(x, s.activation);
+  if (s.residual)
+    x += to_float(static_cast<const T*>(s.residual)[worker * s.residual_batch + row * s.residual_ld + column]);
+  static_cast<T*>(s.out)[worker * s.out_batch + row * s.out_ld + column] = from_float<T>(x);
+}
+
+// A warp's 32 rows, turned in shared memory so that its lanes hold neighbouring columns.
+template <typename T>
+struct StoreEpilogue {
+  template <int BN>
+  static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
+                                             float (&v)[BN / 2], float* buffer, int lane) {
+    const StoreArgs& s = p.store;
+    const int rows = (int)min64(32, p.rows - row);
+#pragma unroll
+    for (int g = 0; g < BN / 2; g += 32) {
+      if (column + g >= p.columns || rows <= 0) break;
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) buffer[lane * kStageRow + j] = v[g + j];
+      __syncwarp();
+      const int64_t j = column + g + lane;
+      if (j < p.columns) {
+        const float bias = s.bias ? s.bias[tile.worker * s.bias_batch + j] : 0.f;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j, buffer[r * kStageRow + lane], bias);
+      }
+    }
+  }
+};
+
+// Sums of one piece of the contracted index, for join_kernel.
+struct PartialEpilogue {
+  template <int BN>
+  static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
+                                             float (&v)[BN / 2], float* buffer, int lane) {
+    const int64_t ld = (int64_t)p.tiles_n * BN;
+    float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * kTileRows + row + lane) * ld + column;
+    if (row + lane < p.rows) {
+#pragma unroll
+      for (int j = 0; j < BN / 2; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    }
+  }
+};
+
+// The pieces' sums in order, and what is done with them.
+template <typename T, int BN>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p) {
+  dq_pdl_enter();
+  const int64_t ld = (int64_t)p.tiles_n * BN, tall = (int64_t)p.tiles_m * kTileRows;
+  const int64_t column = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (column >= p.columns) return;
+  for (int64_t r = blockIdx.y; r < p.rows * p.workers; r += gridDim.y) {
+    const int worker = (int)(r / p.rows);
+    const int64_t row = r - worker * p.rows;
+    const float* from = p.partial + (worker * tall + row) * ld + column;
+    float x = 0.f;
+    for (int s = 0; s < p.splits; ++s, from += p.workers * tall * ld) x += *from;
+    store_value<T>(p.store, worker, row, column, x,
+                   p.store.bias ? p.store.bias[worker * p.store.bias_batch + column] : 0.f);
+  }
+}
+
+template <int BN>
+cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, void* scratch, uint32_t* err,
+                          cudaStream_t stream, uint64_t* launches) {
+  ProductArgs args{};
+  if (!product_args<BN>(p, err, &args)) return cudaErrorInvalidValue;
+  args.store = store;
+  args.splits = splits;
+  if (splits == 1)
+    return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });
+  args.partial = static_cast<float*>(scratch);
+  const cudaError_t st = launch_product<BN, PartialEpilogue>(args, stream, launches);
+  if (st != cudaSuccess) return st;
+  ++*launches;
+  const dim3 grid((unsigned)ceil_div(p.columns, 256), (unsigned)min64(p.rows * p.workers, 65535));
+  return with_dtype(store.out_dtype, [&](auto t) {
+    return launch_pdl(join_kernel<decltype(t), BN>, grid, dim3(256), 0, stream, args);
+  });
+}
+
+}  // namespace
+
+cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void* scratch, uint32_t* err,
+                                 cudaStream_t stream, uint64_t* launches) {
+  if (p.rows == 0 || p.columns == 0) return cudaSuccess;
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  const int64_t wide = ceil_div(p.rows, kTileRows) * ceil_div(p.columns, 256) * p.workers;
+  if (wide >= sms / 2) return store_product<256>(p, store, 1, scratch, err, stream, launches);
+  // Few tiles: narrow ones, and the contracted index in pieces of at least 8 blocks.
+  const int64_t tiles = ceil_div(p.rows, kTileRows) * ceil_div(p.columns, 64) * p.workers;
+  int64_t splits = scratch ? min64(sms / tiles, ceil_div(p.depth, kBlockDepth) * p.terms.count / 8) : 1;
+  while (splits > 1 && (size_t)(splits * tiles) * kTileRows * 64 * 4 > kProductScratch) --splits;
+  splits = min64(splits, ceil_div(p.depth, kBlockDepth));
+  return store_product<64>(p, store, splits < 1 ? 1 : (int)splits, scratch, err, stream, launches);
+}
+
+// ---- parts ----
+namespace {
+
+template <typename T>
+__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, bool packs) {
+  dq_pdl_enter();
+  const int64_t across = a.ld / 8, total = across * a.rows * a.workers;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t r = i / across;
+    const int column = (int)(i - r * across) * 8;
+    const int64_t worker = r / a.rows, row = r - worker * a.rows;
+    float x[8] = {};
+    bool counts = true;
+    if (a.targets) {
+      const int64_t t = token_at(a.targets, a.token_bits, r);
+      counts = t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
+    }
+    if (counts) read8(static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column, (int)min64(8, a.columns - column), packs, x);
+    write_parts(x, a.to, r * a.ld + column, a.part, a.parts, a.half);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_split(const SplitArgs& a, cudaStream_t stream, uint64_t* launches) {
+  const int64_t total = a.ld / 8 * a.rows * a.workers;
+  if (total == 0) return cudaSuccess;
+  const int64_t size = a.dtype == DQGAN_F32 ? 4 : 2;
+  const bool packs = ((uintptr_t)a.from & 15) == 0 && a.from_ld * size % 16 == 0 && a.batch * size % 16 == 0;
+  const int sms = device_sms();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  ++*launches;
+  const dim3 grid((unsigned)min64(ceil_div(total, 256), (int64_t)sms * 8));
+  return with_dtype(a.dtype, [&](auto t) { return launch_pdl(split_kernel<decltype(t)>, grid, dim3(256), 0, stream, a, packs); });
+}
+
+cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, cudaStream_t stream,
+                         uint64_t* launches, ProductOperand* out) {
+  const bool as_is = !m.targets && (half ? m.dtype == DQGAN_F16 : m.dtype == DQGAN_BF16 && parts == 1);
+  out->shared = m.batch == 0 && m.workers > 1;
+  out->half = half;
+  out->across = false;
+  if (as_is && operand_in_place(m.data, m.ld, m.batch)) {
+    out->data = m.data;
+    out->ld = m.ld;
+    out->batch = m.batch;
+    out->parts = 1;
+    out->part = 0;
+    return cudaSuccess;
+  }
+  SplitArgs s{};
+  s.from = m.data;
+  s.batch = m.batch;
+  s.from_ld = m.ld;
+  s.dtype = m.dtype;
+  s.to = buffer;
+  s.ld = round8(m.columns);
+  s.rows = m.rows;
+  s.columns = m.columns;
+  s.workers = out->shared ? 1 : m.workers;
+  s.part = s.ld * s.rows * s.workers;
+  s.parts = parts;
+  s.half = half;
+  s.targets = m.targets;
+  s.weights = m.weights;
+  s.token_bits = m.token_bits;
+  s.vocab = m.vocab;
+  out->data = buffer;
+  out->ld = s.ld;
+  out->batch = s.ld * s.rows;
+  out->part = s.part;
+  out->parts = parts;
+  return launch_split(s, stream, launches);
+}
+
+}  // namespace dq

@@ -1,0 +1,208 @@
+// Matrix products of the token-model operators on the tensor cores (not part
+// of the C-ABI): what a product is, and its launchers.
+//
+// A product is D[i][j] = sum over k of A[i][k] B[j][k] for every worker, with
+// 16-bit operands, fp32 sums, and an epilogue.  Operands in 32 bits, and
+// values computed in 32 bits, come as a sum of parts of 16 bits (x = x0 + x1 +
+// ..., each the rounding of what the ones before leave), and the product as
+// the sum over pairs of parts that matter ("terms").
+#pragma once
+
+#include "operators.cuh"
+
+namespace dq {
+
+// A 16-bit operand as it lies in memory.  Element (i, k) of worker m and part
+// p is data[p * part + m * batch + i * ld + k], or with `across` data[p * part +
+// m * batch + k * ld + i].  Base and strides are multiples of 16 bytes.
+struct ProductOperand {
+  const void* data = nullptr;
+  int64_t ld = 0, batch = 0, part = 0;
+  int32_t parts = 1;
+  bool across = false;
+  bool shared = false;  // one matrix for all workers
+  bool half = false;    // f16; else bf16 (both operands alike)
+};
+
+struct ProductTerms {
+  int32_t count = 1;
+  uint8_t a[6] = {}, b[6] = {};
+};
+// All pairs of parts whose product is above the rounding of the last part: of
+// (2, 1), (2, 2) and (3, 3) parts those with i + j < max.
+ProductTerms product_terms(int a_parts, int b_parts);
+
+// What is done with the sums.  Row i and column j of worker m.
+struct StoreArgs {
+  void* out;             // out + m * out_batch + i * out_ld + j
+  int64_t out_batch, out_ld;
+  int32_t out_dtype;
+  void* pre;             // the sum with the bias, of the same type, or nullptr
+  int64_t pre_batch, pre_ld;
+  const void* residual;  // of the same type, added last, or nullptr
+  int64_t residual_batch, residual_ld;
+  const float* bias;     // bias + m * bias_batch + j, or nullptr
+  int64_t bias_batch;
+  const float* add;      // fp32 values added to the sum (add + m * add_batch + i * add_ld + j), or nullptr; may be out
+  int64_t add_batch, add_ld;
+  int32_t activation;
+};
+
+struct SoftmaxArgs {
+  const void* targets;    // one a row, worker m's at + m * m_rows
+  int32_t token_bits;
+  const float* weights;   // one a row, or nullptr
+  int64_t first;          // the first column's place in the vocabulary
+  int64_t vocab;
+  float2* stats;          // forward: (maximum, sum of exp(z - maximum)) of row r's columns in slot s at [(m * slots + s) * rows + r]
+  int32_t slots, slot;    // slots of a row; the first of this product's
+  float* target_logit;    // forward: one a row
+  const float* lse;       // gradient
+  float scale;
+  void* grad;             // gradient in bf16 parts: [part][worker][row][grad_ld]
+  int64_t grad_ld, grad_part;
+  int32_t grad_parts;
+};
+
+struct ProductArgs {
+  CUtensorMap a, b;
+  int64_t rows, columns;    // of D, per worker
+  int32_t workers;
+  int32_t kblocks;          // blocks of 64 of the contracted index
+  int32_t chunk;            // terms of 64 that one accumulator in tensor memory sums
+  int32_t splits;           // pieces of the contracted index that are summed apart
+  int32_t tiles_m, tiles_n;
+  ProductTerms terms;
+  uint8_t a_across, b_across, a_shared, b_shared, half;
+  float* partial;           // splits > 1: [split][worker][tiles_m * 128][tiles_n * BN]
+  uint32_t* err;
+  StoreArgs store;
+  SoftmaxArgs softmax;
+};
+
+struct Product {
+  ProductOperand a, b;
+  int64_t rows, columns, depth;
+  int32_t workers;
+  ProductTerms terms;
+};
+
+// Scratch of the products of one operator: partial sums of products that are split.
+constexpr size_t kProductScratch = (size_t)40 << 20;
+
+// `splittable`: kProductScratch bytes at scratch, or nullptr.
+cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void* scratch, uint32_t* err,
+                                 cudaStream_t stream, uint64_t* launches);
+// Rows of a matrix turned into 16-bit parts, [part][worker][row][ld] with ld a
+// multiple of 8; the columns up to ld are 0.
+struct SplitArgs {
+  const void* from;       // worker m's row r at + m * batch + r * from_ld
+  int64_t batch, from_ld;
+  int32_t dtype;          // of the values
+  void* to;
+  int64_t ld, part;       // elements
+  int32_t parts;
+  bool half;              // to f16 (one part, from f16); else bf16
+  int64_t rows, columns;
+  int32_t workers;
+  // Rows that do not count become 0: those whose target is outside [0, vocab) or whose weight is 0.
+  const void* targets;    // or nullptr: all rows count
+  const float* weights;   // or nullptr
+  int32_t token_bits;
+  int64_t vocab;
+};
+cudaError_t launch_split(const SplitArgs& a, cudaStream_t stream, uint64_t* launches);
+
+// Whether a matrix of a 16-bit type can be an operand as it lies.
+inline bool operand_in_place(const void* p, int64_t ld, int64_t batch) {
+  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && batch % 8 == 0 && ld < ((int64_t)1 << 38) && batch < ((int64_t)1 << 38);
+}
+
+// Whether row r of a loss counts.
+__device__ __forceinline__ int64_t token_at(const void* ids, int bits, int64_t r) {
+  return bits == 32 ? (int64_t) static_cast<const int32_t*>(ids)[r] : static_cast<const int64_t*>(ids)[r];
+}
+
+// act(u), and its slope.
+__device__ __forceinline__ float gelu_cdf(float u) { return 0.5f * (1.f + erff(u * 0.70710678118654752f)); }
+__device__ __forceinline__ float sigmoid(float u) { return 1.f / (1.f + __expf(-u)); }
+__device__ __forceinline__ float activate(float u, int activation) {
+  switch (activation) {
+    case DQGAN_RELU: return u > 0.f ? u : (u != u ? u : 0.f);
+    case DQGAN_GELU: return u * gelu_cdf(u);
+    case DQGAN_SILU: return u * sigmoid(u);
+  }
+  return u;
+}
+
+// Eight values of a row, 16 bytes at a time where `packs` says that rows allow it; 0 from `count` on.
+template <typename T>
+__device__ __forceinline__ void read8(const T* from, int count, bool packs, float (&x)[8]) {
+  constexpr int E = 16 / (int)sizeof(T);
+  if (packs && count >= 8) {
+#pragma unroll
+    for (int i = 0; i < 8; i += E) {
+      const uint4 pack = *reinterpret_cast<const uint4*>(from + i);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 v = pair_of<T>(pack, e);
+        x[i + e] = v.x;
+        x[i + e + 1] = v.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(from[i]) : 0.f;
+  }
+}
+
+// x's rounding to bf16, and what it leaves.  A finite value stays finite; a value that is not leaves nothing.
+__device__ __forceinline__ __nv_bfloat16 take_part(float& x) {
+  __nv_bfloat16 h = __float2bfloat16_rn(x);
+  float back = __bfloat162float(h);
+  if (isinf(back) && !isinf(x)) {
+    h = __float2bfloat16_rz(x);
+    back = __bfloat162float(h);
+  }
+  x = isfinite(back) ? x - back : 0.f;
+  return h;
+}
+
+__device__ __forceinline__ void write_parts(float (&x)[8], void* to, int64_t at, int64_t part, int parts, bool half) {
+  if (half) {
+    uint4 pack;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) set_pair<__half>(pack, i, make_float2(x[i], x[i + 1]));
+    *reinterpret_cast<uint4*>(static_cast<__half*>(to) + at) = pack;
+    return;
+  }
+  for (int q = 0; q < parts; ++q) {
+    uint4 pack;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      __nv_bfloat162 both;
+      both.x = take_part(x[i]);
+      both.y = take_part(x[i + 1]);
+      reinterpret_cast<__nv_bfloat162*>(&pack)[i / 2] = both;
+    }
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(to) + q * part + at) = pack;
+  }
+}
+
+// A matrix of the caller's: worker m's row r at data + m * batch + r * ld.
+struct MatrixArgs {
+  const void* data;
+  int64_t ld, batch;  // batch 0: one for all workers
+  int32_t dtype;
+  int64_t rows, columns;
+  int32_t workers;
+  const void* targets = nullptr;  // as in SplitArgs
+  const float* weights = nullptr;
+  int32_t token_bits = 32;
+  int64_t vocab = 0;
+};
+// The operand that it is: as it lies, or split into `buffer`.
+cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, cudaStream_t stream,
+                         uint64_t* launches, ProductOperand* out);
+
+}  // namespace dq

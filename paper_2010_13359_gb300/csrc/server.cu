@@ -1858,31 +1858,21 @@ cudaError_t launch_lookahead(const float* w, const float* h, float* out, int64_t
 
 namespace dq {
 
-namespace {
-
-using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                              const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// cuTensorMapEncodeTiled through the runtime's driver entry point (no link
-// against libcuda); nullptr if it is unavailable.
-EncodeFn tensor_map_encoder() {
-  static const EncodeFn encode = []() -> EncodeFn {
+TensorMapEncoder tensor_map_encoder() {
+  static const TensorMapEncoder encode = []() -> TensorMapEncoder {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
         q != cudaDriverEntryPointSuccess)
       return nullptr;
-    return reinterpret_cast<EncodeFn>(fn);
+    return reinterpret_cast<TensorMapEncoder>(fn);
   }();
   return encode;
 }
 
-}  // namespace
-
 bool encode_words_map(const uint8_t* msgs, int64_t msg_stride, int64_t off_payload, int64_t payload_words,
                       int32_t M, bool swizzle128, int32_t box_words, CUtensorMap* out) {
-  const EncodeFn encode = tensor_map_encoder();
+  const TensorMapEncoder encode = tensor_map_encoder();
   if (!encode || M < 1 || (swizzle128 && box_words != 32)) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)(off_payload / 4 + payload_words), (cuuint64_t)M};
   const cuuint64_t strides[1] = {(cuuint64_t)msg_stride};
@@ -1895,7 +1885,7 @@ bool encode_words_map(const uint8_t* msgs, int64_t msg_stride, int64_t off_paylo
 }
 
 bool encode_params_map(float* w, int64_t d, int32_t box_rows, CUtensorMap* out) {
-  const EncodeFn encode = tensor_map_encoder();
+  const TensorMapEncoder encode = tensor_map_encoder();
   if (!encode || d < 32 || ((uintptr_t)w & 15u) != 0 || box_rows < 1 || box_rows > 256) return false;
   const cuuint64_t dims[2] = {32u, (cuuint64_t)(d / 32)};
   const cuuint64_t strides[1] = {128u};

@@ -1,0 +1,342 @@
+// Softmax cross entropy of the workers' output layers over a large vocabulary,
+// without keeping the logits.
+//
+//   z = x W^T;  lse = log sum_v exp z_v;  loss = c (lse - z_t)
+//   dz = scale c (exp(z - lse) - [v = t]);  dx = dz W;  dW = dz^T x
+//
+// The forward pass leaves of each row's 128 (or 32) logits their maximum and the sum of their
+// exponentials, in the product's epilogue; a second kernel joins them in order.
+// The gradient takes the vocabulary in pieces: a piece's logits are computed
+// again, their epilogue writes dz in 16-bit parts into scratch, and two products
+// take it from there.  So the step costs four products of 2 rows vocab width
+// operations where kept logits would cost three, and dW's, whose result is fp32,
+// reads dz in two bf16 parts (three for fp32 activations).
+#include "product_kernel.cuh"
+
+namespace dq {
+
+namespace {
+
+int act_parts(int dtype) { return dtype == DQGAN_F32 ? 3 : dtype == DQGAN_F16 ? 2 : 1; }
+// Of the weights in the logits, whose loss is fp32, and in dx.
+int logit_weight_parts(const TokenLossShape& s) {
+  return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 || s.weight_dtype == DQGAN_F32 ? 2 : 1;
+}
+int grad_weight_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 ? 2 : 1; }
+int grad_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : 2; }
+bool half_logits(const TokenLossShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
+
+constexpr int64_t kGradBytes = (int64_t)512 << 20, kWeightBytes = (int64_t)1 << 30;
+constexpr int kFewTiles = 76;  // below: narrow tiles
+
+// Columns of a piece of the vocabulary, a multiple of 256.
+int64_t piece_of(const TokenLossShape& s) {
+  const int64_t by_grad = kGradBytes / ((int64_t)s.workers * s.max_rows * 2 * grad_parts(s));
+  const int64_t by_weight = kWeightBytes / ((int64_t)s.workers * s.width * 2 * logit_weight_parts(s));
+  const int64_t most = by_grad < by_weight ? by_grad : by_weight;
+  const int64_t whole = ceil_div(s.vocab, 256) * 256;
+  return most < 256 ? 256 : most < whole ? most / 256 * 256 : whole;
+}
+
+bool narrow(int64_t rows, int32_t workers, int64_t columns) {
+  return ceil_div(rows, kTileRows) * ceil_div(columns, 256) * workers < kFewTiles;
+}
+
+int64_t most_slots(int64_t vocab) {
+  const int64_t wide = 2 * ceil_div(vocab, 256), thin = 2 * ceil_div(vocab, 64);
+  const int64_t few = thin < 8 * kFewTiles ? thin : 8 * kFewTiles;
+  return wide > few ? wide : few;
+}
+
+struct Scratch {
+  uint32_t* err;
+  void* products;
+  void *x, *x_half, *w, *grad;
+  float2* stats;
+  float *target_logit, *lse, *dx;
+  size_t bytes;
+};
+
+Scratch scratch_of(const TokenLossShape& s, void* base) {
+  Scratch c{};
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    void* p = static_cast<char*>(base) + at;
+    at += (size_t)ceil_div(bytes, 1024) * 1024;
+    return p;
+  };
+  const int64_t rows = (int64_t)s.workers * s.max_rows, piece = piece_of(s);
+  c.err = static_cast<uint32_t*>(take(1024));
+  c.products = take(kProductScratch);
+  c.x = take(rows * round8(s.width) * 2 * act_parts(s.dtype));
+  c.x_half = take(half_logits(s) ? rows * round8(s.width) * 2 : 0);
+  c.w = take((int64_t)s.workers * piece * round8(s.width) * 2 * logit_weight_parts(s));
+  c.grad = take(rows * piece * 2 * grad_parts(s));
+  c.stats = static_cast<float2*>(take(rows * most_slots(s.vocab) * 8));
+  c.target_logit = static_cast<float*>(take(rows * 4));
+  c.lse = static_cast<float*>(take(rows * 4));
+  c.dx = static_cast<float*>(take(piece < s.vocab ? rows * s.width * 4 : 0));
+  c.bytes = at;
+  return c;
+}
+
+__device__ __forceinline__ int64_t counting_target(const SoftmaxArgs& s, int64_t r) {
+  const int64_t t = token_at(s.targets, s.token_bits, r);
+  return t >= 0 && t < s.vocab && !(s.weights && s.weights[r] == 0.f) ? t : -1;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct StatsEpilogue {
+  template <int BN>
+  static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
+                                             float (&v)[BN / 2], float*, int lane) {
+    const SoftmaxArgs& s = p.softmax;
+    if (row + lane >= p.rows) return;
+    const int64_t r = tile.worker * p.rows + row + lane;
+    const int valid = (int)max64(0, min64(BN / 2, p.columns - column));
+    float most = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < BN / 2; ++j) {
+      if (j >= valid) v[j] = -INFINITY;
+      most = fmaxf(most, v[j]);
+    }
+    const float from = most == -INFINITY ? 0.f : most;
+    const int64_t place = counting_target(s, r) - s.first - column;
+    const int t = place >= 0 && place < valid ? (int)place : -1;
+    float z = 0.f;
+#pragma unroll
+    for (int j = 0; j < BN / 2; ++j) {
+      sum += exp2f((v[j] - from) * kLog2e);
+      z = t == j ? v[j] : z;
+    }
+    const int slot = s.slot + (int)(column / (BN / 2));
+    s.stats[((int64_t)tile.worker * s.slots + slot) * p.rows + row + lane] = make_float2(most, sum);
+    if (t >= 0) s.target_logit[r] = z;
+  }
+};
+
+// The gradient of the logits, in parts.
+struct GradEpilogue {
+  template <int BN>
+  static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
+                                             float (&v)[BN / 2], float*, int lane) {
+    const SoftmaxArgs& s = p.softmax;
+    if (row + lane >= p.rows) return;
+    const int64_t r = tile.worker * p.rows + row + lane;
+    const int64_t target = counting_target(s, r), t = target - s.first - column;
+    const float lse = s.lse[r], factor = target < 0 ? 0.f : s.weights ? s.scale * s.weights[r] : s.scale;
+#pragma unroll
+    for (int g = 0; g < BN / 2; g += 8) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float q = exp2f((v[g + j] - lse) * kLog2e);
+        x[j] = target < 0 ? 0.f : factor * (g + j == t ? q - 1.f : q);
+      }
+      write_parts(x, s.grad, r * s.grad_ld + column + g, s.grad_part, s.grad_parts, false);
+    }
+  }
+};
+
+// A row's lse and loss from its slots: eight warps take them in turn, joined in order.
+__global__ void __launch_bounds__(256) join_stats_kernel(const SoftmaxArgs s, int64_t rows, int32_t workers, float* loss,
+                                                         float* lse) {
+  dq_pdl_enter();
+  __shared__ float2 part[8][32];
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * 32 + lane;
+  float most = -INFINITY, sum = 0.f;
+  const auto join = [&](float2 x) {
+    if (x.x > most) {
+      sum = sum * exp2f((most - x.x) * kLog2e) + x.y;
+      most = x.x;
+    } else if (x.x == most) {
+      sum += x.y;
+    } else {
+      // a NaN maximum cannot be: the sum holds it
+      sum = fmaf(x.y, exp2f((x.x - most) * kLog2e), sum);
+    }
+  };
+  if (r < rows * workers) {
+    const int64_t worker = r / rows, row = r - worker * rows;
+    for (int i = warp; i < s.slots; i += 8) join(s.stats[(worker * s.slots + i) * rows + row]);
+  }
+  part[warp][lane] = make_float2(most, sum);
+  __syncthreads();
+  if (warp > 0 || r >= rows * workers) return;
+  most = -INFINITY;
+  sum = 0.f;
+  for (int w = 0; w < 8; ++w) join(part[w][lane]);
+  const bool counts = counting_target(s, r) >= 0;
+  const float all = most + logf(sum);
+  const float c = s.weights ? s.weights[r] : 1.f;
+  if (loss) loss[r] = counts ? c * (all - s.target_logit[r]) : 0.f;
+  if (lse) lse[r] = counts ? all : 0.f;
+}
+
+template <typename Epilogue>
+cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool thin, uint32_t* err, cudaStream_t stream,
+                            uint64_t* launches) {
+  ProductArgs args{};
+  if (!(thin ? product_args<64>(p, err, &args) : product_args<256>(p, err, &args))) return cudaErrorInvalidValue;
+  args.softmax = softmax;
+  return thin ? launch_product<64, Epilogue>(args, stream, launches) : launch_product<256, Epilogue>(args, stream, launches);
+}
+
+}  // namespace
+
+size_t token_loss_scratch_bytes(const TokenLossShape& s) { return scratch_of(s, nullptr).bytes; }
+
+cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint64_t* launches) {
+  const TokenLossShape& s = a.shape;
+  const Scratch c = scratch_of(s, a.scratch);
+  const bool half = half_logits(s);
+  const int64_t wsize = s.weight_dtype == DQGAN_F32 ? 4 : 2, piece = piece_of(s);
+  cudaError_t st = cudaSuccess;
+  if (a.rows == 0) {  // gradients of nothing
+    for (int m = 0; m < s.workers && st == cudaSuccess; ++m)
+      if (a.backward && a.dweight && !a.accumulate)
+        st = cudaMemsetAsync(a.dweight + m * a.g_stride, 0, (size_t)(s.vocab * s.width) * 4, stream);
+    return st;
+  }
+
+  SoftmaxArgs soft{};
+  soft.targets = a.targets;
+  soft.token_bits = s.token_bits;
+  soft.weights = a.weights;
+  soft.vocab = s.vocab;
+  soft.stats = c.stats;
+  soft.target_logit = c.target_logit;
+  soft.lse = a.lse ? a.lse : c.lse;
+  soft.scale = a.scale;
+  soft.grad = c.grad;
+
+  // x: of the gradient, the rows that do not count as zeros, whatever they hold
+  ProductOperand x_logits, x_grad;
+  MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.width, s.workers};
+  if (a.forward || a.dx || a.dweight) {
+    if (half) st = make_operand(x, 1, true, c.x_half, stream, launches, &x_logits);
+    if (a.backward) {
+      x.targets = a.targets;
+      x.weights = a.weights;
+      x.token_bits = s.token_bits;
+      x.vocab = s.vocab;
+    }
+    if (st == cudaSuccess && (!half || a.backward))
+      st = make_operand(x, act_parts(s.dtype), false, c.x, stream, launches, &x_grad);
+    if (!half) x_logits = x_grad;
+    if (st != cudaSuccess) return st;
+  }
+
+  // columns [first, first + count) of the vocabulary as an operand
+  const auto weights = [&](int64_t first, int64_t count, int parts, bool as_half, ProductOperand* out) {
+    const MatrixArgs w{static_cast<const char*>(a.weight) + first * s.width * wsize, s.width, a.p_stride, s.weight_dtype,
+                       count, s.width, s.workers};
+    return make_operand(w, parts, as_half, c.w, stream, launches, out);
+  };
+  Product logits;
+  logits.rows = a.rows;
+  logits.depth = s.width;
+  logits.workers = s.workers;
+  logits.a = x_logits;
+  const int logit_parts = half ? 1 : logit_weight_parts(s);
+
+  if (a.forward) {
+    // all at once where the weights can be read as they lie
+    const bool whole = (half || (s.weight_dtype == DQGAN_BF16 && logit_parts == 1)) &&
+                       operand_in_place(a.weight, s.width, a.p_stride);
+    const int64_t step = whole ? s.vocab : piece;
+    const bool thin = narrow(a.rows, s.workers, step < s.vocab ? step : s.vocab);
+    const int64_t columns = thin ? 32 : 128;
+    soft.slots = (int32_t)(ceil_div(s.vocab, 2 * columns) * 2);
+    for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += step) {
+      logits.columns = s.vocab - first < step ? s.vocab - first : step;
+      if ((st = weights(first, logits.columns, logit_parts, half, &logits.b)) != cudaSuccess) break;
+      logits.terms = product_terms(logits.a.parts, logits.b.parts);
+      soft.first = first;
+      soft.slot = (int32_t)(first / columns);
+      st = softmax_product<StatsEpilogue>(logits, soft, thin, c.err, stream, launches);
+    }
+    if (st != cudaSuccess) return st;
+    ++*launches;
+    st = launch_pdl(join_stats_kernel, dim3((unsigned)ceil_div(a.rows * s.workers, 32)), dim3(256), 0, stream, soft, a.rows,
+                    s.workers, a.loss, const_cast<float*>(soft.lse));
+    if (st != cudaSuccess) return st;
+  }
+
+  if (!a.backward || (!a.dx && !a.dweight)) return st;
+  for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += piece) {
+    const int64_t count = s.vocab - first < piece ? s.vocab - first : piece;
+    logits.columns = count;
+    if ((st = weights(first, count, logit_parts, half, &logits.b)) != cudaSuccess) return st;
+    logits.terms = product_terms(logits.a.parts, logits.b.parts);
+    soft.first = first;
+    soft.grad_ld = piece;
+    soft.grad_part = (int64_t)s.workers * a.rows * piece;
+    soft.grad_parts = grad_parts(s);
+    st = softmax_product<GradEpilogue>(logits, soft, narrow(a.rows, s.workers, count), c.err, stream, launches);
+    if (st != cudaSuccess) return st;
+    ProductOperand d;
+    d.data = c.grad;
+    d.ld = piece;
+    d.batch = a.rows * piece;
+    d.part = soft.grad_part;
+    d.parts = soft.grad_parts;
+    if (a.dweight) {
+      Product p;
+      p.rows = count;
+      p.columns = s.width;
+      p.depth = a.rows;
+      p.workers = s.workers;
+      p.a = d;
+      p.b = x_grad;
+      p.a.across = p.b.across = true;
+      p.terms = product_terms(p.a.parts, p.b.parts);
+      StoreArgs out{};
+      float* const to = a.dweight + first * s.width;
+      out.out = to;
+      out.out_ld = s.width;
+      out.out_batch = a.g_stride;
+      out.out_dtype = DQGAN_F32;
+      if (a.accumulate) {
+        out.add = to;
+        out.add_ld = s.width;
+        out.add_batch = a.g_stride;
+      }
+      if ((st = launch_product_store(p, out, c.products, c.err, stream, launches)) != cudaSuccess) return st;
+    }
+    if (a.dx) {
+      Product p;
+      p.rows = a.rows;
+      p.columns = s.width;
+      p.depth = count;
+      p.workers = s.workers;
+      p.a = d;
+      if (s.dtype == DQGAN_BF16) p.a.parts = 1;
+      // the logits' parts serve where they are bf16 (their first ones)
+      p.b = logits.b;
+      if (half) st = weights(first, count, grad_weight_parts(s), false, &p.b);
+      if (st != cudaSuccess) return st;
+      p.b.parts = grad_weight_parts(s);
+      p.b.across = true;
+      p.terms = product_terms(p.a.parts, p.b.parts);
+      StoreArgs out{};
+      const int64_t dense = a.rows * s.width;
+      if (first > 0) {
+        out.add = c.dx;
+        out.add_ld = s.width;
+        out.add_batch = dense;
+      }
+      const bool last = first + count == s.vocab;
+      out.out = last ? a.dx : c.dx;
+      out.out_ld = last ? a.dx_ld : s.width;
+      out.out_batch = last ? a.rows * a.dx_ld : dense;
+      out.out_dtype = last ? s.dtype : DQGAN_F32;
+      st = launch_product_store(p, out, c.products, c.err, stream, launches);
+    }
+  }
+  return st;
+}
+
+}  // namespace dq

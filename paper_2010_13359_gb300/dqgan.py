@@ -53,6 +53,7 @@ class Config(ctypes.Structure):
 assert ctypes.sizeof(Config) == 56
 
 F32, BF16, F16 = 0, 1, 2
+NONE, RELU, GELU, SILU = 0, 1, 2, 3
 
 SERVER_OMD, SERVER_OADAM = 0, 1
 OADAM_ADAPTIVE, OADAM_BIAS_CORRECTION = 1, 2
@@ -128,6 +129,9 @@ def load_library(path: str = LIBRARY) -> ctypes.CDLL:
         "dqgan_layer_norm_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
         "dqgan_embedding_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
         "dqgan_distillation_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_linear_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_token_loss_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
+        "dqgan_gradient_clip_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
         "dqgan_operator_destroy": (ctypes.c_int, [H]),
         "dqgan_operator_synchronize": (ctypes.c_int, [H]),
         "dqgan_operator_launch_count": (u64, [H]),
@@ -139,6 +143,13 @@ def load_library(path: str = LIBRARY) -> ctypes.CDLL:
         "dqgan_distillation_forward": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, P, P, P]),
         "dqgan_distillation_backward": (ctypes.c_int, [H, i64, P, i64, P, P, P, i64, P, P, f32, P, i64]),
         "dqgan_distillation_step": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, P, f32, P, P, P, i64]),
+        "dqgan_linear_forward": (ctypes.c_int, [H, i64, P, i64, P, i64, P, i64, P, i64, P, i64, P, i64]),
+        "dqgan_linear_backward": (ctypes.c_int, [H, i64, P, i64, P, i64, P, i64, P, i64, P, i64, P, P, i64, i32]),
+        "dqgan_token_loss_forward": (ctypes.c_int, [H, i64, P, i64, P, i64, P, P, P, P]),
+        "dqgan_token_loss_backward": (ctypes.c_int, [H, i64, P, i64, P, i64, P, P, P, f32, P, i64, P, i64, i32]),
+        "dqgan_token_loss_step": (ctypes.c_int, [H, i64, P, i64, P, i64, P, P, f32, P, P, P, i64, P, i64, i32]),
+        "dqgan_gradient_norm": (ctypes.c_int, [H, i64, P, P]),
+        "dqgan_gradient_clip": (ctypes.c_int, [H, i64, P, P, f32, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
