@@ -73,18 +73,6 @@ struct SlopeArgs {
   bool dy_packs, pre_packs;
 };
 
-__device__ __forceinline__ float activation_slope(float u, int activation) {
-  switch (activation) {
-    case DQGAN_RELU: return u > 0.f ? 1.f : (u != u ? u : 0.f);
-    case DQGAN_GELU: return fmaf(u * 0.39894228040143268f, expf(-0.5f * u * u), gelu_cdf(u));
-    case DQGAN_SILU: {
-      const float s = sigmoid(u);
-      return s * fmaf(u, 1.f - s, 1.f);
-    }
-  }
-  return 1.f;
-}
-
 // du of a block of rows and 256 columns, in parts, and the columns' sums.
 template <typename T>
 __global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
@@ -105,7 +93,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
         float u[8];
         read8(static_cast<const T*>(a.pre) + row * a.pre_ld + column, count, a.pre_packs, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= activation_slope(u[i], a.activation);
+        for (int i = 0; i < 8; ++i) x[i] *= activation_slope<sizeof(T) == 4>(u[i], a.activation);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

@@ -1,11 +1,13 @@
 // The kernel of the matrix products: tcgen05 with both operands brought to
 // shared memory by TMA and the sums in tensor memory.
 //
-// One block an SM walks over tiles of 128 x BN results.  One warp's thread
+// One block an SM walks over tiles of 128 x 64 results, or a pair of blocks (a
+// cluster; their SMs' tensor cores work as one) over tiles of 256 x 256, of which
+// each block loads half of either operand and keeps the sums of 128 rows.  One warp's thread
 // loads blocks of 64 of the contracted index into a ring of stages, another's
-// multiplies them, and eight warps take the sums out of tensor memory, two
-// accumulators in turn, so that an epilogue runs beside the next tile's
-// products.
+// (in a pair the first block's) multiplies them, and eight warps take the sums out
+// of tensor memory, two accumulators in turn, so that an epilogue runs beside the
+// next tile's products.
 //
 // The tensor cores' own sums are rounded towards zero, by up to one unit in the
 // last place each 16 products: over thousands of them the error grows past that
@@ -22,41 +24,71 @@ namespace dq {
 constexpr int kProductThreads = 384;  // 4 warps that load and multiply, 8 that take the sums
 constexpr int kTileRows = 128;
 constexpr int kBlockDepth = 64;       // 128 bytes: a row of the 128-byte swizzle
-constexpr int kStageRow = 33;         // floats: rows of the transposing buffers
 
 template <int BN>
 struct ProductShape {
+  static constexpr int kPair = BN == 256 ? 2 : 1;  // blocks that work on a tile
+  static constexpr int kRows = kPair * kTileRows;  // of a tile
+  static constexpr int kBColumns = BN / kPair;     // of the second operand that a block loads
   static constexpr int kABytes = kTileRows * kBlockDepth * 2;
-  static constexpr int kBBytes = BN * kBlockDepth * 2;
+  static constexpr int kBBytes = kBColumns * kBlockDepth * 2;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-  static constexpr int kTurnBytes = 8 * 32 * kStageRow * 4;
+  static constexpr int kStages = BN == 256 ? 6 : 8;
+  static constexpr int kTurnBytes = 8 * 32 * 32 * 4;
   // stages, transposing buffers, barriers; and what it takes to start on a boundary of 1024 bytes
   static constexpr int kSmem = kStages * kStageBytes + kTurnBytes + 256 + 1024;
 };
 
 // ---- tcgen05 ----
+template <int kPair>
 __device__ __forceinline__ void tensor_memory_allocate(uint32_t* to, uint32_t columns) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
-               : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  if constexpr (kPair == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
 }
+template <int kPair>
 __device__ __forceinline__ void tensor_memory_free(uint32_t at, uint32_t columns) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+  if constexpr (kPair == 2)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+  else
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
 }
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Arrives at `bar` (in a pair, of both blocks) when the products so far are done.
+template <int kPair>
 __device__ __forceinline__ void tensor_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
-               : "memory");
+  if constexpr (kPair == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     smem_addr(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
+                 : "memory");
 }
+template <int kPair>
 __device__ __forceinline__ void tensor_multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
-      : "memory");
+  if constexpr (kPair == 2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+        : "memory");
 }
 // 32 columns of this warp's 32 lanes: lane l gets row l.
 __device__ __forceinline__ void tensor_load32(uint32_t at, uint32_t (&v)[32]) {
@@ -71,13 +103,38 @@ __device__ __forceinline__ void tensor_load32(uint32_t at, uint32_t (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// The address of the pair's first block's object at the place of this block's.
+__device__ __forceinline__ uint32_t first_block(const void* p) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_addr(p)));
+  return at;
+}
+__device__ __forceinline__ uint32_t block_in_pair() {
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  return rank;
+}
+__device__ __forceinline__ void pair_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// A box into this block's shared memory, counted by the barrier at `bar` (shared::cluster: a pair's is the first block's).
+template <int kPair>
 __device__ __forceinline__ void tma_load_4d(void* dst_smem, const void* tmap, int32_t x, int32_t y, int32_t z, int32_t w,
-                                            uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-          smem_addr(dst_smem)),
-      "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_addr(bar))
-      : "memory");
+                                            uint32_t bar) {
+  if constexpr (kPair == 2)
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            smem_addr(dst_smem)),
+        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            smem_addr(dst_smem)),
+        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
 }
 
 // Shared-memory descriptor of an operand's 16 (contracted) x 64... slice with the 128-byte swizzle.  Rows along the
@@ -86,6 +143,27 @@ __device__ __forceinline__ void tma_load_4d(void* dst_smem, const void* tmap, in
 __device__ __forceinline__ uint64_t operand_descriptor(uint32_t at, bool across) {
   const uint64_t lead = across ? (kBlockDepth * 128) >> 4 : 1;
   return (uint64_t)((at & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// A warp's 32 x 32 sums, turned in shared memory: lane l puts row l, 16 bytes at a time, and gets eight columns (l & 3)
+// of rows l / 4, 8 + l / 4, ... (turned8), or column l of any row (turned1).  The packs of row r stand in the order
+// pack ^ (r & 7), so that none of these meet in a bank.
+__device__ __forceinline__ void turn_put(float* buffer, const float* v, int lane) {
+  __syncwarp();
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    *reinterpret_cast<float4*>(buffer + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+  __syncwarp();
+}
+__device__ __forceinline__ void turned8(const float* buffer, int r, int lane, float (&x)[8]) {
+  const int c = 2 * (lane & 3);
+  const float4 low = *reinterpret_cast<const float4*>(buffer + r * 32 + (c ^ (r & 7)) * 4);
+  const float4 high = *reinterpret_cast<const float4*>(buffer + r * 32 + ((c + 1) ^ (r & 7)) * 4);
+  x[0] = low.x, x[1] = low.y, x[2] = low.z, x[3] = low.w;
+  x[4] = high.x, x[5] = high.y, x[6] = high.z, x[7] = high.w;
+}
+__device__ __forceinline__ float turned1(const float* buffer, int r, int lane) {
+  return buffer[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + (lane & 3)];
 }
 
 struct ProductTile {
@@ -106,18 +184,18 @@ __device__ __forceinline__ ProductTile product_tile(const ProductArgs& p, int64_
   constexpr int kGroup = 8;
   const int group = in / (kGroup * p.tiles_n), left = in - group * kGroup * p.tiles_n;
   const int high = p.tiles_m - group * kGroup < kGroup ? p.tiles_m - group * kGroup : kGroup;
-  tile.row = (int64_t)(group * kGroup + left % high) * kTileRows;
+  tile.row = (int64_t)(group * kGroup + left % high) * ProductShape<BN>::kRows;
   tile.column = (int64_t)(left / high) * BN;
   tile.begin = (int)((int64_t)p.kblocks * tile.split / p.splits);
   tile.end = (int)((int64_t)p.kblocks * (tile.split + 1) / p.splits);
   return tile;
 }
 
-// The sums of one warp: row `row` of this lane, columns [column, column + BN / 2).
 template <int BN, typename Epilogue>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductArgs p) {
   dq_pdl_enter();
   using S = ProductShape<BN>;
+  constexpr int kPair = S::kPair;
   extern __shared__ __align__(1024) uint8_t raw[];
   uint8_t* const smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
   float* const turn = reinterpret_cast<float*>(smem + S::kStages * S::kStageBytes);
@@ -130,66 +208,73 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   constexpr uint32_t kColumns = 2 * BN;
 
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int rank = kPair == 2 ? (int)block_in_pair() : 0;
   if (threadIdx.x == 0) {
+    // full and sum_empty of a pair's first block count for both, empty and sum_full are each block's own
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(sum_full + s, 1);
-      mbar_init(sum_empty + s, 8);
+      mbar_init(sum_empty + s, 8 * kPair);
     }
     mbar_fence_init();
   }
-  if (warp == 2) tensor_memory_allocate(at_shared, kColumns);
+  if (warp == 2) tensor_memory_allocate<kPair>(at_shared, kColumns);
   tensor_fence_before();
   __syncthreads();
+  if constexpr (kPair == 2) pair_barrier();
   tensor_fence_after();
   const uint32_t sums = *at_shared;
 
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
+  const int64_t first = blockIdx.x / kPair, step = gridDim.x / kPair;
   const int terms = p.terms.count;
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 0 && lane == 0) {
       uint32_t n = 0;  // stages filled so far
       bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (int64_t t = first; ok && t < tiles; t += step) {
         const ProductTile tile = product_tile<BN>(p, t);
         const int wa = p.a_shared ? 0 : tile.worker, wb = p.b_shared ? 0 : tile.worker;
+        const int row = (int)tile.row + rank * kTileRows, column = (int)tile.column + rank * S::kBColumns;
         for (int k = tile.begin; ok && k < tile.end; ++k)
           for (int term = 0; term < terms; ++term, ++n) {
             const int s = n % S::kStages;
             if (!(ok = mbar_wait_bounded(empty + s, (n / S::kStages & 1) ^ 1, p.err))) break;
-            mbar_arrive_expect_tx(full + s, S::kStageBytes);
+            if (rank == 0) mbar_arrive_expect_tx(full + s, kPair * S::kStageBytes);
+            const uint32_t bar = kPair == 2 ? first_block(full + s) : smem_addr(full + s);
             uint8_t* const a = smem + s * S::kStageBytes;
             uint8_t* const b = a + S::kABytes;
             const int pa = p.terms.a[term], pb = p.terms.b[term];
             if (p.a_across)
               for (int i = 0; i < kTileRows / 64; ++i)
-                tma_load_4d(a + i * 8192, &p.a, (int)tile.row + 64 * i, k * kBlockDepth, wa, pa, full + s);
+                tma_load_4d<kPair>(a + i * 8192, &p.a, row + 64 * i, k * kBlockDepth, wa, pa, bar);
             else
-              tma_load_4d(a, &p.a, k * kBlockDepth, (int)tile.row, wa, pa, full + s);
+              tma_load_4d<kPair>(a, &p.a, k * kBlockDepth, row, wa, pa, bar);
             if (p.b_across)
-              for (int i = 0; i < BN / 64; ++i)
-                tma_load_4d(b + i * 8192, &p.b, (int)tile.column + 64 * i, k * kBlockDepth, wb, pb, full + s);
+              for (int i = 0; i < S::kBColumns / 64; ++i)
+                tma_load_4d<kPair>(b + i * 8192, &p.b, column + 64 * i, k * kBlockDepth, wb, pb, bar);
             else
-              tma_load_4d(b, &p.b, k * kBlockDepth, (int)tile.column, wb, pb, full + s);
+              tma_load_4d<kPair>(b, &p.b, k * kBlockDepth, column, wb, pb, bar);
           }
       }
-      // what is still on its way into shared memory arrives before the block ends
-      for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
-        mbar_wait_bounded(full + i % S::kStages, i / S::kStages & 1, p.err);
-    } else if (warp == 1 && lane == 0) {
+      // what is still on its way into shared memory (of a pair, both blocks') arrives before the block ends
+      if (rank == 0)
+        for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
+          mbar_wait_bounded(full + i % S::kStages, i / S::kStages & 1, p.err);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
       // D in fp32 | type and direction of A and B | N / 8 | M / 16
       const uint32_t kind = 1u << 4 | (p.half ? 0u : 1u << 7 | 1u << 10) | (uint32_t)p.a_across << 15 |
-                            (uint32_t)p.b_across << 16 | (uint32_t)(BN / 8) << 17 | (uint32_t)(kTileRows / 16) << 24;
+                            (uint32_t)p.b_across << 16 | (uint32_t)(BN / 8) << 17 | (uint32_t)(S::kRows / 16) << 24;
       const uint64_t da = operand_descriptor(smem_addr(smem), p.a_across);
       const uint64_t db = operand_descriptor(smem_addr(smem + S::kABytes), p.b_across);
       const uint32_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
       uint32_t n = 0, c = 0;  // stages used, accumulators filled
       bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (int64_t t = first; ok && t < tiles; t += step) {
         const ProductTile tile = product_tile<BN>(p, t);
         const int total = (tile.end - tile.begin) * terms;
         for (int done = 0; ok && done < total; done += p.chunk, ++c) {
@@ -204,10 +289,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const uint64_t at = (uint64_t)(s * (S::kStageBytes >> 4));
 #pragma unroll
             for (int k = 0; k < kBlockDepth / 16; ++k)
-              tensor_multiply(d, da + at + k * step_a, db + at + k * step_b, kind, i > 0 || k > 0);
-            tensor_commit(empty + s);
+              tensor_multiply<kPair>(d, da + at + k * step_a, db + at + k * step_b, kind, i > 0 || k > 0);
+            tensor_commit<kPair>(empty + s);
           }
-          if (ok) tensor_commit(sum_full + (c & 1));
+          if (ok) tensor_commit<kPair>(sum_full + (c & 1));
         }
       }
       // the products end before the block does
@@ -217,10 +302,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int sub = warp & 3, half = (warp - 4) / 4;
-    float* const buffer = turn + (warp - 4) * 32 * kStageRow;
+    float* const buffer = turn + (warp - 4) * 32 * 32;
     uint32_t c = 0;
     bool ok = true;
-    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+    for (int64_t t = first; ok && t < tiles; t += step) {
       const ProductTile tile = product_tile<BN>(p, t);
       const int total = (tile.end - tile.begin) * terms;
       float v[BN / 2];
@@ -239,15 +324,23 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
         tensor_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(sum_empty + (c & 1));
+        if (lane == 0) {
+          if constexpr (kPair == 2)
+            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(sum_empty + (c & 1)))
+                         : "memory");
+          else
+            mbar_arrive(sum_empty + (c & 1));
+        }
       }
-      if (ok) Epilogue::template run<BN>(p, tile, tile.row + 32 * sub, tile.column + half * (BN / 2), v, buffer, lane);
+      if (ok)
+        Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + half * (BN / 2), v, buffer, lane);
     }
   }
   tensor_fence_before();
   __syncthreads();
+  if constexpr (kPair == 2) pair_barrier();
   tensor_fence_after();
-  if (warp == 2) tensor_memory_free(sums, kColumns);
+  if (warp == 2) tensor_memory_free<kPair>(sums, kColumns);
 }
 
 // Host: the tensor map of an operand.  `box`: rows of the tile along the operand's own index.
@@ -276,7 +369,7 @@ inline bool product_args(const Product& p, uint32_t* err, ProductArgs* out) {
   out->kblocks = (int32_t)ceil_div(p.depth, kBlockDepth);
   out->chunk = 8;
   out->splits = 1;
-  out->tiles_m = (int32_t)ceil_div(p.rows, kTileRows);
+  out->tiles_m = (int32_t)ceil_div(p.rows, ProductShape<BN>::kRows);
   out->tiles_n = (int32_t)ceil_div(p.columns, BN);
   out->terms = p.terms;
   out->a_across = p.a.across;
@@ -288,20 +381,52 @@ inline bool product_args(const Product& p, uint32_t* err, ProductArgs* out) {
   return p.rows <= INT32_MAX && p.columns <= INT32_MAX && p.depth <= INT32_MAX &&
          (int64_t)out->tiles_m * out->tiles_n <= INT32_MAX &&
          encode_operand(p.a, p.rows, p.depth, p.workers, kTileRows, &out->a) &&
-         encode_operand(p.b, p.columns, p.depth, p.workers, BN, &out->b);
+         encode_operand(p.b, p.columns, p.depth, p.workers, ProductShape<BN>::kBColumns, &out->b);
+}
+
+// Tiles that the device works on at once.
+template <int BN, typename Epilogue>
+inline cudaError_t product_slots(int* slots) {
+  static std::atomic<int> kept[kKeptDevices];
+  using S = ProductShape<BN>;
+  if (S::kPair == 1) return resident_ctas(product_kernel<BN, Epilogue>, kProductThreads, S::kSmem, S::kSmem, kept, slots);
+  int dev = 0;
+  cudaError_t st = cudaGetDevice(&dev);
+  if (st != cudaSuccess) return st;
+  if (dev < 0 || dev >= kKeptDevices) return cudaErrorInvalidDevice;
+  *slots = kept[dev].load(std::memory_order_acquire);
+  if (*slots != 0) return cudaSuccess;
+  if ((st = cudaFuncSetAttribute(product_kernel<BN, Epilogue>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) !=
+      cudaSuccess)
+    return st;
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = S::kPair;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3(2 * 1024);
+  lc.blockDim = dim3(kProductThreads);
+  lc.dynamicSmemBytes = S::kSmem;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  int clusters = 0;
+  if ((st = cudaOccupancyMaxActiveClusters(&clusters, product_kernel<BN, Epilogue>, &lc)) != cudaSuccess) return st;
+  if (clusters < 1) return cudaErrorInvalidConfiguration;
+  *slots = clusters;
+  kept[dev].store(clusters, std::memory_order_release);
+  return cudaSuccess;
 }
 
 template <int BN, typename Epilogue>
 inline cudaError_t launch_product(const ProductArgs& p, cudaStream_t stream, uint64_t* launches) {
-  static std::atomic<int> kept[kKeptDevices];
-  int ctas = 0;
-  const cudaError_t st = resident_ctas(product_kernel<BN, Epilogue>, kProductThreads, ProductShape<BN>::kSmem,
-                                       ProductShape<BN>::kSmem, kept, &ctas);
+  using S = ProductShape<BN>;
+  int slots = 0;
+  const cudaError_t st = product_slots<BN, Epilogue>(&slots);
   if (st != cudaSuccess) return st;
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
-  const int grid = (int)(tiles < ctas ? tiles : ctas);
+  const int grid = (int)(tiles < slots ? tiles : slots) * S::kPair;
   ++*launches;
-  return launch_pdl(product_kernel<BN, Epilogue>, dim3(grid), dim3(kProductThreads), ProductShape<BN>::kSmem, stream, p);
+  return launch_pdl_cluster(product_kernel<BN, Epilogue>, S::kPair, dim3(grid), dim3(kProductThreads), S::kSmem, stream, p);
 }
 
 }  // namespace dq

@@ -24,13 +24,39 @@ __device__ __forceinline__ void store_value(const StoreArgs& s, int worker, int6
   if (s.add) x += s.add[worker * s.add_batch + row * s.add_ld + column];
   x += bias;
   if (s.pre) static_cast<T*>(s.pre)[worker * s.pre_batch + row * s.pre_ld + column] = from_float<T>(x);
-  x = activate(x, s.activation);
+  x = activate<sizeof(T) == 4>(x, s.activation);
   if (s.residual)
     x += to_float(static_cast<const T*>(s.residual)[worker * s.residual_batch + row * s.residual_ld + column]);
   static_cast<T*>(s.out)[worker * s.out_batch + row * s.out_ld + column] = from_float<T>(x);
 }
 
-// A warp's 32 rows, turned in shared memory so that its lanes hold neighbouring columns.
+// The same of eight columns, in packs.
+template <typename T>
+__device__ __forceinline__ void store8(const StoreArgs& s, int worker, int64_t row, int64_t column, float (&x)[8], const float (&bias)[8]) {
+  if (s.add) {
+    float a[8];
+    read8(s.add + worker * s.add_batch + row * s.add_ld + column, 8, true, a);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += a[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] += bias[i];
+  if (s.pre) write8(x, static_cast<T*>(s.pre) + worker * s.pre_batch + row * s.pre_ld + column);
+  if (s.activation != DQGAN_NONE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = activate<sizeof(T) == 4>(x[i], s.activation);
+  }
+  if (s.residual) {
+    float r[8];
+    read8(static_cast<const T*>(s.residual) + worker * s.residual_batch + row * s.residual_ld + column, 8, true, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += r[i];
+  }
+  write8(x, static_cast<T*>(s.out) + worker * s.out_batch + row * s.out_ld + column);
+}
+
+// A warp's 32 rows, turned so that its lanes hold neighbouring columns: eight each where packs of 16 bytes can be
+// written (16384 rows of 4096 x 4096 in bf16: 275 us a product by packs, 620 by single values), else one.
 template <typename T>
 struct StoreEpilogue {
   template <int BN>
@@ -41,15 +67,27 @@ struct StoreEpilogue {
 #pragma unroll
     for (int g = 0; g < BN / 2; g += 32) {
       if (column + g >= p.columns || rows <= 0) break;
-      __syncwarp();
+      turn_put(buffer, v + g, lane);
+      if (s.packs && column + g + 32 <= p.columns) {
+        const int64_t j = column + g + 8 * (lane & 3);
+        float bias[8] = {};
+        if (s.bias) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) buffer[lane * kStageRow + j] = v[g + j];
-      __syncwarp();
-      const int64_t j = column + g + lane;
-      if (j < p.columns) {
-        const float bias = s.bias ? s.bias[tile.worker * s.bias_batch + j] : 0.f;
+          for (int i = 0; i < 8; ++i) bias[i] = s.bias[tile.worker * s.bias_batch + j + i];
+        }
+#pragma unroll
+        for (int r = lane / 4; r < 32; r += 8) {
+          float x[8];
+          turned8(buffer, r, lane, x);
+          if (r < rows) store8<T>(s, tile.worker, row + r, j, x, bias);
+        }
+      } else {
+        const int64_t j = column + g + lane;
+        if (j < p.columns) {
+          const float bias = s.bias ? s.bias[tile.worker * s.bias_batch + j] : 0.f;
 #pragma unroll 4
-        for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j, buffer[r * kStageRow + lane], bias);
+          for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j, turned1(buffer, r, lane), bias);
+        }
       }
     }
   }
@@ -61,7 +99,7 @@ struct PartialEpilogue {
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
                                              float (&v)[BN / 2], float* buffer, int lane) {
     const int64_t ld = (int64_t)p.tiles_n * BN;
-    float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * kTileRows + row + lane) * ld + column;
+    float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * ProductShape<BN>::kRows + row + lane) * ld + column;
     if (row + lane < p.rows) {
 #pragma unroll
       for (int j = 0; j < BN / 2; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
@@ -73,7 +111,7 @@ struct PartialEpilogue {
 template <typename T, int BN>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p) {
   dq_pdl_enter();
-  const int64_t ld = (int64_t)p.tiles_n * BN, tall = (int64_t)p.tiles_m * kTileRows;
+  const int64_t ld = (int64_t)p.tiles_n * BN, tall = (int64_t)p.tiles_m * ProductShape<BN>::kRows;
   const int64_t column = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (column >= p.columns) return;
   for (int64_t r = blockIdx.y; r < p.rows * p.workers; r += gridDim.y) {
@@ -93,6 +131,13 @@ cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, 
   ProductArgs args{};
   if (!product_args<BN>(p, err, &args)) return cudaErrorInvalidValue;
   args.store = store;
+  const int64_t size = store.out_dtype == DQGAN_F32 ? 4 : 2;
+  const auto packs = [&](const void* at, int64_t ld, int64_t batch, int64_t of) {
+    return !at || (((uintptr_t)at & 15) == 0 && ld * of % 16 == 0 && (p.workers == 1 || batch * of % 16 == 0));
+  };
+  args.store.packs = packs(store.out, store.out_ld, store.out_batch, size) && packs(store.pre, store.pre_ld, store.pre_batch, size) &&
+                     packs(store.residual, store.residual_ld, store.residual_batch, size) &&
+                     packs(store.add, store.add_ld, store.add_batch, 4);
   args.splits = splits;
   if (splits == 1)
     return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });

@@ -46,6 +46,7 @@ struct StoreArgs {
   const float* add;      // fp32 values added to the sum (add + m * add_batch + i * add_ld + j), or nullptr; may be out
   int64_t add_batch, add_ld;
   int32_t activation;
+  bool packs;            // all of them can be read and written 16 bytes at a time (set by the launcher)
 };
 
 struct SoftmaxArgs {
@@ -74,7 +75,7 @@ struct ProductArgs {
   int32_t tiles_m, tiles_n;
   ProductTerms terms;
   uint8_t a_across, b_across, a_shared, b_shared, half;
-  float* partial;           // splits > 1: [split][worker][tiles_m * 128][tiles_n * BN]
+  float* partial;           // splits > 1: [split][worker][rows of whole tiles][columns of whole tiles]
   uint32_t* err;
   StoreArgs store;
   SoftmaxArgs softmax;
@@ -123,16 +124,59 @@ __device__ __forceinline__ int64_t token_at(const void* ids, int bits, int64_t r
   return bits == 32 ? (int64_t) static_cast<const int32_t*>(ids)[r] : static_cast<const int64_t*>(ids)[r];
 }
 
+__device__ __forceinline__ float exp2_approx(float x) {  // 2 units; below 2^-126: 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Phi(u) and exp(-u^2 / 2).  For results of 16 bits: Abramowitz and Stegun 7.1.26, erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2)
+// with t = 1 / (1 + p x), off by at most 1.5e-7, which is a fifth of erff's instructions.
+template <bool kExact>
+__device__ __forceinline__ float2 normal_cdf(float u) {
+  if constexpr (kExact) return make_float2(0.5f * erfcf(u * -0.70710678118654752f), expf(-0.5f * u * u));
+  const float x = fabsf(u) * 0.70710678118654752f;
+  const float e = exp2_approx(u * u * -0.72134752044448170f);
+  const float t = reciprocal_approx(fmaf(0.3275911f, x, 1.f));
+  const float tail = 0.5f * e * t *
+                     fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return make_float2(u > 0.f ? 1.f - tail : tail, e);
+}
+template <bool kExact>
+__device__ __forceinline__ float logistic(float u) {
+  if constexpr (kExact) return 1.f / (1.f + expf(-u));
+  return reciprocal_approx(1.f + exp2_approx(u * -1.4426950408889634f));
+}
+
 // act(u), and its slope.
-__device__ __forceinline__ float gelu_cdf(float u) { return 0.5f * (1.f + erff(u * 0.70710678118654752f)); }
-__device__ __forceinline__ float sigmoid(float u) { return 1.f / (1.f + __expf(-u)); }
+template <bool kExact>
 __device__ __forceinline__ float activate(float u, int activation) {
   switch (activation) {
     case DQGAN_RELU: return u > 0.f ? u : (u != u ? u : 0.f);
-    case DQGAN_GELU: return u * gelu_cdf(u);
-    case DQGAN_SILU: return u * sigmoid(u);
+    case DQGAN_GELU: return u * normal_cdf<kExact>(u).x;
+    case DQGAN_SILU: return u * logistic<kExact>(u);
   }
   return u;
+}
+template <bool kExact>
+__device__ __forceinline__ float activation_slope(float u, int activation) {
+  switch (activation) {
+    case DQGAN_RELU: return u > 0.f ? 1.f : (u != u ? u : 0.f);
+    case DQGAN_GELU: {
+      const float2 f = normal_cdf<kExact>(u);
+      return fmaf(u * 0.39894228040143268f, f.y, f.x);
+    }
+    case DQGAN_SILU: {
+      const float s = logistic<kExact>(u);
+      return s * fmaf(u, 1.f - s, 1.f);
+    }
+  }
+  return 1.f;
 }
 
 // Eight values of a row, 16 bytes at a time where `packs` says that rows allow it; 0 from `count` on.
@@ -153,6 +197,19 @@ __device__ __forceinline__ void read8(const T* from, int count, bool packs, floa
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(from[i]) : 0.f;
+  }
+}
+
+// Eight values to 16-byte packs.
+template <typename T>
+__device__ __forceinline__ void write8(const float (&x)[8], T* to) {
+  constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 8; i += E) {
+    uint4 pack;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) set_pair<T>(pack, e, make_float2(x[i + e], x[i + e + 1]));
+    *reinterpret_cast<uint4*>(to + i) = pack;
   }
 }
 

@@ -107,7 +107,7 @@ struct StatsEpilogue {
     float z = 0.f;
 #pragma unroll
     for (int j = 0; j < BN / 2; ++j) {
-      sum += exp2f((v[j] - from) * kLog2e);
+      sum += exp2_approx((v[j] - from) * kLog2e);
       z = t == j ? v[j] : z;
     }
     const int slot = s.slot + (int)(column / (BN / 2));
@@ -116,25 +116,40 @@ struct StatsEpilogue {
   }
 };
 
-// The gradient of the logits, in parts.
+// The gradient of the logits, in parts; turned as a stored product is.
 struct GradEpilogue {
   template <int BN>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], float*, int lane) {
+                                             float (&v)[BN / 2], float* buffer, int lane) {
     const SoftmaxArgs& s = p.softmax;
-    if (row + lane >= p.rows) return;
-    const int64_t r = tile.worker * p.rows + row + lane;
-    const int64_t target = counting_target(s, r), t = target - s.first - column;
-    const float lse = s.lse[r], factor = target < 0 ? 0.f : s.weights ? s.scale * s.weights[r] : s.scale;
+    const int64_t first = tile.worker * p.rows + row;
+    int64_t target = -1;
+    float lse = 0.f, factor = 0.f;
+    if (row + lane < p.rows) {
+      target = counting_target(s, first + lane);
+      lse = s.lse[first + lane];
+      factor = s.weights ? s.scale * s.weights[first + lane] : s.scale;
+    }
+    const int rows = (int)min64(32, p.rows - row);
+    // the target's column here; -1: elsewhere; -2: the row does not count
+    const int64_t place = target - s.first - column;
+    const int t = target < 0 ? -2 : place >= 0 && place < BN / 2 ? (int)place : -1;
 #pragma unroll
-    for (int g = 0; g < BN / 2; g += 8) {
-      float x[8];
+    for (int g = 0; g < BN / 2; g += 32) {
+      if (column + g >= p.columns || rows <= 0) break;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float q = exp2f((v[g + j] - lse) * kLog2e);
-        x[j] = target < 0 ? 0.f : factor * (g + j == t ? q - 1.f : q);
+      for (int j = 0; j < 32; ++j) {
+        const float q = exp2_approx((v[g + j] - lse) * kLog2e);
+        v[g + j] = t == -2 ? 0.f : factor * (g + j == t ? q - 1.f : q);
       }
-      write_parts(x, s.grad, r * s.grad_ld + column + g, s.grad_part, s.grad_parts, false);
+      turn_put(buffer, v + g, lane);
+#pragma unroll
+      for (int r = lane / 4; r < 32; r += 8) {
+        float x[8];
+        turned8(buffer, r, lane, x);
+        if (r < rows)
+          write_parts(x, s.grad, (first + r) * s.grad_ld + column + g + 8 * (lane & 3), s.grad_part, s.grad_parts, false);
+      }
     }
   }
 };
