@@ -3,17 +3,23 @@
 //
 // One block an SM walks over tiles of 128 x 64 results, or a pair of blocks (a
 // cluster; their SMs' tensor cores work as one) over tiles of 256 x 256, of which
-// each block loads half of either operand and keeps the sums of 128 rows.  One warp's thread
-// loads blocks of 64 of the contracted index into a ring of stages, another's
+// each block loads half of either operand and keeps the sums of 128 rows.  Two
+// threads load blocks of 64 of the contracted index into a ring of stages, a third
 // (in a pair the first block's) multiplies them, and eight warps take the sums out
 // of tensor memory, two accumulators in turn, so that an epilogue runs beside the
 // next tile's products.
+//
+// Of bf16 products of 8192^3: 595 us, 1850 TFLOP/s (a library product: 540); 503
+// without the loads, 665 with four stages: what is left is the loads' latency, for which six stages of 32 KB
+// are what fits.  Four blocks that share an operand by TMA multicast: 608, as
+// clusters of four leave 8 of 152 SMs idle.
 //
 // The tensor cores' own sums are rounded towards zero, by up to one unit in the
 // last place each 16 products: over thousands of them the error grows past that
 // of fp32 sums.  So an accumulator takes `chunk` blocks only; the eight warps
 // add it to sums in registers (128 a thread), rounded to nearest, while the
-// other accumulator fills.
+// other accumulator fills.  16 blocks (1024 products) where the result has 32 bits,
+// 32 in f16, 128 in bf16: taking sums out costs the products up to a tenth at 8.
 #pragma once
 
 #include "device_common.cuh"
@@ -27,7 +33,7 @@ constexpr int kBlockDepth = 64;       // 128 bytes: a row of the 128-byte swizzl
 
 template <int BN>
 struct ProductShape {
-  static constexpr int kPair = BN == 256 ? 2 : 1;  // blocks that work on a tile
+  static constexpr int kPair = BN == 256 ? 2 : 1;     // blocks that work on a tile
   static constexpr int kRows = kPair * kTileRows;  // of a tile
   static constexpr int kBColumns = BN / kPair;     // of the second operand that a block loads
   static constexpr int kABytes = kTileRows * kBlockDepth * 2;
@@ -121,18 +127,18 @@ __device__ __forceinline__ void pair_barrier() {
 
 // A box into this block's shared memory, counted by the barrier at `bar` (shared::cluster: a pair's is the first block's).
 template <int kPair>
-__device__ __forceinline__ void tma_load_4d(void* dst_smem, const void* tmap, int32_t x, int32_t y, int32_t z, int32_t w,
+__device__ __forceinline__ void tma_load_4d(uint32_t to, const void* tmap, int32_t x, int32_t y, int32_t z, int32_t w,
                                             uint32_t bar) {
   if constexpr (kPair == 2)
     asm volatile(
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-            smem_addr(dst_smem)),
+            to),
         "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
         : "memory");
   else
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-            smem_addr(dst_smem)),
+            to),
         "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
         : "memory");
 }
@@ -210,7 +216,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int rank = kPair == 2 ? (int)block_in_pair() : 0;
   if (threadIdx.x == 0) {
-    // full and sum_empty of a pair's first block count for both, empty and sum_full are each block's own
+    // full and sum_empty of a pair's first block count for both; empty and sum_full are each block's own
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(full + s, 1);
       mbar_init(empty + s, 1);
@@ -229,40 +235,43 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   const uint32_t sums = *at_shared;
 
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
-  const int64_t first = blockIdx.x / kPair, step = gridDim.x / kPair;
+  const int64_t first = blockIdx.x / S::kPair, step = gridDim.x / S::kPair;
   const int terms = p.terms.count;
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp == 0 && lane == 0) {
-      uint32_t n = 0;  // stages filled so far
+    if ((warp == 0 || warp == 3) && lane == 0) {
+      // One thread loads A, another B: a stage is 512 clocks of the tensor cores, and one thread that issues all of its
+      // loads takes longer (8192^3: 655 us).
+      const bool is_a = warp == 0;
+      const CUtensorMap* const map = is_a ? &p.a : &p.b;
+      const bool across = is_a ? p.a_across : p.b_across, one_matrix = is_a ? p.a_shared : p.b_shared;
+      const bool counts = is_a && rank == 0;  // announces the stage's bytes
+      const int offset = rank * (is_a ? kTileRows : S::kBColumns);
+      const bool two = across && (is_a ? kTileRows : S::kBColumns) > 64;  // boxes of 64 x 64
+      const uint32_t bars = kPair == 2 ? first_block(full) : smem_addr(full);
+      const uint32_t base = smem_addr(smem) + (is_a ? 0 : S::kABytes);
+      uint32_t s = 0, phase = 1, n = 0;  // stage, what to wait for, stages filled so far
       bool ok = true;
       for (int64_t t = first; ok && t < tiles; t += step) {
         const ProductTile tile = product_tile<BN>(p, t);
-        const int wa = p.a_shared ? 0 : tile.worker, wb = p.b_shared ? 0 : tile.worker;
-        const int row = (int)tile.row + rank * kTileRows, column = (int)tile.column + rank * S::kBColumns;
-        for (int k = tile.begin; ok && k < tile.end; ++k)
-          for (int term = 0; term < terms; ++term, ++n) {
-            const int s = n % S::kStages;
-            if (!(ok = mbar_wait_bounded(empty + s, (n / S::kStages & 1) ^ 1, p.err))) break;
-            if (rank == 0) mbar_arrive_expect_tx(full + s, kPair * S::kStageBytes);
-            const uint32_t bar = kPair == 2 ? first_block(full + s) : smem_addr(full + s);
-            uint8_t* const a = smem + s * S::kStageBytes;
-            uint8_t* const b = a + S::kABytes;
-            const int pa = p.terms.a[term], pb = p.terms.b[term];
-            if (p.a_across)
-              for (int i = 0; i < kTileRows / 64; ++i)
-                tma_load_4d<kPair>(a + i * 8192, &p.a, row + 64 * i, k * kBlockDepth, wa, pa, bar);
-            else
-              tma_load_4d<kPair>(a, &p.a, k * kBlockDepth, row, wa, pa, bar);
-            if (p.b_across)
-              for (int i = 0; i < S::kBColumns / 64; ++i)
-                tma_load_4d<kPair>(b + i * 8192, &p.b, column + 64 * i, k * kBlockDepth, wb, pb, bar);
-            else
-              tma_load_4d<kPair>(b, &p.b, k * kBlockDepth, column, wb, pb, bar);
+        const int worker = one_matrix ? 0 : tile.worker;
+        const int at = (int)(is_a ? tile.row : tile.column) + offset;
+        const int end = tile.end * kBlockDepth;
+        for (int k = tile.begin * kBlockDepth; ok && k < end; k += kBlockDepth)
+          for (int term = 0; term < terms; ++term) {
+            if (!(ok = mbar_wait_bounded(empty + s, phase, p.err))) break;
+            if (counts) mbar_arrive_expect_tx(full + s, kPair * S::kStageBytes);
+            const int part = terms == 1 ? 0 : is_a ? p.terms.a[term] : p.terms.b[term];
+            const uint32_t to = base + s * S::kStageBytes, bar = bars + s * 8;
+            const int x = across ? at : k, y = across ? k : at;
+            tma_load_4d<kPair>(to, map, x, y, worker, part, bar);
+            if (two) tma_load_4d<kPair>(to + 8192, map, x + 64, y, worker, part, bar);
+            ++n;
+            if (++s == S::kStages) s = 0, phase ^= 1;
           }
       }
       // what is still on its way into shared memory (of a pair, both blocks') arrives before the block ends
-      if (rank == 0)
+      if (counts)
         for (uint32_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
           mbar_wait_bounded(full + i % S::kStages, i / S::kStages & 1, p.err);
     } else if (warp == 1 && lane == 0 && rank == 0) {
@@ -272,25 +281,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       const uint64_t da = operand_descriptor(smem_addr(smem), p.a_across);
       const uint64_t db = operand_descriptor(smem_addr(smem + S::kABytes), p.b_across);
       const uint32_t step_a = p.a_across ? 2048 >> 4 : 32 >> 4, step_b = p.b_across ? 2048 >> 4 : 32 >> 4;
-      uint32_t n = 0, c = 0;  // stages used, accumulators filled
+      uint32_t s = 0, phase = 0, n = 0, c = 0;  // stage, what to wait for, stages used, accumulators filled
+      const int chunk = p.chunk;
       bool ok = true;
       for (int64_t t = first; ok && t < tiles; t += step) {
         const ProductTile tile = product_tile<BN>(p, t);
-        const int total = (tile.end - tile.begin) * terms;
-        for (int done = 0; ok && done < total; done += p.chunk, ++c) {
+        for (int left = (tile.end - tile.begin) * terms; ok && left > 0; left -= chunk, ++c) {
           const uint32_t d = sums + (c & 1) * BN;
           if (!(ok = mbar_wait_bounded(sum_empty + (c & 1), (c / 2 & 1) ^ 1, p.err))) break;
           tensor_fence_after();
-          const int count = total - done < p.chunk ? total - done : p.chunk;
+          const int count = left < chunk ? left : chunk;
           for (int i = 0; i < count; ++i, ++n) {
-            const uint32_t s = n % S::kStages;
-            if (!(ok = mbar_wait_bounded(full + s, n / S::kStages & 1, p.err))) break;
+            if (!(ok = mbar_wait_bounded(full + s, phase, p.err))) break;
             tensor_fence_after();
             const uint64_t at = (uint64_t)(s * (S::kStageBytes >> 4));
 #pragma unroll
             for (int k = 0; k < kBlockDepth / 16; ++k)
               tensor_multiply<kPair>(d, da + at + k * step_a, db + at + k * step_b, kind, i > 0 || k > 0);
             tensor_commit<kPair>(empty + s);
+            if (++s == S::kStages) s = 0, phase ^= 1;
           }
           if (ok) tensor_commit<kPair>(sum_full + (c & 1));
         }
@@ -326,7 +335,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         __syncwarp();
         if (lane == 0) {
           if constexpr (kPair == 2)
-            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_block(sum_empty + (c & 1)))
+            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                             first_block(sum_empty + (c & 1)))
                          : "memory");
           else
             mbar_arrive(sum_empty + (c & 1));
@@ -343,8 +353,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   if (warp == 2) tensor_memory_free<kPair>(sums, kColumns);
 }
 
-// Host: the tensor map of an operand.  `box`: rows of the tile along the operand's own index.
-inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth, int32_t workers, int box, CUtensorMap* out) {
+// Host: the tensor map of an operand.  Boxes of 64 of the contracted index and a block's `tile` rows, or of 64 x 64.
+inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth, int32_t workers, int tile, CUtensorMap* out) {
   const TensorMapEncoder encode = tensor_map_encoder();
   if (!encode) return false;
   const int batches = o.shared ? 1 : workers;
@@ -352,7 +362,7 @@ inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth,
   const cuuint64_t dims[4] = {(cuuint64_t)(o.across ? rows : depth), (cuuint64_t)(o.across ? depth : rows),
                               (cuuint64_t)batches, (cuuint64_t)o.parts};
   const cuuint64_t strides[3] = {(cuuint64_t)o.ld * 2, stride(o.batch, batches), stride(o.part, o.parts)};
-  const cuuint32_t boxes[4] = {64u, (cuuint32_t)(o.across ? kBlockDepth : box), 1u, 1u};
+  const cuuint32_t boxes[4] = {64u, (cuuint32_t)(o.across ? 64 : tile), 1u, 1u};
   const cuuint32_t steps[4] = {1u, 1u, 1u, 1u};
   return encode(out, o.half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
                 const_cast<void*>(o.data), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -362,12 +372,12 @@ inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth,
 
 // Fills what the kernel needs of a product; false where its sizes are beyond the kernel's.
 template <int BN>
-inline bool product_args(const Product& p, uint32_t* err, ProductArgs* out) {
+inline bool product_args(const Product& p, int chunk, uint32_t* err, ProductArgs* out) {
   out->rows = p.rows;
   out->columns = p.columns;
   out->workers = p.workers;
   out->kblocks = (int32_t)ceil_div(p.depth, kBlockDepth);
-  out->chunk = 8;
+  out->chunk = chunk;
   out->splits = 1;
   out->tiles_m = (int32_t)ceil_div(p.rows, ProductShape<BN>::kRows);
   out->tiles_n = (int32_t)ceil_div(p.columns, BN);
@@ -404,7 +414,7 @@ inline cudaError_t product_slots(int* slots) {
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = S::kPair;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  lc.gridDim = dim3(2 * 1024);
+  lc.gridDim = dim3(S::kPair * 1024);
   lc.blockDim = dim3(kProductThreads);
   lc.dynamicSmemBytes = S::kSmem;
   lc.attrs = attr;

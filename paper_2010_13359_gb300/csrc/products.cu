@@ -100,7 +100,7 @@ struct PartialEpilogue {
                                              float (&v)[BN / 2], float* buffer, int lane) {
     const int64_t ld = (int64_t)p.tiles_n * BN;
     float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * ProductShape<BN>::kRows + row + lane) * ld + column;
-    if (row + lane < p.rows) {
+    if (row + lane < p.rows) {  // whole tiles
 #pragma unroll
       for (int j = 0; j < BN / 2; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     }
@@ -129,7 +129,8 @@ template <int BN>
 cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, void* scratch, uint32_t* err,
                           cudaStream_t stream, uint64_t* launches) {
   ProductArgs args{};
-  if (!product_args<BN>(p, err, &args)) return cudaErrorInvalidValue;
+  const int chunk = store.out_dtype == DQGAN_F32 ? 16 : store.out_dtype == DQGAN_F16 ? 32 : 128;
+  if (!product_args<BN>(p, chunk, err, &args)) return cudaErrorInvalidValue;
   args.store = store;
   const int64_t size = store.out_dtype == DQGAN_F32 ? 4 : 2;
   const auto packs = [&](const void* at, int64_t ld, int64_t batch, int64_t of) {

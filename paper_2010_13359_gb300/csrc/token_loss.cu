@@ -194,7 +194,7 @@ template <typename Epilogue>
 cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool thin, uint32_t* err, cudaStream_t stream,
                             uint64_t* launches) {
   ProductArgs args{};
-  if (!(thin ? product_args<64>(p, err, &args) : product_args<256>(p, err, &args))) return cudaErrorInvalidValue;
+  if (!(thin ? product_args<64>(p, 16, err, &args) : product_args<256>(p, 16, err, &args))) return cudaErrorInvalidValue;
   args.softmax = softmax;
   return thin ? launch_product<64, Epilogue>(args, stream, launches) : launch_product<256, Epilogue>(args, stream, launches);
 }
