@@ -40,7 +40,7 @@ struct ProductShape {
   static constexpr int kBBytes = kBColumns * kBlockDepth * 2;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = BN == 256 ? 6 : 8;
-  static constexpr int kTurnBytes = 8 * 32 * 32 * 4;
+  static constexpr int kTurnBytes = 8 * 4096;
   // stages, transposing buffers, barriers; and what it takes to start on a boundary of 1024 bytes
   static constexpr int kSmem = kStages * kStageBytes + kTurnBytes + 256 + 1024;
 };
@@ -151,26 +151,59 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t at, bool across)
   return (uint64_t)((at & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-// A warp's 32 x 32 sums, turned in shared memory: lane l puts row l, 16 bytes at a time, and gets eight columns (l & 3)
-// of rows l / 4, 8 + l / 4, ... (turned8), or column l of any row (turned1).  The packs of row r stand in the order
-// pack ^ (r & 7), so that none of these meet in a bank.
-__device__ __forceinline__ void turn_put(float* buffer, const float* v, int lane) {
-  __syncwarp();
+// What a warp has ready of its 32 rows, 64 bytes of a row at a time, goes through two buffers of shared memory in turn
+// and from there by TMA.  Lane l holds row l; its packs of 16 bytes stand in the order of the 64-byte swizzle, in which
+// eight lanes' packs meet in no bank.  What lies outside the matrix is not written.
+struct TurnStore {
+  uint8_t* buffer;  // 2 x 2048 bytes
+  int lane;
+  uint32_t n = 0;
+
+  __device__ __forceinline__ void put(const uint4 (&packs)[4], const CUtensorMap* map, int column, int row, int worker, int part) {
+    uint8_t* const to = buffer + (n & 1) * 2048;
+    ++n;
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    __syncwarp();
 #pragma unroll
-  for (int c = 0; c < 8; ++c)
-    *reinterpret_cast<float4*>(buffer + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-  __syncwarp();
-}
-__device__ __forceinline__ void turned8(const float* buffer, int r, int lane, float (&x)[8]) {
-  const int c = 2 * (lane & 3);
-  const float4 low = *reinterpret_cast<const float4*>(buffer + r * 32 + (c ^ (r & 7)) * 4);
-  const float4 high = *reinterpret_cast<const float4*>(buffer + r * 32 + ((c + 1) ^ (r & 7)) * 4);
-  x[0] = low.x, x[1] = low.y, x[2] = low.z, x[3] = low.w;
-  x[4] = high.x, x[5] = high.y, x[6] = high.z, x[7] = high.w;
-}
-__device__ __forceinline__ float turned1(const float* buffer, int r, int lane) {
-  return buffer[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + (lane & 3)];
-}
+    for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(to + lane * 64 + ((c ^ (lane / 2 & 3)) * 16)) = packs[c];
+    fence_proxy_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(column),
+                   "r"(row), "r"(worker), "r"(part), "r"(smem_addr(to))
+                   : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+
+  // 32 columns as T
+  template <typename T>
+  __device__ __forceinline__ void put32(const float (&x)[32], const CUtensorMap* map, int column, int row, int worker) {
+    constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 32; i += 4 * E) {
+      uint4 packs[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < E; e += 2) set_pair<T>(packs[c], e, make_float2(x[i + c * E + e], x[i + c * E + e + 1]));
+      put(packs, map, column + i, row, worker, 0);
+    }
+  }
+
+  // single values, for matrices that TMA cannot write: column l of row r, from 32 columns that lane r holds
+  __device__ __forceinline__ void turn(const float (&x)[32]) {
+    float* const to = reinterpret_cast<float*>(buffer);
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      *reinterpret_cast<float4*>(to + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    __syncwarp();
+  }
+  __device__ __forceinline__ float turned(int r) const {
+    return reinterpret_cast<const float*>(buffer)[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + (lane & 3)];
+  }
+};
 
 struct ProductTile {
   int worker, split;
@@ -204,7 +237,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   constexpr int kPair = S::kPair;
   extern __shared__ __align__(1024) uint8_t raw[];
   uint8_t* const smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
-  float* const turn = reinterpret_cast<float*>(smem + S::kStages * S::kStageBytes);
+  uint8_t* const turn = smem + S::kStages * S::kStageBytes;
   uint64_t* const full = reinterpret_cast<uint64_t*>(smem + S::kStages * S::kStageBytes + S::kTurnBytes);
   uint64_t* const empty = full + S::kStages;
   uint64_t* const sum_full = empty + S::kStages;
@@ -311,7 +344,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int sub = warp & 3, half = (warp - 4) / 4;
-    float* const buffer = turn + (warp - 4) * 32 * 32;
+    TurnStore store{turn + (warp - 4) * 4096, lane};
     uint32_t c = 0;
     bool ok = true;
     for (int64_t t = first; ok && t < tiles; t += step) {
@@ -343,8 +376,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         }
       }
       if (ok)
-        Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + half * (BN / 2), v, buffer, lane);
+        Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + half * (BN / 2), v, store);
     }
+    bulk_wait_all();
   }
   tensor_fence_before();
   __syncthreads();
@@ -368,6 +402,24 @@ inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth,
                 const_cast<void*>(o.data), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Host: the tensor map of a matrix that is stored, [parts][workers][rows][columns], in boxes of 64 bytes of 32 rows.
+inline bool encode_result(void* data, int32_t dtype, int64_t columns, int64_t rows, int32_t workers, int32_t parts, int64_t ld,
+                          int64_t batch, int64_t part, CUtensorMap* out) {
+  const TensorMapEncoder encode = tensor_map_encoder();
+  if (!encode) return false;
+  const int64_t size = dtype == DQGAN_F32 ? 4 : 2;
+  const auto stride = [&](int64_t s, int count) { return (cuuint64_t)((count > 1 ? s : ld) * size); };
+  const cuuint64_t dims[4] = {(cuuint64_t)columns, (cuuint64_t)rows, (cuuint64_t)workers, (cuuint64_t)parts};
+  const cuuint64_t strides[3] = {(cuuint64_t)(ld * size), stride(batch, workers), stride(part, parts)};
+  const cuuint32_t boxes[4] = {(cuuint32_t)(64 / size), 32u, 1u, 1u};
+  const cuuint32_t steps[4] = {1u, 1u, 1u, 1u};
+  const CUtensorMapDataType type = dtype == DQGAN_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == DQGAN_F16  ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                         : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return encode(out, type, 4, data, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Fills what the kernel needs of a product; false where its sizes are beyond the kernel's.

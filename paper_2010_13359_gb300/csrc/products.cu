@@ -30,63 +30,64 @@ __device__ __forceinline__ void store_value(const StoreArgs& s, int worker, int6
   static_cast<T*>(s.out)[worker * s.out_batch + row * s.out_ld + column] = from_float<T>(x);
 }
 
-// The same of eight columns, in packs.
+// 32 values of a row, 16 bytes at a time, up to `count`.
 template <typename T>
-__device__ __forceinline__ void store8(const StoreArgs& s, int worker, int64_t row, int64_t column, float (&x)[8], const float (&bias)[8]) {
-  if (s.add) {
-    float a[8];
-    read8(s.add + worker * s.add_batch + row * s.add_ld + column, 8, true, a);
+__device__ __forceinline__ void add32(const T* from, int64_t count, float (&x)[32]) {
+  constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += a[i];
+  for (int i = 0; i < 32; i += E) {
+    if (i + E <= count) {
+      const uint4 pack = *reinterpret_cast<const uint4*>(from + i);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 v = pair_of<T>(pack, e);
+        x[i + e] += v.x;
+        x[i + e + 1] += v.y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (i + e < count) x[i + e] += to_float(from[i + e]);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] += bias[i];
-  if (s.pre) write8(x, static_cast<T*>(s.pre) + worker * s.pre_batch + row * s.pre_ld + column);
-  if (s.activation != DQGAN_NONE) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = activate<sizeof(T) == 4>(x[i], s.activation);
-  }
-  if (s.residual) {
-    float r[8];
-    read8(static_cast<const T*>(s.residual) + worker * s.residual_batch + row * s.residual_ld + column, 8, true, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] += r[i];
-  }
-  write8(x, static_cast<T*>(s.out) + worker * s.out_batch + row * s.out_ld + column);
 }
 
-// A warp's 32 rows, turned so that its lanes hold neighbouring columns: eight each where packs of 16 bytes can be
-// written (16384 rows of 4096 x 4096 in bf16: 275 us a product by packs, 620 by single values), else one.
+// A warp's 32 rows, by TMA where results are on 16-byte boundaries, else turned in shared memory and stored by single
+// values.
 template <typename T>
 struct StoreEpilogue {
   template <int BN>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], float* buffer, int lane) {
+                                             const float (&v)[BN / 2], TurnStore& store) {
     const StoreArgs& s = p.store;
+    const int lane = store.lane;
     const int rows = (int)min64(32, p.rows - row);
+    if (rows <= 0) return;
+    const float* const bias = s.bias ? s.bias + tile.worker * s.bias_batch : nullptr;
 #pragma unroll
     for (int g = 0; g < BN / 2; g += 32) {
-      if (column + g >= p.columns || rows <= 0) break;
-      turn_put(buffer, v + g, lane);
-      if (s.packs && column + g + 32 <= p.columns) {
-        const int64_t j = column + g + 8 * (lane & 3);
-        float bias[8] = {};
-        if (s.bias) {
+      const int64_t j = column + g, count = p.columns - j;
+      if (count <= 0) break;
+      float x[32];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) bias[i] = s.bias[tile.worker * s.bias_batch + j + i];
-        }
+      for (int i = 0; i < 32; ++i) x[i] = v[g + i];
+      const float b = bias && lane < count ? bias[j + lane] : 0.f;
+      if (s.packs) {
+        if (s.add && lane < rows) add32(s.add + tile.worker * s.add_batch + (row + lane) * s.add_ld + j, count, x);
+        if (bias) {
 #pragma unroll
-        for (int r = lane / 4; r < 32; r += 8) {
-          float x[8];
-          turned8(buffer, r, lane, x);
-          if (r < rows) store8<T>(s, tile.worker, row + r, j, x, bias);
+          for (int i = 0; i < 32; ++i) x[i] += __shfl_sync(kFullMask, b, i);
         }
+        if (s.pre) store.put32<T>(x, &p.pre, (int)j, (int)row, tile.worker);
+        activate_all<sizeof(T) == 4>(x, s.activation);
+        if (s.residual && lane < rows)
+          add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
+        store.put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
       } else {
-        const int64_t j = column + g + lane;
-        if (j < p.columns) {
-          const float bias = s.bias ? s.bias[tile.worker * s.bias_batch + j] : 0.f;
+        store.turn(x);
+        if (lane < count) {
 #pragma unroll 4
-          for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j, turned1(buffer, r, lane), bias);
+          for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j + lane, store.turned(r), b);
         }
       }
     }
@@ -97,7 +98,8 @@ struct StoreEpilogue {
 struct PartialEpilogue {
   template <int BN>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], float* buffer, int lane) {
+                                             const float (&v)[BN / 2], TurnStore& store) {
+    const int lane = store.lane;
     const int64_t ld = (int64_t)p.tiles_n * BN;
     float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * ProductShape<BN>::kRows + row + lane) * ld + column;
     if (row + lane < p.rows) {  // whole tiles
@@ -134,12 +136,18 @@ cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, 
   args.store = store;
   const int64_t size = store.out_dtype == DQGAN_F32 ? 4 : 2;
   const auto packs = [&](const void* at, int64_t ld, int64_t batch, int64_t of) {
-    return !at || (((uintptr_t)at & 15) == 0 && ld * of % 16 == 0 && (p.workers == 1 || batch * of % 16 == 0));
+    return !at || (((uintptr_t)at & 15) == 0 && ld * of % 16 == 0 && ld * of < ((int64_t)1 << 40) &&
+                   (p.workers == 1 || (batch * of % 16 == 0 && batch * of < ((int64_t)1 << 40))));
   };
   args.store.packs = packs(store.out, store.out_ld, store.out_batch, size) && packs(store.pre, store.pre_ld, store.pre_batch, size) &&
                      packs(store.residual, store.residual_ld, store.residual_batch, size) &&
                      packs(store.add, store.add_ld, store.add_batch, 4);
   args.splits = splits;
+  if (splits == 1 && args.store.packs &&
+      !(encode_result(store.out, store.out_dtype, p.columns, p.rows, p.workers, 1, store.out_ld, store.out_batch, 0, &args.out) &&
+        (!store.pre || encode_result(store.pre, store.out_dtype, p.columns, p.rows, p.workers, 1, store.pre_ld, store.pre_batch, 0,
+                                     &args.pre))))
+    return cudaErrorInvalidValue;
   if (splits == 1)
     return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });
   args.partial = static_cast<float*>(scratch);

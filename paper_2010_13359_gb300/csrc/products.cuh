@@ -46,7 +46,7 @@ struct StoreArgs {
   const float* add;      // fp32 values added to the sum (add + m * add_batch + i * add_ld + j), or nullptr; may be out
   int64_t add_batch, add_ld;
   int32_t activation;
-  bool packs;            // all of them can be read and written 16 bytes at a time (set by the launcher)
+  bool packs;            // all of them can be read and written 16 bytes at a time, and by TMA (set by the launcher)
 };
 
 struct SoftmaxArgs {
@@ -67,6 +67,7 @@ struct SoftmaxArgs {
 
 struct ProductArgs {
   CUtensorMap a, b;
+  CUtensorMap out, pre;     // results, where TMA can write them (pre: of StoreArgs)
   int64_t rows, columns;    // of D, per worker
   int32_t workers;
   int32_t kblocks;          // blocks of 64 of the contracted index
@@ -163,6 +164,19 @@ __device__ __forceinline__ float activate(float u, int activation) {
   }
   return u;
 }
+template <bool kExact, int N>
+__device__ __forceinline__ void activate_all(float (&x)[N], int activation) {
+  if (activation == DQGAN_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = activate<kExact>(x[i], DQGAN_GELU);
+  } else if (activation == DQGAN_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = activate<kExact>(x[i], DQGAN_SILU);
+  } else if (activation == DQGAN_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = activate<kExact>(x[i], DQGAN_RELU);
+  }
+}
 template <bool kExact>
 __device__ __forceinline__ float activation_slope(float u, int activation) {
   switch (activation) {
@@ -197,19 +211,6 @@ __device__ __forceinline__ void read8(const T* from, int count, bool packs, floa
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(from[i]) : 0.f;
-  }
-}
-
-// Eight values to 16-byte packs.
-template <typename T>
-__device__ __forceinline__ void write8(const float (&x)[8], T* to) {
-  constexpr int E = 16 / (int)sizeof(T);
-#pragma unroll
-  for (int i = 0; i < 8; i += E) {
-    uint4 pack;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) set_pair<T>(pack, e, make_float2(x[i + e], x[i + e + 1]));
-    *reinterpret_cast<uint4*>(to + i) = pack;
   }
 }
 

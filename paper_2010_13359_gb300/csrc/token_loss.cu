@@ -90,8 +90,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct StatsEpilogue {
   template <int BN>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], float*, int lane) {
+                                             float (&v)[BN / 2], TurnStore& store) {
     const SoftmaxArgs& s = p.softmax;
+    const int lane = store.lane;
     if (row + lane >= p.rows) return;
     const int64_t r = tile.worker * p.rows + row + lane;
     const int valid = (int)max64(0, min64(BN / 2, p.columns - column));
@@ -116,39 +117,44 @@ struct StatsEpilogue {
   }
 };
 
-// The gradient of the logits, in parts; turned as a stored product is.
+// The gradient of the logits, in parts.
 struct GradEpilogue {
   template <int BN>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], float* buffer, int lane) {
+                                             float (&v)[BN / 2], TurnStore& store) {
     const SoftmaxArgs& s = p.softmax;
+    const int lane = store.lane;
     const int64_t first = tile.worker * p.rows + row;
     int64_t target = -1;
     float lse = 0.f, factor = 0.f;
+    if (row >= p.rows) return;
     if (row + lane < p.rows) {
       target = counting_target(s, first + lane);
-      lse = s.lse[first + lane];
+      lse = s.lse[first + lane] * kLog2e;
       factor = s.weights ? s.scale * s.weights[first + lane] : s.scale;
     }
-    const int rows = (int)min64(32, p.rows - row);
     // the target's column here; -1: elsewhere; -2: the row does not count
     const int64_t place = target - s.first - column;
     const int t = target < 0 ? -2 : place >= 0 && place < BN / 2 ? (int)place : -1;
 #pragma unroll
     for (int g = 0; g < BN / 2; g += 32) {
-      if (column + g >= p.columns || rows <= 0) break;
+      if (column + g >= p.columns) break;
+      float x[32];
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
-        const float q = exp2_approx((v[g + j] - lse) * kLog2e);
-        v[g + j] = t == -2 ? 0.f : factor * (g + j == t ? q - 1.f : q);
+        const float q = exp2_approx(fmaf(v[g + j], kLog2e, -lse));
+        x[j] = t == -2 ? 0.f : factor * (g + j == t ? q - 1.f : q);
       }
-      turn_put(buffer, v + g, lane);
+      for (int part = 0; part < s.grad_parts; ++part) {
+        uint4 packs[4];
 #pragma unroll
-      for (int r = lane / 4; r < 32; r += 8) {
-        float x[8];
-        turned8(buffer, r, lane, x);
-        if (r < rows)
-          write_parts(x, s.grad, (first + r) * s.grad_ld + column + g + 8 * (lane & 3), s.grad_part, s.grad_parts, false);
+        for (int j = 0; j < 32; j += 2) {
+          __nv_bfloat162 both;
+          both.x = take_part(x[j]);
+          both.y = take_part(x[j + 1]);
+          reinterpret_cast<__nv_bfloat162*>(&packs[j / 8])[j % 8 / 2] = both;
+        }
+        store.put(packs, &p.out, (int)column + g, (int)row, tile.worker, part);
       }
     }
   }
@@ -196,6 +202,9 @@ cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool t
   ProductArgs args{};
   if (!(thin ? product_args<64>(p, 16, err, &args) : product_args<256>(p, 16, err, &args))) return cudaErrorInvalidValue;
   args.softmax = softmax;
+  if (softmax.grad && !encode_result(softmax.grad, DQGAN_BF16, p.columns, p.rows, p.workers, softmax.grad_parts, softmax.grad_ld,
+                                     p.rows * softmax.grad_ld, softmax.grad_part, &args.out))
+    return cudaErrorInvalidValue;
   return thin ? launch_product<64, Epilogue>(args, stream, launches) : launch_product<256, Epilogue>(args, stream, launches);
 }
 
@@ -225,7 +234,6 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
   soft.target_logit = c.target_logit;
   soft.lse = a.lse ? a.lse : c.lse;
   soft.scale = a.scale;
-  soft.grad = c.grad;
 
   // x: of the gradient, the rows that do not count as zeros, whatever they hold
   ProductOperand x_logits, x_grad;
@@ -287,6 +295,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
     if ((st = weights(first, count, logit_parts, half, &logits.b)) != cudaSuccess) return st;
     logits.terms = product_terms(logits.a.parts, logits.b.parts);
     soft.first = first;
+    soft.grad = c.grad;
     soft.grad_ld = piece;
     soft.grad_part = (int64_t)s.workers * a.rows * piece;
     soft.grad_parts = grad_parts(s);
