@@ -11,6 +11,8 @@
 // layers, takes as many as keep the products' error near 2^-17 (two parts) or
 // 2^-24 (three).  f16 values that do not lie as f16 in memory are two bf16 parts
 // (all of their 11 bits, at any exponent).
+#include <type_traits>
+
 #include "device_common.cuh"
 #include "products.cuh"
 
@@ -73,34 +75,64 @@ struct SlopeArgs {
   bool dy_packs, pre_packs;
 };
 
-// du of a block of rows and 256 columns, in parts, and the columns' sums.
-template <typename T>
-__global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
+// du of a block of rows and 256 columns, in parts, and the columns' sums.  Bound by memory: 8 bytes a value in bf16 with
+// GELU (dy, u, two parts).  Where rows are on 16-byte boundaries four of them a warp are on their way at once.
+template <typename T, bool kSlope>
+__global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
   dq_pdl_enter();
   __shared__ float turn[8][kGradColumns];
+  constexpr int kAhead = 4, E = 16 / (int)sizeof(T), kPacks = 8 / E;
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int64_t column = (int64_t)blockIdx.x * kGradColumns + lane * 8;
   const int64_t worker = blockIdx.z;
   const int64_t first = (int64_t)blockIdx.y * a.block_rows, last = min(first + a.block_rows, a.rows);
   const int count = (int)max((int64_t)0, min((int64_t)8, a.columns - column));
   float sum[8] = {};
+  const T* const dy = static_cast<const T*>(a.dy) + worker * a.rows * a.dy_ld + column;
+  const T* const pre = kSlope ? static_cast<const T*>(a.pre) + worker * a.rows * a.pre_ld + column : nullptr;
+  const auto row = [&](int64_t r, float (&x)[8], const float (&u)[8]) {
+    if constexpr (kSlope) scale_by_slope<sizeof(T) == 4>(x, u, a.activation);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i >= count) x[i] = 0.f;
+      sum[i] += x[i];
+    }
+    if (a.to) write_parts(x, a.to, (worker * a.rows + r) * a.ld + column, a.part, a.parts, a.half);
+  };
+  const auto unpack = [](const uint4 (&packs)[kPacks], float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float2 v = pair_of<T>(packs[i / E], i % E);
+      x[i] = v.x;
+      x[i + 1] = v.y;
+    }
+  };
+  int64_t r = first + warp;
+  if (count == 8 && a.dy_packs && (!kSlope || a.pre_packs)) {
+    for (; r + 8 * (kAhead - 1) < last; r += 8 * kAhead) {
+      uint4 d[kAhead][kPacks], p[kAhead][kPacks];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (int q = 0; q < kPacks; ++q) {
+          d[k][q] = reinterpret_cast<const uint4*>(dy + (r + 8 * k) * a.dy_ld)[q];
+          if constexpr (kSlope) p[k][q] = reinterpret_cast<const uint4*>(pre + (r + 8 * k) * a.pre_ld)[q];
+        }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        float x[8], u[8] = {};
+        unpack(d[k], x);
+        if constexpr (kSlope) unpack(p[k], u);
+        row(r + 8 * k, x, u);
+      }
+    }
+  }
   if (count > 0)
-    for (int64_t r = first + warp; r < last; r += 8) {
-      const int64_t row = worker * a.rows + r;
-      float x[8];
-      read8(static_cast<const T*>(a.dy) + row * a.dy_ld + column, count, a.dy_packs, x);
-      if (a.pre) {
-        float u[8];
-        read8(static_cast<const T*>(a.pre) + row * a.pre_ld + column, count, a.pre_packs, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= activation_slope<sizeof(T) == 4>(u[i], a.activation);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i >= count) x[i] = 0.f;
-        sum[i] += x[i];
-      }
-      if (a.to) write_parts(x, a.to, row * a.ld + column, a.part, a.parts, a.half);
+    for (; r < last; r += 8) {
+      float x[8], u[8] = {};
+      read8(dy + r * a.dy_ld, count, a.dy_packs, x);
+      if constexpr (kSlope) read8(pre + r * a.pre_ld, count, a.pre_packs, u);
+      row(r, x, u);
     }
   if (a.sums) {
 #pragma unroll
@@ -115,16 +147,108 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeArgs a) {
   }
 }
 
-// db: the blocks' sums in order.
+// db: the blocks' sums, eight warps in turn and then in order.
 __global__ void __launch_bounds__(256) bias_kernel(const float* sums, int blocks, int64_t columns, float* dbias,
                                                    int64_t g_stride, int accumulate) {
   dq_pdl_enter();
-  const int64_t j = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, worker = blockIdx.y;
-  if (j >= columns) return;
+  __shared__ double part[8][32];
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int64_t j = (int64_t)blockIdx.x * 32 + lane, worker = blockIdx.y;
   double s = 0.;
-  for (int b = 0; b < blocks; ++b) s += sums[(worker * blocks + b) * columns + j];
+  if (j < columns) {
+#pragma unroll 4
+    for (int b = warp; b < blocks; b += 8) s += sums[(worker * blocks + b) * columns + j];
+  }
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp > 0 || j >= columns) return;
+  for (int w = 1; w < 8; ++w) s += part[w][lane];
   float* const to = dbias + worker * g_stride + j;
   *to = accumulate ? *to + (float)s : (float)s;
+}
+
+// A few rows: what bounds them is the weights' bytes, each read once.  A warp takes two rows of W at a time, 16 bytes a
+// lane, and kRows rows of x beside them from L1; fp32 sums, no parts.  (One row of 4096 x 4096 in bf16: see the
+// tiles' kernel at 24 us.)
+template <typename T, typename E, int kRows, bool kPacks>
+__global__ void __launch_bounds__(256) few_rows_kernel(const T* x, int64_t x_ld, const E* weight, int64_t p_stride, int64_t inputs,
+                                                       int64_t outputs, int rows, const StoreArgs store) {
+  dq_pdl_enter();
+  constexpr int kOut = 2, kLane = 8;
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int64_t worker = blockIdx.y, first = ((int64_t)blockIdx.x * 8 + warp) * kOut;
+  if (first >= outputs) return;
+  x += worker * rows * x_ld;
+  weight += worker * p_stride + first * inputs;
+  const int outs = (int)min((int64_t)kOut, outputs - first);
+  float sum[kOut][kRows] = {};
+  if constexpr (kPacks) {
+#pragma unroll 4
+    for (int64_t k = lane * kLane; k < inputs; k += 32 * kLane) {  // whole packs: inputs is a multiple of eight
+      float w[kOut][8];
+#pragma unroll
+      for (int o = 0; o < kOut; ++o)
+        if (o < outs) read8(weight + o * inputs + k, 8, true, w[o]);
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        if (r >= rows) break;
+        float v[8];
+        read8(x + r * x_ld + k, 8, true, v);
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[o][r] = fmaf(w[o][i], v[i], sum[o][r]);
+      }
+    }
+  } else {
+#pragma unroll 4
+    for (int64_t k = lane; k < inputs; k += 32) {
+      float w[kOut];
+#pragma unroll
+      for (int o = 0; o < kOut; ++o) w[o] = o < outs ? to_float(weight[o * inputs + k]) : 0.f;
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        if (r >= rows) break;
+        const float v = to_float(x[r * x_ld + k]);
+#pragma unroll
+        for (int o = 0; o < kOut; ++o) sum[o][r] = fmaf(w[o], v, sum[o][r]);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 0; o < kOut; ++o)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum[o][r] += __shfl_xor_sync(kFullMask, sum[o][r], d);
+      if (lane == o * kRows + r && o < outs && r < rows)
+        store_value<T>(store, (int)worker, r, first + o, sum[o][r],
+                       store.bias ? store.bias[worker * store.bias_batch + first + o] : 0.f);
+    }
+}
+
+constexpr int kFewRows = 8;
+
+template <typename T, typename E>
+cudaError_t few_rows(const LinearArgs& a, const StoreArgs& store, cudaStream_t stream, uint64_t* launches) {
+  const LinearShape& s = a.shape;
+  const auto on_packs = [](const void* p, int64_t ld, int64_t batch, int64_t size) {
+    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && batch * size % 16 == 0;
+  };
+  const bool packs = s.inputs % 8 == 0 && on_packs(a.x, a.x_ld, 0, sizeof(T)) && on_packs(a.weight, s.inputs, a.p_stride, sizeof(E));
+  const auto run = [&](auto rows, auto in_packs) {
+    ++*launches;
+    return launch_pdl(few_rows_kernel<T, E, decltype(rows)::value, decltype(in_packs)::value>,
+                      dim3((unsigned)ceil_div(s.outputs, 16), (unsigned)s.workers), dim3(256), 0, stream,
+                      static_cast<const T*>(a.x), a.x_ld, static_cast<const E*>(a.weight), a.p_stride, s.inputs, s.outputs,
+                      (int)a.rows, store);
+  };
+  const auto by_rows = [&](auto in_packs) {
+    return a.rows == 1   ? run(std::integral_constant<int, 1>{}, in_packs)
+           : a.rows <= 4 ? run(std::integral_constant<int, 4>{}, in_packs)
+                         : run(std::integral_constant<int, kFewRows>{}, in_packs);
+  };
+  return packs ? by_rows(std::true_type{}) : by_rows(std::false_type{});
 }
 
 }  // namespace
@@ -135,17 +259,6 @@ cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint
   const LinearShape& s = a.shape;
   const Scratch c = scratch_of(s, a.scratch);
   const bool half = half_forward(s);
-  Product p;
-  p.rows = a.rows;
-  p.columns = s.outputs;
-  p.depth = s.inputs;
-  p.workers = s.workers;
-  const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
-  const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
-  cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.a);
-  if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
-  if (st != cudaSuccess) return st;
-  p.terms = product_terms(p.a.parts, p.b.parts);
   StoreArgs out{};
   out.out = a.y;
   out.out_ld = a.y_ld;
@@ -160,6 +273,22 @@ cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint
   out.bias = a.bias;
   out.bias_batch = a.b_stride;
   out.activation = s.activation;
+  if (a.rows <= kFewRows)
+    return with_dtype(s.dtype, [&](auto t) {
+      using T = decltype(t);
+      return s.weight_dtype == DQGAN_F32 ? few_rows<T, float>(a, out, stream, launches) : few_rows<T, T>(a, out, stream, launches);
+    });
+  Product p;
+  p.rows = a.rows;
+  p.columns = s.outputs;
+  p.depth = s.inputs;
+  p.workers = s.workers;
+  const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+  const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
+  cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.a);
+  if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
+  if (st != cudaSuccess) return st;
+  p.terms = product_terms(p.a.parts, p.b.parts);
   return launch_product_store(p, out, c.products, c.err, stream, launches);
 }
 
@@ -205,18 +334,19 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     k.to = direct ? nullptr : c.d;
     k.sums = a.dbias ? c.sums : nullptr;
     const int64_t wide = ceil_div(s.outputs, kGradColumns);
-    // four blocks an SM, of 64 rows at least
-    int64_t blocks = ceil_div((int64_t)sms * 4, wide * s.workers);
+    // eight blocks an SM, of 64 rows at least
+    int64_t blocks = ceil_div((int64_t)sms * 8, wide * s.workers);
     k.block_rows = (int32_t)(ceil_div(ceil_div(a.rows, blocks), kGradRows) * kGradRows);
     blocks = ceil_div(a.rows, k.block_rows);
     ++*launches;
     st = blocks > 65535 ? cudaErrorInvalidValue : with_dtype(s.dtype, [&](auto t) {
-      return launch_pdl(slope_kernel<decltype(t)>, dim3((unsigned)wide, (unsigned)blocks, (unsigned)s.workers), dim3(256), 0,
-                        stream, k);
+      const dim3 grid((unsigned)wide, (unsigned)blocks, (unsigned)s.workers);
+      return k.pre ? launch_pdl(slope_kernel<decltype(t), true>, grid, dim3(256), 0, stream, k)
+                   : launch_pdl(slope_kernel<decltype(t), false>, grid, dim3(256), 0, stream, k);
     });
     if (st == cudaSuccess && a.dbias) {
       ++*launches;
-      st = launch_pdl(bias_kernel, dim3((unsigned)ceil_div(s.outputs, 256), (unsigned)s.workers), dim3(256), 0, stream,
+      st = launch_pdl(bias_kernel, dim3((unsigned)ceil_div(s.outputs, 32), (unsigned)s.workers), dim3(256), 0, stream,
                       (const float*)c.sums, (int)blocks, s.outputs, a.dbias, a.g_stride, a.accumulate);
     }
     if (!direct) {

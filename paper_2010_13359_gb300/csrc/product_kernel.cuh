@@ -153,7 +153,7 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t at, bool across)
 
 // What a warp has ready of its 32 rows, 64 bytes of a row at a time, goes through two buffers of shared memory in turn
 // and from there by TMA.  Lane l holds row l; its packs of 16 bytes stand in the order of the 64-byte swizzle, in which
-// eight lanes' packs meet in no bank.  What lies outside the matrix is not written.
+// eight lanes' packs meet in no bank.  Rows outside the matrix are not written, and columns by 16 bytes.
 struct TurnStore {
   uint8_t* buffer;  // 2 x 2048 bytes
   int lane;
@@ -194,6 +194,7 @@ struct TurnStore {
   // single values, for matrices that TMA cannot write: column l of row r, from 32 columns that lane r holds
   __device__ __forceinline__ void turn(const float (&x)[32]) {
     float* const to = reinterpret_cast<float*>(buffer);
+    if (lane == 0) bulk_wait_read_all();
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < 8; ++c)
@@ -206,28 +207,48 @@ struct TurnStore {
 };
 
 struct ProductTile {
-  int worker, split;
+  int worker;
   int64_t row, column;  // of the tile's first result
   int begin, end;       // blocks of the contracted index
+  int64_t piece;        // of a split tile: its place among all pieces; else -1
 };
 
+// Item t of the walk: the whole tiles, then the pieces of the split ones.
 template <int BN>
 __device__ __forceinline__ ProductTile product_tile(const ProductArgs& p, int64_t t) {
   ProductTile tile;
-  const int per_split = p.tiles_m * p.tiles_n;
-  const int64_t which = t / per_split;
-  const int in = (int)(t - which * per_split);
-  tile.split = (int)(which % p.splits);
-  tile.worker = (int)(which / p.splits);
+  int piece = 0, pieces = 1;
+  tile.piece = -1;
+  if (t >= p.whole) {
+    tile.piece = t - p.whole;
+    pieces = p.pieces;
+    piece = (int)(tile.piece % pieces);
+    t = p.whole + tile.piece / pieces;
+  }
+  const int per_worker = p.tiles_m * p.tiles_n;
+  tile.worker = (int)(t / per_worker);
+  const int in = (int)(t - (int64_t)tile.worker * per_worker);
   // eight rows of tiles at a time: what runs at once shares operands in L2
   constexpr int kGroup = 8;
   const int group = in / (kGroup * p.tiles_n), left = in - group * kGroup * p.tiles_n;
   const int high = p.tiles_m - group * kGroup < kGroup ? p.tiles_m - group * kGroup : kGroup;
   tile.row = (int64_t)(group * kGroup + left % high) * ProductShape<BN>::kRows;
   tile.column = (int64_t)(left / high) * BN;
-  tile.begin = (int)((int64_t)p.kblocks * tile.split / p.splits);
-  tile.end = (int)((int64_t)p.kblocks * (tile.split + 1) / p.splits);
+  tile.begin = (int)((int64_t)p.kblocks * piece / pieces);
+  tile.end = (int)((int64_t)p.kblocks * (piece + 1) / pieces);
   return tile;
+}
+
+// Items of a product: whole tiles, and pieces.
+__host__ __device__ inline int64_t product_items(const ProductArgs& p) {
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.workers;
+  return p.whole + (tiles - p.whole) * p.pieces;
+}
+
+// Where a warp keeps its sums of a piece: four columns of 32 rows after another.
+template <int BN>
+__device__ __forceinline__ float4* piece_sums(const ProductArgs& p, int64_t piece, int rank, int warp, int lane) {
+  return reinterpret_cast<float4*>(p.partial) + ((piece * ProductShape<BN>::kPair + rank) * 8 + warp) * (32 * BN / 8) + lane;
 }
 
 template <int BN, typename Epilogue>
@@ -267,7 +288,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   tensor_fence_after();
   const uint32_t sums = *at_shared;
 
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
+  const int64_t tiles = product_items(p);
   const int64_t first = blockIdx.x / S::kPair, step = gridDim.x / S::kPair;
   const int terms = p.terms.count;
   if (warp < 4) {
@@ -375,8 +396,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             mbar_arrive(sum_empty + (c & 1));
         }
       }
-      if (ok)
+      if (!ok) break;
+      if (tile.piece >= 0) {
+        float4* const to = piece_sums<BN>(p, tile.piece, rank, warp - 4, lane);
+#pragma unroll
+        for (int j = 0; j < BN / 8; ++j) to[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      } else {
         Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + half * (BN / 2), v, store);
+      }
     }
     bulk_wait_all();
   }
@@ -385,6 +412,35 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   if constexpr (kPair == 2) pair_barrier();
   tensor_fence_after();
   if (warp == 2) tensor_memory_free<kPair>(sums, kColumns);
+}
+
+// The pieces' sums of the split tiles in order, and what is done with them.  A block a tile and half of a pair.
+template <int BN, typename Epilogue>
+__global__ void __launch_bounds__(256, 1) join_kernel(const __grid_constant__ ProductArgs p) {
+  dq_pdl_enter();
+  using S = ProductShape<BN>;
+  __shared__ __align__(1024) uint8_t turn[S::kTurnBytes];
+  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int rank = (int)blockIdx.x % S::kPair;
+  const int64_t first = (int64_t)(blockIdx.x / S::kPair) * p.pieces;
+  const ProductTile tile = product_tile<BN>(p, p.whole + first);
+  float v[BN / 2];
+#pragma unroll
+  for (int i = 0; i < BN / 2; ++i) v[i] = 0.f;
+  for (int piece = 0; piece < p.pieces; ++piece) {
+    const float4* const from = piece_sums<BN>(p, first + piece, rank, warp, lane);
+#pragma unroll
+    for (int j = 0; j < BN / 8; ++j) {
+      const float4 x = from[32 * j];
+      v[4 * j] = __fadd_rn(v[4 * j], x.x);
+      v[4 * j + 1] = __fadd_rn(v[4 * j + 1], x.y);
+      v[4 * j + 2] = __fadd_rn(v[4 * j + 2], x.z);
+      v[4 * j + 3] = __fadd_rn(v[4 * j + 3], x.w);
+    }
+  }
+  TurnStore store{turn + warp * 4096, lane};
+  Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * (warp & 3), tile.column + warp / 4 * (BN / 2), v, store);
+  bulk_wait_all();
 }
 
 // Host: the tensor map of an operand.  Boxes of 64 of the contracted index and a block's `tile` rows, or of 64 x 64.
@@ -430,7 +486,6 @@ inline bool product_args(const Product& p, int chunk, uint32_t* err, ProductArgs
   out->workers = p.workers;
   out->kblocks = (int32_t)ceil_div(p.depth, kBlockDepth);
   out->chunk = chunk;
-  out->splits = 1;
   out->tiles_m = (int32_t)ceil_div(p.rows, ProductShape<BN>::kRows);
   out->tiles_n = (int32_t)ceil_div(p.columns, BN);
   out->terms = p.terms;
@@ -440,6 +495,8 @@ inline bool product_args(const Product& p, int chunk, uint32_t* err, ProductArgs
   out->b_shared = p.b.shared;
   out->half = p.a.half;
   out->err = err;
+  out->whole = (int64_t)out->tiles_m * out->tiles_n * p.workers;
+  out->pieces = 1;
   return p.rows <= INT32_MAX && p.columns <= INT32_MAX && p.depth <= INT32_MAX &&
          (int64_t)out->tiles_m * out->tiles_n <= INT32_MAX &&
          encode_operand(p.a, p.rows, p.depth, p.workers, kTileRows, &out->a) &&
@@ -483,12 +540,16 @@ template <int BN, typename Epilogue>
 inline cudaError_t launch_product(const ProductArgs& p, cudaStream_t stream, uint64_t* launches) {
   using S = ProductShape<BN>;
   int slots = 0;
-  const cudaError_t st = product_slots<BN, Epilogue>(&slots);
+  cudaError_t st = product_slots<BN, Epilogue>(&slots);
   if (st != cudaSuccess) return st;
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits * p.workers;
-  const int grid = (int)(tiles < slots ? tiles : slots) * S::kPair;
+  const int64_t items = product_items(p);
+  const int grid = (int)(items < slots ? items : slots) * S::kPair;
   ++*launches;
-  return launch_pdl_cluster(product_kernel<BN, Epilogue>, S::kPair, dim3(grid), dim3(kProductThreads), S::kSmem, stream, p);
+  st = launch_pdl_cluster(product_kernel<BN, Epilogue>, S::kPair, dim3(grid), dim3(kProductThreads), S::kSmem, stream, p);
+  const int64_t split = (int64_t)p.tiles_m * p.tiles_n * p.workers - p.whole;
+  if (st != cudaSuccess || split == 0) return st;
+  ++*launches;
+  return launch_pdl(join_kernel<BN, Epilogue>, dim3((unsigned)(split * S::kPair)), dim3(256), 0, stream, p);
 }
 
 }  // namespace dq

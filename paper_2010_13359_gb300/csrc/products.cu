@@ -19,17 +19,6 @@ ProductTerms product_terms(int a_parts, int b_parts) {
 
 namespace {
 
-template <typename T>
-__device__ __forceinline__ void store_value(const StoreArgs& s, int worker, int64_t row, int64_t column, float x, float bias) {
-  if (s.add) x += s.add[worker * s.add_batch + row * s.add_ld + column];
-  x += bias;
-  if (s.pre) static_cast<T*>(s.pre)[worker * s.pre_batch + row * s.pre_ld + column] = from_float<T>(x);
-  x = activate<sizeof(T) == 4>(x, s.activation);
-  if (s.residual)
-    x += to_float(static_cast<const T*>(s.residual)[worker * s.residual_batch + row * s.residual_ld + column]);
-  static_cast<T*>(s.out)[worker * s.out_batch + row * s.out_ld + column] = from_float<T>(x);
-}
-
 // 32 values of a row, 16 bytes at a time, up to `count`.
 template <typename T>
 __device__ __forceinline__ void add32(const T* from, int64_t count, float (&x)[32]) {
@@ -72,7 +61,7 @@ struct StoreEpilogue {
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = v[g + i];
       const float b = bias && lane < count ? bias[j + lane] : 0.f;
-      if (s.packs) {
+      if (s.packs && (count >= 32 || p.columns * (int)sizeof(T) % 16 == 0)) {
         if (s.add && lane < rows) add32(s.add + tile.worker * s.add_batch + (row + lane) * s.add_ld + j, count, x);
         if (bias) {
 #pragma unroll
@@ -94,46 +83,51 @@ struct StoreEpilogue {
   }
 };
 
-// Sums of one piece of the contracted index, for join_kernel.
-struct PartialEpilogue {
-  template <int BN>
-  static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             const float (&v)[BN / 2], TurnStore& store) {
-    const int lane = store.lane;
-    const int64_t ld = (int64_t)p.tiles_n * BN;
-    float* const to = p.partial + (((int64_t)tile.split * p.workers + tile.worker) * p.tiles_m * ProductShape<BN>::kRows + row + lane) * ld + column;
-    if (row + lane < p.rows) {  // whole tiles
-#pragma unroll
-      for (int j = 0; j < BN / 2; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-    }
-  }
+// How a product is cut: tiles of 256 x 256 for pairs of blocks, or of 128 x 64 for single ones; and of the tiles
+// that do not fill the GPU for a last time, the contracted index in pieces.
+struct Cut {
+  int width;
+  int64_t whole;
+  int pieces;
 };
 
-// The pieces' sums in order, and what is done with them.
-template <typename T, int BN>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs p) {
-  dq_pdl_enter();
-  const int64_t ld = (int64_t)p.tiles_n * BN, tall = (int64_t)p.tiles_m * ProductShape<BN>::kRows;
-  const int64_t column = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (column >= p.columns) return;
-  for (int64_t r = blockIdx.y; r < p.rows * p.workers; r += gridDim.y) {
-    const int worker = (int)(r / p.rows);
-    const int64_t row = r - worker * p.rows;
-    const float* from = p.partial + (worker * tall + row) * ld + column;
-    float x = 0.f;
-    for (int s = 0; s < p.splits; ++s, from += p.workers * tall * ld) x += *from;
-    store_value<T>(p.store, worker, row, column, x,
-                   p.store.bias ? p.store.bias[worker * p.store.bias_batch + column] : 0.f);
+// By the time that the busiest block needs, in units of a block of 64 of the contracted index of a 256 x 256 tile (0.3 us).  A
+// tile's end costs as much as 12 of them (3 of a narrow tile, whose blocks take 0.6: 24 KB to load instead of 32); pieces
+// cost a second kernel, 10, their sums' way through memory, 0.3 each, and one load after another there, 1 for each of a tile's.
+Cut cut_product(const Product& p, int64_t slots) {
+  const int64_t depth = ceil_div(p.depth, kBlockDepth), length = depth * p.terms.count;
+  Cut best{256, 0, 1};
+  double least = 1e300;
+  for (int width = 64; width <= 256; width += 192) {
+    const bool wide = width == 256;
+    const int64_t tiles = ceil_div(p.rows, wide ? 256 : 128) * ceil_div(p.columns, width) * p.workers;
+    const int64_t at_once = wide ? slots / 2 : slots, rest = tiles % at_once, whole = tiles - rest;
+    const double block = wide ? 1. : 0.6, end = wide ? 12. : 3., sums = wide ? 0.3 : 0.04;
+    for (int pieces = 1; pieces <= 32 && pieces <= depth; ++pieces) {
+      const int64_t items = rest * pieces;
+      if (pieces > 1 && (rest == 0 || (size_t)items * (wide ? 1 << 18 : 1 << 15) > kProductScratch)) break;
+      double time = (double)(whole / at_once) * (length * block + end) +
+                    (double)ceil_div(items, at_once) * (ceil_div(depth, pieces) * p.terms.count * block + end);
+      if (pieces > 1) time += 10. + items * sums + pieces;
+      if (time < least) {
+        least = time;
+        best = {width, pieces > 1 ? whole : tiles, pieces};
+      }
+    }
   }
+  return best;
 }
 
 template <int BN>
-cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, void* scratch, uint32_t* err,
+cudaError_t store_product(const Product& p, const StoreArgs& store, const Cut& cut, void* scratch, uint32_t* err,
                           cudaStream_t stream, uint64_t* launches) {
   ProductArgs args{};
   const int chunk = store.out_dtype == DQGAN_F32 ? 16 : store.out_dtype == DQGAN_F16 ? 32 : 128;
   if (!product_args<BN>(p, chunk, err, &args)) return cudaErrorInvalidValue;
   args.store = store;
+  args.whole = cut.whole;
+  args.pieces = cut.pieces;
+  args.partial = static_cast<float*>(scratch);
   const int64_t size = store.out_dtype == DQGAN_F32 ? 4 : 2;
   const auto packs = [&](const void* at, int64_t ld, int64_t batch, int64_t of) {
     return !at || (((uintptr_t)at & 15) == 0 && ld * of % 16 == 0 && ld * of < ((int64_t)1 << 40) &&
@@ -142,22 +136,12 @@ cudaError_t store_product(const Product& p, const StoreArgs& store, int splits, 
   args.store.packs = packs(store.out, store.out_ld, store.out_batch, size) && packs(store.pre, store.pre_ld, store.pre_batch, size) &&
                      packs(store.residual, store.residual_ld, store.residual_batch, size) &&
                      packs(store.add, store.add_ld, store.add_batch, 4);
-  args.splits = splits;
-  if (splits == 1 && args.store.packs &&
+  if (args.store.packs &&
       !(encode_result(store.out, store.out_dtype, p.columns, p.rows, p.workers, 1, store.out_ld, store.out_batch, 0, &args.out) &&
         (!store.pre || encode_result(store.pre, store.out_dtype, p.columns, p.rows, p.workers, 1, store.pre_ld, store.pre_batch, 0,
                                      &args.pre))))
     return cudaErrorInvalidValue;
-  if (splits == 1)
-    return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });
-  args.partial = static_cast<float*>(scratch);
-  const cudaError_t st = launch_product<BN, PartialEpilogue>(args, stream, launches);
-  if (st != cudaSuccess) return st;
-  ++*launches;
-  const dim3 grid((unsigned)ceil_div(p.columns, 256), (unsigned)min64(p.rows * p.workers, 65535));
-  return with_dtype(store.out_dtype, [&](auto t) {
-    return launch_pdl(join_kernel<decltype(t), BN>, grid, dim3(256), 0, stream, args);
-  });
+  return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });
 }
 
 }  // namespace
@@ -166,15 +150,10 @@ cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void*
                                  cudaStream_t stream, uint64_t* launches) {
   if (p.rows == 0 || p.columns == 0) return cudaSuccess;
   const int sms = device_sms();
-  if (sms <= 0) return cudaErrorInvalidDevice;
-  const int64_t wide = ceil_div(p.rows, kTileRows) * ceil_div(p.columns, 256) * p.workers;
-  if (wide >= sms / 2) return store_product<256>(p, store, 1, scratch, err, stream, launches);
-  // Few tiles: narrow ones, and the contracted index in pieces of at least 8 blocks.
-  const int64_t tiles = ceil_div(p.rows, kTileRows) * ceil_div(p.columns, 64) * p.workers;
-  int64_t splits = scratch ? min64(sms / tiles, ceil_div(p.depth, kBlockDepth) * p.terms.count / 8) : 1;
-  while (splits > 1 && (size_t)(splits * tiles) * kTileRows * 64 * 4 > kProductScratch) --splits;
-  splits = min64(splits, ceil_div(p.depth, kBlockDepth));
-  return store_product<64>(p, store, splits < 1 ? 1 : (int)splits, scratch, err, stream, launches);
+  if (sms <= 1) return cudaErrorInvalidDevice;
+  const Cut cut = cut_product(p, sms);
+  return cut.width == 256 ? store_product<256>(p, store, cut, scratch, err, stream, launches)
+                          : store_product<64>(p, store, cut, scratch, err, stream, launches);
 }
 
 // ---- parts ----

@@ -72,11 +72,12 @@ struct ProductArgs {
   int32_t workers;
   int32_t kblocks;          // blocks of 64 of the contracted index
   int32_t chunk;            // terms of 64 that one accumulator in tensor memory sums
-  int32_t splits;           // pieces of the contracted index that are summed apart
+  int32_t pieces;           // of the contracted index, that are summed apart in the tiles from `whole` on
+  int64_t whole;
   int32_t tiles_m, tiles_n;
   ProductTerms terms;
   uint8_t a_across, b_across, a_shared, b_shared, half;
-  float* partial;           // splits > 1: [split][worker][rows of whole tiles][columns of whole tiles]
+  float* partial;           // the pieces' sums
   uint32_t* err;
   StoreArgs store;
   SoftmaxArgs softmax;
@@ -89,10 +90,10 @@ struct Product {
   ProductTerms terms;
 };
 
-// Scratch of the products of one operator: partial sums of products that are split.
-constexpr size_t kProductScratch = (size_t)40 << 20;
+// Scratch of the products of one operator: the sums of pieces.
+constexpr size_t kProductScratch = (size_t)80 << 20;
 
-// `splittable`: kProductScratch bytes at scratch, or nullptr.
+// scratch: kProductScratch bytes.
 cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void* scratch, uint32_t* err,
                                  cudaStream_t stream, uint64_t* launches);
 // Rows of a matrix turned into 16-bit parts, [part][worker][row][ld] with ld a
@@ -193,6 +194,21 @@ __device__ __forceinline__ float activation_slope(float u, int activation) {
   return 1.f;
 }
 
+// x times the slope at u.
+template <bool kExact, int N>
+__device__ __forceinline__ void scale_by_slope(float (&x)[N], const float (&u)[N], int activation) {
+  if (activation == DQGAN_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= activation_slope<kExact>(u[i], DQGAN_GELU);
+  } else if (activation == DQGAN_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= activation_slope<kExact>(u[i], DQGAN_SILU);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= activation_slope<kExact>(u[i], DQGAN_RELU);
+  }
+}
+
 // Eight values of a row, 16 bytes at a time where `packs` says that rows allow it; 0 from `count` on.
 template <typename T>
 __device__ __forceinline__ void read8(const T* from, int count, bool packs, float (&x)[8]) {
@@ -245,6 +261,18 @@ __device__ __forceinline__ void write_parts(float (&x)[8], void* to, int64_t at,
     }
     *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(to) + q * part + at) = pack;
   }
+}
+
+// One result: the sum of a product, and what is done with it.
+template <typename T>
+__device__ __forceinline__ void store_value(const StoreArgs& s, int worker, int64_t row, int64_t column, float x, float bias) {
+  if (s.add) x += s.add[worker * s.add_batch + row * s.add_ld + column];
+  x += bias;
+  if (s.pre) static_cast<T*>(s.pre)[worker * s.pre_batch + row * s.pre_ld + column] = from_float<T>(x);
+  x = activate<sizeof(T) == 4>(x, s.activation);
+  if (s.residual)
+    x += to_float(static_cast<const T*>(s.residual)[worker * s.residual_batch + row * s.residual_ld + column]);
+  static_cast<T*>(s.out)[worker * s.out_batch + row * s.out_ld + column] = from_float<T>(x);
 }
 
 // A matrix of the caller's: worker m's row r at data + m * batch + r * ld.

@@ -71,6 +71,11 @@ LINEAR = [  # workers, rows, inputs, outputs, dtype, weight dtype, activation, p
     (2, 900, 300, 2100, 0, 0, 2, 0, 0, True),
     (16, 33, 96, 160, 2, 2, 0, 0, 0, False),
     (1, 20000, 48, 24, 1, 1, 0, 0, 0, False),
+    (2, 70, 61, 125, 1, 1, 2, 3, 0, False),
+    (1, 300, 509, 1021, 2, 2, 0, 3, 0, False),
+    (1, 1400, 1021, 2301, 1, 1, 1, 3, 0, False),
+    (2, 8, 4104, 77, 1, 0, 3, 0, 0, False),
+    (1, 9, 2050, 130, 0, 0, 0, 2, 0, False),
 ]
 
 
