@@ -96,24 +96,35 @@ struct StatsEpilogue {
     if (row + lane >= p.rows) return;
     const int64_t r = tile.worker * p.rows + row + lane;
     const int valid = (int)max64(0, min64(BN / 2, p.columns - column));
-    float most = -INFINITY, sum = 0.f;
+    if (valid < BN / 2) {
 #pragma unroll
-    for (int j = 0; j < BN / 2; ++j) {
-      if (j >= valid) v[j] = -INFINITY;
-      most = fmaxf(most, v[j]);
+      for (int j = 0; j < BN / 2; ++j)
+        if (j >= valid) v[j] = -INFINITY;
     }
-    const float from = most == -INFINITY ? 0.f : most;
+    float four[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < BN / 2; ++j) four[j & 3] = fmaxf(four[j & 3], v[j]);
+    const float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
     const int64_t place = counting_target(s, r) - s.first - column;
     const int t = place >= 0 && place < valid ? (int)place : -1;
-    float z = 0.f;
+    if (t >= 0) {  // one row of 250 here, where the vocabulary has 32,000 entries
+      float z = 0.f;
 #pragma unroll
-    for (int j = 0; j < BN / 2; ++j) {
-      sum += exp2_approx((v[j] - from) * kLog2e);
-      z = t == j ? v[j] : z;
+      for (int j = 0; j < BN / 2; ++j) z += t == j ? v[j] : 0.f;
+      s.target_logit[r] = z;
     }
+    const float from = (most == -INFINITY ? 0.f : most) * -kLog2e;
+    float2 sums[2] = {};
+#pragma unroll
+    for (int j = 0; j < BN / 2; j += 4) {
+      const float2 a = fma2(make_float2(v[j], v[j + 1]), both(kLog2e), both(from));
+      const float2 b = fma2(make_float2(v[j + 2], v[j + 3]), both(kLog2e), both(from));
+      sums[0] = add2(sums[0], make_float2(exp2_approx(a.x), exp2_approx(a.y)));
+      sums[1] = add2(sums[1], make_float2(exp2_approx(b.x), exp2_approx(b.y)));
+    }
+    const float2 sum = add2(sums[0], sums[1]);
     const int slot = s.slot + (int)(column / (BN / 2));
-    s.stats[((int64_t)tile.worker * s.slots + slot) * p.rows + row + lane] = make_float2(most, sum);
-    if (t >= 0) s.target_logit[r] = z;
+    s.stats[((int64_t)tile.worker * s.slots + slot) * p.rows + row + lane] = make_float2(most, sum.x + sum.y);
   }
 };
 
@@ -133,26 +144,34 @@ struct GradEpilogue {
       lse = s.lse[first + lane] * kLog2e;
       factor = s.weights ? s.scale * s.weights[first + lane] : s.scale;
     }
-    // the target's column here; -1: elsewhere; -2: the row does not count
+    if (target < 0) factor = 0.f;  // the row does not count: see below where its logits are not finite
     const int64_t place = target - s.first - column;
-    const int t = target < 0 ? -2 : place >= 0 && place < BN / 2 ? (int)place : -1;
+    const int t = target >= 0 && place >= 0 && place < BN / 2 ? (int)place : -1;
 #pragma unroll
     for (int g = 0; g < BN / 2; g += 32) {
       if (column + g >= p.columns) break;
-      float x[32];
+      float2 x[16];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) {
-        const float q = exp2_approx(fmaf(v[g + j], kLog2e, -lse));
-        x[j] = t == -2 ? 0.f : factor * (g + j == t ? q - 1.f : q);
+      for (int j = 0; j < 16; ++j) {
+        const float2 e = fma2(make_float2(v[g + 2 * j], v[g + 2 * j + 1]), both(kLog2e), both(-lse));
+        x[j] = mul2(make_float2(exp2_approx(e.x), exp2_approx(e.y)), both(factor));
+      }
+      if (__any_sync(kFullMask, target < 0 || (t >= g && t < g + 32))) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (t == g + 2 * j) x[j].x -= factor;
+          if (t == g + 2 * j + 1) x[j].y -= factor;
+          if (target < 0) x[j] = make_float2(0.f, 0.f);
+        }
       }
       for (int part = 0; part < s.grad_parts; ++part) {
         uint4 packs[4];
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          __nv_bfloat162 both;
-          both.x = take_part(x[j]);
-          both.y = take_part(x[j + 1]);
-          reinterpret_cast<__nv_bfloat162*>(&packs[j / 8])[j % 8 / 2] = both;
+        for (int j = 0; j < 16; ++j) {
+          const __nv_bfloat162 h = __float22bfloat162_rn(x[j]);
+          const uint32_t bits = reinterpret_cast<const uint32_t&>(h);
+          reinterpret_cast<uint32_t*>(&packs[j / 4])[j % 4] = bits;
+          x[j] = add2(x[j], make_float2(-__uint_as_float(bits << 16), -__uint_as_float(bits & 0xffff0000u)));
         }
         store.put(packs, &p.out, (int)column + g, (int)row, tile.worker, part);
       }
@@ -160,35 +179,42 @@ struct GradEpilogue {
   }
 };
 
-// A row's lse and loss from its slots: eight warps take them in turn, joined in order.
+// A row's lse and loss from its slots: eight warps take 32 rows' slots in turn, four loads at once, joined in order.
 __global__ void __launch_bounds__(256) join_stats_kernel(const SoftmaxArgs s, int64_t rows, int32_t workers, float* loss,
                                                          float* lse) {
   dq_pdl_enter();
   __shared__ float2 part[8][32];
+  constexpr int kAhead = 8;
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int64_t r = (int64_t)blockIdx.x * 32 + lane;
   float most = -INFINITY, sum = 0.f;
+  // sums of exponentials from one maximum to another's; of -inf nothing has been added
+  const auto scale = [](float from, float to) { return from == to ? 1.f : exp2_approx((from - to) * kLog2e); };
   const auto join = [&](float2 x) {
-    if (x.x > most) {
-      sum = sum * exp2f((most - x.x) * kLog2e) + x.y;
-      most = x.x;
-    } else if (x.x == most) {
-      sum += x.y;
-    } else {
-      // a NaN maximum cannot be: the sum holds it
-      sum = fmaf(x.y, exp2f((x.x - most) * kLog2e), sum);
-    }
+    const float top = fmaxf(most, x.x);
+    sum = sum * scale(most, top) + x.y * scale(x.x, top);
+    most = top;
   };
   if (r < rows * workers) {
     const int64_t worker = r / rows, row = r - worker * rows;
-    for (int i = warp; i < s.slots; i += 8) join(s.stats[(worker * s.slots + i) * rows + row]);
+    const float2* const from = s.stats + worker * s.slots * rows + row;
+    for (int i = warp; i < s.slots; i += 8 * kAhead) {
+      float2 x[kAhead];
+      float top = most;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) x[k] = i + 8 * k < s.slots ? from[(i + 8 * k) * rows] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) top = fmaxf(top, x[k].x);
+      sum *= scale(most, top);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) sum = fmaf(x[k].y, scale(x[k].x, top), sum);
+      most = top;
+    }
   }
   part[warp][lane] = make_float2(most, sum);
   __syncthreads();
   if (warp > 0 || r >= rows * workers) return;
-  most = -INFINITY;
-  sum = 0.f;
-  for (int w = 0; w < 8; ++w) join(part[w][lane]);
+  for (int w = 1; w < 8; ++w) join(part[w][lane]);
   const bool counts = counting_target(s, r) >= 0;
   const float all = most + logf(sum);
   const float c = s.weights ? s.weights[r] : 1.f;
