@@ -579,7 +579,7 @@ typedef struct dqgan_operator dqgan_operator;
 /* Create an operator on the current device, with its scratch space (layer
  * norm and embedding: for the gradients; distillation has none; linear: its operands as the
  * tensor cores read them; token loss: besides those a piece of the logits' gradient, up to
- * 512 MB; clipping: the blocks' sums).  On error
+ * 1 GB; clipping: the blocks' sums).  On error
  * *out is NULL, dqgan_operator_last_error(NULL) holds the reason and nothing
  * stays allocated.  The test hook DQGAN_TEST_FAIL_ALLOC of dqgan_create
  * applies here too. */

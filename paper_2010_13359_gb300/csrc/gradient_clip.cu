@@ -4,9 +4,9 @@
 //   n = sqrt(sum over all tensors of g^2);  out = min(1, max_norm / (n + eps)) g
 //
 // Two passes, bound by memory: the norm reads every value, the clipping reads it
-// again and writes it.  Both cut the tensors into units of 16,384 values and give
-// each block a run of them; the second pass walks them backwards, so that it finds
-// in L2 what the first one read last.
+// again and writes it.  Both cut the tensors into units of up to 16,384 values and
+// give each block a run of them; the second pass walks them backwards, so that it
+// finds in L2 what the first one read last.
 //
 // A block's thread sums the squares of at most 64 values of a unit in fp32, then in
 // fp64, and the blocks' sums are joined in a fixed order.  Where a thread's fp32 sum
@@ -18,7 +18,7 @@ namespace dq {
 
 namespace {
 
-constexpr int kClipThreads = 256, kUnit = 16384;
+constexpr int kClipThreads = 256, kMostUnit = 16384, kLeastUnit = 2048;
 constexpr int kTableTensors = 640;  // of one launch: kernel parameters are limited to 32,764 bytes
 constexpr int kMaxTables = 8;
 constexpr int kClipBlocks = 152 * 4;
@@ -39,8 +39,10 @@ struct ClipLaunch {
 struct ClipArgs {
   ClipLaunch tables[kMaxTables];
   int32_t count_tables, table;
+  int32_t norm_table;  // the first that has units: its second pass writes the norms
   int32_t workers;
   int32_t count;  // tensors of this table
+  int32_t unit;   // values
   double max_norm, eps;
   float* norms;
 };
@@ -137,8 +139,8 @@ __global__ void __launch_bounds__(kClipThreads) norm_kernel(const __grid_constan
   for (int64_t u = begin; u < end; ++u) {
     const int64_t worker = u / l.units, unit = u - worker * l.units;
     const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
-    const int64_t at = (unit - t.unit) * kUnit;
-    sum += unit_squares(static_cast<const T*>(t.from) + worker * t.from_stride + at, (int)min64(kUnit, t.size - at));
+    const int64_t at = (unit - t.unit) * a.unit;
+    sum += unit_squares(static_cast<const T*>(t.from) + worker * t.from_stride + at, (int)min64(a.unit, t.size - at));
     if (u + 1 == end || unit + 1 == l.units) {
       const double total = block_sum_double(sum, shared);
       if (threadIdx.x == 0) l.sums[blockIdx.x + worker] = total;
@@ -182,6 +184,7 @@ __device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float fa
   if ((int)threadIdx.x < head) one(threadIdx.x);
   if ((int)threadIdx.x < n - tail) one(tail + threadIdx.x);
   const uint4* const body = reinterpret_cast<const uint4*>(from + head);
+  const bool wide = ((uintptr_t)(to + head) & 31) == 0;
   for (int i = (int)threadIdx.x; i < packs; i += 4 * kClipThreads) {
     uint4 pack[4];
 #pragma unroll
@@ -198,8 +201,16 @@ __device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float fa
         set_pair<O>(out[e / F], e % F, make_float2(v.x * factor, v.y * factor));
       }
       uint4* const at = reinterpret_cast<uint4*>(to + head) + (int64_t)(i + k * kClipThreads) * (sizeof(out) / 16);
-#pragma unroll
-      for (int q = 0; q < (int)(sizeof(out) / 16); ++q) __stcs(at + q, out[q]);
+      if constexpr (sizeof(out) == 32) {
+        if (wide)
+          asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(out[0].x), "r"(out[0].y),
+                       "r"(out[0].z), "r"(out[0].w), "r"(out[1].x), "r"(out[1].y), "r"(out[1].z), "r"(out[1].w)
+                       : "memory");
+        else
+          __stcs(at, out[0]), __stcs(at + 1, out[1]);
+      } else {
+        __stcs(at, out[0]);
+      }
     }
   }
 }
@@ -219,11 +230,13 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
       const double norm = worker_norm(a, worker, shared);
       factor = isfinite(norm) ? (float)fmin(1., a.max_norm / (norm + a.eps)) : 1.f;
       known = worker;
+      // one block has the worker's first unit of the last table that is walked
+      if (a.norms && threadIdx.x == 0 && a.table == a.norm_table && worker * l.units >= begin) a.norms[worker] = (float)norm;
     }
     const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
-    const int64_t at = (unit - t.unit) * kUnit;
+    const int64_t at = (unit - t.unit) * a.unit;
     scale_unit(static_cast<const T*>(t.from) + worker * t.from_stride + at,
-               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(kUnit, t.size - at), factor);
+               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), factor);
   }
 }
 
@@ -236,6 +249,10 @@ cudaError_t launch_clip(const ClipShape& s, int64_t count, const dqgan_tensor* f
   a.eps = s.eps;
   a.norms = norms;
   a.count_tables = (int32_t)ceil_div(count, kTensors);
+  int64_t values = 0;
+  for (int64_t k = 0; k < count; ++k) values += from[k].size;
+  a.unit = kMostUnit;  // smaller where the GPU has blocks to spare
+  while (a.unit > kLeastUnit && values / a.unit * s.workers < kClipBlocks) a.unit /= 2;
   ClipTable<kTensors> table{};
   const auto fill = [&](int i) {
     a.table = i;
@@ -244,7 +261,7 @@ cudaError_t launch_clip(const ClipShape& s, int64_t count, const dqgan_tensor* f
     for (int64_t k = (int64_t)i * kTensors; k < count && k < (int64_t)(i + 1) * kTensors; ++k) {
       if (from[k].size == 0) continue;
       table.t[a.count++] = {from[k].data, to ? to[k].data : nullptr, from[k].size, from[k].stride, to ? to[k].stride : 0, units};
-      units += ceil_div(from[k].size, kUnit);
+      units += ceil_div(from[k].size, a.unit);
     }
     ClipLaunch& l = a.tables[i];
     l.units = units;
@@ -259,7 +276,8 @@ cudaError_t launch_clip(const ClipShape& s, int64_t count, const dqgan_tensor* f
     st = launch_pdl(norm_kernel<T, kTensors>, dim3((unsigned)a.tables[i].blocks), dim3(kClipThreads), 0, stream, a, table);
   }
   if (st != cudaSuccess) return st;
-  if (norms) {
+  while (a.norm_table < a.count_tables - 1 && a.tables[a.norm_table].units == 0) ++a.norm_table;
+  if (norms && (!to || values == 0)) {
     ++*launches;
     st = launch_pdl(norms_kernel, dim3((unsigned)s.workers), dim3(kClipThreads), 0, stream, a);
   }

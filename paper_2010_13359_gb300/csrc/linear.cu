@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
       if (i >= count) x[i] = 0.f;
       sum[i] += x[i];
     }
-    if (a.to) write_parts(x, a.to, (worker * a.rows + r) * a.ld + column, a.part, a.parts, a.half);
+    if (a.to) write_parts<sizeof(T) == 4>(x, a.to, (worker * a.rows + r) * a.ld + column, a.part, a.parts, a.half);
   };
   const auto unpack = [](const uint4 (&packs)[kPacks], float (&x)[8]) {
 #pragma unroll

@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         mbar_wait_bounded(empty + i % S::kStages, i / S::kStages & 1, p.err);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int sub = warp & 3, half = (warp - 4) / 4;
     TurnStore store{turn + (warp - 4) * 4096, lane};
     uint32_t c = 0;

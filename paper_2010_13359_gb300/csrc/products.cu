@@ -75,8 +75,14 @@ struct StoreEpilogue {
       } else {
         store.turn(x);
         if (lane < count) {
+          if (!s.add && !s.pre && !s.residual && s.activation == DQGAN_NONE) {
+            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + row * s.out_ld + j + lane;
+#pragma unroll 8
+            for (int r = 0; r < rows; ++r) to[r * s.out_ld] = from_float<T>(store.turned(r) + b);
+          } else {
 #pragma unroll 4
-          for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j + lane, store.turned(r), b);
+            for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j + lane, store.turned(r), b);
+          }
         }
       }
     }
@@ -174,7 +180,7 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, bool pack
       counts = t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
     }
     if (counts) read8(static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column, (int)min64(8, a.columns - column), packs, x);
-    write_parts(x, a.to, r * a.ld + column, a.part, a.parts, a.half);
+    write_parts<true>(x, a.to, r * a.ld + column, a.part, a.parts, a.half);
   }
 }
 

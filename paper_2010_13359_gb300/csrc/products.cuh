@@ -165,19 +165,32 @@ __device__ __forceinline__ float activate(float u, int activation) {
   }
   return u;
 }
-// u Phi(u) of two values, as normal_cdf<false>, with two fp32 operations to an instruction.
-__device__ __forceinline__ float2 gelu2(float2 u) {
-  const float2 x = make_float2(fabsf(u.x), fabsf(u.y));
+// 1 - Phi(|u|) and exp(-u^2 / 2) of two values as normal_cdf<false>, two fp32 operations to an instruction.
+__device__ __forceinline__ void normal_tails(float2 u, float2 x, float2* tail, float2* e) {
   const float2 d = fma2(x, both(0.3275911f * 0.70710678118654752f), both(1.f));
   const float2 t = make_float2(reciprocal_approx(d.x), reciprocal_approx(d.y));
-  const float2 e = mul2(mul2(u, u), both(-0.72134752044448170f));
+  const float2 power = mul2(mul2(u, u), both(-0.72134752044448170f));
+  *e = make_float2(exp2_approx(power.x), exp2_approx(power.y));
   float2 f = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
   f = fma2(f, t, both(0.5f * 1.421413741f));
   f = fma2(f, t, both(0.5f * -0.284496736f));
   f = fma2(f, t, both(0.5f * 0.254829592f));
-  // |u| (1 - Phi(|u|)), which u Phi(u) is less than max(u, 0)
-  const float2 tail = mul2(mul2(mul2(f, t), x), make_float2(exp2_approx(e.x), exp2_approx(e.y)));
+  *tail = mul2(mul2(f, t), *e);
+}
+__device__ __forceinline__ float2 gelu2(float2 u) {
+  const float2 x = make_float2(fabsf(u.x), fabsf(u.y));
+  float2 tail, e;
+  normal_tails(u, x, &tail, &e);
+  tail = mul2(tail, x);  // what u Phi(u) is less than max(u, 0)
   return make_float2(fmaxf(u.x, 0.f) - tail.x, fmaxf(u.y, 0.f) - tail.y);
+}
+__device__ __forceinline__ float2 gelu_slope2(float2 u) {
+  const float2 x = make_float2(fabsf(u.x), fabsf(u.y));
+  float2 tail, e;
+  normal_tails(u, x, &tail, &e);
+  // u phi(u) - (1 - Phi(u)) for u > 0, and the slopes at u and -u add up to 1
+  const float2 h = fma2(mul2(x, both(0.39894228040143268f)), e, make_float2(-tail.x, -tail.y));
+  return make_float2(u.x > 0.f ? 1.f + h.x : -h.x, u.y > 0.f ? 1.f + h.y : -h.y);
 }
 
 template <bool kExact, int N>
@@ -219,7 +232,14 @@ __device__ __forceinline__ float activation_slope(float u, int activation) {
 // x times the slope at u.
 template <bool kExact, int N>
 __device__ __forceinline__ void scale_by_slope(float (&x)[N], const float (&u)[N], int activation) {
-  if (activation == DQGAN_GELU) {
+  if (activation == DQGAN_GELU && !kExact) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 s = gelu_slope2(make_float2(u[i], u[i + 1]));
+      x[i] *= s.x;
+      x[i + 1] *= s.y;
+    }
+  } else if (activation == DQGAN_GELU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] *= activation_slope<kExact>(u[i], DQGAN_GELU);
   } else if (activation == DQGAN_SILU) {
@@ -264,6 +284,16 @@ __device__ __forceinline__ __nv_bfloat16 take_part(float& x) {
   return h;
 }
 
+// The same of two values, in a few instructions: one that is not finite, or rounds to what is not, leaves NaN.
+__device__ __forceinline__ uint32_t take_parts2(float2& x) {
+  const __nv_bfloat162 h = __float22bfloat162_rn(x);
+  const uint32_t bits = reinterpret_cast<const uint32_t&>(h);
+  x = add2(x, make_float2(-__uint_as_float(bits << 16), -__uint_as_float(bits & 0xffff0000u)));
+  return bits;
+}
+
+// kSafe: as take_part.
+template <bool kSafe>
 __device__ __forceinline__ void write_parts(float (&x)[8], void* to, int64_t at, int64_t part, int parts, bool half) {
   if (half) {
     uint4 pack;
@@ -276,10 +306,17 @@ __device__ __forceinline__ void write_parts(float (&x)[8], void* to, int64_t at,
     uint4 pack;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      __nv_bfloat162 both;
-      both.x = take_part(x[i]);
-      both.y = take_part(x[i + 1]);
-      reinterpret_cast<__nv_bfloat162*>(&pack)[i / 2] = both;
+      if constexpr (kSafe) {
+        __nv_bfloat162 h;
+        h.x = take_part(x[i]);
+        h.y = take_part(x[i + 1]);
+        reinterpret_cast<__nv_bfloat162*>(&pack)[i / 2] = h;
+      } else {
+        float2 v = make_float2(x[i], x[i + 1]);
+        reinterpret_cast<uint32_t*>(&pack)[i / 2] = take_parts2(v);
+        x[i] = v.x;
+        x[i + 1] = v.y;
+      }
     }
     *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(to) + q * part + at) = pack;
   }

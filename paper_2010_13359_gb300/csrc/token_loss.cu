@@ -26,7 +26,7 @@ int grad_weight_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3
 int grad_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : 2; }
 bool half_logits(const TokenLossShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
 
-constexpr int64_t kGradBytes = (int64_t)512 << 20, kWeightBytes = (int64_t)1 << 30;
+constexpr int64_t kGradBytes = (int64_t)1 << 30, kWeightBytes = (int64_t)1 << 30;
 constexpr int kFewTiles = 76;  // below: narrow tiles
 
 // Columns of a piece of the vocabulary, a multiple of 256.
@@ -167,12 +167,7 @@ struct GradEpilogue {
       for (int part = 0; part < s.grad_parts; ++part) {
         uint4 packs[4];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const __nv_bfloat162 h = __float22bfloat162_rn(x[j]);
-          const uint32_t bits = reinterpret_cast<const uint32_t&>(h);
-          reinterpret_cast<uint32_t*>(&packs[j / 4])[j % 4] = bits;
-          x[j] = add2(x[j], make_float2(-__uint_as_float(bits << 16), -__uint_as_float(bits & 0xffff0000u)));
-        }
+        for (int j = 0; j < 16; ++j) reinterpret_cast<uint32_t*>(&packs[j / 4])[j % 4] = take_parts2(x[j]);
         store.put(packs, &p.out, (int)column + g, (int)row, tile.worker, part);
       }
     }
