@@ -52,9 +52,8 @@ struct ClipTable {
   ClipTensor t[kTensors];
 };
 
-// A table's units over all workers go to its blocks in runs; so block b's sum for worker m has place b + m to itself.
-__device__ __forceinline__ int64_t first_unit(const ClipLaunch& l, int workers, int64_t block) {
-  return (int64_t)((unsigned __int128)(l.units * workers) * block / l.blocks);
+__device__ __forceinline__ int64_t first_unit(const ClipArgs& a, const ClipLaunch& l, int64_t block) {
+  return clip_first_unit(l.units, a.workers, block, l.blocks);
 }
 
 __device__ __forceinline__ double block_sum_double(double x, double* shared) {
@@ -134,7 +133,7 @@ __global__ void __launch_bounds__(kClipThreads) norm_kernel(const __grid_constan
   dq_pdl_enter();
   __shared__ double shared[kClipThreads / 32];
   const ClipLaunch& l = a.tables[a.table];
-  const int64_t begin = first_unit(l, a.workers, blockIdx.x), end = first_unit(l, a.workers, (int64_t)blockIdx.x + 1);
+  const int64_t begin = first_unit(a, l, blockIdx.x), end = first_unit(a, l, (int64_t)blockIdx.x + 1);
   double sum = 0.;
   for (int64_t u = begin; u < end; ++u) {
     const int64_t worker = u / l.units, unit = u - worker * l.units;
@@ -155,10 +154,9 @@ __device__ __forceinline__ double worker_norm(const ClipArgs& a, int64_t worker,
   for (int i = 0; i < a.count_tables; ++i) {
     const ClipLaunch& l = a.tables[i];
     if (l.units == 0) continue;
-    const int64_t all = l.units * a.workers;
     // the blocks that hold the worker's first and last unit
-    const int64_t first = (int64_t)(((unsigned __int128)(worker * l.units + 1) * l.blocks - 1) / all);
-    const int64_t last = (int64_t)(((unsigned __int128)((worker + 1) * l.units) * l.blocks - 1) / all);
+    const int64_t first = clip_block_of(l.units, a.workers, worker * l.units, l.blocks);
+    const int64_t last = clip_block_of(l.units, a.workers, (worker + 1) * l.units - 1, l.blocks);
     for (int64_t b = first + threadIdx.x; b <= last; b += kClipThreads) sum += l.sums[b + worker];
   }
   return sqrt(block_sum_double(sum, shared));
@@ -172,10 +170,10 @@ __global__ void __launch_bounds__(kClipThreads) norms_kernel(const __grid_consta
 }
 
 template <typename T, typename O>
-__device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float factor) {
+__device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float shift, float factor) {
   constexpr int E = 16 / (int)sizeof(T);
   const int head = head_of(from, n);
-  const auto one = [&](int i) { to[i] = from_float<O>(to_float(from[i]) * factor); };
+  const auto one = [&](int i) { to[i] = from_float<O>(to_float(from[i]) * shift * factor); };
   if ((((uintptr_t)(to + head)) & 15) != 0) {  // the two sides' packs do not meet
     for (int i = (int)threadIdx.x; i < n; i += kClipThreads) one(i);
     return;
@@ -198,7 +196,7 @@ __device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float fa
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
         const float2 v = pair_of<T>(pack[k], e);
-        set_pair<O>(out[e / F], e % F, make_float2(v.x * factor, v.y * factor));
+        set_pair<O>(out[e / F], e % F, make_float2(v.x * shift * factor, v.y * shift * factor));
       }
       uint4* const at = reinterpret_cast<uint4*>(to + head) + (int64_t)(i + k * kClipThreads) * (sizeof(out) / 16);
       if constexpr (sizeof(out) == 32) {
@@ -221,14 +219,17 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
   dq_pdl_enter();
   __shared__ double shared[kClipThreads / 32];
   const ClipLaunch& l = a.tables[a.table];
-  const int64_t begin = first_unit(l, a.workers, blockIdx.x), end = first_unit(l, a.workers, (int64_t)blockIdx.x + 1);
+  const int64_t begin = first_unit(a, l, blockIdx.x), end = first_unit(a, l, (int64_t)blockIdx.x + 1);
   int64_t known = -1;
-  float factor = 1.f;
+  float shift = 1.f, factor = 1.f;
   for (int64_t u = end - 1; u >= begin; --u) {
     const int64_t worker = u / l.units, unit = u - worker * l.units;
     if (worker != known) {
       const double norm = worker_norm(a, worker, shared);
-      factor = isfinite(norm) ? (float)fmin(1., a.max_norm / (norm + a.eps)) : 1.f;
+      const double scale = isfinite(norm) ? fmin(1., a.max_norm / (norm + a.eps)) : 1.;
+      // a factor below fp32's range, which large values bring back into it, in two steps; a power of two is exact
+      shift = scale < 0x1p-150 ? 0x1p-126f : scale < 0x1p-64 ? 0x1p-64f : 1.f;
+      factor = (float)(scale / shift);
       known = worker;
       // one block has the worker's first unit of the last table that is walked
       if (a.norms && threadIdx.x == 0 && a.table == a.norm_table && worker * l.units >= begin) a.norms[worker] = (float)norm;
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
     const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
     const int64_t at = (unit - t.unit) * a.unit;
     scale_unit(static_cast<const T*>(t.from) + worker * t.from_stride + at,
-               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), factor);
+               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), shift, factor);
   }
 }
 

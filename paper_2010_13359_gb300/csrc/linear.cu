@@ -167,67 +167,102 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* sums, int blocks
   *to = accumulate ? *to + (float)s : (float)s;
 }
 
-// A few rows: what bounds them is the weights' bytes, each read once.  A warp takes two rows of W at a time, 16 bytes a
-// lane, and kRows rows of x beside them from L1; fp32 sums, no parts.  (One row of 4096 x 4096 in bf16: see the
-// tiles' kernel at 24 us.)
+// Sums over a warp's lanes of kValues values each (a power of two, at most 32): lane l gets one of them.  Each step sends
+// half of what is left to the lane that keeps that half.
+template <int kValues>
+__device__ __forceinline__ int sum_over_lanes(float (&x)[kValues], int lane) {
+  int which = 0;
+  int d = 16;
+#pragma unroll
+  for (int h = kValues / 2; h > 0; h /= 2, d /= 2) {
+    const bool upper = lane & d;
+    if (upper) which += h;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float send = upper ? x[i] : x[i + h], keep = upper ? x[i + h] : x[i];
+      x[i] = keep + __shfl_xor_sync(kFullMask, send, d);
+    }
+  }
+  for (; d > 0; d /= 2) x[0] += __shfl_xor_sync(kFullMask, x[0], d);
+  return which;
+}
+
+// A few rows: what bounds them is the weights' bytes, each read once.  A warp takes four rows of W, 16 bytes (32 of fp32) a
+// lane at a time, and kRows rows of x beside them from L1; 1, 2, 4 or 8 warps share the inputs.  fp32 sums of
+// products of the values as they are, without parts.  4096 x 4096 in bf16: 8.9 us for one row (5.0 at the copy's
+// bandwidth), 14 for two, 17 for four, 23 for eight; the tiles need 16.4 for any number up to 128.  1024 x 4096: 3.4, 4.6,
+// 7.8, 9.0 and 8.9; 8192 x 1024: 6.1, 6.8, 8.3, 11.8 and 14.2.  So up to four rows come here, and up to eight
+// where the tiles would have to split fp32 weights first.
 template <typename T, typename E, int kRows, bool kPacks>
 __global__ void __launch_bounds__(256) few_rows_kernel(const T* x, int64_t x_ld, const E* weight, int64_t p_stride, int64_t inputs,
-                                                       int64_t outputs, int rows, const StoreArgs store) {
+                                                       int64_t outputs, int rows, int sharing, const StoreArgs store) {
   dq_pdl_enter();
-  constexpr int kOut = 2, kLane = 8;
+  constexpr int kOut = 4, kValues = kOut * kRows;
+  __shared__ float part[8][kValues];
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
-  const int64_t worker = blockIdx.y, first = ((int64_t)blockIdx.x * 8 + warp) * kOut;
-  if (first >= outputs) return;
+  const int64_t worker = blockIdx.y, group = (int64_t)blockIdx.x * (8 / sharing) + warp / sharing, first = group * kOut;
+  const int share = warp % sharing;
   x += worker * rows * x_ld;
-  weight += worker * p_stride + first * inputs;
-  const int outs = (int)min((int64_t)kOut, outputs - first);
-  float sum[kOut][kRows] = {};
-  if constexpr (kPacks) {
-#pragma unroll 4
-    for (int64_t k = lane * kLane; k < inputs; k += 32 * kLane) {  // whole packs: inputs is a multiple of eight
-      float w[kOut][8];
+  weight += worker * p_stride;
+  // rows beyond the last are the last's, and not stored
+  const E* w[kOut];
 #pragma unroll
-      for (int o = 0; o < kOut; ++o)
-        if (o < outs) read8(weight + o * inputs + k, 8, true, w[o]);
+  for (int o = 0; o < kOut; ++o) w[o] = weight + min64(first + o, outputs - 1) * inputs;
+  float2 sum[kValues] = {};
+  if (first < outputs) {
+    if constexpr (kPacks) {
+#pragma unroll 2
+      for (int64_t k = share * 256 + lane * 8; k < inputs; k += 256 * sharing) {  // whole packs: inputs is a multiple of eight
+        float a[kOut][8];
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        if (r >= rows) break;
-        float v[8];
-        read8(x + r * x_ld + k, 8, true, v);
+        for (int o = 0; o < kOut; ++o) read8(w[o] + k, 8, true, a[o]);
 #pragma unroll
-        for (int o = 0; o < kOut; ++o)
+        for (int r = 0; r < kRows; ++r) {
+          float v[8];
+          read8(x + min(r, rows - 1) * x_ld + k, 8, true, v);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum[o][r] = fmaf(w[o][i], v[i], sum[o][r]);
+          for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2)
+              sum[o * kRows + r] = fma2(make_float2(a[o][i], a[o][i + 1]), make_float2(v[i], v[i + 1]), sum[o * kRows + r]);
+        }
       }
-    }
-  } else {
-#pragma unroll 4
-    for (int64_t k = lane; k < inputs; k += 32) {
-      float w[kOut];
+    } else {
+#pragma unroll 2
+      for (int64_t k = share * 32 + lane; k < inputs; k += 32 * sharing) {
+        float a[kOut];
 #pragma unroll
-      for (int o = 0; o < kOut; ++o) w[o] = o < outs ? to_float(weight[o * inputs + k]) : 0.f;
+        for (int o = 0; o < kOut; ++o) a[o] = to_float(w[o][k]);
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        if (r >= rows) break;
-        const float v = to_float(x[r * x_ld + k]);
+        for (int r = 0; r < kRows; ++r) {
+          const float v = to_float(x[min(r, rows - 1) * x_ld + k]);
 #pragma unroll
-        for (int o = 0; o < kOut; ++o) sum[o][r] = fmaf(w[o], v, sum[o][r]);
+          for (int o = 0; o < kOut; ++o) sum[o * kRows + r].x = fmaf(a[o], v, sum[o * kRows + r].x);
+        }
       }
     }
   }
+  float one[kValues];
 #pragma unroll
-  for (int o = 0; o < kOut; ++o)
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) sum[o][r] += __shfl_xor_sync(kFullMask, sum[o][r], d);
-      if (lane == o * kRows + r && o < outs && r < rows)
-        store_value<T>(store, (int)worker, r, first + o, sum[o][r],
-                       store.bias ? store.bias[worker * store.bias_batch + first + o] : 0.f);
-    }
+  for (int i = 0; i < kValues; ++i) one[i] = sum[i].x + sum[i].y;
+  const int which = sum_over_lanes(one, lane);
+  part[warp][which] = one[0];  // equal lanes write equal values
+  __syncthreads();
+  // the shares of a group's sums in order
+  const int t = (int)threadIdx.x;
+  if (t < 8 / sharing * kValues) {
+    const int g = t / kValues, i = t % kValues, r = i % kRows;
+    const int64_t column = ((int64_t)blockIdx.x * (8 / sharing) + g) * kOut + i / kRows;
+    float s = 0.f;
+    for (int w = 0; w < sharing; ++w) s += part[g * sharing + w][i];
+    if (column < outputs && r < rows)
+      store_value<T>(store, (int)worker, r, column, s, store.bias ? store.bias[worker * store.bias_batch + column] : 0.f);
+  }
 }
 
 constexpr int kFewRows = 8;
+
+bool has_few_rows(const LinearShape& s, int64_t rows) { return rows <= (s.weight_dtype == DQGAN_F32 ? kFewRows : kFewRows / 2); }
 
 template <typename T, typename E>
 cudaError_t few_rows(const LinearArgs& a, const StoreArgs& store, cudaStream_t stream, uint64_t* launches) {
@@ -236,15 +271,19 @@ cudaError_t few_rows(const LinearArgs& a, const StoreArgs& store, cudaStream_t s
     return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && batch * size % 16 == 0;
   };
   const bool packs = s.inputs % 8 == 0 && on_packs(a.x, a.x_ld, 0, sizeof(T)) && on_packs(a.weight, s.inputs, a.p_stride, sizeof(E));
+  // as many warps as have something to do, 256 inputs (32 without packs) each
+  const int64_t steps = ceil_div(s.inputs, packs ? 256 : 32);
+  const int sharing = steps >= 8 ? 8 : steps >= 4 ? 4 : steps >= 2 ? 2 : 1;
   const auto run = [&](auto rows, auto in_packs) {
     ++*launches;
     return launch_pdl(few_rows_kernel<T, E, decltype(rows)::value, decltype(in_packs)::value>,
-                      dim3((unsigned)ceil_div(s.outputs, 16), (unsigned)s.workers), dim3(256), 0, stream,
+                      dim3((unsigned)ceil_div(s.outputs, 32 / sharing), (unsigned)s.workers), dim3(256), 0, stream,
                       static_cast<const T*>(a.x), a.x_ld, static_cast<const E*>(a.weight), a.p_stride, s.inputs, s.outputs,
-                      (int)a.rows, store);
+                      (int)a.rows, sharing, store);
   };
   const auto by_rows = [&](auto in_packs) {
     return a.rows == 1   ? run(std::integral_constant<int, 1>{}, in_packs)
+           : a.rows == 2 ? run(std::integral_constant<int, 2>{}, in_packs)
            : a.rows <= 4 ? run(std::integral_constant<int, 4>{}, in_packs)
                          : run(std::integral_constant<int, kFewRows>{}, in_packs);
   };
@@ -273,7 +312,7 @@ cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint
   out.bias = a.bias;
   out.bias_batch = a.b_stride;
   out.activation = s.activation;
-  if (a.rows <= kFewRows)
+  if (has_few_rows(s, a.rows))
     return with_dtype(s.dtype, [&](auto t) {
       using T = decltype(t);
       return s.weight_dtype == DQGAN_F32 ? few_rows<T, float>(a, out, stream, launches) : few_rows<T, T>(a, out, stream, launches);

@@ -163,6 +163,14 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
 size_t token_loss_scratch_bytes(const TokenLossShape& s);
 cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint64_t* launches);
 
+// The clipping cuts tensors into units; the units of all workers, one worker's after another's, go to blocks in runs.  So
+// block b's sum for worker m has the place b + m to itself.
+__host__ __device__ constexpr int64_t clip_first_unit(int64_t units, int32_t workers, int64_t block, int32_t blocks) {
+  return (int64_t)((unsigned __int128)(units * workers) * block / blocks);
+}
+__host__ __device__ constexpr int64_t clip_block_of(int64_t units, int32_t workers, int64_t unit, int32_t blocks) {
+  return (int64_t)(((unsigned __int128)(unit + 1) * blocks - 1) / (units * workers));
+}
 size_t clip_scratch_bytes(const ClipShape& s);
 // to: the tensors' places, or nullptr (norms alone).
 cudaError_t launch_gradient_clip(const ClipShape& s, int64_t count, const dqgan_tensor* from, const dqgan_tensor* to,

@@ -5,7 +5,7 @@
 // cluster; their SMs' tensor cores work as one) over tiles of 256 x 256, of which
 // each block loads half of either operand and keeps the sums of 128 rows.  Two
 // threads load blocks of 64 of the contracted index into a ring of stages, a third
-// (in a pair the first block's) multiplies them, and eight warps take the sums out
+// (in a pair the first block's) multiplies them, and eight or sixteen warps take the sums out
 // of tensor memory, two accumulators in turn, so that an epilogue runs beside the
 // next tile's products.
 //
@@ -16,10 +16,11 @@
 //
 // The tensor cores' own sums are rounded towards zero, by up to one unit in the
 // last place each 16 products: over thousands of them the error grows past that
-// of fp32 sums.  So an accumulator takes `chunk` blocks only; the eight warps
-// add it to sums in registers (128 a thread), rounded to nearest, while the
-// other accumulator fills.  16 blocks (1024 products) where the result has 32 bits,
-// 32 in f16, 128 in bf16: taking sums out costs the products up to a tenth at 8.
+// of fp32 sums.  So an accumulator takes `chunk` blocks only; the warps
+// add it to sums in registers (64 a thread), rounded to nearest, while the
+// other accumulator fills.  16 blocks (1024 products) where the result has 32 bits
+// (12, two for each pair of parts, where the operands have), 32 in f16, 128 in bf16: taking sums out costs the products up
+// to a tenth at 8.
 #pragma once
 
 #include "device_common.cuh"
@@ -27,11 +28,12 @@
 
 namespace dq {
 
-constexpr int kProductThreads = 384;  // 4 warps that load and multiply, 8 that take the sums
 constexpr int kTileRows = 128;
 constexpr int kBlockDepth = 64;       // 128 bytes: a row of the 128-byte swizzle
 
-template <int BN>
+// kWarps: those that take the sums, of a tile of 256 columns.  Sixteen hide more of an epilogue's latencies (8 x 2048 rows of
+// 1024 x 4096 with GELU: 114 us, 131 with eight), eight spill less and store from two buffers (without: 95 and 100).
+template <int BN, int kWarps = 8>
 struct ProductShape {
   static constexpr int kPair = BN == 256 ? 2 : 1;     // blocks that work on a tile
   static constexpr int kRows = kPair * kTileRows;  // of a tile
@@ -40,10 +42,21 @@ struct ProductShape {
   static constexpr int kBBytes = kBColumns * kBlockDepth * 2;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = BN == 256 ? 6 : 8;
-  static constexpr int kTurnBytes = 8 * 4096;
+  // four warps that load and multiply, and those that take the sums: a quarter of the rows and kWidth columns each
+  static constexpr int kSumWarps = BN == 256 ? kWarps : 8;
+  static constexpr int kThreads = 128 + 32 * kSumWarps;
+  static constexpr int kWidth = BN / (kSumWarps / 4);
+  static constexpr int kBuffers = 16 / kSumWarps;  // of TurnStore
+  // registers of either kind; together at most those that the block is launched with, 96 * 640 or 168 * 384
+  static constexpr int kFewRegisters = kSumWarps == 16 ? 56 : 64, kManyRegisters = kSumWarps == 16 ? 104 : 216;
+  static_assert(128 * kFewRegisters + 32 * kSumWarps * kManyRegisters <= (65536 / kThreads / 8 * 8) * kThreads, "registers");
+  static constexpr int kTurnBytes = 16 * 2048;
   // stages, transposing buffers, barriers; and what it takes to start on a boundary of 1024 bytes
   static constexpr int kSmem = kStages * kStageBytes + kTurnBytes + 256 + 1024;
 };
+
+template <int BN, typename Epilogue>
+using ShapeOf = ProductShape<BN, Epilogue::kWarps>;
 
 // ---- tcgen05 ----
 template <int kPair>
@@ -151,18 +164,19 @@ __device__ __forceinline__ uint64_t operand_descriptor(uint32_t at, bool across)
   return (uint64_t)((at & 0x3ffff) >> 4) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 
-// What a warp has ready of its 32 rows, 64 bytes of a row at a time, goes through two buffers of shared memory in turn
-// and from there by TMA.  Lane l holds row l; its packs of 16 bytes stand in the order of the 64-byte swizzle, in which
-// eight lanes' packs meet in no bank.  Rows outside the matrix are not written, and columns by 16 bytes.
+// What a warp has ready of its 32 rows, 64 bytes of a row at a time, goes through shared memory and from there by TMA.
+// Lane l holds row l; its packs of 16 bytes stand in the order of the 64-byte swizzle, in which eight lanes' packs meet in
+// no bank.  Rows outside the matrix are not written, and columns by 16 bytes.
+template <int kBuffers>
 struct TurnStore {
-  uint8_t* buffer;  // 2 x 2048 bytes
+  uint8_t* buffer;  // kBuffers x 2048 bytes, used in turn
   int lane;
   uint32_t n = 0;
 
   __device__ __forceinline__ void put(const uint4 (&packs)[4], const CUtensorMap* map, int column, int row, int worker, int part) {
-    uint8_t* const to = buffer + (n & 1) * 2048;
+    uint8_t* const to = buffer + (n % kBuffers) * 2048;
     ++n;
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kBuffers - 1) : "memory");
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4*>(to + lane * 64 + ((c ^ (lane / 2 & 3)) * 16)) = packs[c];
@@ -191,18 +205,18 @@ struct TurnStore {
     }
   }
 
-  // single values, for matrices that TMA cannot write: column l of row r, from 32 columns that lane r holds
-  __device__ __forceinline__ void turn(const float (&x)[32]) {
-    float* const to = reinterpret_cast<float*>(buffer);
+  // Single values, for matrices that TMA cannot write: 16 columns that lane r holds of row r; then column l & 15 of row
+  // 2 i + l / 16.
+  __device__ __forceinline__ void turn(const float* x) {
     if (lane == 0) bulk_wait_read_all();
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
-      *reinterpret_cast<float4*>(to + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<float4*>(buffer + lane * 64 + ((c ^ (lane / 2 & 3)) * 16)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
     __syncwarp();
   }
-  __device__ __forceinline__ float turned(int r) const {
-    return reinterpret_cast<const float*>(buffer)[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + (lane & 3)];
+  __device__ __forceinline__ float turned(int i) const {
+    return *reinterpret_cast<const float*>(buffer + (2 * i + lane / 16) * 64 + (((lane & 15) / 4) ^ (i & 3)) * 16 + (lane & 3) * 4);
   }
 };
 
@@ -246,15 +260,15 @@ __host__ __device__ inline int64_t product_items(const ProductArgs& p) {
 }
 
 // Where a warp keeps its sums of a piece: four columns of 32 rows after another.
-template <int BN>
+template <typename S>
 __device__ __forceinline__ float4* piece_sums(const ProductArgs& p, int64_t piece, int rank, int warp, int lane) {
-  return reinterpret_cast<float4*>(p.partial) + ((piece * ProductShape<BN>::kPair + rank) * 8 + warp) * (32 * BN / 8) + lane;
+  return reinterpret_cast<float4*>(p.partial) + ((piece * S::kPair + rank) * S::kSumWarps + warp) * (8 * S::kWidth) + lane;
 }
 
 template <int BN, typename Epilogue>
-__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(ShapeOf<BN, Epilogue>::kThreads, 1) product_kernel(const __grid_constant__ ProductArgs p) {
   dq_pdl_enter();
-  using S = ProductShape<BN>;
+  using S = ShapeOf<BN, Epilogue>;
   constexpr int kPair = S::kPair;
   extern __shared__ __align__(1024) uint8_t raw[];
   uint8_t* const smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
@@ -277,7 +291,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(sum_full + s, 1);
-      mbar_init(sum_empty + s, 8 * kPair);
+      mbar_init(sum_empty + s, S::kSumWarps * kPair);
     }
     mbar_fence_init();
   }
@@ -292,7 +306,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   const int64_t first = blockIdx.x / S::kPair, step = gridDim.x / S::kPair;
   const int terms = p.terms.count;
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kFewRegisters));
     if ((warp == 0 || warp == 3) && lane == 0) {
       // One thread loads A, another B: a stage is 512 clocks of the tensor cores, and one thread that issues all of its
       // loads takes longer (8192^3: 655 us).
@@ -363,23 +377,23 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         mbar_wait_bounded(empty + i % S::kStages, i / S::kStages & 1, p.err);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    const int sub = warp & 3, half = (warp - 4) / 4;
-    TurnStore store{turn + (warp - 4) * 4096, lane};
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kManyRegisters));
+    const int sub = warp & 3, slice = (warp - 4) / 4;
+    TurnStore<S::kBuffers> store{turn + (warp - 4) * (S::kTurnBytes / S::kSumWarps), lane};
     uint32_t c = 0;
     bool ok = true;
     for (int64_t t = first; ok && t < tiles; t += step) {
       const ProductTile tile = product_tile<BN>(p, t);
       const int total = (tile.end - tile.begin) * terms;
-      float v[BN / 2];
+      float v[S::kWidth];
 #pragma unroll
-      for (int i = 0; i < BN / 2; ++i) v[i] = 0.f;
+      for (int i = 0; i < S::kWidth; ++i) v[i] = 0.f;
       for (int done = 0; done < total; done += p.chunk, ++c) {
         if (!(ok = mbar_wait_bounded(sum_full + (c & 1), c / 2 & 1, p.err))) break;
         tensor_fence_after();
-        const uint32_t from = sums + ((uint32_t)(32 * sub) << 16) + (c & 1) * BN + half * (BN / 2);
+        const uint32_t from = sums + ((uint32_t)(32 * sub) << 16) + (c & 1) * BN + slice * S::kWidth;
 #pragma unroll
-        for (int i = 0; i < BN / 2; i += 32) {
+        for (int i = 0; i < S::kWidth; i += 32) {
           uint32_t x[32];
           tensor_load32(from + i, x);
 #pragma unroll
@@ -398,11 +412,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
       if (!ok) break;
       if (tile.piece >= 0) {
-        float4* const to = piece_sums<BN>(p, tile.piece, rank, warp - 4, lane);
+        float4* const to = piece_sums<S>(p, tile.piece, rank, warp - 4, lane);
 #pragma unroll
-        for (int j = 0; j < BN / 8; ++j) to[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int j = 0; j < S::kWidth / 4; ++j) to[32 * j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
       } else {
-        Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + half * (BN / 2), v, store);
+        Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + slice * S::kWidth, v, store);
       }
     }
     bulk_wait_all();
@@ -416,21 +430,21 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 
 // The pieces' sums of the split tiles in order, and what is done with them.  A block a tile and half of a pair.
 template <int BN, typename Epilogue>
-__global__ void __launch_bounds__(256, 1) join_kernel(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(32 * ShapeOf<BN, Epilogue>::kSumWarps, 1) join_kernel(const __grid_constant__ ProductArgs p) {
   dq_pdl_enter();
-  using S = ProductShape<BN>;
+  using S = ShapeOf<BN, Epilogue>;
   __shared__ __align__(1024) uint8_t turn[S::kTurnBytes];
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int rank = (int)blockIdx.x % S::kPair;
   const int64_t first = (int64_t)(blockIdx.x / S::kPair) * p.pieces;
   const ProductTile tile = product_tile<BN>(p, p.whole + first);
-  float v[BN / 2];
+  float v[S::kWidth];
 #pragma unroll
-  for (int i = 0; i < BN / 2; ++i) v[i] = 0.f;
+  for (int i = 0; i < S::kWidth; ++i) v[i] = 0.f;
   for (int piece = 0; piece < p.pieces; ++piece) {
-    const float4* const from = piece_sums<BN>(p, first + piece, rank, warp, lane);
+    const float4* const from = piece_sums<S>(p, first + piece, rank, warp, lane);
 #pragma unroll
-    for (int j = 0; j < BN / 8; ++j) {
+    for (int j = 0; j < S::kWidth / 4; ++j) {
       const float4 x = from[32 * j];
       v[4 * j] = __fadd_rn(v[4 * j], x.x);
       v[4 * j + 1] = __fadd_rn(v[4 * j + 1], x.y);
@@ -438,8 +452,8 @@ __global__ void __launch_bounds__(256, 1) join_kernel(const __grid_constant__ Pr
       v[4 * j + 3] = __fadd_rn(v[4 * j + 3], x.w);
     }
   }
-  TurnStore store{turn + warp * 4096, lane};
-  Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * (warp & 3), tile.column + warp / 4 * (BN / 2), v, store);
+  TurnStore<S::kBuffers> store{turn + warp * (S::kTurnBytes / S::kSumWarps), lane};
+  Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * (warp & 3), tile.column + warp / 4 * S::kWidth, v, store);
   bulk_wait_all();
 }
 
@@ -507,8 +521,8 @@ inline bool product_args(const Product& p, int chunk, uint32_t* err, ProductArgs
 template <int BN, typename Epilogue>
 inline cudaError_t product_slots(int* slots) {
   static std::atomic<int> kept[kKeptDevices];
-  using S = ProductShape<BN>;
-  if (S::kPair == 1) return resident_ctas(product_kernel<BN, Epilogue>, kProductThreads, S::kSmem, S::kSmem, kept, slots);
+  using S = ShapeOf<BN, Epilogue>;
+  if (S::kPair == 1) return resident_ctas(product_kernel<BN, Epilogue>, S::kThreads, S::kSmem, S::kSmem, kept, slots);
   int dev = 0;
   cudaError_t st = cudaGetDevice(&dev);
   if (st != cudaSuccess) return st;
@@ -524,7 +538,7 @@ inline cudaError_t product_slots(int* slots) {
   attr[0].val.clusterDim.x = S::kPair;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   lc.gridDim = dim3(S::kPair * 1024);
-  lc.blockDim = dim3(kProductThreads);
+  lc.blockDim = dim3(S::kThreads);
   lc.dynamicSmemBytes = S::kSmem;
   lc.attrs = attr;
   lc.numAttrs = 1;
@@ -538,18 +552,18 @@ inline cudaError_t product_slots(int* slots) {
 
 template <int BN, typename Epilogue>
 inline cudaError_t launch_product(const ProductArgs& p, cudaStream_t stream, uint64_t* launches) {
-  using S = ProductShape<BN>;
+  using S = ShapeOf<BN, Epilogue>;
   int slots = 0;
   cudaError_t st = product_slots<BN, Epilogue>(&slots);
   if (st != cudaSuccess) return st;
   const int64_t items = product_items(p);
   const int grid = (int)(items < slots ? items : slots) * S::kPair;
   ++*launches;
-  st = launch_pdl_cluster(product_kernel<BN, Epilogue>, S::kPair, dim3(grid), dim3(kProductThreads), S::kSmem, stream, p);
+  st = launch_pdl_cluster(product_kernel<BN, Epilogue>, S::kPair, dim3(grid), dim3(S::kThreads), S::kSmem, stream, p);
   const int64_t split = (int64_t)p.tiles_m * p.tiles_n * p.workers - p.whole;
   if (st != cudaSuccess || split == 0) return st;
   ++*launches;
-  return launch_pdl(join_kernel<BN, Epilogue>, dim3((unsigned)(split * S::kPair)), dim3(256), 0, stream, p);
+  return launch_pdl(join_kernel<BN, Epilogue>, dim3((unsigned)(split * S::kPair)), dim3(32 * S::kSumWarps), 0, stream, p);
 }
 
 }  // namespace dq

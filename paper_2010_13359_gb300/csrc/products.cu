@@ -43,18 +43,19 @@ __device__ __forceinline__ void add32(const T* from, int64_t count, float (&x)[3
 
 // A warp's 32 rows, by TMA where results are on 16-byte boundaries, else turned in shared memory and stored by single
 // values.
-template <typename T>
+template <typename T, int kSumWarps>
 struct StoreEpilogue {
-  template <int BN>
+  static constexpr int kWarps = kSumWarps;
+  template <int BN, typename S = ProductShape<BN, kWarps>>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             const float (&v)[BN / 2], TurnStore& store) {
+                                             const float (&v)[S::kWidth], TurnStore<S::kBuffers>& store) {
     const StoreArgs& s = p.store;
     const int lane = store.lane;
     const int rows = (int)min64(32, p.rows - row);
     if (rows <= 0) return;
     const float* const bias = s.bias ? s.bias + tile.worker * s.bias_batch : nullptr;
 #pragma unroll
-    for (int g = 0; g < BN / 2; g += 32) {
+    for (int g = 0; g < S::kWidth; g += 32) {
       const int64_t j = column + g, count = p.columns - j;
       if (count <= 0) break;
       float x[32];
@@ -67,21 +68,27 @@ struct StoreEpilogue {
 #pragma unroll
           for (int i = 0; i < 32; ++i) x[i] += __shfl_sync(kFullMask, b, i);
         }
-        if (s.pre) store.put32<T>(x, &p.pre, (int)j, (int)row, tile.worker);
+        if (s.pre) store.template put32<T>(x, &p.pre, (int)j, (int)row, tile.worker);
         activate_all<sizeof(T) == 4>(x, s.activation);
         if (s.residual && lane < rows)
           add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
-        store.put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
+        store.template put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
       } else {
-        store.turn(x);
-        if (lane < count) {
+#pragma unroll
+        for (int q = 0; q < 32; q += 16) {
+          const int64_t at = j + q + (lane & 15);
+          const float one = __shfl_sync(kFullMask, b, q + (lane & 15));
+          store.turn(x + q);
+          if (at >= p.columns) continue;
           if (!s.add && !s.pre && !s.residual && s.activation == DQGAN_NONE) {
-            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + row * s.out_ld + j + lane;
+            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + row * s.out_ld + at;
 #pragma unroll 8
-            for (int r = 0; r < rows; ++r) to[r * s.out_ld] = from_float<T>(store.turned(r) + b);
+            for (int i = 0; i < 16; ++i)
+              if (2 * i + lane / 16 < rows) to[(2 * i + lane / 16) * s.out_ld] = from_float<T>(store.turned(i) + one);
           } else {
 #pragma unroll 4
-            for (int r = 0; r < rows; ++r) store_value<T>(s, tile.worker, row + r, j + lane, store.turned(r), b);
+            for (int i = 0; i < 16; ++i)
+              if (2 * i + lane / 16 < rows) store_value<T>(s, tile.worker, row + 2 * i + lane / 16, at, store.turned(i), one);
           }
         }
       }
@@ -128,7 +135,7 @@ template <int BN>
 cudaError_t store_product(const Product& p, const StoreArgs& store, const Cut& cut, void* scratch, uint32_t* err,
                           cudaStream_t stream, uint64_t* launches) {
   ProductArgs args{};
-  const int chunk = store.out_dtype == DQGAN_F32 ? 16 : store.out_dtype == DQGAN_F16 ? 32 : 128;
+  const int chunk = p.terms.count == 6 ? 12 : store.out_dtype == DQGAN_F32 ? 16 : store.out_dtype == DQGAN_F16 ? 32 : 128;
   if (!product_args<BN>(p, chunk, err, &args)) return cudaErrorInvalidValue;
   args.store = store;
   args.whole = cut.whole;
@@ -147,7 +154,10 @@ cudaError_t store_product(const Product& p, const StoreArgs& store, const Cut& c
         (!store.pre || encode_result(store.pre, store.out_dtype, p.columns, p.rows, p.workers, 1, store.pre_ld, store.pre_batch, 0,
                                      &args.pre))))
     return cudaErrorInvalidValue;
-  return with_dtype(store.out_dtype, [&](auto t) { return launch_product<BN, StoreEpilogue<decltype(t)>>(args, stream, launches); });
+  return with_dtype(store.out_dtype, [&](auto t) {
+    return BN == 256 && store.activation != DQGAN_NONE ? launch_product<BN, StoreEpilogue<decltype(t), BN == 256 ? 16 : 8>>(args, stream, launches)
+                                                       : launch_product<BN, StoreEpilogue<decltype(t), 8>>(args, stream, launches);
+  });
 }
 
 }  // namespace

@@ -88,51 +88,55 @@ __device__ __forceinline__ int64_t counting_target(const SoftmaxArgs& s, int64_t
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct StatsEpilogue {
-  template <int BN>
+  static constexpr int kWarps = 8;
+  template <int BN, typename S = ProductShape<BN, kWarps>>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], TurnStore& store) {
+                                             float (&v)[S::kWidth], TurnStore<S::kBuffers>& store) {
+    constexpr int kWidth = S::kWidth;
     const SoftmaxArgs& s = p.softmax;
     const int lane = store.lane;
     if (row + lane >= p.rows) return;
     const int64_t r = tile.worker * p.rows + row + lane;
-    const int valid = (int)max64(0, min64(BN / 2, p.columns - column));
-    if (valid < BN / 2) {
+    const int valid = (int)max64(0, min64(kWidth, p.columns - column));
+    if (valid < kWidth) {
 #pragma unroll
-      for (int j = 0; j < BN / 2; ++j)
+      for (int j = 0; j < kWidth; ++j)
         if (j >= valid) v[j] = -INFINITY;
     }
     float four[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int j = 0; j < BN / 2; ++j) four[j & 3] = fmaxf(four[j & 3], v[j]);
+    for (int j = 0; j < kWidth; ++j) four[j & 3] = fmaxf(four[j & 3], v[j]);
     const float most = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
     const int64_t place = counting_target(s, r) - s.first - column;
     const int t = place >= 0 && place < valid ? (int)place : -1;
     if (t >= 0) {  // one row of 250 here, where the vocabulary has 32,000 entries
       float z = 0.f;
 #pragma unroll
-      for (int j = 0; j < BN / 2; ++j) z += t == j ? v[j] : 0.f;
+      for (int j = 0; j < kWidth; ++j) z += t == j ? v[j] : 0.f;
       s.target_logit[r] = z;
     }
     const float from = (most == -INFINITY ? 0.f : most) * -kLog2e;
     float2 sums[2] = {};
 #pragma unroll
-    for (int j = 0; j < BN / 2; j += 4) {
+    for (int j = 0; j < kWidth; j += 4) {
       const float2 a = fma2(make_float2(v[j], v[j + 1]), both(kLog2e), both(from));
       const float2 b = fma2(make_float2(v[j + 2], v[j + 3]), both(kLog2e), both(from));
       sums[0] = add2(sums[0], make_float2(exp2_approx(a.x), exp2_approx(a.y)));
       sums[1] = add2(sums[1], make_float2(exp2_approx(b.x), exp2_approx(b.y)));
     }
     const float2 sum = add2(sums[0], sums[1]);
-    const int slot = s.slot + (int)(column / (BN / 2));
+    const int slot = s.slot + (int)(column / kWidth);
     s.stats[((int64_t)tile.worker * s.slots + slot) * p.rows + row + lane] = make_float2(most, sum.x + sum.y);
   }
 };
 
 // The gradient of the logits, in parts.
 struct GradEpilogue {
-  template <int BN>
+  static constexpr int kWarps = 8;
+  template <int BN, typename S = ProductShape<BN, kWarps>>
   static __device__ __forceinline__ void run(const ProductArgs& p, const ProductTile& tile, int64_t row, int64_t column,
-                                             float (&v)[BN / 2], TurnStore& store) {
+                                             float (&v)[S::kWidth], TurnStore<S::kBuffers>& store) {
+    constexpr int kWidth = S::kWidth;
     const SoftmaxArgs& s = p.softmax;
     const int lane = store.lane;
     const int64_t first = tile.worker * p.rows + row;
@@ -146,9 +150,9 @@ struct GradEpilogue {
     }
     if (target < 0) factor = 0.f;  // the row does not count: see below where its logits are not finite
     const int64_t place = target - s.first - column;
-    const int t = target >= 0 && place >= 0 && place < BN / 2 ? (int)place : -1;
+    const int t = target >= 0 && place >= 0 && place < kWidth ? (int)place : -1;
 #pragma unroll
-    for (int g = 0; g < BN / 2; g += 32) {
+    for (int g = 0; g < kWidth; g += 32) {
       if (column + g >= p.columns) break;
       float2 x[16];
 #pragma unroll
@@ -221,7 +225,8 @@ template <typename Epilogue>
 cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool thin, uint32_t* err, cudaStream_t stream,
                             uint64_t* launches) {
   ProductArgs args{};
-  if (!(thin ? product_args<64>(p, 16, err, &args) : product_args<256>(p, 16, err, &args))) return cudaErrorInvalidValue;
+  const int chunk = p.terms.count == 6 ? 12 : 16;
+  if (!(thin ? product_args<64>(p, chunk, err, &args) : product_args<256>(p, chunk, err, &args))) return cudaErrorInvalidValue;
   args.softmax = softmax;
   if (softmax.grad && !encode_result(softmax.grad, DQGAN_BF16, p.columns, p.rows, p.workers, softmax.grad_parts, softmax.grad_ld,
                                      p.rows * softmax.grad_ld, softmax.grad_part, &args.out))
@@ -292,8 +297,8 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
                        operand_in_place(a.weight, s.width, a.p_stride);
     const int64_t step = whole ? s.vocab : piece;
     const bool thin = narrow(a.rows, s.workers, step < s.vocab ? step : s.vocab);
-    const int64_t columns = thin ? 32 : 128;
-    soft.slots = (int32_t)(ceil_div(s.vocab, 2 * columns) * 2);
+    const int64_t columns = thin ? ProductShape<64>::kWidth : ProductShape<256>::kWidth;  // of a slot
+    soft.slots = (int32_t)(2 * ceil_div(s.vocab, 2 * columns));
     for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += step) {
       logits.columns = s.vocab - first < step ? s.vocab - first : step;
       if ((st = weights(first, logits.columns, logit_parts, half, &logits.b)) != cudaSuccess) break;
