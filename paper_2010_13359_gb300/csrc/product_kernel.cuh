@@ -205,19 +205,21 @@ struct TurnStore {
     }
   }
 
-  // Single values, for matrices that TMA cannot write: 16 columns that lane r holds of row r; then column l & 15 of row
-  // 2 i + l / 16.
+  // Single values, for matrices that TMA cannot write: kTurn columns that lane r holds of row r; then column l % kTurn of
+  // row i * kTurned + l / kTurn.
+  static constexpr int kTurn = 16 * kBuffers, kTurned = 32 / kTurn;
+  __device__ __forceinline__ float* turned_pack(int row, int c) const {  // no two of what a warp reads or writes at once meet in a bank
+    return reinterpret_cast<float*>(buffer + row * (4 * kTurn) + ((c ^ (kBuffers == 2 ? row & 7 : row / 2 & 3)) * 16));
+  }
   __device__ __forceinline__ void turn(const float* x) {
     if (lane == 0) bulk_wait_read_all();
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      *reinterpret_cast<float4*>(buffer + lane * 64 + ((c ^ (lane / 2 & 3)) * 16)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    for (int c = 0; c < kTurn / 4; ++c)
+      *reinterpret_cast<float4*>(turned_pack(lane, c)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
     __syncwarp();
   }
-  __device__ __forceinline__ float turned(int i) const {
-    return *reinterpret_cast<const float*>(buffer + (2 * i + lane / 16) * 64 + (((lane & 15) / 4) ^ (i & 3)) * 16 + (lane & 3) * 4);
-  }
+  __device__ __forceinline__ float turned(int i) const { return turned_pack(i * kTurned + lane / kTurn, lane % kTurn / 4)[lane & 3]; }
 };
 
 struct ProductTile {
@@ -428,15 +430,17 @@ __global__ void __launch_bounds__(ShapeOf<BN, Epilogue>::kThreads, 1) product_ke
   if (warp == 2) tensor_memory_free<kPair>(sums, kColumns);
 }
 
-// The pieces' sums of the split tiles in order, and what is done with them.  A block a tile and half of a pair.
+// The pieces' sums of the split tiles in order, and what is done with them.  A warp for each of the
+// tile's, two to a block.
 template <int BN, typename Epilogue>
-__global__ void __launch_bounds__(32 * ShapeOf<BN, Epilogue>::kSumWarps, 1) join_kernel(const __grid_constant__ ProductArgs p) {
+__global__ void __launch_bounds__(64) join_kernel(const __grid_constant__ ProductArgs p) {
   dq_pdl_enter();
   using S = ShapeOf<BN, Epilogue>;
-  __shared__ __align__(1024) uint8_t turn[S::kTurnBytes];
-  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
-  const int rank = (int)blockIdx.x % S::kPair;
-  const int64_t first = (int64_t)(blockIdx.x / S::kPair) * p.pieces;
+  constexpr int kBlocks = S::kPair * S::kSumWarps / 2;  // of a tile
+  __shared__ __align__(1024) uint8_t turn[2 * 2048 * S::kBuffers];
+  const int in = (int)(blockIdx.x % kBlocks) * 2 + (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  const int rank = in / S::kSumWarps, warp = in % S::kSumWarps;
+  const int64_t first = (int64_t)(blockIdx.x / kBlocks) * p.pieces;
   const ProductTile tile = product_tile<BN>(p, p.whole + first);
   float v[S::kWidth];
 #pragma unroll
@@ -452,7 +456,7 @@ __global__ void __launch_bounds__(32 * ShapeOf<BN, Epilogue>::kSumWarps, 1) join
       v[4 * j + 3] = __fadd_rn(v[4 * j + 3], x.w);
     }
   }
-  TurnStore<S::kBuffers> store{turn + warp * (S::kTurnBytes / S::kSumWarps), lane};
+  TurnStore<S::kBuffers> store{turn + threadIdx.x / 32 * (2048 * S::kBuffers), lane};
   Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * (warp & 3), tile.column + warp / 4 * S::kWidth, v, store);
   bulk_wait_all();
 }
@@ -563,7 +567,7 @@ inline cudaError_t launch_product(const ProductArgs& p, cudaStream_t stream, uin
   const int64_t split = (int64_t)p.tiles_m * p.tiles_n * p.workers - p.whole;
   if (st != cudaSuccess || split == 0) return st;
   ++*launches;
-  return launch_pdl(join_kernel<BN, Epilogue>, dim3((unsigned)(split * S::kPair)), dim3(32 * S::kSumWarps), 0, stream, p);
+  return launch_pdl(join_kernel<BN, Epilogue>, dim3((unsigned)(split * S::kPair * S::kSumWarps / 2)), dim3(64), 0, stream, p);
 }
 
 }  // namespace dq

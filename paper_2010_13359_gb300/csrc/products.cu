@@ -74,21 +74,23 @@ struct StoreEpilogue {
           add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
         store.template put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
       } else {
+        constexpr int kTurn = TurnStore<S::kBuffers>::kTurn, kTurned = TurnStore<S::kBuffers>::kTurned;
 #pragma unroll
-        for (int q = 0; q < 32; q += 16) {
-          const int64_t at = j + q + (lane & 15);
-          const float one = __shfl_sync(kFullMask, b, q + (lane & 15));
+        for (int q = 0; q < 32; q += kTurn) {
+          const int64_t at = j + q + lane % kTurn;
+          const float one = __shfl_sync(kFullMask, b, q + lane % kTurn);
           store.turn(x + q);
           if (at >= p.columns) continue;
           if (!s.add && !s.pre && !s.residual && s.activation == DQGAN_NONE) {
-            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + row * s.out_ld + at;
+            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + (row + lane / kTurn) * s.out_ld + at;
 #pragma unroll 8
-            for (int i = 0; i < 16; ++i)
-              if (2 * i + lane / 16 < rows) to[(2 * i + lane / 16) * s.out_ld] = from_float<T>(store.turned(i) + one);
+            for (int i = 0; i < 32 / kTurned; ++i)
+              if (i * kTurned + lane / kTurn < rows) to[i * kTurned * s.out_ld] = from_float<T>(store.turned(i) + one);
           } else {
 #pragma unroll 4
-            for (int i = 0; i < 16; ++i)
-              if (2 * i + lane / 16 < rows) store_value<T>(s, tile.worker, row + 2 * i + lane / 16, at, store.turned(i), one);
+            for (int i = 0; i < 32 / kTurned; ++i)
+              if (i * kTurned + lane / kTurn < rows)
+                store_value<T>(s, tile.worker, row + i * kTurned + lane / kTurn, at, store.turned(i), one);
           }
         }
       }
