@@ -405,8 +405,8 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
 /*
  * Operators of a token model's workers.  The paper leaves F(w; xi), the
  * stochastic gradient a worker compresses, to the caller's model; for a model
- * over tokens these calls are the ends of that gradient that a matrix
- * product does not cover, batched over the workers like
+ * over tokens these calls are the parts that such a gradient is made of, batched
+ * over the workers like
  * dqgan_workers_compress_all: worker m reads its parameters at
  * params + m * p_stride (its lookahead point, or p_stride = 0: one vector for
  * all workers) and writes its gradient at g + m * g_stride (the row the
@@ -445,7 +445,13 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *     nothing before the first row's first value or after the last row's last.
  *   - Parameters, gradients, statistics and losses are fp32, and so is all
  *     arithmetic: sums, softmax statistics and norms are held in 32 bits
- *     and a 16-bit result is rounded once.  Every sum has a fixed order, so the
+ *     and a 16-bit result is rounded once.  (Weights of linear layers and of
+ *     the token loss may be of the activations' type.)  The products of these two multiply 16-bit
+ *     values: operands that are fp32, or computed in fp32 (the gradients of u
+ *     and of z), are rounded to one bf16 value where the result is bf16, and
+ *     taken as the sum of two (off by 2^-16 of themselves) where it is f16, an
+ *     fp32 gradient or a loss; of three (2^-24) where the activations are fp32.
+ *     A value that is not finite makes what it enters not finite.  Every sum has a fixed order, so the
  *     same call on the same data gives the same bits.  Exponentials below 2^-126
  *     may be taken as 0, and the last digits of a result depend on whether its
  *     row fits on chip.

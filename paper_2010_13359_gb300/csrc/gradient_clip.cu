@@ -8,6 +8,8 @@
 // give each block a run of them; the second pass walks them backwards, so that it
 // finds in L2 what the first one read last.
 //
+// Up to 2^18 values a worker take one launch of a cluster each.
+//
 // A block's thread sums the squares of at most 64 values of a unit in fp32, then in
 // fp64, and the blocks' sums are joined in a fixed order.  Where a thread's fp32 sum
 // leaves [2^-80, 2^120], its squares are taken again in fp64.
@@ -46,6 +48,9 @@ struct ClipArgs {
   double max_norm, eps;
   float* norms;
 };
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 template <int kTensors>
 struct ClipTable {
@@ -169,6 +174,17 @@ __global__ void __launch_bounds__(kClipThreads) norms_kernel(const __grid_consta
   if (threadIdx.x == 0) a.norms[blockIdx.x] = (float)norm;
 }
 
+// The factor of a worker's values, in two steps: one below fp32's range, which large values bring back into it, by a power
+// of two first, which is exact.
+struct ClipFactor {
+  float shift, factor;
+};
+__device__ __forceinline__ ClipFactor clip_factor(const ClipArgs& a, double norm) {
+  const double scale = isfinite(norm) ? fmin(1., a.max_norm / (norm + a.eps)) : 1.;
+  const float shift = scale < 0x1p-150 ? 0x1p-126f : scale < 0x1p-64 ? 0x1p-64f : 1.f;
+  return {shift, (float)(scale / shift)};
+}
+
 template <typename T, typename O>
 __device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float shift, float factor) {
   constexpr int E = 16 / (int)sizeof(T);
@@ -221,15 +237,12 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
   const ClipLaunch& l = a.tables[a.table];
   const int64_t begin = first_unit(a, l, blockIdx.x), end = first_unit(a, l, (int64_t)blockIdx.x + 1);
   int64_t known = -1;
-  float shift = 1.f, factor = 1.f;
+  ClipFactor f{1.f, 1.f};
   for (int64_t u = end - 1; u >= begin; --u) {
     const int64_t worker = u / l.units, unit = u - worker * l.units;
     if (worker != known) {
       const double norm = worker_norm(a, worker, shared);
-      const double scale = isfinite(norm) ? fmin(1., a.max_norm / (norm + a.eps)) : 1.;
-      // a factor below fp32's range, which large values bring back into it, in two steps; a power of two is exact
-      shift = scale < 0x1p-150 ? 0x1p-126f : scale < 0x1p-64 ? 0x1p-64f : 1.f;
-      factor = (float)(scale / shift);
+      f = clip_factor(a, norm);
       known = worker;
       // one block has the worker's first unit of the last table that is walked
       if (a.norms && threadIdx.x == 0 && a.table == a.norm_table && worker * l.units >= begin) a.norms[worker] = (float)norm;
@@ -237,8 +250,50 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
     const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
     const int64_t at = (unit - t.unit) * a.unit;
     scale_unit(static_cast<const T*>(t.from) + worker * t.from_stride + at,
-               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), shift, factor);
+               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), f.shift, f.factor);
   }
+}
+
+// Few values: a cluster of eight blocks a worker does both passes in one launch, its sums exchanged through shared memory.
+constexpr int kFewBlocks = 8;
+constexpr int64_t kFewValues = 1 << 18;
+template <typename T, typename O, int kTensors>
+__global__ void __launch_bounds__(kClipThreads) few_values_kernel(const __grid_constant__ ClipArgs a,
+                                                                   const __grid_constant__ ClipTable<kTensors> table, bool scale) {
+  dq_pdl_enter();
+  __shared__ double shared[kClipThreads / 32], sums[kFewBlocks];
+  cluster_arrive();  // every block of the cluster runs before another touches its shared memory
+  const ClipLaunch& l = a.tables[0];
+  const int64_t worker = blockIdx.x / kFewBlocks;
+  const int rank = (int)(blockIdx.x % kFewBlocks);
+  double sum = 0.;
+  const auto each = [&](int64_t unit, auto&& f) {
+    const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
+    const int64_t at = (unit - t.unit) * a.unit;
+    f(t, static_cast<const T*>(t.from) + worker * t.from_stride + at, at, (int)min64(a.unit, t.size - at));
+  };
+  int64_t unit = rank;
+  for (; unit < l.units; unit += kFewBlocks)
+    each(unit, [&](const ClipTensor&, const T* from, int64_t, int n) { sum += unit_squares(from, n); });
+  sum = block_sum_double(sum, shared);
+  cluster_wait();
+  if (threadIdx.x < kFewBlocks) {
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(sums + rank)), "r"((uint32_t)threadIdx.x));
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(sum) : "memory");
+  }
+  cluster_arrive();
+  cluster_wait();
+  double total = 0.;
+  for (int i = 0; i < kFewBlocks; ++i) total += sums[i];
+  const double norm = sqrt(total);
+  if (a.norms && rank == 0 && threadIdx.x == 0) a.norms[worker] = (float)norm;
+  if (!scale) return;
+  const ClipFactor f = clip_factor(a, norm);
+  for (unit -= kFewBlocks; unit >= 0; unit -= kFewBlocks)
+    each(unit, [&](const ClipTensor& t, const T* from, int64_t at, int n) {
+      scale_unit(from, static_cast<O*>(t.to) + worker * t.to_stride + at, n, f.shift, f.factor);
+    });
 }
 
 template <typename T, typename O, int kTensors>
@@ -270,6 +325,13 @@ cudaError_t launch_clip(const ClipShape& s, int64_t count, const dqgan_tensor* f
     l.sums = static_cast<double*>(scratch) + (int64_t)i * (kClipBlocks + s.workers);
   };
   cudaError_t st = cudaSuccess;
+  if (a.count_tables == 1 && values > 0 && values <= kFewValues) {
+    a.unit = kLeastUnit;
+    fill(0);
+    ++*launches;
+    return launch_pdl_cluster(few_values_kernel<T, O, kTensors>, kFewBlocks, dim3((unsigned)s.workers * kFewBlocks), dim3(kClipThreads),
+                              0, stream, a, table, to != nullptr);
+  }
   for (int i = 0; i < a.count_tables && st == cudaSuccess; ++i) {
     fill(i);
     if (a.tables[i].units == 0) continue;

@@ -80,7 +80,7 @@ struct SlopeArgs {
 template <typename T, bool kSlope>
 __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
   dq_pdl_enter();
-  __shared__ float turn[8][kGradColumns];
+  __shared__ __align__(16) float turn[8][kGradColumns];
   constexpr int kAhead = 4, E = 16 / (int)sizeof(T), kPacks = 8 / E;
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int64_t column = (int64_t)blockIdx.x * kGradColumns + lane * 8;
@@ -108,7 +108,8 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
     }
   };
   int64_t r = first + warp;
-  if (count == 8 && a.dy_packs && (!kSlope || a.pre_packs)) {
+  const bool packs = a.dy_packs && (!kSlope || a.pre_packs);
+  if (packs && count == 8) {
     for (; r + 8 * (kAhead - 1) < last; r += 8 * kAhead) {
       uint4 d[kAhead][kPacks], p[kAhead][kPacks];
 #pragma unroll
@@ -127,13 +128,35 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
       }
     }
   }
-  if (count > 0)
+  if (packs) {
+    if (count > 0)
+      for (; r < last; r += 8) {
+        float x[8], u[8] = {};
+        read8(dy + r * a.dy_ld, count, true, x);
+        if constexpr (kSlope) read8(pre + r * a.pre_ld, count, true, u);
+        row(r, x, u);
+      }
+  } else {
+    // a row's 256 values one a lane at a time, turned to eight a lane
+    const int wide = (int)min((int64_t)kGradColumns, a.columns - (int64_t)blockIdx.x * kGradColumns);
+    const auto fetch = [&](const T* at, float (&x)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 32 * i + lane < wide ? to_float(at[32 * i + lane - 8 * lane]) : 0.f;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn[warp][32 * i + lane] = x[i];
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(&turn[warp][8 * lane + i]);
+    };
     for (; r < last; r += 8) {
-      float x[8], u[8] = {};
-      read8(dy + r * a.dy_ld, count, a.dy_packs, x);
-      if constexpr (kSlope) read8(pre + r * a.pre_ld, count, a.pre_packs, u);
-      row(r, x, u);
+      alignas(16) float x[8], u[8] = {};
+      fetch(dy + r * a.dy_ld, x);
+      if constexpr (kSlope) fetch(pre + r * a.pre_ld, u);
+      if (count > 0) row(r, x, u);
     }
+    __syncwarp();
+  }
   if (a.sums) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) turn[warp][lane * 8 + i] = sum[i];

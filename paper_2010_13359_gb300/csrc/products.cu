@@ -216,7 +216,7 @@ cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer
   out->shared = m.batch == 0 && m.workers > 1;
   out->half = half;
   out->across = false;
-  if (as_is && operand_in_place(m.data, m.ld, m.batch)) {
+  if (as_is && operand_in_place(m.data, m.ld, m.workers > 1 ? m.batch : 0)) {
     out->data = m.data;
     out->ld = m.ld;
     out->batch = m.batch;

@@ -42,11 +42,12 @@ bool narrow(int64_t rows, int32_t workers, int64_t columns) {
   return ceil_div(rows, kTileRows) * ceil_div(columns, 256) * workers < kFewTiles;
 }
 
-int64_t most_slots(int64_t vocab) {
-  const int64_t wide = 2 * ceil_div(vocab, 256), thin = 2 * ceil_div(vocab, 64);
-  const int64_t few = thin < 8 * kFewTiles ? thin : 8 * kFewTiles;
-  return wide > few ? wide : few;
-}
+// Slots that the scratch space has for a row: those of wide tiles, and of narrow ones where a vocabulary is small enough
+// for them (in pieces a large one's could have narrow tiles too).
+constexpr int64_t wide_slots(int64_t vocab) { return 2 * ceil_div(vocab, 256); }
+constexpr int64_t thin_slots(int64_t vocab) { return 2 * ceil_div(vocab, 64); }
+bool thin_fits(int64_t vocab) { return thin_slots(vocab) <= 8 * kFewTiles; }
+int64_t most_slots(int64_t vocab) { return thin_fits(vocab) ? thin_slots(vocab) : wide_slots(vocab); }
 
 struct Scratch {
   uint32_t* err;
@@ -294,11 +295,11 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
   if (a.forward) {
     // all at once where the weights can be read as they lie
     const bool whole = (half || (s.weight_dtype == DQGAN_BF16 && logit_parts == 1)) &&
-                       operand_in_place(a.weight, s.width, a.p_stride);
+                       operand_in_place(a.weight, s.width, s.workers > 1 ? a.p_stride : 0);
     const int64_t step = whole ? s.vocab : piece;
-    const bool thin = narrow(a.rows, s.workers, step < s.vocab ? step : s.vocab);
+    const bool thin = thin_fits(s.vocab) && narrow(a.rows, s.workers, step < s.vocab ? step : s.vocab);
     const int64_t columns = thin ? ProductShape<64>::kWidth : ProductShape<256>::kWidth;  // of a slot
-    soft.slots = (int32_t)(2 * ceil_div(s.vocab, 2 * columns));
+    soft.slots = (int32_t)(thin ? thin_slots(s.vocab) : wide_slots(s.vocab));
     for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += step) {
       logits.columns = s.vocab - first < step ? s.vocab - first : step;
       if ((st = weights(first, logits.columns, logit_parts, half, &logits.b)) != cudaSuccess) break;
