@@ -29,8 +29,12 @@ int grad_parts(const LinearShape& s) {
 bool half_forward(const LinearShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
 bool half_backward(const LinearShape& s) { return half_forward(s) && exact_slope(s.activation); }
 
-constexpr int kGradRows = 64;  // least rows of a block of slope_kernel
-constexpr int kGradColumns = 256;
+constexpr int kGradColumns = 256;   // of a block of slope_kernel
+constexpr int kGradBlocks = 152 * 8;
+// Blocks of a worker's rows: what fills the GPU eight times, of eight rows at least.
+int64_t most_row_blocks(const LinearShape& s) {
+  return ceil_div(kGradBlocks, ceil_div(s.outputs, kGradColumns) * s.workers);
+}
 
 struct Scratch {
   uint32_t* err;
@@ -54,7 +58,7 @@ Scratch scratch_of(const LinearShape& s, void* base) {
   c.x = take(rows * round8(s.inputs) * 2 * act_parts(s.dtype));
   c.w = take((int64_t)s.workers * s.outputs * round8(s.inputs) * 2 * weight_parts(s));
   c.d = take(rows * round8(s.outputs) * 2 * grad_parts(s));
-  c.sums = static_cast<float*>(take((int64_t)s.workers * ceil_div(s.max_rows, kGradRows) * s.outputs * 4));
+  c.sums = static_cast<float*>(take(s.workers * most_row_blocks(s) * s.outputs * 4));
   c.bytes = at;
   return c;
 }
@@ -366,8 +370,6 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     }
     return st;
   }
-  const int sms = device_sms();
-  if (sms <= 0) return cudaErrorInvalidDevice;
   const bool half = half_backward(s);
   const int parts = half ? 1 : grad_parts(s);
   const MatrixArgs dy{a.dy, a.dy_ld, a.rows * a.dy_ld, s.dtype, a.rows, s.outputs, s.workers};
@@ -396,12 +398,10 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     k.to = direct ? nullptr : c.d;
     k.sums = a.dbias ? c.sums : nullptr;
     const int64_t wide = ceil_div(s.outputs, kGradColumns);
-    // eight blocks an SM, of 64 rows at least
-    int64_t blocks = ceil_div((int64_t)sms * 8, wide * s.workers);
-    k.block_rows = (int32_t)(ceil_div(ceil_div(a.rows, blocks), kGradRows) * kGradRows);
-    blocks = ceil_div(a.rows, k.block_rows);
+    k.block_rows = (int32_t)(ceil_div(ceil_div(a.rows, most_row_blocks(s)), 8) * 8);
+    const int64_t blocks = ceil_div(a.rows, k.block_rows);
     ++*launches;
-    st = blocks > 65535 ? cudaErrorInvalidValue : with_dtype(s.dtype, [&](auto t) {
+    st = with_dtype(s.dtype, [&](auto t) {
       const dim3 grid((unsigned)wide, (unsigned)blocks, (unsigned)s.workers);
       return k.pre ? launch_pdl(slope_kernel<decltype(t), true>, grid, dim3(256), 0, stream, k)
                    : launch_pdl(slope_kernel<decltype(t), false>, grid, dim3(256), 0, stream, k);

@@ -76,6 +76,9 @@ LINEAR = [  # workers, rows, inputs, outputs, dtype, weight dtype, activation, p
     (1, 1400, 1021, 2301, 1, 1, 1, 3, 0, False),
     (2, 8, 4104, 77, 1, 0, 3, 0, 0, False),
     (1, 9, 2050, 130, 0, 0, 0, 2, 0, False),
+    (1, 20, 65536, 9, 1, 1, 0, 0, 0, False),
+    (1, 20, 9, 65536, 1, 1, 2, 0, 0, False),
+    (200, 10, 16, 24, 1, 1, 2, 0, 0, False),
 ]
 
 
@@ -185,6 +188,8 @@ LOSS = [  # workers, rows, vocab, width, dtype, weight dtype, token bits, pad, s
     (1, 700, 8200, 72, 0, 0, 32, 0, 0, False, 0.05),
     (2, 600, 4100, 136, 2, 2, 32, 0, 0, False, 0.05),
     (1, 257, 20000, 104, 1, 0, 32, 0, 0, False, 1.0),
+    (100, 5, 40, 24, 1, 1, 32, 0, 0, False, 0.2),
+    (1, 33, 70, 65536, 1, 1, 32, 0, 0, False, 0.0),
 ]
 
 
