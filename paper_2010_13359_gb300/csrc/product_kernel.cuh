@@ -9,7 +9,7 @@
 // of tensor memory, two accumulators in turn, so that an epilogue runs beside the
 // next tile's products.
 //
-// Of bf16 products of 8192^3: 595 us, 1850 TFLOP/s (a library product: 540); 503
+// Of bf16 products of 8192^3: 578 us, 1900 TFLOP/s (a library product: 541); 503
 // without the loads, 665 with four stages: what is left is the loads' latency, for which six stages of 32 KB
 // are what fits.  Four blocks that share an operand by TMA multicast: 608, as
 // clusters of four leave 8 of 152 SMs idle.
@@ -17,7 +17,7 @@
 // The tensor cores' own sums are rounded towards zero, by up to one unit in the
 // last place each 16 products: over thousands of them the error grows past that
 // of fp32 sums.  So an accumulator takes `chunk` blocks only; the warps
-// add it to sums in registers (64 a thread), rounded to nearest, while the
+// add it to sums in registers (128 or 64 a thread), rounded to nearest, while the
 // other accumulator fills.  16 blocks (1024 products) where the result has 32 bits
 // (12, two for each pair of parts, where the operands have), 32 in f16, 128 in bf16: taking sums out costs the products up
 // to a tenth at 8.

@@ -1,5 +1,7 @@
 // Matrix products that are stored: with bias, activation, residual, or added to
 // what is there; and the splitting of operands into 16-bit parts.
+#include <initializer_list>
+
 #include "product_kernel.cuh"
 
 namespace dq {
@@ -118,9 +120,9 @@ Cut cut_product(const Product& p, int64_t slots) {
     const int64_t tiles = ceil_div(p.rows, wide ? 256 : 128) * ceil_div(p.columns, width) * p.workers;
     const int64_t at_once = wide ? slots / 2 : slots, rest = tiles % at_once, whole = tiles - rest;
     const double block = wide ? 1. : 0.6, end = wide ? 12. : 3., sums = wide ? 0.3 : 0.04;
-    for (int pieces = 1; pieces <= 32 && pieces <= depth; ++pieces) {
+    for (const int pieces : {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 16, 24, 32}) {
       const int64_t items = rest * pieces;
-      if (pieces > 1 && (rest == 0 || (size_t)items * (wide ? 1 << 18 : 1 << 15) > kProductScratch)) break;
+      if (pieces > 1 && (rest == 0 || pieces > depth || (size_t)items * (wide ? 1 << 18 : 1 << 15) > kProductScratch)) break;
       double time = (double)(whole / at_once) * (length * block + end) +
                     (double)ceil_div(items, at_once) * (ceil_div(depth, pieces) * p.terms.count * block + end);
       if (pieces > 1) time += 10. + items * sums + pieces;
