@@ -351,8 +351,10 @@ cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint
   p.workers = s.workers;
   const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
   const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
-  cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.a);
-  if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
+  Splits splits{stream, launches};
+  cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, splits, &p.a);
+  if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, splits, &p.b);
+  if (st == cudaSuccess) st = splits.flush();
   if (st != cudaSuccess) return st;
   p.terms = product_terms(p.a.parts, p.b.parts);
   return launch_product_store(p, out, c.products, c.err, stream, launches);
@@ -375,8 +377,18 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
   const MatrixArgs dy{a.dy, a.dy_ld, a.rows * a.dy_ld, s.dtype, a.rows, s.outputs, s.workers};
   const bool direct = s.activation == DQGAN_NONE && (half || (s.dtype == DQGAN_BF16 && parts == 1)) &&
                       operand_in_place(a.dy, a.dy_ld, a.rows * a.dy_ld);
-  ProductOperand d;
-  if (direct) st = make_operand(dy, parts, half, c.d, stream, launches, &d);
+  ProductOperand d, weight, x;
+  Splits splits{stream, launches};
+  if (direct) st = make_operand(dy, parts, half, c.d, splits, &d);
+  if (st == cudaSuccess && a.dx) {
+    const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
+    st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, splits, &weight);
+  }
+  if (st == cudaSuccess && a.dweight) {
+    const MatrixArgs rows{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+    st = make_operand(rows, half ? 1 : act_parts(s.dtype), half, c.x, splits, &x);
+  }
+  if (st == cudaSuccess) st = splits.flush();
   if (st == cudaSuccess && (!direct || a.dbias)) {
     const int size = s.dtype == DQGAN_F32 ? 4 : 2;
     SlopeArgs k{};
@@ -429,9 +441,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     p.workers = s.workers;
     p.a = d;
     if (s.dtype == DQGAN_BF16) p.a.parts = 1;
-    const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
-    st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, stream, launches, &p.b);
-    if (st != cudaSuccess) return st;
+    p.b = weight;
     p.b.across = true;
     p.terms = product_terms(p.a.parts, p.b.parts);
     StoreArgs out{};
@@ -448,9 +458,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     p.depth = a.rows;
     p.workers = s.workers;
     p.a = d;
-    const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
-    st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, stream, launches, &p.b);
-    if (st != cudaSuccess) return st;
+    p.b = x;
     p.a.across = p.b.across = true;
     p.terms = product_terms(p.a.parts, p.b.parts);
     StoreArgs out{};

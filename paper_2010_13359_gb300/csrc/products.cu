@@ -179,11 +179,14 @@ cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void*
 // ---- parts ----
 namespace {
 
+// 8 values of one of two matrices a thread; the second one's follow the first one's.
 template <typename T>
-__global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, bool packs) {
+__global__ void __launch_bounds__(256) split_kernel(const SplitArgs first, const SplitArgs second) {
   dq_pdl_enter();
-  const int64_t across = a.ld / 8, total = across * a.rows * a.workers;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+  const int64_t of_first = first.ld / 8 * first.rows * first.workers, total = of_first + second.ld / 8 * second.rows * second.workers;
+  for (int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; at < total; at += (int64_t)gridDim.x * blockDim.x) {
+    const SplitArgs& a = at < of_first ? first : second;
+    const int64_t i = at < of_first ? at : at - of_first, across = a.ld / 8;
     const int64_t r = i / across;
     const int column = (int)(i - r * across) * 8;
     const int64_t worker = r / a.rows, row = r - worker * a.rows;
@@ -193,27 +196,36 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs a, bool pack
       const int64_t t = token_at(a.targets, a.token_bits, r);
       counts = t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
     }
-    if (counts) read8(static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column, (int)min64(8, a.columns - column), packs, x);
+    if (counts) read8(static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column, (int)min64(8, a.columns - column), a.packs, x);
     write_parts<true>(x, a.to, r * a.ld + column, a.part, a.parts, a.half);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_split(const SplitArgs& a, cudaStream_t stream, uint64_t* launches) {
-  const int64_t total = a.ld / 8 * a.rows * a.workers;
-  if (total == 0) return cudaSuccess;
+cudaError_t Splits::add(const SplitArgs& a) {
+  cudaError_t st = cudaSuccess;
+  if (a.rows == 0 || a.workers == 0) return st;
+  if (count == 2 || (count == 1 && pending[0].dtype != a.dtype)) st = flush();
+  pending[count] = a;
   const int64_t size = a.dtype == DQGAN_F32 ? 4 : 2;
-  const bool packs = ((uintptr_t)a.from & 15) == 0 && a.from_ld * size % 16 == 0 && a.batch * size % 16 == 0;
+  pending[count++].packs = ((uintptr_t)a.from & 15) == 0 && a.from_ld * size % 16 == 0 && (a.workers == 1 || a.batch * size % 16 == 0);
+  return st;
+}
+
+cudaError_t Splits::flush() {
+  if (count == 0) return cudaSuccess;
+  const SplitArgs first = pending[0], second = count == 2 ? pending[1] : SplitArgs{};
+  count = 0;
+  const int64_t total = first.ld / 8 * first.rows * first.workers + second.ld / 8 * second.rows * second.workers;
   const int sms = device_sms();
   if (sms <= 0) return cudaErrorInvalidDevice;
   ++*launches;
   const dim3 grid((unsigned)min64(ceil_div(total, 256), (int64_t)sms * 8));
-  return with_dtype(a.dtype, [&](auto t) { return launch_pdl(split_kernel<decltype(t)>, grid, dim3(256), 0, stream, a, packs); });
+  return with_dtype(first.dtype, [&](auto t) { return launch_pdl(split_kernel<decltype(t)>, grid, dim3(256), 0, stream, first, second); });
 }
 
-cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, cudaStream_t stream,
-                         uint64_t* launches, ProductOperand* out) {
+cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, Splits& splits, ProductOperand* out) {
   const bool as_is = !m.targets && (half ? m.dtype == DQGAN_F16 : m.dtype == DQGAN_BF16 && parts == 1);
   out->shared = m.batch == 0 && m.workers > 1;
   out->half = half;
@@ -248,7 +260,7 @@ cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer
   out->batch = s.ld * s.rows;
   out->part = s.part;
   out->parts = parts;
-  return launch_split(s, stream, launches);
+  return splits.add(s);
 }
 
 }  // namespace dq

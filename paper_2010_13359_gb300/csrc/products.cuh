@@ -113,8 +113,17 @@ struct SplitArgs {
   const float* weights;   // or nullptr
   int32_t token_bits;
   int64_t vocab;
+  bool packs;             // rows can be read 16 bytes at a time (set by Splits)
 };
-cudaError_t launch_split(const SplitArgs& a, cudaStream_t stream, uint64_t* launches);
+// Matrices that are to be split, two of one type to a launch.  What is added has to be flushed before it is read.
+struct Splits {
+  cudaStream_t stream;
+  uint64_t* launches;
+  SplitArgs pending[2] = {};
+  int count = 0;
+  cudaError_t add(const SplitArgs& a);
+  cudaError_t flush();
+};
 
 // Whether a matrix of a 16-bit type can be an operand as it lies.
 inline bool operand_in_place(const void* p, int64_t ld, int64_t batch) {
@@ -347,7 +356,6 @@ struct MatrixArgs {
   int64_t vocab = 0;
 };
 // The operand that it is: as it lies, or split into `buffer`.
-cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, cudaStream_t stream,
-                         uint64_t* launches, ProductOperand* out);
+cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, Splits& splits, ProductOperand* out);
 
 }  // namespace dq

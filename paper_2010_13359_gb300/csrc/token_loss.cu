@@ -264,9 +264,10 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
 
   // x: of the gradient, the rows that do not count as zeros, whatever they hold
   ProductOperand x_logits, x_grad;
+  Splits splits{stream, launches};
   MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.width, s.workers};
   if (a.forward || a.dx || a.dweight) {
-    if (half) st = make_operand(x, 1, true, c.x_half, stream, launches, &x_logits);
+    if (half) st = make_operand(x, 1, true, c.x_half, splits, &x_logits);
     if (a.backward) {
       x.targets = a.targets;
       x.weights = a.weights;
@@ -274,7 +275,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
       x.vocab = s.vocab;
     }
     if (st == cudaSuccess && (!half || a.backward))
-      st = make_operand(x, act_parts(s.dtype), false, c.x, stream, launches, &x_grad);
+      st = make_operand(x, act_parts(s.dtype), false, c.x, splits, &x_grad);
     if (!half) x_logits = x_grad;
     if (st != cudaSuccess) return st;
   }
@@ -283,7 +284,8 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
   const auto weights = [&](int64_t first, int64_t count, int parts, bool as_half, ProductOperand* out) {
     const MatrixArgs w{static_cast<const char*>(a.weight) + first * s.width * wsize, s.width, a.p_stride, s.weight_dtype,
                        count, s.width, s.workers};
-    return make_operand(w, parts, as_half, c.w, stream, launches, out);
+    const cudaError_t made = make_operand(w, parts, as_half, c.w, splits, out);
+    return made == cudaSuccess ? splits.flush() : made;  // with what x needs, the first time
   };
   Product logits;
   logits.rows = a.rows;
