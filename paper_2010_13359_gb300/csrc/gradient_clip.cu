@@ -133,7 +133,7 @@ __device__ __forceinline__ double unit_squares(const T* p, int n) {
 }
 
 template <typename T, int kTensors>
-__global__ void __launch_bounds__(kClipThreads) norm_kernel(const __grid_constant__ ClipArgs a,
+__global__ void __launch_bounds__(kClipThreads, 4) norm_kernel(const __grid_constant__ ClipArgs a,
                                                              const __grid_constant__ ClipTable<kTensors> table) {
   dq_pdl_enter();
   __shared__ double shared[kClipThreads / 32];
@@ -186,12 +186,34 @@ __device__ __forceinline__ ClipFactor clip_factor(const ClipArgs& a, double norm
 }
 
 template <typename T, typename O>
-__device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float shift, float factor) {
+__device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float shift, float factor, const T* begin, const T* end) {
   constexpr int E = 16 / (int)sizeof(T);
   const int head = head_of(from, n);
   const auto one = [&](int i) { to[i] = from_float<O>(to_float(from[i]) * shift * factor); };
-  if ((((uintptr_t)(to + head)) & 15) != 0) {  // the two sides' packs do not meet
-    for (int i = (int)threadIdx.x; i < n; i += kClipThreads) one(i);
+  if ((((uintptr_t)(to + head)) & 15) != 0) {  // the two sides' packs do not meet: the places' ones, shifted out of the tensor's
+    constexpr int F = 16 / (int)sizeof(O);
+    const int first = head_of(to, n), eights = (n - first) / 8, rest = first + eights * 8;
+    if ((int)threadIdx.x < first) one(threadIdx.x);
+    if ((int)threadIdx.x < n - rest) one(rest + threadIdx.x);
+    for (int i = (int)threadIdx.x; i < eights; i += 2 * kClipThreads) {
+      float x[2][8];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (i + k * kClipThreads < eights) read8_near(from + first + 8 * (i + k * kClipThreads), 8, begin, end, x[k]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (i + k * kClipThreads >= eights) break;
+        uint4* const at = reinterpret_cast<uint4*>(to + first + 8 * (i + k * kClipThreads));
+#pragma unroll
+        for (int q = 0; q < 8 / F; ++q) {
+          uint4 pack;
+#pragma unroll
+          for (int e = 0; e < F; e += 2)
+            set_pair<O>(pack, e, make_float2(x[k][q * F + e] * shift * factor, x[k][q * F + e + 1] * shift * factor));
+          __stcs(at + q, pack);
+        }
+      }
+    }
     return;
   }
   const int packs = (n - head) / E, tail = head + packs * E;
@@ -230,7 +252,7 @@ __device__ __forceinline__ void scale_unit(const T* from, O* to, int n, float sh
 }
 
 template <typename T, typename O, int kTensors>
-__global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_constant__ ClipArgs a,
+__global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_constant__ ClipArgs a,
                                                               const __grid_constant__ ClipTable<kTensors> table) {
   dq_pdl_enter();
   __shared__ double shared[kClipThreads / 32];
@@ -250,7 +272,8 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
     const ClipTensor& t = table.t[tensor_of(table, a.count, unit)];
     const int64_t at = (unit - t.unit) * a.unit;
     scale_unit(static_cast<const T*>(t.from) + worker * t.from_stride + at,
-               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), f.shift, f.factor);
+               static_cast<O*>(t.to) + worker * t.to_stride + at, (int)min64(a.unit, t.size - at), f.shift, f.factor,
+               static_cast<const T*>(t.from) + worker * t.from_stride, static_cast<const T*>(t.from) + worker * t.from_stride + t.size);
   }
 }
 
@@ -292,7 +315,7 @@ __global__ void __launch_bounds__(kClipThreads) few_values_kernel(const __grid_c
   const ClipFactor f = clip_factor(a, norm);
   for (unit -= kFewBlocks; unit >= 0; unit -= kFewBlocks)
     each(unit, [&](const ClipTensor& t, const T* from, int64_t at, int n) {
-      scale_unit(from, static_cast<O*>(t.to) + worker * t.to_stride + at, n, f.shift, f.factor);
+      scale_unit(from, static_cast<O*>(t.to) + worker * t.to_stride + at, n, f.shift, f.factor, from - at, from - at + t.size);
     });
 }
 

@@ -84,7 +84,7 @@ struct SlopeArgs {
 template <typename T, bool kSlope>
 __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
   dq_pdl_enter();
-  __shared__ __align__(16) float turn[8][kGradColumns];
+  __shared__ float turn[8][kGradColumns];
   constexpr int kAhead = 4, E = 16 / (int)sizeof(T), kPacks = 8 / E;
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
   const int64_t column = (int64_t)blockIdx.x * kGradColumns + lane * 8;
@@ -141,25 +141,17 @@ __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
         row(r, x, u);
       }
   } else {
-    // a row's 256 values one a lane at a time, turned to eight a lane
-    const int wide = (int)min((int64_t)kGradColumns, a.columns - (int64_t)blockIdx.x * kGradColumns);
-    const auto fetch = [&](const T* at, float (&x)[8]) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 32 * i + lane < wide ? to_float(at[32 * i + lane - 8 * lane]) : 0.f;
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) turn[warp][32 * i + lane] = x[i];
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(&turn[warp][8 * lane + i]);
-    };
-    for (; r < last; r += 8) {
-      alignas(16) float x[8], u[8] = {};
-      fetch(dy + r * a.dy_ld, x);
-      if constexpr (kSlope) fetch(pre + r * a.pre_ld, u);
-      if (count > 0) row(r, x, u);
-    }
-    __syncwarp();
+    const int64_t rows = (int64_t)gridDim.z * a.rows - 1;
+    const T* const dy_end = static_cast<const T*>(a.dy) + rows * a.dy_ld + a.columns;
+    const T* const pre_end = kSlope ? static_cast<const T*>(a.pre) + rows * a.pre_ld + a.columns : nullptr;
+    if (count > 0)
+#pragma unroll 2
+      for (; r < last; r += 8) {
+        float x[8], u[8] = {};
+        read8_near(dy + r * a.dy_ld, count, a.dy, dy_end, x);
+        if constexpr (kSlope) read8_near(pre + r * a.pre_ld, count, a.pre, pre_end, u);
+        row(r, x, u);
+      }
   }
   if (a.sums) {
 #pragma unroll

@@ -271,6 +271,53 @@ __device__ __forceinline__ uint4 funnel16(const uint4& a, const uint4& b, int s)
                     __funnelshift_r(u[2], u[3], bits), __funnelshift_r(u[3], u[4], bits));
 }
 
+// Eight values of a row, 16 bytes at a time where `packs` says that rows allow it; 0 from `count` on.
+template <typename T>
+__device__ __forceinline__ void read8(const T* from, int count, bool packs, float (&x)[8]) {
+  constexpr int E = 16 / (int)sizeof(T);
+  if (packs && count >= 8) {
+#pragma unroll
+    for (int i = 0; i < 8; i += E) {
+      const uint4 pack = *reinterpret_cast<const uint4*>(from + i);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 v = pair_of<T>(pack, e);
+        x[i + e] = v.x;
+        x[i + e + 1] = v.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(from[i]) : 0.f;
+  }
+}
+
+// The same of rows that are not on 16-byte boundaries: shifted out of the aligned packs that hold them, where those lie
+// inside the matrix, [begin, end).
+template <typename T>
+__device__ __forceinline__ void read8_near(const T* from, int count, const void* begin, const void* end, float (&x)[8]) {
+  constexpr int E = 16 / (int)sizeof(T), kPacks = 8 / E;
+  const uintptr_t base = (uintptr_t)from & ~(uintptr_t)15;
+  if (count >= 8 && base >= (uintptr_t)begin && base + 16 * (kPacks + 1) <= (uintptr_t)end) {
+    const int shift = (int)((uintptr_t)from & 15);
+    uint4 packs[kPacks + 1];
+#pragma unroll
+    for (int q = 0; q <= kPacks; ++q) packs[q] = reinterpret_cast<const uint4*>(base)[q];
+#pragma unroll
+    for (int q = 0; q < kPacks; ++q) {
+      const uint4 pack = funnel16(packs[q], packs[q + 1], shift);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const float2 v = pair_of<T>(pack, e);
+        x[q * E + e] = v.x;
+        x[q * E + e + 1] = v.y;
+      }
+    }
+  } else {
+    read8(from, count, false, x);
+  }
+}
+
 // Rows that do not start or end on 16-byte boundaries are read as the aligned packs of 16 bytes that hold them.  Gaps
 // between rows may be read along, but nothing before the first row's first value or after the last row's last: those of
 // worker m's rows whose packs stay clear of that.  near: the rows from either end whose packs may not; heads: a pack

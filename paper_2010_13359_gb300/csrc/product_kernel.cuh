@@ -205,21 +205,20 @@ struct TurnStore {
     }
   }
 
-  // Single values, for matrices that TMA cannot write: kTurn columns that lane r holds of row r; then column l % kTurn of
-  // row i * kTurned + l / kTurn.
-  static constexpr int kTurn = 16 * kBuffers, kTurned = 32 / kTurn;
-  __device__ __forceinline__ float* turned_pack(int row, int c) const {  // no two of what a warp reads or writes at once meet in a bank
-    return reinterpret_cast<float*>(buffer + row * (4 * kTurn) + ((c ^ (kBuffers == 2 ? row & 7 : row / 2 & 3)) * 16));
-  }
+  // Single values, for matrices that TMA cannot write (of two buffers): 32 columns that lane r holds of row r; then column l
+  // of any row.  No two of the packs that a warp writes or the values that it reads at once meet in a bank.
   __device__ __forceinline__ void turn(const float* x) {
-    if (lane == 0) bulk_wait_read_all();
+    static_assert(kBuffers == 2, "32 x 32 values");
+    float* const to = reinterpret_cast<float*>(buffer);
     __syncwarp();
 #pragma unroll
-    for (int c = 0; c < kTurn / 4; ++c)
-      *reinterpret_cast<float4*>(turned_pack(lane, c)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    for (int c = 0; c < 8; ++c)
+      *reinterpret_cast<float4*>(to + lane * 32 + (c ^ (lane & 7)) * 4) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
     __syncwarp();
   }
-  __device__ __forceinline__ float turned(int i) const { return turned_pack(i * kTurned + lane / kTurn, lane % kTurn / 4)[lane & 3]; }
+  __device__ __forceinline__ float turned(int r) const {
+    return reinterpret_cast<const float*>(buffer)[r * 32 + ((lane / 4) ^ (r & 7)) * 4 + (lane & 3)];
+  }
 };
 
 struct ProductTile {
@@ -477,6 +476,10 @@ inline bool encode_operand(const ProductOperand& o, int64_t rows, int64_t depth,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Results that TMA cannot write (product_rows.cu).
+template <int BN>
+cudaError_t launch_product_rows(const ProductArgs& args, cudaStream_t stream, uint64_t* launches);
 
 // Host: the tensor map of a matrix that is stored, [parts][workers][rows][columns], in boxes of 64 bytes of 32 rows.
 inline bool encode_result(void* data, int32_t dtype, int64_t columns, int64_t rows, int32_t workers, int32_t parts, int64_t ld,

@@ -43,8 +43,7 @@ __device__ __forceinline__ void add32(const T* from, int64_t count, float (&x)[3
   }
 }
 
-// A warp's 32 rows, by TMA where results are on 16-byte boundaries, else turned in shared memory and stored by single
-// values.
+// A warp's 32 rows, by TMA.
 template <typename T, int kSumWarps>
 struct StoreEpilogue {
   static constexpr int kWarps = kSumWarps;
@@ -64,38 +63,16 @@ struct StoreEpilogue {
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = v[g + i];
       const float b = bias && lane < count ? bias[j + lane] : 0.f;
-      if (s.packs && (count >= 32 || p.columns * (int)sizeof(T) % 16 == 0)) {
-        if (s.add && lane < rows) add32(s.add + tile.worker * s.add_batch + (row + lane) * s.add_ld + j, count, x);
-        if (bias) {
+      if (s.add && lane < rows) add32(s.add + tile.worker * s.add_batch + (row + lane) * s.add_ld + j, count, x);
+      if (bias) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] += __shfl_sync(kFullMask, b, i);
-        }
-        if (s.pre) store.template put32<T>(x, &p.pre, (int)j, (int)row, tile.worker);
-        activate_all<sizeof(T) == 4>(x, s.activation);
-        if (s.residual && lane < rows)
-          add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
-        store.template put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
-      } else {
-        constexpr int kTurn = TurnStore<S::kBuffers>::kTurn, kTurned = TurnStore<S::kBuffers>::kTurned;
-#pragma unroll
-        for (int q = 0; q < 32; q += kTurn) {
-          const int64_t at = j + q + lane % kTurn;
-          const float one = __shfl_sync(kFullMask, b, q + lane % kTurn);
-          store.turn(x + q);
-          if (at >= p.columns) continue;
-          if (!s.add && !s.pre && !s.residual && s.activation == DQGAN_NONE) {
-            T* const to = static_cast<T*>(s.out) + tile.worker * s.out_batch + (row + lane / kTurn) * s.out_ld + at;
-#pragma unroll 8
-            for (int i = 0; i < 32 / kTurned; ++i)
-              if (i * kTurned + lane / kTurn < rows) to[i * kTurned * s.out_ld] = from_float<T>(store.turned(i) + one);
-          } else {
-#pragma unroll 4
-            for (int i = 0; i < 32 / kTurned; ++i)
-              if (i * kTurned + lane / kTurn < rows)
-                store_value<T>(s, tile.worker, row + i * kTurned + lane / kTurn, at, store.turned(i), one);
-          }
-        }
+        for (int i = 0; i < 32; ++i) x[i] += __shfl_sync(kFullMask, b, i);
       }
+      if (s.pre) store.template put32<T>(x, &p.pre, (int)j, (int)row, tile.worker);
+      activate_all<sizeof(T) == 4>(x, s.activation);
+      if (s.residual && lane < rows)
+        add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
+      store.template put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
     }
   }
 };
@@ -150,11 +127,11 @@ cudaError_t store_product(const Product& p, const StoreArgs& store, const Cut& c
     return !at || (((uintptr_t)at & 15) == 0 && ld * of % 16 == 0 && ld * of < ((int64_t)1 << 40) &&
                    (p.workers == 1 || (batch * of % 16 == 0 && batch * of < ((int64_t)1 << 40))));
   };
-  args.store.packs = packs(store.out, store.out_ld, store.out_batch, size) && packs(store.pre, store.pre_ld, store.pre_batch, size) &&
+  const bool by_tma = p.columns * size % 16 == 0 && packs(store.out, store.out_ld, store.out_batch, size) && packs(store.pre, store.pre_ld, store.pre_batch, size) &&
                      packs(store.residual, store.residual_ld, store.residual_batch, size) &&
                      packs(store.add, store.add_ld, store.add_batch, 4);
-  if (args.store.packs &&
-      !(encode_result(store.out, store.out_dtype, p.columns, p.rows, p.workers, 1, store.out_ld, store.out_batch, 0, &args.out) &&
+  if (!by_tma) return launch_product_rows<BN>(args, stream, launches);
+  if (!(encode_result(store.out, store.out_dtype, p.columns, p.rows, p.workers, 1, store.out_ld, store.out_batch, 0, &args.out) &&
         (!store.pre || encode_result(store.pre, store.out_dtype, p.columns, p.rows, p.workers, 1, store.pre_ld, store.pre_batch, 0,
                                      &args.pre))))
     return cudaErrorInvalidValue;
@@ -196,7 +173,14 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs first, const
       const int64_t t = token_at(a.targets, a.token_bits, r);
       counts = t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
     }
-    if (counts) read8(static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column, (int)min64(8, a.columns - column), a.packs, x);
+    if (counts) {
+      const T* const from = static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column;
+      const int count = (int)min64(8, a.columns - column);
+      if (a.packs)
+        read8(from, count, true, x);
+      else
+        read8_near(from, count, a.from, static_cast<const T*>(a.from) + (a.workers - 1) * a.batch + (a.rows - 1) * a.from_ld + a.columns, x);
+    }
     write_parts<true>(x, a.to, r * a.ld + column, a.part, a.parts, a.half);
   }
 }

@@ -46,7 +46,6 @@ struct StoreArgs {
   const float* add;      // fp32 values added to the sum (add + m * add_batch + i * add_ld + j), or nullptr; may be out
   int64_t add_batch, add_ld;
   int32_t activation;
-  bool packs;            // all of them can be read and written 16 bytes at a time, and by TMA (set by the launcher)
 };
 
 struct SoftmaxArgs {
@@ -257,27 +256,6 @@ __device__ __forceinline__ void scale_by_slope(float (&x)[N], const float (&u)[N
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] *= activation_slope<kExact>(u[i], DQGAN_RELU);
-  }
-}
-
-// Eight values of a row, 16 bytes at a time where `packs` says that rows allow it; 0 from `count` on.
-template <typename T>
-__device__ __forceinline__ void read8(const T* from, int count, bool packs, float (&x)[8]) {
-  constexpr int E = 16 / (int)sizeof(T);
-  if (packs && count >= 8) {
-#pragma unroll
-    for (int i = 0; i < 8; i += E) {
-      const uint4 pack = *reinterpret_cast<const uint4*>(from + i);
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float2 v = pair_of<T>(pack, e);
-        x[i + e] = v.x;
-        x[i + e + 1] = v.y;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(from[i]) : 0.f;
   }
 }
 

@@ -79,6 +79,8 @@ LINEAR = [  # workers, rows, inputs, outputs, dtype, weight dtype, activation, p
     (1, 20, 65536, 9, 1, 1, 0, 0, 0, False),
     (1, 20, 9, 65536, 1, 1, 2, 0, 0, False),
     (200, 10, 16, 24, 1, 1, 2, 0, 0, False),
+    (2, 600, 130, 1301, 1, 1, 3, 3, 1, False),
+    (3, 100, 77, 203, 0, 0, 2, 3, 3, False),
 ]
 
 
@@ -267,6 +269,9 @@ CLIP = [  # workers, sizes, dtype, out dtype, pad, shift
     (700, (50, 20_000), 1, 1, 0, 0),
     (2, tuple(37 * (i % 11) for i in range(1500)), 2, 2, 1, 0),
     (1, (30_000_001,), 0, 0, 0, 1),
+    (3, (40_001, 20_000, 8, 15, 16_385), 0, 0, 3, 2),
+    (2, (70_003, 33_333, 5), 1, 0, 5, 3),
+    (2, (70_003, 33_333, 9), 2, 2, 7, 5),
 ]
 
 
