@@ -77,22 +77,17 @@ struct StoreEpilogue {
   }
 };
 
-// How a product is cut: tiles of 256 x 256 for pairs of blocks, or of 128 x 64 for single ones; and of the tiles
-// that do not fill the GPU for a last time, the contracted index in pieces.
-struct Cut {
-  int width;
-  int64_t whole;
-  int pieces;
-};
+}  // namespace
 
 // By the time that the busiest block needs, in units of a block of 64 of the contracted index of a 256 x 256 tile (0.3 us).  A
 // tile's end costs as much as 12 of them (3 of a narrow tile, whose blocks take 0.6: 24 KB to load instead of 32); pieces
 // cost a second kernel, 10, their sums' way through memory, 0.3 each, and one load after another there, 1 for each of a tile's.
-Cut cut_product(const Product& p, int64_t slots) {
+Cut cut_product(const Product& p, int64_t slots, int only) {
   const int64_t depth = ceil_div(p.depth, kBlockDepth), length = depth * p.terms.count;
   Cut best{256, 0, 1};
   double least = 1e300;
   for (int width = 64; width <= 256; width += 192) {
+    if (only != 0 && width != only) continue;
     const bool wide = width == 256;
     const int64_t tiles = ceil_div(p.rows, wide ? 256 : 128) * ceil_div(p.columns, width) * p.workers;
     const int64_t at_once = wide ? slots / 2 : slots, rest = tiles % at_once, whole = tiles - rest;
@@ -111,6 +106,8 @@ Cut cut_product(const Product& p, int64_t slots) {
   }
   return best;
 }
+
+namespace {
 
 template <int BN>
 cudaError_t store_product(const Product& p, const StoreArgs& store, const Cut& cut, void* scratch, uint32_t* err,
@@ -148,7 +145,7 @@ cudaError_t launch_product_store(const Product& p, const StoreArgs& store, void*
   if (p.rows == 0 || p.columns == 0) return cudaSuccess;
   const int sms = device_sms();
   if (sms <= 1) return cudaErrorInvalidDevice;
-  const Cut cut = cut_product(p, sms);
+  const Cut cut = cut_product(p, sms, 0);
   return cut.width == 256 ? store_product<256>(p, store, cut, scratch, err, stream, launches)
                           : store_product<64>(p, store, cut, scratch, err, stream, launches);
 }

@@ -89,6 +89,16 @@ struct Product {
   ProductTerms terms;
 };
 
+// How a product is cut: tiles of 256 x 256 for pairs of blocks, or of 128 x 64 for single ones; and of the tiles
+// that do not fill the GPU for a last time, those from `whole` on, the contracted index in pieces.
+struct Cut {
+  int width;
+  int64_t whole;
+  int pieces;
+};
+// For `slots` SMs; `only`: tiles of that width, 0: of either.
+Cut cut_product(const Product& p, int64_t slots, int only);
+
 // Scratch of the products of one operator: the sums of pieces.
 constexpr size_t kProductScratch = (size_t)80 << 20;
 

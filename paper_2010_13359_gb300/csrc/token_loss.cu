@@ -223,12 +223,18 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const SoftmaxArgs s, in
 }
 
 template <typename Epilogue>
-cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool thin, uint32_t* err, cudaStream_t stream,
+cudaError_t softmax_product(const Product& p, const SoftmaxArgs& softmax, bool thin, const Scratch& c, cudaStream_t stream,
                             uint64_t* launches) {
   ProductArgs args{};
   const int chunk = p.terms.count == 6 ? 12 : 16;
-  if (!(thin ? product_args<64>(p, chunk, err, &args) : product_args<256>(p, chunk, err, &args))) return cudaErrorInvalidValue;
+  if (!(thin ? product_args<64>(p, chunk, c.err, &args) : product_args<256>(p, chunk, c.err, &args))) return cudaErrorInvalidValue;
   args.softmax = softmax;
+  const int sms = device_sms();
+  if (sms <= 1) return cudaErrorInvalidDevice;
+  const Cut cut = cut_product(p, sms, thin ? 64 : 256);
+  args.whole = cut.whole;
+  args.pieces = cut.pieces;
+  args.partial = static_cast<float*>(c.products);
   if (softmax.grad && !encode_result(softmax.grad, DQGAN_BF16, p.columns, p.rows, p.workers, softmax.grad_parts, softmax.grad_ld,
                                      p.rows * softmax.grad_ld, softmax.grad_part, &args.out))
     return cudaErrorInvalidValue;
@@ -308,7 +314,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
       logits.terms = product_terms(logits.a.parts, logits.b.parts);
       soft.first = first;
       soft.slot = (int32_t)(first / columns);
-      st = softmax_product<StatsEpilogue>(logits, soft, thin, c.err, stream, launches);
+      st = softmax_product<StatsEpilogue>(logits, soft, thin, c, stream, launches);
     }
     if (st != cudaSuccess) return st;
     ++*launches;
@@ -328,7 +334,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
     soft.grad_ld = piece;
     soft.grad_part = (int64_t)s.workers * a.rows * piece;
     soft.grad_parts = grad_parts(s);
-    st = softmax_product<GradEpilogue>(logits, soft, narrow(a.rows, s.workers, count), c.err, stream, launches);
+    st = softmax_product<GradEpilogue>(logits, soft, narrow(a.rows, s.workers, count), c, stream, launches);
     if (st != cudaSuccess) return st;
     ProductOperand d;
     d.data = c.grad;

@@ -192,6 +192,9 @@ LOSS = [  # workers, rows, vocab, width, dtype, weight dtype, token bits, pad, s
     (1, 257, 20000, 104, 1, 0, 32, 0, 0, False, 1.0),
     (100, 5, 40, 24, 1, 1, 32, 0, 0, False, 0.2),
     (1, 33, 70, 65536, 1, 1, 32, 0, 0, False, 0.0),
+    (1, 300, 600, 4096, 1, 1, 32, 0, 0, False, 0.1),  # few tiles: their logits' sums in pieces
+    (2, 600, 2000, 3000, 0, 0, 32, 0, 0, False, 0.1),
+    (1, 300, 600, 2048, 2, 0, 32, 0, 0, False, 0.1),
 ]
 
 
