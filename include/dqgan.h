@@ -713,7 +713,8 @@ DQGAN_API int dqgan_linear_backward(dqgan_operator* op, int64_t rows, const void
 
 /*
  * Cross entropy of workers * rows rows (rows <= max_rows) of the output layer
- * z = x W^T, whose logits are nowhere kept.  weight: vocab rows of width values,
+ * z = x W^T, whose logits are nowhere kept (those of up to eight rows a worker pass
+ * through scratch).  weight: vocab rows of width values,
  * contiguous, worker m's at weight + m * p_stride elements of weight_dtype (0:
  * shared, else >= vocab * width).  targets: one a row, worker m's at + m * rows.
  * weights: c of each row, or NULL (ones).  A row whose target is outside

@@ -11,8 +11,6 @@
 // layers, takes as many as keep the products' error near 2^-17 (two parts) or
 // 2^-24 (three).  f16 values that do not lie as f16 in memory are two bf16 parts
 // (all of their 11 bits, at any exponent).
-#include <type_traits>
-
 #include "device_common.cuh"
 #include "products.cuh"
 
@@ -40,7 +38,7 @@ struct Scratch {
   uint32_t* err;
   void* products;
   void *x, *w, *d;
-  float* sums;
+  float *sums, *few;
   size_t bytes;
 };
 
@@ -59,6 +57,7 @@ Scratch scratch_of(const LinearShape& s, void* base) {
   c.w = take((int64_t)s.workers * s.outputs * round8(s.inputs) * 2 * weight_parts(s));
   c.d = take(rows * round8(s.outputs) * 2 * grad_parts(s));
   c.sums = static_cast<float*>(take(s.workers * most_row_blocks(s) * s.outputs * 4));
+  c.few = static_cast<float*>(take((int64_t)s.workers * (s.max_rows < kFewRows ? s.max_rows : kFewRows) * s.outputs * 4));
   c.bytes = at;
   return c;
 }
@@ -186,128 +185,7 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* sums, int blocks
   *to = accumulate ? *to + (float)s : (float)s;
 }
 
-// Sums over a warp's lanes of kValues values each (a power of two, at most 32): lane l gets one of them.  Each step sends
-// half of what is left to the lane that keeps that half.
-template <int kValues>
-__device__ __forceinline__ int sum_over_lanes(float (&x)[kValues], int lane) {
-  int which = 0;
-  int d = 16;
-#pragma unroll
-  for (int h = kValues / 2; h > 0; h /= 2, d /= 2) {
-    const bool upper = lane & d;
-    if (upper) which += h;
-#pragma unroll
-    for (int i = 0; i < h; ++i) {
-      const float send = upper ? x[i] : x[i + h], keep = upper ? x[i + h] : x[i];
-      x[i] = keep + __shfl_xor_sync(kFullMask, send, d);
-    }
-  }
-  for (; d > 0; d /= 2) x[0] += __shfl_xor_sync(kFullMask, x[0], d);
-  return which;
-}
-
-// A few rows: what bounds them is the weights' bytes, each read once.  A warp takes four rows of W, 16 bytes (32 of fp32) a
-// lane at a time, and kRows rows of x beside them from L1; 1, 2, 4 or 8 warps share the inputs.  fp32 sums of
-// products of the values as they are, without parts.  4096 x 4096 in bf16: 8.9 us for one row (5.0 at the copy's
-// bandwidth), 14 for two, 17 for four, 23 for eight; the tiles need 16.4 for any number up to 128.  1024 x 4096: 3.4, 4.6,
-// 7.8, 9.0 and 8.9; 8192 x 1024: 6.1, 6.8, 8.3, 11.8 and 14.2.  So up to four rows come here, and up to eight
-// where the tiles would have to split fp32 weights first.
-template <typename T, typename E, int kRows, bool kPacks>
-__global__ void __launch_bounds__(256) few_rows_kernel(const T* x, int64_t x_ld, const E* weight, int64_t p_stride, int64_t inputs,
-                                                       int64_t outputs, int rows, int sharing, const StoreArgs store) {
-  dq_pdl_enter();
-  constexpr int kOut = 4, kValues = kOut * kRows;
-  __shared__ float part[8][kValues];
-  const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
-  const int64_t worker = blockIdx.y, group = (int64_t)blockIdx.x * (8 / sharing) + warp / sharing, first = group * kOut;
-  const int share = warp % sharing;
-  x += worker * rows * x_ld;
-  weight += worker * p_stride;
-  // rows beyond the last are the last's, and not stored
-  const E* w[kOut];
-#pragma unroll
-  for (int o = 0; o < kOut; ++o) w[o] = weight + min64(first + o, outputs - 1) * inputs;
-  float2 sum[kValues] = {};
-  if (first < outputs) {
-    if constexpr (kPacks) {
-#pragma unroll 2
-      for (int64_t k = share * 256 + lane * 8; k < inputs; k += 256 * sharing) {  // whole packs: inputs is a multiple of eight
-        float a[kOut][8];
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) read8(w[o] + k, 8, true, a[o]);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          float v[8];
-          read8(x + min(r, rows - 1) * x_ld + k, 8, true, v);
-#pragma unroll
-          for (int o = 0; o < kOut; ++o)
-#pragma unroll
-            for (int i = 0; i < 8; i += 2)
-              sum[o * kRows + r] = fma2(make_float2(a[o][i], a[o][i + 1]), make_float2(v[i], v[i + 1]), sum[o * kRows + r]);
-        }
-      }
-    } else {
-#pragma unroll 2
-      for (int64_t k = share * 32 + lane; k < inputs; k += 32 * sharing) {
-        float a[kOut];
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) a[o] = to_float(w[o][k]);
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          const float v = to_float(x[min(r, rows - 1) * x_ld + k]);
-#pragma unroll
-          for (int o = 0; o < kOut; ++o) sum[o * kRows + r].x = fmaf(a[o], v, sum[o * kRows + r].x);
-        }
-      }
-    }
-  }
-  float one[kValues];
-#pragma unroll
-  for (int i = 0; i < kValues; ++i) one[i] = sum[i].x + sum[i].y;
-  const int which = sum_over_lanes(one, lane);
-  part[warp][which] = one[0];  // equal lanes write equal values
-  __syncthreads();
-  // the shares of a group's sums in order
-  const int t = (int)threadIdx.x;
-  if (t < 8 / sharing * kValues) {
-    const int g = t / kValues, i = t % kValues, r = i % kRows;
-    const int64_t column = ((int64_t)blockIdx.x * (8 / sharing) + g) * kOut + i / kRows;
-    float s = 0.f;
-    for (int w = 0; w < sharing; ++w) s += part[g * sharing + w][i];
-    if (column < outputs && r < rows)
-      store_value<T>(store, (int)worker, r, column, s, store.bias ? store.bias[worker * store.bias_batch + column] : 0.f);
-  }
-}
-
-constexpr int kFewRows = 8;
-
 bool has_few_rows(const LinearShape& s, int64_t rows) { return rows <= (s.weight_dtype == DQGAN_F32 ? kFewRows : kFewRows / 2); }
-
-template <typename T, typename E>
-cudaError_t few_rows(const LinearArgs& a, const StoreArgs& store, cudaStream_t stream, uint64_t* launches) {
-  const LinearShape& s = a.shape;
-  const auto on_packs = [](const void* p, int64_t ld, int64_t batch, int64_t size) {
-    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0 && batch * size % 16 == 0;
-  };
-  const bool packs = s.inputs % 8 == 0 && on_packs(a.x, a.x_ld, 0, sizeof(T)) && on_packs(a.weight, s.inputs, a.p_stride, sizeof(E));
-  // as many warps as have something to do, 256 inputs (32 without packs) each
-  const int64_t steps = ceil_div(s.inputs, packs ? 256 : 32);
-  const int sharing = steps >= 8 ? 8 : steps >= 4 ? 4 : steps >= 2 ? 2 : 1;
-  const auto run = [&](auto rows, auto in_packs) {
-    ++*launches;
-    return launch_pdl(few_rows_kernel<T, E, decltype(rows)::value, decltype(in_packs)::value>,
-                      dim3((unsigned)ceil_div(s.outputs, 32 / sharing), (unsigned)s.workers), dim3(256), 0, stream,
-                      static_cast<const T*>(a.x), a.x_ld, static_cast<const E*>(a.weight), a.p_stride, s.inputs, s.outputs,
-                      (int)a.rows, sharing, store);
-  };
-  const auto by_rows = [&](auto in_packs) {
-    return a.rows == 1   ? run(std::integral_constant<int, 1>{}, in_packs)
-           : a.rows == 2 ? run(std::integral_constant<int, 2>{}, in_packs)
-           : a.rows <= 4 ? run(std::integral_constant<int, 4>{}, in_packs)
-                         : run(std::integral_constant<int, kFewRows>{}, in_packs);
-  };
-  return packs ? by_rows(std::true_type{}) : by_rows(std::false_type{});
-}
 
 }  // namespace
 
@@ -331,18 +209,15 @@ cudaError_t launch_linear_forward(const LinearArgs& a, cudaStream_t stream, uint
   out.bias = a.bias;
   out.bias_batch = a.b_stride;
   out.activation = s.activation;
+  const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+  const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
   if (has_few_rows(s, a.rows))
-    return with_dtype(s.dtype, [&](auto t) {
-      using T = decltype(t);
-      return s.weight_dtype == DQGAN_F32 ? few_rows<T, float>(a, out, stream, launches) : few_rows<T, T>(a, out, stream, launches);
-    });
+    return launch_few_rows(x, w, out, stream, launches);
   Product p;
   p.rows = a.rows;
   p.columns = s.outputs;
   p.depth = s.inputs;
   p.workers = s.workers;
-  const MatrixArgs x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
-  const MatrixArgs w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
   Splits splits{stream, launches};
   cudaError_t st = make_operand(x, half ? 1 : act_parts(s.dtype), half, c.x, splits, &p.a);
   if (st == cudaSuccess) st = make_operand(w, half ? 1 : weight_parts(s), half, c.w, splits, &p.b);
@@ -362,6 +237,18 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
       if (a.dweight) st = cudaMemsetAsync(a.dweight + m * a.g_stride, 0, (size_t)s.outputs * s.inputs * 4, stream);
       if (a.dbias && st == cudaSuccess) st = cudaMemsetAsync(a.dbias + m * a.g_stride, 0, (size_t)s.outputs * 4, stream);
     }
+    return st;
+  }
+  const MatrixArgs few_w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
+  if (a.rows <= kFewRows && few_across_fits(few_w, a.rows)) {
+    const MatrixArgs few_dy{a.dy, a.dy_ld, a.rows * a.dy_ld, s.dtype, a.rows, s.outputs, s.workers};
+    const MatrixArgs few_x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
+    st = launch_few_slopes(few_dy, s.activation == DQGAN_NONE ? nullptr : a.pre, a.pre_ld, s.activation, c.few, a.dbias, a.g_stride,
+                           a.accumulate, stream, launches);
+    if (st == cudaSuccess && a.dx)
+      st = launch_few_across(c.few, few_w, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
+    if (st == cudaSuccess && a.dweight)
+      st = launch_few_outer(c.few, few_x, s.outputs, a.dweight, a.g_stride, a.accumulate, stream, launches);
     return st;
   }
   const bool half = half_backward(s);

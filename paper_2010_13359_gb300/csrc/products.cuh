@@ -346,4 +346,22 @@ struct MatrixArgs {
 // The operand that it is: as it lies, or split into `buffer`.
 cudaError_t make_operand(const MatrixArgs& m, int parts, bool half, void* buffer, Splits& splits, ProductOperand* out);
 
+// Products of up to kFewRows rows a worker (few_rows.cu).  x: rows; w: weights, w.rows x w.columns; d: fp32, [worker][row][w.rows].
+constexpr int kFewRows = 8;
+// x W^T, and what is done with it; the result has x's type or fp32.
+cudaError_t launch_few_rows(const MatrixArgs& x, const MatrixArgs& w, const StoreArgs& store, cudaStream_t stream, uint64_t* launches);
+// du = dy act'(pre) (pre: nullptr for no activation), and its sums over the rows (or dbias nullptr).
+cudaError_t launch_few_slopes(const MatrixArgs& dy, const void* pre, int64_t pre_ld, int activation, float* du, float* dbias,
+                              int64_t g_stride, int accumulate, cudaStream_t stream, uint64_t* launches);
+// d^T x, outputs x x.columns, worker m's at out + m * batch.  x's rows that do not count are left out.
+cudaError_t launch_few_outer(const float* d, const MatrixArgs& x, int64_t outputs, float* out, int64_t batch, int accumulate,
+                             cudaStream_t stream, uint64_t* launches);
+// d W.  scratch: kProductScratch bytes.  few_across_fits: whether the kernels' scratch and grids hold it.
+bool few_across_fits(const MatrixArgs& w, int64_t rows);
+cudaError_t launch_few_across(const float* d, const MatrixArgs& w, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
+                              void* scratch, cudaStream_t stream, uint64_t* launches);
+// loss and lse of rows of x.vocab logits (forward), and the gradient in their place (backward; without forward: from lse).
+cudaError_t launch_few_loss(float* z, const MatrixArgs& x, float scale, bool forward, bool backward, float* loss, float* lse,
+                            cudaStream_t stream, uint64_t* launches);
+
 }  // namespace dq

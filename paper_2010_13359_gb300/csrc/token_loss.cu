@@ -54,7 +54,7 @@ struct Scratch {
   void* products;
   void *x, *x_half, *w, *grad;
   float2* stats;
-  float *target_logit, *lse, *dx;
+  float *target_logit, *lse, *dx, *few;
   size_t bytes;
 };
 
@@ -77,6 +77,7 @@ Scratch scratch_of(const TokenLossShape& s, void* base) {
   c.target_logit = static_cast<float*>(take(rows * 4));
   c.lse = static_cast<float*>(take(rows * 4));
   c.dx = static_cast<float*>(take(piece < s.vocab ? rows * s.width * 4 : 0));
+  c.few = static_cast<float*>(take((int64_t)s.workers * (s.max_rows < kFewRows ? s.max_rows : kFewRows) * s.vocab * 4));
   c.bytes = at;
   return c;
 }
@@ -267,6 +268,30 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
   soft.target_logit = c.target_logit;
   soft.lse = a.lse ? a.lse : c.lse;
   soft.scale = a.scale;
+
+  // A few rows: without tiles, their logits and those's gradient in scratch.
+  const MatrixArgs few_w{a.weight, s.width, a.p_stride, s.weight_dtype, s.vocab, s.width, s.workers};
+  if (a.rows <= kFewRows && few_across_fits(few_w, a.rows)) {
+    MatrixArgs few_x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.width, s.workers};
+    few_x.targets = a.targets;
+    few_x.weights = a.weights;
+    few_x.token_bits = s.token_bits;
+    few_x.vocab = s.vocab;
+    StoreArgs z{};
+    z.out = c.few;
+    z.out_ld = s.vocab;
+    z.out_batch = a.rows * s.vocab;
+    z.out_dtype = DQGAN_F32;
+    const bool backward = a.backward && (a.dx || a.dweight);
+    if (!a.forward && !backward) return st;
+    st = launch_few_rows(few_x, few_w, z, stream, launches);
+    if (st == cudaSuccess) st = launch_few_loss(c.few, few_x, a.scale, a.forward, backward, a.loss, a.lse, stream, launches);
+    if (st == cudaSuccess && backward && a.dx)
+      st = launch_few_across(c.few, few_w, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
+    if (st == cudaSuccess && backward && a.dweight)
+      st = launch_few_outer(c.few, few_x, s.vocab, a.dweight, a.g_stride, a.accumulate, stream, launches);
+    return st;
+  }
 
   // x: of the gradient, the rows that do not count as zeros, whatever they hold
   ProductOperand x_logits, x_grad;

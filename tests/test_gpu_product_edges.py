@@ -221,10 +221,10 @@ def test_two_host_threads(P):  # noqa: F811
 @pytest.mark.parametrize("shape", [
     (1, 65536, 5000, 16, 1, 1, 32, 0, 0, False, 0.05),     # the gradient in two pieces of the vocabulary
     (2, 30000, 4500, 24, 2, 2, 32, 0, 0, False, 0.05),     # the same with operands of both 16-bit types
-    (1, 3, 4200, 65536, 1, 0, 32, 0, 0, False, 0.0),       # the weights' parts in pieces
+    (1, 10, 4200, 65536, 1, 0, 32, 0, 0, False, 0.0),       # the weights' parts in pieces
     (1, 40000, 4400, 40, 0, 0, 64, 0, 0, False, 0.05),
     # few rows of pieces that have few tiles, of a vocabulary too large for narrow ones' slots
-    (1, 5, 20000, 14000, 1, 0, 32, 0, 0, False, 0.0),
+    (1, 12, 20000, 14000, 1, 0, 32, 0, 0, False, 0.0),
 ], ids=str)
 def test_token_loss_in_pieces(P, shape):  # noqa: F811
     token_loss_case(P, shape)

@@ -81,6 +81,9 @@ LINEAR = [  # workers, rows, inputs, outputs, dtype, weight dtype, activation, p
     (200, 10, 16, 24, 1, 1, 2, 0, 0, False),
     (2, 600, 130, 1301, 1, 1, 3, 3, 1, False),
     (3, 100, 77, 203, 0, 0, 2, 3, 3, False),
+    (2, 8, 1300, 2101, 1, 1, 2, 3, 1, True),
+    (5, 6, 2052, 500, 2, 0, 1, 0, 0, False),
+    (1, 2, 4096, 1024, 0, 0, 3, 0, 0, False),
 ]
 
 
@@ -195,6 +198,9 @@ LOSS = [  # workers, rows, vocab, width, dtype, weight dtype, token bits, pad, s
     (1, 300, 600, 4096, 1, 1, 32, 0, 0, False, 0.1),  # few tiles: their logits' sums in pieces
     (2, 600, 2000, 3000, 0, 0, 32, 0, 0, False, 0.1),
     (1, 300, 600, 2048, 2, 0, 32, 0, 0, False, 0.1),
+    (3, 8, 5001, 260, 1, 1, 32, 3, 1, False, 0.4),
+    (2, 6, 3000, 1001, 0, 0, 64, 0, 0, True, 0.3),
+    (1, 2, 20011, 512, 2, 2, 32, 0, 0, False, 0.0),
 ]
 
 
