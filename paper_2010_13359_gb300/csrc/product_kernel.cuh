@@ -109,7 +109,7 @@ __device__ __forceinline__ void tensor_multiply(uint32_t d, uint64_t a, uint64_t
         ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
         : "memory");
 }
-// 32 columns of this warp's 32 lanes: lane l gets row l.
+// 32 columns of this warp's 32 lanes: lane l gets row l.  The warp executes it as one.
 __device__ __forceinline__ void tensor_load32(uint32_t at, uint32_t (&v)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -296,6 +296,7 @@ __global__ void __launch_bounds__(ShapeOf<BN, Epilogue>::kThreads, 1) product_ke
     }
     mbar_fence_init();
   }
+  __syncwarp();
   if (warp == 2) tensor_memory_allocate<kPair>(at_shared, kColumns);
   tensor_fence_before();
   __syncthreads();
@@ -390,7 +391,9 @@ __global__ void __launch_bounds__(ShapeOf<BN, Epilogue>::kThreads, 1) product_ke
 #pragma unroll
       for (int i = 0; i < S::kWidth; ++i) v[i] = 0.f;
       for (int done = 0; done < total; done += p.chunk, ++c) {
-        if (!(ok = mbar_wait_bounded(sum_full + (c & 1), c / 2 & 1, p.err))) break;
+        // each lane polls for itself, and all go on or none: what follows is executed by whole warps
+        if (!(ok = __all_sync(kFullMask, mbar_wait_bounded(sum_full + (c & 1), c / 2 & 1, p.err)))) break;
+        __syncwarp();
         tensor_fence_after();
         const uint32_t from = sums + ((uint32_t)(32 * sub) << 16) + (c & 1) * BN + slice * S::kWidth;
 #pragma unroll
@@ -419,9 +422,11 @@ __global__ void __launch_bounds__(ShapeOf<BN, Epilogue>::kThreads, 1) product_ke
       } else {
         Epilogue::template run<BN>(p, tile, tile.row + rank * kTileRows + 32 * sub, tile.column + slice * S::kWidth, v, store);
       }
+      __syncwarp();  // lanes whose rows are outside the matrix may come first
     }
     bulk_wait_all();
   }
+  __syncwarp();  // the single threads' lanes
   tensor_fence_before();
   __syncthreads();
   if constexpr (kPair == 2) pair_barrier();
