@@ -447,9 +447,10 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *     arithmetic: sums, softmax statistics and norms are held in 32 bits
  *     and a 16-bit result is rounded once.  (Weights of linear layers and of
  *     the token loss may be of the activations' type.)  The products of these two multiply 16-bit
- *     values: operands that are fp32, or computed in fp32 (the gradients of u
- *     and of z), are rounded to one bf16 value where the result is bf16, and
- *     taken as the sum of two (off by 2^-16 of themselves) where it is f16, an
+ *     values: fp32 weights are taken as the sum of two (off by 2^-16 of themselves); other operands
+ *     that are fp32, or computed in fp32 (the gradients of u
+ *     and of z), and the weights in the token loss's dx, are rounded to one bf16 value where the result is bf16, and
+ *     taken as the sum of two where it is f16, an
  *     fp32 gradient or a loss; of three (2^-24) where the activations are fp32.
  *     A value that is not finite makes what it enters not finite.  Every sum has a fixed order, so the
  *     same call on the same data gives the same bits.  Exponentials below 2^-126
@@ -692,8 +693,6 @@ DQGAN_API int dqgan_distillation_step(dqgan_operator* op, int64_t rows, const vo
  * outputs).  bias: fp32, worker m's at bias + m * b_stride (0: shared), or NULL.
  * residual: r, rows of outputs values, or NULL; y may be residual.  pre: receives
  * u = x W^T + b, which the backward pass of an activation needs, or NULL.
- * Products of 16-bit rows with fp32 weights take the weights rounded to bf16
- * (bf16 rows), or with 16 of their bits (f16 rows).
  */
 DQGAN_API int dqgan_linear_forward(dqgan_operator* op, int64_t rows, const void* x, int64_t x_stride,
                                    const void* weight, int64_t p_stride, const float* bias, int64_t b_stride,
