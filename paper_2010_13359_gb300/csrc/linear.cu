@@ -5,14 +5,14 @@
 //
 // Three products a layer (2 rows inputs outputs operations each), bound by the
 // tensor cores where there are some hundred rows, by the weights' bytes below.
-// How many 16-bit parts an operand has follows from the result's type.  fp32 weights
-// of 16-bit rows are two (2^-16 of them is left out).  In one part the weights at a lookahead point would be those at the
-// point itself wherever they differ by less than 2^-9 of them, and a result's error 1.4 times its own rounding's (8 x 2048
-// bf16 rows of 1024 x 4096 with GELU: 242 us, 154 with one part).  du
-// takes one part in what has 16 bits (a second rounding of the size of the result's own); what is
-// summed into fp32 gradients, and all of fp32
-// layers, takes as many as keep the products' error near 2^-17 (two parts) or
-// 2^-24 (three).  f16 values that do not lie as f16 in memory are two bf16 parts
+// How many 16-bit parts an operand has follows from the result's type.  What has
+// 32 bits (fp32 weights, and du where the slope is not 0 or 1) is two parts in a result of 16 bits and three in
+// fp32 gradients and all of fp32 layers, so that 2^-16 or 2^-24 of it is left out beside the result's own rounding.  (In
+// one part du would be rounded a second time, and weights at a lookahead point would be those at the point itself
+// wherever they differ by less than 2^-9 of them.  The gradient of 8 x 2048 bf16 rows of 1024 x 4096 with
+// GELU: 538 us, 359 with du as one part in dx and two in dW, whose errors were 1.4 and 2.2 times larger;
+// the forward pass with fp32 weights 242 us, 154 with one part of them and an error 1.4 times larger.)
+// f16 values that do not lie as f16 in memory are two bf16 parts
 // (all of their 11 bits, at any exponent).
 #include "device_common.cuh"
 #include "products.cuh"
@@ -27,7 +27,7 @@ int weight_parts(const LinearShape& s) {
 }
 bool exact_slope(int activation) { return activation == DQGAN_NONE || activation == DQGAN_RELU; }  // du has dy's values
 int grad_parts(const LinearShape& s) {
-  return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 || !exact_slope(s.activation) ? 2 : 1;
+  return s.dtype == DQGAN_F32 || !exact_slope(s.activation) ? 3 : s.dtype == DQGAN_F16 ? 2 : 1;
 }
 bool half_forward(const LinearShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
 bool half_backward(const LinearShape& s) { return half_forward(s) && exact_slope(s.activation); }
@@ -83,8 +83,8 @@ struct SlopeArgs {
   bool dy_packs, pre_packs;
 };
 
-// du of a block of rows and 256 columns, in parts, and the columns' sums.  Bound by memory: 8 bytes a value in bf16 with
-// GELU (dy, u, two parts).  Where rows are on 16-byte boundaries four of them a warp are on their way at once.
+// du of a block of rows and 256 columns, in parts, and the columns' sums.  Bound by memory: 10 bytes a value in bf16 with
+// GELU (dy, u, three parts).  Where rows are on 16-byte boundaries four of them a warp are on their way at once.
 template <typename T, bool kSlope>
 __global__ void __launch_bounds__(256, 3) slope_kernel(const SlopeArgs a) {
   dq_pdl_enter();
@@ -324,7 +324,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     p.depth = s.outputs;
     p.workers = s.workers;
     p.a = d;
-    if (s.dtype == DQGAN_BF16) p.a.parts = 1;
+    if (s.dtype != DQGAN_F32 && p.a.parts > 2) p.a.parts = 2;
     p.b = weight;
     p.b.across = true;
     p.terms = product_terms(p.a.parts, p.b.parts);
