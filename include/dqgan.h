@@ -447,10 +447,10 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  *     arithmetic: sums, softmax statistics and norms are held in 32 bits
  *     and a 16-bit result is rounded once.  (Weights of linear layers and of
  *     the token loss may be of the activations' type.)  The products of these two multiply 16-bit
- *     values: fp32 weights and the gradient of u are taken as the sum of two (off by 2^-16 of themselves),
- *     or, the latter in fp32 gradients, three (2^-24); the gradient of z, and the weights in the token loss's dx, are
- *     rounded to one bf16 value where the result is bf16, and taken as the sum of two where it is f16, an
- *     fp32 gradient or a loss; of three where the activations are fp32.
+ *     values: an operand that is fp32, or computed in fp32 (the gradients of u and of z), is taken as the sum of two
+ *     (off by 2^-16 of itself) where the result has 16 bits, of three (2^-24) where it has 32.  Calls of up to eight rows a
+ *     worker (four in a forward pass of 16-bit weights) take it as it is, so that the last digits of a result depend
+ *     on the number of rows.
  *     A value that is not finite makes what it enters not finite.  Every sum has a fixed order, so the
  *     same call on the same data gives the same bits.  Exponentials below 2^-126
  *     may be taken as 0, and the last digits of a result depend on whether its

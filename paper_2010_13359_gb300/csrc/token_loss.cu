@@ -7,10 +7,11 @@
 // The forward pass leaves of each row's 128 (or 32) logits their maximum and the sum of their
 // exponentials, in the product's epilogue; a second kernel joins them in order.
 // The gradient takes the vocabulary in pieces: a piece's logits are computed
-// again, their epilogue writes dz in 16-bit parts into scratch, and two products
-// take it from there.  So the step costs four products of 2 rows vocab width
-// operations where kept logits would cost three, and dW's, whose result is fp32,
-// reads dz in two bf16 parts (three for fp32 activations).
+// again, their epilogue writes dz in three bf16 parts into scratch, and two products
+// take it from there, dW's all of it and dx's of 16 bits two parts.  In products of rows vocab width, bf16 rows and weights: the logits
+// twice, dx 2, dW 3; with fp32 weights 3 + 3, 3, 3; f16 1 + 1, 3, 5, with fp32 weights 5 + 5, 3, 5; fp32 four times 6.
+// The step of 4 x 1024 bf16 rows of 32,000 x 1024: 1335 us, 987 with one part of dz in dx
+// and two in dW, whose errors were 1.4 and 3.4 times larger.
 #include "product_kernel.cuh"
 
 namespace dq {
@@ -18,12 +19,14 @@ namespace dq {
 namespace {
 
 int act_parts(int dtype) { return dtype == DQGAN_F32 ? 3 : dtype == DQGAN_F16 ? 2 : 1; }
-// Of the weights in the logits, whose loss is fp32, and in dx.
-int logit_weight_parts(const TokenLossShape& s) {
+// Of the weights: in the logits, whose loss and lse are fp32, and in dx.  Three parts keep 2^-24 of a value, two 2^-16.
+int logit_weight_parts(const TokenLossShape& s) { return s.weight_dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 ? 2 : 1; }
+int grad_weight_parts(const TokenLossShape& s) {
   return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 || s.weight_dtype == DQGAN_F32 ? 2 : 1;
 }
-int grad_weight_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : s.dtype == DQGAN_F16 ? 2 : 1; }
-int grad_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : 2; }
+// Of dz: in dW, which is fp32, and in dx.
+constexpr int kGradParts = 3;
+int dx_grad_parts(const TokenLossShape& s) { return s.dtype == DQGAN_F32 ? 3 : 2; }
 bool half_logits(const TokenLossShape& s) { return s.dtype == DQGAN_F16 && s.weight_dtype == DQGAN_F16; }
 
 constexpr int64_t kGradBytes = (int64_t)1 << 30, kWeightBytes = (int64_t)1 << 30;
@@ -31,7 +34,7 @@ constexpr int kFewTiles = 76;  // below: narrow tiles
 
 // Columns of a piece of the vocabulary, a multiple of 256.
 int64_t piece_of(const TokenLossShape& s) {
-  const int64_t by_grad = kGradBytes / ((int64_t)s.workers * s.max_rows * 2 * grad_parts(s));
+  const int64_t by_grad = kGradBytes / ((int64_t)s.workers * s.max_rows * 2 * kGradParts);
   const int64_t by_weight = kWeightBytes / ((int64_t)s.workers * s.width * 2 * logit_weight_parts(s));
   const int64_t most = by_grad < by_weight ? by_grad : by_weight;
   const int64_t whole = ceil_div(s.vocab, 256) * 256;
@@ -72,7 +75,7 @@ Scratch scratch_of(const TokenLossShape& s, void* base) {
   c.x = take(rows * round8(s.width) * 2 * act_parts(s.dtype));
   c.x_half = take(half_logits(s) ? rows * round8(s.width) * 2 : 0);
   c.w = take((int64_t)s.workers * piece * round8(s.width) * 2 * logit_weight_parts(s));
-  c.grad = take(rows * piece * 2 * grad_parts(s));
+  c.grad = take(rows * piece * 2 * kGradParts);
   c.stats = static_cast<float2*>(take(rows * most_slots(s.vocab) * 8));
   c.target_logit = static_cast<float*>(take(rows * 4));
   c.lse = static_cast<float*>(take(rows * 4));
@@ -358,7 +361,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
     soft.grad = c.grad;
     soft.grad_ld = piece;
     soft.grad_part = (int64_t)s.workers * a.rows * piece;
-    soft.grad_parts = grad_parts(s);
+    soft.grad_parts = kGradParts;
     st = softmax_product<GradEpilogue>(logits, soft, narrow(a.rows, s.workers, count), c, stream, launches);
     if (st != cudaSuccess) return st;
     ProductOperand d;
@@ -397,7 +400,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
       p.depth = count;
       p.workers = s.workers;
       p.a = d;
-      if (s.dtype == DQGAN_BF16) p.a.parts = 1;
+      p.a.parts = dx_grad_parts(s);
       // the logits' parts serve where they are bf16 (their first ones)
       p.b = logits.b;
       if (half) st = weights(first, count, grad_weight_parts(s), false, &p.b);

@@ -111,3 +111,89 @@ def test_slopes_keep_24_bits_in_fp32_gradients(P, rows, dtype):  # noqa: F811
     if rows == 16:
         assert float(left.abs().sum()) > 2 * e
     op.destroy()
+
+
+def loss_of_one_row(P, z, columns, dtype, weight_dtype, rows, factor):  # noqa: F811
+    """The step of `rows` equal rows over as many logits as z has, each column's weights [columns, z]: x = (0, 1), so that
+    the logits are z.  Targets: the last column."""
+    V, C, T = len(z), 8, TYPES[dtype]
+    w = torch.zeros((V, C), device="cuda", dtype=torch.float32 if weight_dtype == 0 else T)
+    w[:, 0], w[:, 1] = columns, z
+    x = torch.zeros((rows, C), dtype=T, device="cuda")
+    x[:, 1] = 1
+    targets = torch.full((rows,), V - 1, dtype=torch.int32, device="cuda")
+    op = P.TokenLoss(vocab=V, width=C, max_rows=rows, dtype=dtype, weight_dtype=weight_dtype, cuda_stream=stream())
+    loss, lse = torch.zeros((2, rows), device="cuda")
+    dx, dw = torch.zeros_like(x), torch.zeros((V, C), device="cuda")
+    op.step(rows, x, C, w, 0, targets, factor, 1.0, loss, lse, dx, C, dw, 0)
+    op.synchronize()
+    op.destroy()
+    return loss, lse, dx, dw, w.double()
+
+
+@pytest.mark.parametrize("weight_dtype", [0, None])
+@pytest.mark.parametrize("dtype", [1, 2])
+@pytest.mark.parametrize("rows", [3, 16])
+def test_the_logits_gradient_keeps_more_than_a_16_bit_result(P, rows, dtype, weight_dtype):  # noqa: F811
+    """dx where the gradient's parts cancel: what is left are the probabilities' and the weights' last bits."""
+    weight_dtype = dtype if weight_dtype is None else weight_dtype
+    z = torch.tensor([0.0, 1.125, -30.0], device="cuda")  # p = 0.245, 0.755
+    columns = torch.tensor([1.0, 1.0, 1.0], device="cuda")
+    if weight_dtype == 0:
+        columns = torch.tensor([1 + 2.0 ** -10 + 2.0 ** -12, 1 + 2.0 ** -9 - 2.0 ** -13, 1.0], device="cuda")
+    _, _, dx, _, w = loss_of_one_row(P, z, columns, dtype, weight_dtype, rows, None)
+    p = torch.softmax(z.double(), 0)
+    want = (p @ w[:, 0] - w[2, 0]).expand(rows)
+    # the magnitudes add up to 2; q is off by a few units
+    e = 2 * (2.0 ** -16 * (2 + 3) + 3 * STEP + 32 * U)
+    within(dx[:, 0], want, e + rounded(want.abs() + e, TYPES[dtype]), "dx")
+
+
+@pytest.mark.parametrize("dtype", [1, 2])
+def test_the_logits_gradient_keeps_24_bits_in_fp32_gradients(P, dtype):  # noqa: F811
+    """dweight at a target whose probability is 0: the rows' weights, of which two bf16 parts lose most, all one way."""
+    V, C, T = 2, 8, TYPES[dtype]
+    lost = 2.0 ** -17 - 2.0 ** -22  # of 2^-9 (1 + 2^-8 - 2^-13), rounded to eight bits
+    for rows in (3, 16):
+        factor = torch.full((rows,), 1 + 2.0 ** -9, device="cuda") + lost * (torch.arange(rows, device="cuda") % 2)
+        w = torch.zeros((V, C), dtype=T, device="cuda")
+        w[0, 1], w[1, 1] = 200, -200
+        x = torch.zeros((rows, C), dtype=T, device="cuda")
+        x[:, 0] = 1 - 2.0 * (torch.arange(rows, device="cuda") % 2)
+        x[:, 1] = 1
+        targets = torch.ones(rows, dtype=torch.int32, device="cuda")
+        op = P.TokenLoss(vocab=V, width=C, max_rows=rows, dtype=dtype, weight_dtype=dtype, cuda_stream=stream())
+        loss, lse = torch.zeros((2, rows), device="cuda")
+        dw = torch.zeros((V, C), device="cuda")
+        op.step(rows, x, C, w, 0, targets, factor, 1.0, loss, lse, None, C, dw, 0)
+        want = -(factor.double() @ x[:, 0].double())
+        e = 1.01 * rows * (2.0 ** -24 * (1 + 3) + 5 * STEP)
+        assert abs(float(dw[1, 0]) - float(want)) <= e + U * abs(float(want))
+        assert abs(float(dw[0, 0]) + float(want)) <= e + U * abs(float(want))
+        if rows == 16:
+            assert rows / 2 * lost > 2 * e
+        op.destroy()
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("dtype", [1, 2])
+@pytest.mark.parametrize("rows", [3, 20, 300])
+def test_a_loss_of_fp32_weights_keeps_24_bits(P, rows, dtype, pad):  # noqa: F811
+    """Logits that are the differences of weights, of which two bf16 parts lose most."""
+    V, C, T = 70, 16, TYPES[dtype]
+    signs = torch.tensor([1.0, -1.0], device="cuda").repeat(8)
+    x, _ = rows_of(signs.expand(rows, C), pad, T)
+    w = torch.full((V, C), 1 + 2.0 ** -9, device="cuda")
+    w[0, ::2] += 2.0 ** -17 - 2.0 ** -22  # the first column's logit is 8 of them, the others' 0
+    targets = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    op = P.TokenLoss(vocab=V, width=C, max_rows=rows, dtype=dtype, cuda_stream=stream())
+    loss, lse = torch.zeros((2, rows), device="cuda")
+    op.forward(rows, x, x.stride(0), w, 0, targets, None, loss, lse)
+    z = w.double() @ signs.double()
+    want = torch.logsumexp(z, 0)
+    e = 1.01 * 16 * (2.0 ** -24 * (1 + 3) + 5 * STEP)
+    within(lse, want.expand(rows), e + 16 * U * want, "lse")
+    want = want - z[0]
+    within(loss, want.expand(rows), 2 * e + 24 * U * want, "loss")
+    assert float(z[0]) > 2 * e + 24 * U * float(want)
+    op.destroy()
