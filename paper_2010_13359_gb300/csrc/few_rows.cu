@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(1024) few_loss_kernel(float* z, const MatrixAr
   __syncthreads();  // the target's logit has been read
   const int64_t t = counts ? token_at(x.targets, x.token_bits, r) : -1;
   for (int64_t v = threadIdx.x; v < x.vocab; v += 1024) {
-    const float q = expf(row[v] - all);
+    const float q = expf(at_most_0(row[v] - all));
     row[v] = counts ? scale * c * (v == t ? q - 1.f : q) : 0.f;
   }
 }

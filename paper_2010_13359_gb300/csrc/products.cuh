@@ -154,6 +154,12 @@ __device__ __forceinline__ float reciprocal_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// min(x, 0); NaN stays NaN.
+__device__ __forceinline__ float at_most_0(float x) {
+  float y;
+  asm("min.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // Phi(u) and exp(-u^2 / 2).  For results of 16 bits: Abramowitz and Stegun 7.1.26, erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2)
 // with t = 1 / (1 + p x), off by at most 1.5e-7, which is a fifth of erff's instructions.

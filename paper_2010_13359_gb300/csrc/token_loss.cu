@@ -120,12 +120,13 @@ struct StatsEpilogue {
       for (int j = 0; j < kWidth; ++j) z += t == j ? v[j] : 0.f;
       s.target_logit[r] = z;
     }
-    const float from = (most == -INFINITY ? 0.f : most) * -kLog2e;
+    // the differences first: they are exact where they matter, whatever the logits' size
+    const float from = most == -INFINITY ? 0.f : -most;
     float2 sums[2] = {};
 #pragma unroll
     for (int j = 0; j < kWidth; j += 4) {
-      const float2 a = fma2(make_float2(v[j], v[j + 1]), both(kLog2e), both(from));
-      const float2 b = fma2(make_float2(v[j + 2], v[j + 3]), both(kLog2e), both(from));
+      const float2 a = mul2(add2(make_float2(v[j], v[j + 1]), both(from)), both(kLog2e));
+      const float2 b = mul2(add2(make_float2(v[j + 2], v[j + 3]), both(from)), both(kLog2e));
       sums[0] = add2(sums[0], make_float2(exp2_approx(a.x), exp2_approx(a.y)));
       sums[1] = add2(sums[1], make_float2(exp2_approx(b.x), exp2_approx(b.y)));
     }
@@ -150,7 +151,7 @@ struct GradEpilogue {
     if (row >= p.rows) return;
     if (row + lane < p.rows) {
       target = counting_target(s, first + lane);
-      lse = s.lse[first + lane] * kLog2e;
+      lse = s.lse[first + lane];
       factor = s.weights ? s.scale * s.weights[first + lane] : s.scale;
     }
     if (target < 0) factor = 0.f;  // the row does not count: see below where its logits are not finite
@@ -162,7 +163,9 @@ struct GradEpilogue {
       float2 x[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float2 e = fma2(make_float2(v[g + 2 * j], v[g + 2 * j + 1]), both(kLog2e), both(-lse));
+        // no probability is above 1: a logit's own rounding, which may be large, does not lift it over lse
+        const float2 d = add2(make_float2(v[g + 2 * j], v[g + 2 * j + 1]), both(-lse));
+        const float2 e = mul2(make_float2(at_most_0(d.x), at_most_0(d.y)), both(kLog2e));
         x[j] = mul2(make_float2(exp2_approx(e.x), exp2_approx(e.y)), both(factor));
       }
       if (__any_sync(kFullMask, target < 0 || (t >= g && t < g + 32))) {
