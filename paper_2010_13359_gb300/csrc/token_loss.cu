@@ -330,17 +330,15 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
   logits.workers = s.workers;
   logits.a = x_logits;
   const int logit_parts = half ? 1 : logit_weight_parts(s);
+  // Both passes take the same pieces in tiles of the same width, and so sum each logit in the same order: of a row whose
+  // largest logit is far above the others the gradient is 0 only if that logit has the bits that lse was made of.
+  const bool thin = thin_fits(s.vocab) && narrow(a.rows, s.workers, piece < s.vocab ? piece : s.vocab);
 
   if (a.forward) {
-    // all at once where the weights can be read as they lie
-    const bool whole = (half || (s.weight_dtype == DQGAN_BF16 && logit_parts == 1)) &&
-                       operand_in_place(a.weight, s.width, s.workers > 1 ? a.p_stride : 0);
-    const int64_t step = whole ? s.vocab : piece;
-    const bool thin = thin_fits(s.vocab) && narrow(a.rows, s.workers, step < s.vocab ? step : s.vocab);
     const int64_t columns = thin ? ProductShape<64>::kWidth : ProductShape<256>::kWidth;  // of a slot
     soft.slots = (int32_t)(thin ? thin_slots(s.vocab) : wide_slots(s.vocab));
-    for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += step) {
-      logits.columns = s.vocab - first < step ? s.vocab - first : step;
+    for (int64_t first = 0; first < s.vocab && st == cudaSuccess; first += piece) {
+      logits.columns = s.vocab - first < piece ? s.vocab - first : piece;
       if ((st = weights(first, logits.columns, logit_parts, half, &logits.b)) != cudaSuccess) break;
       logits.terms = product_terms(logits.a.parts, logits.b.parts);
       soft.first = first;
@@ -365,7 +363,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
     soft.grad_ld = piece;
     soft.grad_part = (int64_t)s.workers * a.rows * piece;
     soft.grad_parts = kGradParts;
-    st = softmax_product<GradEpilogue>(logits, soft, narrow(a.rows, s.workers, count), c, stream, launches);
+    st = softmax_product<GradEpilogue>(logits, soft, thin, c, stream, launches);
     if (st != cudaSuccess) return st;
     ProductOperand d;
     d.data = c.grad;

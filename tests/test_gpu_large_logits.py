@@ -100,3 +100,20 @@ def test_probabilities_of_large_logits_that_lie_together(P, dtype, size, rows): 
     within(dw[:, 0], rows * p - count, e_p, "dweight")
     assert float(((dw[:, 0].double() + count) / rows).max()) <= 1 + 2.0 ** -15
 
+
+def test_both_passes_sum_a_logit_alike(P):  # noqa: F811
+    """Rows whose target's logit is far above the others, in a vocabulary of two pieces: nothing is left of the gradient
+    unless the second pass has other sums than lse was made of.  The targets are the last columns, in tiles that do not
+    fill the GPU and are cut along the width where a pass takes the whole vocabulary at once."""
+    n, V, C = 20_000, 13_000, 2048
+    w = torch.randn((V, C), generator=gen(1), device="cuda").bfloat16()
+    targets = torch.randint(12_800, V, (n,), generator=gen(2), device="cuda").int()
+    x = (40 * w[targets.long()].float()).bfloat16()  # logits of 8e4, and of at most 1e4 elsewhere
+    op = P.TokenLoss(vocab=V, width=C, max_rows=n, dtype=P.BF16, weight_dtype=P.BF16, cuda_stream=stream())
+    loss, lse = torch.full((2, n), math.nan, device="cuda")
+    dx, dw = torch.full_like(x, math.nan), torch.full((V, C), math.nan, device="cuda")
+    op.step(n, x, C, w, 0, targets, None, 1.0, loss, lse, dx, C, dw, 0)
+    op.synchronize()
+    assert not loss.any() and float(lse.min()) > 7e4
+    assert not dx.any() and not dw.any()
+    op.destroy()
