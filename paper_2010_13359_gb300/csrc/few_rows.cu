@@ -156,13 +156,6 @@ __global__ void __launch_bounds__(256) few_slopes_kernel(const T* dy, int64_t dy
   }
 }
 
-// Rows that count: all, or those with a target and a weight.
-__device__ __forceinline__ bool row_counts(const MatrixArgs& x, int64_t r) {
-  if (!x.targets) return true;
-  const int64_t t = token_at(x.targets, x.token_bits, r);
-  return t >= 0 && t < x.vocab && !(x.weights && x.weights[r] == 0.f);
-}
-
 constexpr int kFewColumns = 1024;  // of a block, four a thread
 constexpr int kFewRun = 256;       // most rows of W that one fp32 sum runs over
 constexpr int kFewOutputs = 64;    // rows of the weights' gradient that a block writes
@@ -276,9 +269,10 @@ __global__ void __launch_bounds__(256) few_across_kernel(const float* d, const M
   }
 }
 
-// The runs' sums: eight warps in turn, and then in order.
+// The runs' sums: eight warps in turn, and then in order.  0 in x's rows that do not count.
 template <typename T>
-__global__ void __launch_bounds__(256) few_join_kernel(const float* sums, int runs, int64_t rows, int64_t columns, T* dx, int64_t dx_ld) {
+__global__ void __launch_bounds__(256) few_join_kernel(const float* sums, int runs, int64_t rows, int64_t columns, const MatrixArgs x, T* dx,
+                                                       int64_t dx_ld) {
   dq_pdl_enter();
   __shared__ float part[8][32];
   const int warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
@@ -292,7 +286,7 @@ __global__ void __launch_bounds__(256) few_join_kernel(const float* sums, int ru
   __syncthreads();
   if (warp > 0 || j >= columns) return;
   for (int w = 1; w < 8; ++w) s += part[w][lane];
-  dx[r * dx_ld + j] = from_float<T>(s);
+  dx[r * dx_ld + j] = from_float<T>(row_counts(x, r) ? s : 0.f);
 }
 
 // A row's lse and loss from its logits, and their gradient in their place.
@@ -379,7 +373,7 @@ cudaError_t launch_few_outer(const float* d, const MatrixArgs& x, int64_t output
   });
 }
 
-cudaError_t launch_few_across(const float* d, const MatrixArgs& w, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
+cudaError_t launch_few_across(const float* d, const MatrixArgs& w, const MatrixArgs& x, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
                               void* scratch, cudaStream_t stream, uint64_t* launches) {
   const int sms = device_sms();
   if (sms <= 0) return cudaErrorInvalidDevice;
@@ -409,7 +403,7 @@ cudaError_t launch_few_across(const float* d, const MatrixArgs& w, int64_t rows,
   return with_dtype(dx_dtype, [&](auto t) {
     using T = decltype(t);
     return launch_pdl(few_join_kernel<T>, dim3((unsigned)ceil_div(w.columns, 32), (unsigned)(rows * w.workers)), dim3(256), 0, stream,
-                      (const float*)sums, (int)runs, rows * w.workers, w.columns, static_cast<T*>(dx), dx_ld);
+                      (const float*)sums, (int)runs, rows * w.workers, w.columns, x, static_cast<T*>(dx), dx_ld);
   });
 }
 

@@ -251,7 +251,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     st = launch_few_slopes(few_dy, s.activation == DQGAN_NONE ? nullptr : a.pre, a.pre_ld, s.activation, c.few, a.dbias, a.g_stride,
                            a.accumulate, stream, launches);
     if (st == cudaSuccess && a.dx)
-      st = launch_few_across(c.few, few_w, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
+      st = launch_few_across(c.few, few_w, few_x, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
     if (st == cudaSuccess && a.dweight)
       st = launch_few_outer(c.few, few_x, s.outputs, a.dweight, a.g_stride, a.accumulate, stream, launches);
     return st;

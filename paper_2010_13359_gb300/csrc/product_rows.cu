@@ -59,6 +59,11 @@ struct RowsEpilogue {
 #pragma unroll
           for (int k = 0; k < 8; ++k) x[k] += to_float(more[k]);
         }
+        if (s.targets) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (!row_counts(s, tile.worker * p.rows + row + min(i + k, rows - 1))) x[k] = 0.f;
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
           if (i + k < rows) out[(i + k) * s.out_ld] = from_float<T>(x[k]);

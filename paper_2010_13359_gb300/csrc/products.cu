@@ -55,6 +55,7 @@ struct StoreEpilogue {
     const int rows = (int)min64(32, p.rows - row);
     if (rows <= 0) return;
     const float* const bias = s.bias ? s.bias + tile.worker * s.bias_batch : nullptr;
+    const bool counts = lane >= rows || row_counts(s, tile.worker * p.rows + row + lane);
 #pragma unroll
     for (int g = 0; g < S::kWidth; g += 32) {
       const int64_t j = column + g, count = p.columns - j;
@@ -72,6 +73,10 @@ struct StoreEpilogue {
       activate_all<sizeof(T) == 4>(x, s.activation);
       if (s.residual && lane < rows)
         add32(static_cast<const T*>(s.residual) + tile.worker * s.residual_batch + (row + lane) * s.residual_ld + j, count, x);
+      if (!counts) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = 0.f;
+      }
       store.template put32<T>(x, &p.out, (int)j, (int)row, tile.worker);
     }
   }
@@ -165,12 +170,7 @@ __global__ void __launch_bounds__(256) split_kernel(const SplitArgs first, const
     const int column = (int)(i - r * across) * 8;
     const int64_t worker = r / a.rows, row = r - worker * a.rows;
     float x[8] = {};
-    bool counts = true;
-    if (a.targets) {
-      const int64_t t = token_at(a.targets, a.token_bits, r);
-      counts = t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
-    }
-    if (counts) {
+    if (row_counts(a, r)) {
       const T* const from = static_cast<const T*>(a.from) + worker * a.batch + row * a.from_ld + column;
       const int count = (int)min64(8, a.columns - column);
       if (a.packs)

@@ -46,6 +46,11 @@ struct StoreArgs {
   const float* add;      // fp32 values added to the sum (add + m * add_batch + i * add_ld + j), or nullptr; may be out
   int64_t add_batch, add_ld;
   int32_t activation;
+  // Rows that do not count are stored as 0, whatever their sums are (0 times what is not finite); as in SplitArgs.
+  const void* targets;
+  const float* weights;
+  int32_t token_bits;
+  int64_t vocab;
 };
 
 struct SoftmaxArgs {
@@ -139,9 +144,15 @@ inline bool operand_in_place(const void* p, int64_t ld, int64_t batch) {
   return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && batch % 8 == 0 && ld < ((int64_t)1 << 38) && batch < ((int64_t)1 << 38);
 }
 
-// Whether row r of a loss counts.
 __device__ __forceinline__ int64_t token_at(const void* ids, int bits, int64_t r) {
   return bits == 32 ? (int64_t) static_cast<const int32_t*>(ids)[r] : static_cast<const int64_t*>(ids)[r];
+}
+// Whether row r counts: where there are targets, if its target is in the vocabulary and its weight is not 0.
+template <typename Args>
+__device__ __forceinline__ bool row_counts(const Args& a, int64_t r) {
+  if (!a.targets) return true;
+  const int64_t t = token_at(a.targets, a.token_bits, r);
+  return t >= 0 && t < a.vocab && !(a.weights && a.weights[r] == 0.f);
 }
 
 __device__ __forceinline__ float exp2_approx(float x) {  // 2 units; below 2^-126: 0
@@ -362,9 +373,9 @@ cudaError_t launch_few_slopes(const MatrixArgs& dy, const void* pre, int64_t pre
 // d^T x, outputs x x.columns, worker m's at out + m * batch.  x's rows that do not count are left out.
 cudaError_t launch_few_outer(const float* d, const MatrixArgs& x, int64_t outputs, float* out, int64_t batch, int accumulate,
                              cudaStream_t stream, uint64_t* launches);
-// d W.  scratch: kProductScratch bytes.  few_across_fits: whether the kernels' scratch and grids hold it.
+// d W; 0 in x's rows that do not count.  scratch: kProductScratch bytes.  few_across_fits: whether the kernels' scratch and grids hold it.
 bool few_across_fits(const MatrixArgs& w, int64_t rows);
-cudaError_t launch_few_across(const float* d, const MatrixArgs& w, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
+cudaError_t launch_few_across(const float* d, const MatrixArgs& w, const MatrixArgs& x, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
                               void* scratch, cudaStream_t stream, uint64_t* launches);
 // loss and lse of rows of x.vocab logits (forward), and the gradient in their place (backward; without forward: from lse).
 cudaError_t launch_few_loss(float* z, const MatrixArgs& x, float scale, bool forward, bool backward, float* loss, float* lse,

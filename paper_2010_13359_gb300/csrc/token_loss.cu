@@ -86,8 +86,7 @@ Scratch scratch_of(const TokenLossShape& s, void* base) {
 }
 
 __device__ __forceinline__ int64_t counting_target(const SoftmaxArgs& s, int64_t r) {
-  const int64_t t = token_at(s.targets, s.token_bits, r);
-  return t >= 0 && t < s.vocab && !(s.weights && s.weights[r] == 0.f) ? t : -1;
+  return row_counts(s, r) ? token_at(s.targets, s.token_bits, r) : -1;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -293,7 +292,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
     st = launch_few_rows(few_x, few_w, z, stream, launches);
     if (st == cudaSuccess) st = launch_few_loss(c.few, few_x, a.scale, a.forward, backward, a.loss, a.lse, stream, launches);
     if (st == cudaSuccess && backward && a.dx)
-      st = launch_few_across(c.few, few_w, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
+      st = launch_few_across(c.few, few_w, few_x, a.rows, a.dx, a.dx_ld, s.dtype, c.products, stream, launches);
     if (st == cudaSuccess && backward && a.dweight)
       st = launch_few_outer(c.few, few_x, s.vocab, a.dweight, a.g_stride, a.accumulate, stream, launches);
     return st;
@@ -417,6 +416,12 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
         out.add_batch = dense;
       }
       const bool last = first + count == s.vocab;
+      if (last) {
+        out.targets = a.targets;
+        out.weights = a.weights;
+        out.token_bits = s.token_bits;
+        out.vocab = s.vocab;
+      }
       out.out = last ? a.dx : c.dx;
       out.out_ld = last ? a.dx_ld : s.width;
       out.out_batch = last ? a.rows * a.dx_ld : dense;
