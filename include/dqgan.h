@@ -748,8 +748,10 @@ DQGAN_API int dqgan_gradient_norm(dqgan_operator* op, int64_t count, const dqgan
 
 /*
  * Writes min(1, max_norm / (norm + eps)) times each tensor to its place (of the
- * same size), worker by worker.  max_norm >= 0.  A worker whose norm is not finite
- * is passed on as it is.  norms: as above, or NULL.  A place may be its tensor (same address, type and stride).
+ * same size), worker by worker.  max_norm >= 0.  A worker with a value that is not
+ * finite is passed on as it is (a norm of finite values beyond fp32's range clips as any other; norms
+ * has infinity there).  norms: as above, or NULL.  A place may be its tensor (same address, type
+ * and stride); a place at the address of another place, or of another tensor, is refused.
  */
 DQGAN_API int dqgan_gradient_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* tensors,
                                   const dqgan_tensor* places, float max_norm, float* norms);

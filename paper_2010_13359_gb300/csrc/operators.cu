@@ -1,5 +1,6 @@
 // C-ABI of the token-model operators (declared in include/dqgan.h): argument
 // checking, ownership of the scratch space and dispatch to the kernels.
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -637,6 +638,36 @@ int check_tensors(dqgan_operator* op, int64_t count, const dqgan_tensor* t, int3
   return DQGAN_OK;
 }
 
+// Places that are read or written by more than one entry: blocks that scale one would race with each other.  Only whole
+// ones (the same address) are looked for.
+int check_places(dqgan_operator* op, int64_t count, const dqgan_tensor* from, const dqgan_tensor* to) {
+  uint16_t order[kMaxTensors];  // of the places, by address
+  int64_t places = 0;
+  bool sorted = true;
+  for (int64_t i = 0; i < count; ++i) {
+    if (to[i].size == 0) continue;
+    sorted = sorted && (places == 0 || (uintptr_t)to[order[places - 1]].data < (uintptr_t)to[i].data);
+    order[places++] = (uint16_t)i;
+  }
+  const auto at = [&](uint16_t i) { return (uintptr_t)to[i].data; };
+  if (!sorted) {
+    std::sort(order, order + places, [&](uint16_t a, uint16_t b) { return at(a) < at(b); });
+    for (int64_t k = 1; k < places; ++k)
+      if (at(order[k - 1]) == at(order[k]))
+        return fail(op, DQGAN_ERR_INVALID_ARG, "places %d and %d: the same address", (int)std::min(order[k - 1], order[k]),
+                    (int)std::max(order[k - 1], order[k]));
+  }
+  for (int64_t i = 0; i < count; ++i) {
+    if (from[i].size == 0 || from[i].data == to[i].data) continue;
+    const uintptr_t address = (uintptr_t)from[i].data;
+    const uint16_t* const found =
+        std::lower_bound(order, order + places, address, [&](uint16_t k, uintptr_t value) { return at(k) < value; });
+    if (found != order + places && at(*found) == address)
+      return fail(op, DQGAN_ERR_INVALID_ARG, "place %d: the address of tensor %lld", (int)*found, (long long)i);
+  }
+  return DQGAN_OK;
+}
+
 int check_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* from) {
   if (int r = check(op, Kind::kGradientClip, "a gradient clipping")) return r;
   if (count < 0 || count > kMaxTensors) return invalid(op, "count outside [0, 4096]");
@@ -689,6 +720,7 @@ int dqgan_gradient_clip(dqgan_operator* op, int64_t count, const dqgan_tensor* t
         (op->clip.dtype != op->clip.out_dtype || (op->clip.workers > 1 && places[i].stride != tensors[i].stride)))
       return fail(op, DQGAN_ERR_INVALID_ARG, "place %lld: the tensor itself in another type or stride", (long long)i);
   }
+  if (int r = check_places(op, count, tensors, places)) return r;
   if (!(max_norm >= 0.f)) return invalid(op, "max_norm is negative or NaN");
   if (!aligned(norms, 4)) return invalid(op, "a pointer is not aligned to its element");
   NvtxRange range("dqgan gradient clip");
