@@ -583,9 +583,12 @@ typedef struct dqgan_tensor {
 typedef struct dqgan_operator dqgan_operator;
 
 /* Create an operator on the current device, with its scratch space (layer
- * norm and embedding: for the gradients; distillation has none; linear: its operands as the
- * tensor cores read them; token loss: besides those a piece of the logits' gradient, up to
- * 1 GB; clipping: the blocks' sums).  On error
+ * norm and embedding: for the gradients; distillation has none; linear and token loss: 80 MB for
+ * products in pieces, and their operands as the tensor cores read them, whether calls need them so
+ * or not, of the token loss a piece of the vocabulary, whose weights and logits' gradient take up to 1 GB
+ * each, or what 256 entries take; its sums take besides 8 bytes a row for 128 entries, 32 where the vocabulary has up to
+ * 19,456; and up to eight rows a worker their logits, or gradient of u, in fp32, where that many rows are computed
+ * without tiles; clipping: the blocks' sums).  On error
  * *out is NULL, dqgan_operator_last_error(NULL) holds the reason and nothing
  * stays allocated.  The test hook DQGAN_TEST_FAIL_ALLOC of dqgan_create
  * applies here too. */

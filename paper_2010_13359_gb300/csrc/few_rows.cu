@@ -407,9 +407,10 @@ cudaError_t launch_few_across(const float* d, const MatrixArgs& w, const MatrixA
   });
 }
 
-bool few_across_fits(const MatrixArgs& w, int64_t rows) {
-  const int64_t one = (int64_t)w.workers * rows * w.columns * 4;
-  return ceil_div(w.rows, kFewRun) * one <= (int64_t)kProductScratch && w.rows <= (int64_t)65535 * kFewOutputs;
+int64_t most_few_rows(int32_t workers, int64_t w_rows, int64_t w_columns, int64_t rows) {
+  if (w_rows > (int64_t)65535 * kFewOutputs) return 0;
+  const int64_t one_row = ceil_div(w_rows, kFewRun) * workers * w_columns * 4;
+  return min64(min64(rows, kFewRows), (int64_t)kProductScratch / one_row);
 }
 
 cudaError_t launch_few_loss(float* z, const MatrixArgs& x, float scale, bool forward, bool backward, float* loss, float* lse,

@@ -62,7 +62,7 @@ Scratch scratch_of(const LinearShape& s, void* base) {
   c.w = take((int64_t)s.workers * s.outputs * round8(s.inputs) * 2 * weight_parts(s));
   c.d = take(rows * round8(s.outputs) * 2 * grad_parts(s));
   c.sums = static_cast<float*>(take(s.workers * most_row_blocks(s) * s.outputs * 4));
-  c.few = static_cast<float*>(take((int64_t)s.workers * (s.max_rows < kFewRows ? s.max_rows : kFewRows) * s.outputs * 4));
+  c.few = static_cast<float*>(take(s.workers * most_few_rows(s.workers, s.outputs, s.inputs, s.max_rows) * s.outputs * 4));
   c.bytes = at;
   return c;
 }
@@ -245,7 +245,7 @@ cudaError_t launch_linear_backward(const LinearArgs& a, cudaStream_t stream, uin
     return st;
   }
   const MatrixArgs few_w{a.weight, s.inputs, a.p_stride, s.weight_dtype, s.outputs, s.inputs, s.workers};
-  if (a.rows <= kFewRows && few_across_fits(few_w, a.rows)) {
+  if (few_rows_fit(few_w, a.rows)) {
     const MatrixArgs few_dy{a.dy, a.dy_ld, a.rows * a.dy_ld, s.dtype, a.rows, s.outputs, s.workers};
     const MatrixArgs few_x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.inputs, s.workers};
     st = launch_few_slopes(few_dy, s.activation == DQGAN_NONE ? nullptr : a.pre, a.pre_ld, s.activation, c.few, a.dbias, a.g_stride,

@@ -373,8 +373,12 @@ cudaError_t launch_few_slopes(const MatrixArgs& dy, const void* pre, int64_t pre
 // d^T x, outputs x x.columns, worker m's at out + m * batch.  x's rows that do not count are left out.
 cudaError_t launch_few_outer(const float* d, const MatrixArgs& x, int64_t outputs, float* out, int64_t batch, int accumulate,
                              cudaStream_t stream, uint64_t* launches);
-// d W; 0 in x's rows that do not count.  scratch: kProductScratch bytes.  few_across_fits: whether the kernels' scratch and grids hold it.
-bool few_across_fits(const MatrixArgs& w, int64_t rows);
+// Most rows a worker, up to `rows` and kFewRows, that the kernels' scratch and grids hold; 0: none.
+int64_t most_few_rows(int32_t workers, int64_t w_rows, int64_t w_columns, int64_t rows);
+inline bool few_rows_fit(const MatrixArgs& w, int64_t rows) {
+  return rows <= kFewRows && most_few_rows(w.workers, w.rows, w.columns, rows) == rows;
+}
+// d W; 0 in x's rows that do not count.  scratch: kProductScratch bytes.
 cudaError_t launch_few_across(const float* d, const MatrixArgs& w, const MatrixArgs& x, int64_t rows, void* dx, int64_t dx_ld, int32_t dx_dtype,
                               void* scratch, cudaStream_t stream, uint64_t* launches);
 // loss and lse of rows of x.vocab logits (forward), and the gradient in their place (backward; without forward: from lse).

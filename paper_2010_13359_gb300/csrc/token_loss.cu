@@ -35,7 +35,7 @@ constexpr int kFewTiles = 76;  // below: narrow tiles
 // Columns of a piece of the vocabulary, a multiple of 256.
 int64_t piece_of(const TokenLossShape& s) {
   const int64_t by_grad = kGradBytes / ((int64_t)s.workers * s.max_rows * 2 * kGradParts);
-  const int64_t by_weight = kWeightBytes / ((int64_t)s.workers * s.width * 2 * logit_weight_parts(s));
+  const int64_t by_weight = kWeightBytes / (s.workers * round8(s.width) * 2 * logit_weight_parts(s));
   const int64_t most = by_grad < by_weight ? by_grad : by_weight;
   const int64_t whole = ceil_div(s.vocab, 256) * 256;
   return most < 256 ? 256 : most < whole ? most / 256 * 256 : whole;
@@ -80,7 +80,7 @@ Scratch scratch_of(const TokenLossShape& s, void* base) {
   c.target_logit = static_cast<float*>(take(rows * 4));
   c.lse = static_cast<float*>(take(rows * 4));
   c.dx = static_cast<float*>(take(piece < s.vocab ? rows * s.width * 4 : 0));
-  c.few = static_cast<float*>(take((int64_t)s.workers * (s.max_rows < kFewRows ? s.max_rows : kFewRows) * s.vocab * 4));
+  c.few = static_cast<float*>(take(s.workers * most_few_rows(s.workers, s.vocab, s.width, s.max_rows) * s.vocab * 4));
   c.bytes = at;
   return c;
 }
@@ -276,7 +276,7 @@ cudaError_t launch_token_loss(const TokenLossArgs& a, cudaStream_t stream, uint6
 
   // A few rows: without tiles, their logits and those's gradient in scratch.
   const MatrixArgs few_w{a.weight, s.width, a.p_stride, s.weight_dtype, s.vocab, s.width, s.workers};
-  if (a.rows <= kFewRows && few_across_fits(few_w, a.rows)) {
+  if (few_rows_fit(few_w, a.rows)) {
     MatrixArgs few_x{a.x, a.x_ld, a.rows * a.x_ld, s.dtype, a.rows, s.width, s.workers};
     few_x.targets = a.targets;
     few_x.weights = a.weights;
