@@ -606,6 +606,11 @@ DQGAN_API int dqgan_operator_destroy(dqgan_operator* op);
  * if a bounded wait in one of its kernels gave up. */
 DQGAN_API int dqgan_operator_synchronize(dqgan_operator* op);
 
+/* As dqgan_selftest_wait_timeout, with the error word of a linear layer or a token loss: the next
+ * dqgan_operator_synchronize returns DQGAN_ERR_TIMEOUT and clears the word.  Other operators have none
+ * (DQGAN_ERR_INVALID_ARG). */
+DQGAN_API int dqgan_operator_selftest_wait_timeout(dqgan_operator* op, uint32_t polls);
+
 /* Kernels the operator has launched so far. */
 DQGAN_API uint64_t dqgan_operator_launch_count(const dqgan_operator* op);
 

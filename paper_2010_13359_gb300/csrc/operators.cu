@@ -263,6 +263,14 @@ int dqgan_operator_synchronize(dqgan_operator* op) {
   return DQGAN_OK;
 }
 
+int dqgan_operator_selftest_wait_timeout(dqgan_operator* op, uint32_t polls) {
+  if (!op) return invalid(nullptr, "operator is NULL");
+  if (!op->waits) return invalid(op, "the operator's kernels do not wait");
+  const uint32_t most = dq::wait_selftest_max_polls();
+  if (polls > most) return fail(op, DQGAN_ERR_INVALID_ARG, "polls must be at most %u", most);
+  return launched(op, dq::launch_wait_selftest(polls ? polls : most, op->waits, op->stream, &op->launches), "self-test");
+}
+
 uint64_t dqgan_operator_launch_count(const dqgan_operator* op) { return op ? op->launches : 0; }
 
 const char* dqgan_operator_last_error(const dqgan_operator* op) { return op ? op->err : tl_operator_err; }

@@ -134,6 +134,7 @@ def load_library(path: str = LIBRARY) -> ctypes.CDLL:
         "dqgan_gradient_clip_create": (ctypes.c_int, [P, ctypes.POINTER(H)]),
         "dqgan_operator_destroy": (ctypes.c_int, [H]),
         "dqgan_operator_synchronize": (ctypes.c_int, [H]),
+        "dqgan_operator_selftest_wait_timeout": (ctypes.c_int, [H, ctypes.c_uint32]),
         "dqgan_operator_launch_count": (u64, [H]),
         "dqgan_operator_last_error": (ctypes.c_char_p, [H]),
         "dqgan_layer_norm_forward": (ctypes.c_int, [H, i64, P, i64, P, P, i64, P, i64, P, P]),

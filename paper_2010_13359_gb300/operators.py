@@ -175,6 +175,10 @@ class Operator:
     def synchronize(self) -> None:
         _check(load_library().dqgan_operator_synchronize(self._h), self._h)
 
+    def selftest_wait_timeout(self, polls: int = 0) -> None:
+        """Enqueue the bounded-wait self-test; the next synchronize() raises DqganError with status ERR_TIMEOUT."""
+        _check(load_library().dqgan_operator_selftest_wait_timeout(self._h, polls), self._h)
+
     def launch_count(self) -> int:
         return int(load_library().dqgan_operator_launch_count(self._h))
 
