@@ -435,7 +435,10 @@ DQGAN_API int dqgan_topk_compress_noalloc(const float* g, float* e, void* out_ms
  * Conventions, where they differ from or add to the ones above:
  *   - An operator handle has its own stream, scratch and error text.  It keeps
  *     nothing of a call for the next one.  Nothing is allocated by the calls
- *     that compute, so they can be captured in a CUDA graph.
+ *     that compute, so they can be captured in a CUDA graph; the graph uses the operator's scratch,
+ *     so it runs neither beside other calls of the operator or graphs of them, nor after the operator is destroyed.
+ *   - The calls that compute are made with the device current that was when the operator was created
+ *     (others are refused).
  *   - Activations are rows of `width` (or `vocab`) values of the config's dtype
  *     at a stride of at least that many elements; worker m's rows follow
  *     worker m - 1's.  Pointers need the alignment of their element only;

@@ -25,6 +25,7 @@ struct dqgan_operator {
   dqgan_token_loss_config token_loss{};
   dqgan_gradient_clip_config clip{};
   uint32_t* waits = nullptr;  // error word of the kernels that wait, at the start of their scratch
+  int device = 0;  // current when it was created: the scratch's
   cudaStream_t stream = nullptr;
   void* scratch = nullptr;
   uint64_t launches = 0;
@@ -75,14 +76,18 @@ int create(Kind kind, void* stream, size_t scratch_bytes, dqgan_operator** out) 
   if (!op) return fail(nullptr, DQGAN_ERR_OOM, "host allocation failed");
   op->kind = kind;
   op->stream = reinterpret_cast<cudaStream_t>(stream);
-  if (scratch_bytes > 0) {
-    const cudaError_t st = dq::device_allocate(&op->scratch, scratch_bytes);
-    if (st != cudaSuccess) {
-      cudaGetLastError();
-      delete op;
-      return fail(nullptr, st == cudaErrorMemoryAllocation ? DQGAN_ERR_OOM : DQGAN_ERR_CUDA, "allocating scratch: %s",
-                  cudaGetErrorString(st));
-    }
+  cudaError_t st = cudaGetDevice(&op->device);
+  if (scratch_bytes > 0)
+    st = dq::device_allocate(&op->scratch, scratch_bytes);
+  else if (st != cudaSuccess) {  // without a GPU: the arguments can be checked all the same
+    cudaGetLastError();
+    st = cudaSuccess;
+  }
+  if (st != cudaSuccess) {
+    cudaGetLastError();
+    delete op;
+    return fail(nullptr, st == cudaErrorMemoryAllocation ? DQGAN_ERR_OOM : DQGAN_ERR_CUDA, "allocating scratch: %s",
+                cudaGetErrorString(st));
   }
   *out = op;
   return DQGAN_OK;
@@ -91,6 +96,9 @@ int create(Kind kind, void* stream, size_t scratch_bytes, dqgan_operator** out) 
 int check(dqgan_operator* op, Kind kind, const char* name) {
   if (!op) return invalid(nullptr, "operator is NULL");
   if (op->kind != kind) return fail(op, DQGAN_ERR_INVALID_ARG, "the operator is not %s", name);
+  int device = 0;  // a launch would run there, away from the scratch and the caller's data
+  if (cudaGetDevice(&device) == cudaSuccess && device != op->device)
+    return fail(op, DQGAN_ERR_INVALID_ARG, "device %d is current, the operator is of device %d", device, op->device);
   return DQGAN_OK;
 }
 

@@ -185,7 +185,7 @@ struct GradEpilogue {
   }
 };
 
-// A row's lse and loss from its slots: eight warps take 32 rows' slots in turn, four loads at once, joined in order.
+// A row's lse and loss from its slots: eight warps take 32 rows' slots in turn, eight loads at once, joined in order.
 __global__ void __launch_bounds__(256) join_stats_kernel(const SoftmaxArgs s, int64_t rows, int32_t workers, float* loss,
                                                          float* lse) {
   dq_pdl_enter();
