@@ -10,7 +10,7 @@
 // fp32 gradients and all of fp32 layers, so that 2^-16 or 2^-24 of it is left out beside the result's own rounding.  (In
 // one part du would be rounded a second time, and weights at a lookahead point would be those at the point itself
 // wherever they differ by less than 2^-9 of them.  The gradient of 8 x 2048 bf16 rows of 1024 x 4096 with
-// GELU: 538 us, 359 with du as one part in dx and two in dW, whose errors were 1.4 and 2.2 times larger;
+// GELU: 538 us, 359 with du as one part in dx and two in dW, whose errors were 1.4 and 7 times larger;
 // the forward pass with fp32 weights 242 us, 154 with one part of them and an error 1.4 times larger.)
 // f16 values that do not lie as f16 in memory are two bf16 parts
 // (all of their 11 bits, at any exponent).

@@ -75,7 +75,8 @@ struct ProductArgs {
   int64_t rows, columns;    // of D, per worker
   int32_t workers;
   int32_t kblocks;          // blocks of 64 of the contracted index
-  int32_t chunk;            // terms of 64 that one accumulator in tensor memory sums
+  int32_t group;            // blocks whose products go to one accumulator in tensor memory, one pair of parts after another
+  int32_t chunk;            // their terms: group * terms.count
   int32_t pieces;           // of the contracted index, that are summed apart in the tiles from `whole` on
   int64_t whole;
   int32_t tiles_m, tiles_n;

@@ -197,3 +197,26 @@ def test_a_loss_of_fp32_weights_keeps_24_bits(P, rows, dtype, pad):  # noqa: F81
     within(loss, want.expand(rows), 2 * e + 24 * U * want, "loss")
     assert float(z[0]) > 2 * e + 24 * U * float(want)
     op.destroy()
+
+
+def test_small_parts_are_summed_before_large_ones(P):  # noqa: F811
+    """320 rows whose gradient at the target is -(1.5 + d), d below 2^-9 of what 24 bits leave: the 1.5 add up exactly, and
+    what lies below them is lost once, when the sum grows past it, not at every step of its own."""
+    rows, V, C, T = 320, 2, 8, torch.bfloat16
+    factor = 1.5 + 2.0 ** -9 * torch.rand(rows, generator=gen(4), device="cuda")
+    w = torch.zeros((V, C), dtype=T, device="cuda")
+    w[0, 1], w[1, 1] = 200, -200
+    x = torch.zeros((rows, C), dtype=T, device="cuda")
+    x[:, :2] = 1
+    targets = torch.ones(rows, dtype=torch.int32, device="cuda")
+    op = P.TokenLoss(vocab=V, width=C, max_rows=rows, dtype=P.BF16, weight_dtype=P.BF16, cuda_stream=stream())
+    loss, lse = torch.zeros((2, rows), device="cuda")
+    dw = torch.zeros((V, C), device="cuda")
+    op.step(rows, x, C, w, 0, targets, factor, 1.0, loss, lse, None, C, dw, 0)
+    want = float(factor.double().sum())
+    # one accumulator: its last unit is 2^-15, those that it grew through add up to as much, each lost twice at most; the
+    # small parts' sums are below 1, in 20 steps each
+    e = 2 * 2 * 2.0 ** -15 + 40 * STEP
+    assert abs(float(dw[1, 0]) + want) <= e, (float(dw[1, 0]), want, e)
+    assert abs(float(dw[0, 0]) - want) <= e
+    op.destroy()
